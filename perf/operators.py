@@ -289,7 +289,7 @@ def run(s):
         dx, dgamma, dbeta = m.layer_norm_backward(s["dy"], saved)
         return {"y": y, "dx": dx, "dgamma": dgamma, "dbeta": dbeta}
     if c["kind"] == "scores":
-        return {"scores": m.q4_scores(s["x"], s["packed"], s["scales"], c["group"])}
+        return {"scores": m.fourbit_scores(s["x"], s["packed"], s["scales"], c["group"])}
     over = dict(left=c["left"], right=c.get("right", 0), sinks=c["sinks"], reach=c["reach"], two_sided=c.get("two_sided", False))
     if c["kind"] == "token":
         o = m.attend_token(s["q"], s["k"], s["v"], s["cache_k"], s["cache_v"], s["pos"], s["bias"], **over)
