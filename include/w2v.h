@@ -510,6 +510,132 @@ int32_t w2v_sample_pairs_noalloc(w2v_handle *h, const int32_t *tokens, uint64_t 
                                  uint32_t negatives, int32_t *centre, int32_t *context, int32_t *negs,
                                  uint64_t cap, uint64_t *n_pairs, w2v_step_stats *stats);
 
+/*
+ * ---- Reader operators (no counterpart in the paper: what a program does with trained vectors) ----
+ * A reader turns the static vector of every word of a token stream into a vector of the word in its
+ * place and answers with words: layer norm over the rows, attention over a window of the word's
+ * sentence, both with their gradients, the same attention for one new word per sequence, and the
+ * product of a few vectors with a whole table held in 4 bits.  All arrays are device memory; all
+ * calls are asynchronous on the handle's stream (arrays that another stream wrote need the caller's
+ * event), and wait only when scratch grows on the first call of a larger size.  Sums, statistics and
+ * softmaxes are held in 32 bits whatever the arrays' type; every result is the same on every call with
+ * the same inputs (nothing is added up in an order that changes).
+ */
+enum { W2V_TYPE_F32 = 0, W2V_TYPE_BF16 = 1, W2V_TYPE_F16 = 2 };
+
+/*
+ * Layer norm of `rows` rows of d columns: y = (x - mean) / sqrt(var + eps) * gamma + beta, var the mean
+ * square distance from the mean.
+ *   x, y        row r starts at element r * stride (any stride >= d, any alignment of whole elements;
+ *               16-byte aligned rows whose length is a multiple of 4 or 8 elements are the fast ones).
+ *               y has the type of x, or any of the three types when x is W2V_TYPE_F32.  y may be x.
+ *   gamma, beta d floats.
+ *   mean, rstd  rows floats each, for the backward call; may be NULL.
+ * Limits: 1 <= d <= 8192, rows < 2^40.  Errors: W2V_ERR_ARG, W2V_ERR_CUDA.
+ */
+int32_t w2v_layer_norm(w2v_handle *h, uint64_t rows, uint32_t d, const void *x, uint64_t x_stride, uint32_t x_type,
+                       const float *gamma, const float *beta, float eps, void *y, uint64_t y_stride, uint32_t y_type,
+                       float *mean, float *rstd);
+
+/*
+ * Its gradient: dx (type of x), and dgamma, dbeta (d floats, written, not added to; zeros for no rows).
+ *   dy  has the type y had.  dx may be dy when their types are the same.
+ */
+int32_t w2v_layer_norm_backward(w2v_handle *h, uint64_t rows, uint32_t d, const void *dy, uint64_t dy_stride, uint32_t y_type,
+                                const void *x, uint64_t x_stride, uint32_t x_type, const float *gamma, const float *mean,
+                                const float *rstd, void *dx, uint64_t dx_stride, float *dgamma, float *dbeta);
+
+/*
+ * Sentence bounds of a token stream (-1 ends a sentence), once per chunk for every layer and direction:
+ *   spans  n pairs of int32: first position of the token's sentence and one past its last.  A sentence
+ *          end, and a word outside [0, vocab), gets an empty pair: it sees nothing and is not seen.
+ */
+int32_t w2v_sentence_spans(w2v_handle *h, const int32_t *tokens, uint64_t n, int32_t *spans);
+
+/* What an attention call sees and how it is laid out. */
+typedef struct {
+    uint32_t type;       /* W2V_TYPE_BF16 or W2V_TYPE_F16: q, k, v, o and their gradients */
+    uint32_t heads;      /* query heads, 1..1024, a multiple of kv_heads */
+    uint32_t kv_heads;   /* head h reads key/value head h / (heads / kv_heads) */
+    uint32_t head_dim;   /* a multiple of 8 in 8..128 */
+    uint32_t left;       /* a word sees this many words before it (below 2^30) */
+    uint32_t right;      /* and after it (0: reads forwards only) */
+    uint32_t sinks;      /* the first words of its sentence that it sees however far back they are, at most 64 */
+    uint32_t buckets;    /* rows of the bias table, 0 = no bias */
+    uint32_t reach;      /* distance from which on every key falls in the last bucket, or nearly; at most 1024 */
+    uint32_t two_sided;  /* 1: the second half of the buckets is for keys after the query */
+    float scale;         /* of the products q.k */
+} w2v_window;
+
+/*
+ * First distance of each bucket of one side (n = buckets, or buckets / 2 when two-sided): the first e = n/2
+ * buckets hold one distance each, bucket e + k starts at ceil(e (reach / e)^(k / (n - e))).  A key after the
+ * query counts as distance 0 when the table is one-sided.  Host function, no handle; starts: n int32, host.
+ * Limits: 2 <= buckets <= 64 (two-sided: even, at least 4), n/2 < reach <= 1024.
+ */
+int32_t w2v_bucket_starts(uint32_t buckets, uint32_t reach, uint32_t two_sided, int32_t *starts);
+
+/*
+ * Attention over the window: for every position i and head, over the keys j of the same sentence with
+ * i - left <= j <= i + right, or j among the sentence's first `sinks` words and before i,
+ *   o(i) = sum_j softmax_j(scale q(i).k(j) + bias[bucket(j - i)][head]) v(j);
+ * a position that sees nothing (a sentence end, a word outside the vocabulary) gets zeros.
+ *   spans       of w2v_sentence_spans.
+ *   q, k, v, o  [n][heads or kv_heads][head_dim], heads side by side, `stride` elements from position to
+ *               position (a multiple of 8; one packed projection can hold q, k and v), 16-byte aligned.
+ *   bias        [buckets][heads] floats, NULL when buckets is 0.
+ *               A bias of -infinity hides a bucket, as one of the lowest float does where another bucket is seen.
+ *   o_full      [n][heads][head_dim] floats, dense, or NULL: o before it is rounded; lse [heads][n] floats, or
+ *               NULL: both for the backward call (o_full only for dbias, whose sums cancel so far that the
+ *               rounding of o would show in them).
+ * Errors: W2V_ERR_ARG, W2V_ERR_NOMEM, W2V_ERR_CUDA.  A block that waits too long on its own pipeline gives
+ * up; w2v_sync then returns W2V_ERR_CUDA.
+ */
+int32_t w2v_attend(w2v_handle *h, const w2v_window *w, uint64_t n, const int32_t *spans, const void *q, uint64_t q_stride,
+                   const void *k, uint64_t k_stride, const void *v, uint64_t v_stride, const float *bias, void *o,
+                   uint64_t o_stride, float *o_full, float *lse);
+
+/*
+ * Its gradient.  d_o is laid out as o; dq as q, dk and dv as k and v (their own strides); gradients of
+ * shared key/value heads are summed over the query heads.  All are written in full (zeros where nothing is seen).
+ *   dbias  [buckets][heads] floats, written; NULL if not wanted.  Needs o_full.
+ */
+int32_t w2v_attend_backward(w2v_handle *h, const w2v_window *w, uint64_t n, const int32_t *spans, const void *q, uint64_t q_stride,
+                            const void *k, uint64_t k_stride, const void *v, uint64_t v_stride, const float *bias, const void *o,
+                            uint64_t o_stride, const float *o_full, const float *lse, const void *d_o, uint64_t do_stride, void *dq,
+                            uint64_t dq_stride, void *dk, uint64_t dk_stride, void *dv, uint64_t dv_stride, float *dbias);
+
+/*
+ * One new word for each of `batch` sequences, over a cache of fixed size: the first `sinks` positions keep
+ * their places, a later position p lies at place sinks + (p - sinks) mod (places - sinks).  Writes k and v into
+ * the place of position pos[b] and gives o of the new word over its window and the sinks.  right and
+ * two_sided must be 0.
+ *   pos       batch int32 (device): position of the new word, counted from 0; negative = an empty place in
+ *             the batch (o is zero, the cache is left alone).  The caller adds one after the call.
+ *   q, o      [batch][heads][head_dim];  k, v  [batch][kv_heads][head_dim];  dense, 16-byte aligned.
+ *   cache_k, cache_v  [batch][places][kv_heads][head_dim], places >= sinks + left + 1.
+ */
+int32_t w2v_attend_token(w2v_handle *h, const w2v_window *w, uint32_t batch, const int32_t *pos, const void *q, const void *k,
+                         const void *v, void *cache_k, void *cache_v, uint64_t places, const float *bias, void *o);
+
+/*
+ * A table in 4 bits: row r is 16 ceil(d / 32) bytes, byte b holds columns 2b (low half) and 2b + 1 (high half)
+ * as value + 8, columns past d hold value 0; every `group` columns (32, 64 or 128) share one bf16 scale,
+ * scales being [n][ceil(d / group)].  Scale = max |x| / 7 rounded to bf16, value = x / scale rounded to the
+ * nearest whole number and held to -7..7 (a group of zeros has scale 0).
+ *   rows  n finite fp32 rows, row_stride >= d elements apart (a table of this handle, for instance).
+ *   packed 16-byte aligned.  Limits: d <= 16384, n < 2^31.
+ */
+int32_t w2v_fourbit_pack(w2v_handle *h, const float *rows, uint64_t n, uint32_t d, uint64_t row_stride, uint32_t group,
+                         uint8_t *packed, void *scales);
+
+/*
+ * out[v][r] = sum over the groups g of scale[r][g] * sum over the group's columns of value[r][c] x[v][c], for m <= 8
+ * vectors x (fp32, x_stride >= d apart) and every row; out fp32, out_stride >= rows apart.
+ */
+int32_t w2v_fourbit_scores(w2v_handle *h, const float *x, uint32_t m, uint64_t x_stride, const uint8_t *packed, const void *scales,
+                           uint64_t rows, uint32_t d, uint32_t group, float *out, uint64_t out_stride);
+
 /* Text of the last error on this handle (never NULL; h == NULL gives a generic text). */
 const char *w2v_last_error(w2v_handle *h);
 

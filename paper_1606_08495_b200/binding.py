@@ -29,6 +29,8 @@ EXPORTS = (
     "w2v_profile_read", "w2v_get_launch_count", "w2v_set_tuning", "w2v_last_error",
     "w2v_sample_pairs_noalloc", "w2v_peer_barrier", "w2v_probe_rows",
     "w2v_selftest_bounded_wait", "w2v_probe_bulk_ring", "w2v_probe_mma_ring",
+    "w2v_layer_norm", "w2v_layer_norm_backward", "w2v_sentence_spans", "w2v_bucket_starts", "w2v_attend",
+    "w2v_attend_backward", "w2v_attend_token", "w2v_fourbit_pack", "w2v_fourbit_scores",
 )
 
 
@@ -39,6 +41,13 @@ class StepStats(C.Structure):
 
     def as_dict(self):
         return {k: int(getattr(self, k)) for k, _ in self._fields_ if k != "reserved"}
+
+
+class Window(C.Structure):
+    """w2v_window: what an attention call sees and how it is laid out."""
+    _fields_ = [("type", C.c_uint32), ("heads", C.c_uint32), ("kv_heads", C.c_uint32), ("head_dim", C.c_uint32),
+                ("left", C.c_uint32), ("right", C.c_uint32), ("sinks", C.c_uint32), ("buckets", C.c_uint32),
+                ("reach", C.c_uint32), ("two_sided", C.c_uint32), ("scale", C.c_float)]
 
 
 class W2VError(RuntimeError):
@@ -93,6 +102,16 @@ def load():
         "w2v_write_rows": [vp, u32, vp, u64, vp],
         "w2v_topk_cosine": [vp, u32, vp, u64, u64, u64, u32, C.c_float, vp, vp],
         "w2v_set_retrieval_kernel": [vp, u32],
+        "w2v_layer_norm": [vp, u64, u32, vp, u64, u32, vp, vp, C.c_float, vp, u64, u32, vp, vp],
+        "w2v_layer_norm_backward": [vp, u64, u32, vp, u64, u32, vp, u64, u32, vp, vp, vp, vp, u64, vp, vp],
+        "w2v_sentence_spans": [vp, vp, u64, vp],
+        "w2v_bucket_starts": [u32, u32, u32, vp],
+        "w2v_attend": [vp, C.POINTER(Window), u64, vp, vp, u64, vp, u64, vp, u64, vp, vp, u64, vp, vp],
+        "w2v_attend_backward": [vp, C.POINTER(Window), u64, vp, vp, u64, vp, u64, vp, u64, vp, vp, u64, vp, vp,
+                                vp, u64, vp, u64, vp, u64, vp, u64, vp],
+        "w2v_attend_token": [vp, C.POINTER(Window), u32, vp, vp, vp, vp, vp, vp, u64, vp, vp],
+        "w2v_fourbit_pack": [vp, vp, u64, u32, u64, u32, vp, vp],
+        "w2v_fourbit_scores": [vp, vp, u32, u64, vp, vp, u64, u32, u32, vp, u64],
         "w2v_set_step": [vp, u64],
         "w2v_set_interleave": [vp, u32, u32],
         "w2v_get_step": [vp, C.POINTER(u64)],
@@ -295,6 +314,56 @@ def w2v_set_retrieval_kernel(h, kind):
     return _check(h, load().w2v_set_retrieval_kernel(h, int(kind)))
 
 
+# The reader operators take device addresses (`data_ptr()`), since rows may be strided views.
+TYPE_F32, TYPE_BF16, TYPE_F16 = 0, 1, 2
+_TYPES = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16}
+
+
+def w2v_layer_norm(h, rows, d, x, x_stride, x_type, gamma, beta, eps, y, y_stride, y_type, mean, rstd):
+    return _check(h, load().w2v_layer_norm(h, rows, d, x, x_stride, x_type, gamma, beta, eps, y, y_stride, y_type, mean, rstd))
+
+
+def w2v_layer_norm_backward(h, rows, d, dy, dy_stride, y_type, x, x_stride, x_type, gamma, mean, rstd, dx, dx_stride,
+                            dgamma, dbeta):
+    return _check(h, load().w2v_layer_norm_backward(h, rows, d, dy, dy_stride, y_type, x, x_stride, x_type, gamma, mean, rstd,
+                                                    dx, dx_stride, dgamma, dbeta))
+
+
+def w2v_sentence_spans(h, tokens, n, spans):
+    return _check(h, load().w2v_sentence_spans(h, tokens, n, spans))
+
+
+def w2v_bucket_starts(buckets, reach, two_sided):
+    """First distance of each bucket of one side (int32 numpy array)."""
+    starts = np.empty(max(1, buckets // 2 if two_sided else buckets), dtype=np.int32)
+    rc = load().w2v_bucket_starts(buckets, reach, int(two_sided), starts.ctypes.data)
+    if rc != W2V_OK:
+        raise W2VError(rc, "buckets must be in 2..64 (two-sided: even, at least 4), reach above half of a side's and at most 1024")
+    return starts
+
+
+def w2v_attend(h, window, n, spans, q, q_stride, k, k_stride, v, v_stride, bias, o, o_stride, o_full, lse):
+    return _check(h, load().w2v_attend(h, window, n, spans, q, q_stride, k, k_stride, v, v_stride, bias, o, o_stride, o_full, lse))
+
+
+def w2v_attend_backward(h, window, n, spans, q, q_stride, k, k_stride, v, v_stride, bias, o, o_stride, o_full, lse,
+                        d_o, do_stride, dq, dq_stride, dk, dk_stride, dv, dv_stride, dbias):
+    return _check(h, load().w2v_attend_backward(h, window, n, spans, q, q_stride, k, k_stride, v, v_stride, bias, o, o_stride,
+                                                o_full, lse, d_o, do_stride, dq, dq_stride, dk, dk_stride, dv, dv_stride, dbias))
+
+
+def w2v_attend_token(h, window, batch, pos, q, k, v, cache_k, cache_v, places, bias, o):
+    return _check(h, load().w2v_attend_token(h, window, batch, pos, q, k, v, cache_k, cache_v, places, bias, o))
+
+
+def w2v_fourbit_pack(h, rows, n, d, row_stride, group, packed, scales):
+    return _check(h, load().w2v_fourbit_pack(h, rows, n, d, row_stride, group, packed, scales))
+
+
+def w2v_fourbit_scores(h, x, m, x_stride, packed, scales, rows, d, group, out, out_stride):
+    return _check(h, load().w2v_fourbit_scores(h, x, m, x_stride, packed, scales, rows, d, group, out, out_stride))
+
+
 def w2v_set_step(h, step_id):
     return _check(h, load().w2v_set_step(h, int(step_id)))
 
@@ -458,6 +527,175 @@ class W2V:
         w2v_topk_cosine(self.h, which, q, q.numel(), cand_lo, cand_hi, K, tau, ids, cs)
         w2v_sync(self.h)
         return ids.view(-1, K).cpu().numpy(), cs.view(-1, K).cpu().numpy()
+
+    # ---- reader operators: tensors on this model's device, results on its stream ----
+    def _on(self, *tensors):
+        for t in tensors:
+            if t is not None and t.device != self.U.device:
+                raise ValueError(f"tensor on {t.device}, this model is on {self.U.device}")
+
+    @staticmethod
+    def _type(t):
+        if t.dtype not in _TYPES:
+            raise TypeError(f"{t.dtype} is not one of float32, bfloat16, float16")
+        return _TYPES[t.dtype]
+
+    def _weights(self, d, *tensors):
+        for t in tensors:
+            if t.dtype != torch.float32 or t.shape != (d,) or not t.is_contiguous():
+                raise ValueError(f"weights must be contiguous float32 of shape ({d},)")
+
+    @staticmethod
+    def _rows(t):
+        """A tensor whose last dimension is dense, as (rows, d, stride between rows, tensor)."""
+        d = t.shape[-1]
+        if t.dim() == 2 and (t.stride(1) == 1 or d == 1) and (t.stride(0) >= d or t.shape[0] <= 1):
+            return t.shape[0], d, max(t.stride(0), d), t
+        t = t.contiguous()
+        return t.numel() // max(d, 1), d, d, t
+
+    def layer_norm(self, x, gamma, beta, eps=1e-5, out_dtype=None):
+        """(y, what layer_norm_backward needs).  x: [..., d], rows of a padded table included."""
+        self._on(x, gamma, beta)
+        rows, d, ld, xv = self._rows(x)
+        self._weights(d, gamma, beta)
+        y = torch.empty(x.shape, dtype=out_dtype or x.dtype, device=x.device)
+        stats = torch.empty(2, rows, dtype=torch.float32, device=x.device)
+        w2v_layer_norm(self.h, rows, d, xv.data_ptr(), ld, self._type(x), gamma.data_ptr(), beta.data_ptr(), eps, y.data_ptr(), d,
+                       self._type(y), stats.data_ptr(), stats.data_ptr() + 4 * rows)
+        return y, (xv, gamma, stats, y.dtype, x.shape)
+
+    def layer_norm_backward(self, dy, saved):
+        """(dx, dgamma, dbeta) from dy and what layer_norm returned."""
+        x, gamma, stats, y_dtype, shape = saved
+        self._on(dy)
+        if dy.dtype != y_dtype or dy.shape != shape:
+            raise ValueError(f"dy must be {y_dtype} of shape {tuple(shape)}")
+        rows, d, ld, dy = self._rows(dy)
+        _, _, ldx, _ = self._rows(x)
+        dx = torch.empty(shape, dtype=x.dtype, device=x.device)
+        dw = torch.empty(2, d, dtype=torch.float32, device=x.device)
+        w2v_layer_norm_backward(self.h, rows, d, dy.data_ptr(), ld, _TYPES[y_dtype], x.data_ptr(), ldx, self._type(x),
+                                gamma.data_ptr(), stats.data_ptr(), stats.data_ptr() + 4 * rows, dx.data_ptr(), d,
+                                dw.data_ptr(), dw.data_ptr() + 4 * d)
+        return dx, dw[0], dw[1]
+
+    def sentence_spans(self, tokens):
+        """[n, 2] int32: sentence bounds of every position of a token stream (-1 ends a sentence)."""
+        self._on(tokens)
+        t = tokens if tokens.dtype == torch.int32 and tokens.is_contiguous() else tokens.to(torch.int32).contiguous()
+        spans = torch.empty(t.numel(), 2, dtype=torch.int32, device=t.device)
+        w2v_sentence_spans(self.h, t.data_ptr(), t.numel(), spans.data_ptr())
+        return spans
+
+    @staticmethod
+    def _heads(t, what):
+        """[n, heads, dim] with dense heads side by side: (tensor, elements from position to position)."""
+        if t.dim() != 3:
+            raise ValueError(f"{what} must be [n, heads, head_dim]")
+        n, heads, dim = t.shape
+        width = heads * dim
+        if t.stride(2) == 1 and (heads == 1 or t.stride(1) == dim) and t.data_ptr() % 16 == 0:
+            if n <= 1:
+                return t, width
+            if t.stride(0) >= width and t.stride(0) % 8 == 0:
+                return t, t.stride(0)
+        t = t.contiguous()
+        return (t if t.data_ptr() % 16 == 0 else t.clone()), width
+
+    def _window(self, q, k, v, bias, left, right, sinks, reach, two_sided, scale):
+        self._on(q, k, v, bias)
+        if not (q.dtype == k.dtype == v.dtype) or q.dtype not in (torch.bfloat16, torch.float16):
+            raise TypeError("q, k and v must all be bfloat16 or all float16")
+        if k.shape != v.shape or k.shape[0] != q.shape[0] or k.shape[-1] != q.shape[-1]:
+            raise ValueError("q [n, heads, dim], k and v [n, kv_heads, dim] do not fit together")
+        if bias is not None and (bias.dtype != torch.float32 or bias.dim() != 2 or bias.shape[1] != q.shape[1] or not bias.is_contiguous()):
+            raise ValueError("bias must be contiguous float32 [buckets, heads]")
+        return Window(_TYPES[q.dtype], q.shape[1], k.shape[1], q.shape[2], left, right, sinks, 0 if bias is None else bias.shape[0],
+                      reach, int(two_sided), q.shape[2] ** -0.5 if scale is None else scale)
+
+    def attend(self, q, k, v, spans, bias=None, left=0, right=0, sinks=0, reach=128, two_sided=False, scale=None, train=False):
+        """o [n, heads, dim] of attention over a window of the sentence (w2v_attend); with train=True
+        (o, what attend_backward needs)."""
+        w = self._window(q, k, v, bias, left, right, sinks, reach, two_sided, scale)
+        n = q.shape[0]
+        if spans.dtype != torch.int32 or spans.shape != (n, 2) or not spans.is_contiguous():
+            raise ValueError(f"spans must be the contiguous int32 [{n}, 2] of sentence_spans")
+        self._on(spans)
+        (q, ldq), (k, ldk), (v, ldv) = self._heads(q, "q"), self._heads(k, "k"), self._heads(v, "v")
+        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        lse = torch.empty(q.shape[1], n, dtype=torch.float32, device=q.device) if train else None
+        full = torch.empty(q.shape, dtype=torch.float32, device=q.device) if train and bias is not None else None
+        w2v_attend(self.h, w, n, spans.data_ptr(), q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv,
+                   None if bias is None else bias.data_ptr(), o.data_ptr(), w.heads * w.head_dim,
+                   None if full is None else full.data_ptr(), None if lse is None else lse.data_ptr())
+        return (o, (w, spans, q, k, v, bias, o, full, lse)) if train else o
+
+    def attend_backward(self, d_o, saved):
+        """(dq, dk, dv, dbias) from d_o and what attend(train=True) returned; dbias is None without a bias."""
+        w, spans, q, k, v, bias, o, full, lse = saved
+        self._on(d_o)
+        if d_o.dtype != q.dtype or d_o.shape != q.shape:
+            raise ValueError(f"d_o must be {q.dtype} of shape {tuple(q.shape)}")
+        d_o, ld_do = self._heads(d_o, "d_o")
+        (q, ldq), (k, ldk), (v, ldv) = self._heads(q, "q"), self._heads(k, "k"), self._heads(v, "v")
+        dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+        dbias = None if bias is None else torch.empty_like(bias)
+        wq, wk = w.heads * w.head_dim, w.kv_heads * w.head_dim
+        w2v_attend_backward(self.h, w, q.shape[0], spans.data_ptr(), q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv,
+                            None if bias is None else bias.data_ptr(), o.data_ptr(), wq, None if full is None else full.data_ptr(),
+                            lse.data_ptr(), d_o.data_ptr(), ld_do, dq.data_ptr(), wq, dk.data_ptr(), wk, dv.data_ptr(), wk,
+                            None if dbias is None else dbias.data_ptr())
+        return dq, dk, dv, dbias
+
+    def attend_token(self, q, k, v, cache_k, cache_v, pos, bias=None, left=0, right=0, sinks=0, reach=128, two_sided=False, scale=None):
+        """o [batch, heads, dim] of one new token per sequence at positions `pos`; writes k and v into the
+        caches [batch, places, kv_heads, dim] (w2v_attend_token)."""
+        w = self._window(q, k, v, bias, left, right, sinks, reach, two_sided, scale)
+        batch = q.shape[0]
+        if pos.dtype != torch.int32 or pos.shape != (batch,) or not pos.is_contiguous():
+            raise ValueError(f"pos must be contiguous int32 of shape ({batch},)")
+        for c in (cache_k, cache_v):
+            if c.dtype != q.dtype or c.dim() != 4 or c.shape[0] != batch or c.shape[2:] != k.shape[1:] or not c.is_contiguous():
+                raise ValueError("caches must be contiguous [batch, places, kv_heads, dim] of the type of q")
+        if cache_k.shape != cache_v.shape:
+            raise ValueError("cache_k and cache_v must have the same shape")
+        self._on(pos, cache_k, cache_v)
+        q, k, v = q.contiguous(), k.contiguous(), v.contiguous()
+        o = torch.empty_like(q)
+        w2v_attend_token(self.h, w, batch, pos.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), cache_k.data_ptr(),
+                         cache_v.data_ptr(), cache_k.shape[1], None if bias is None else bias.data_ptr(), o.data_ptr())
+        return o
+
+    def fourbit_pack(self, rows, group=32):
+        """(packed [n, 16 ceil(d/32)] uint8, scales [n, ceil(d/group)] bfloat16) of fp32 rows [n, d]."""
+        self._on(rows)
+        if rows.dtype != torch.float32 or rows.dim() != 2:
+            raise ValueError("rows must be float32 [n, d]")
+        n, d, ld, rows = self._rows(rows)
+        if d < 1 or group < 1:
+            raise ValueError("d and group must be positive")
+        packed = torch.empty(n, 16 * ((d + 31) // 32), dtype=torch.uint8, device=rows.device)
+        scales = torch.empty(n, (d + group - 1) // group, dtype=torch.bfloat16, device=rows.device)
+        w2v_fourbit_pack(self.h, rows.data_ptr(), n, d, ld, group, packed.data_ptr(), scales.data_ptr())
+        return packed, scales
+
+    def fourbit_scores(self, x, packed, scales, group=32):
+        """[m, rows] fp32: products of m <= 8 fp32 vectors with every row of a table of fourbit_pack."""
+        self._on(x, packed, scales)
+        if x.dtype != torch.float32 or x.dim() != 2:
+            raise ValueError("x must be float32 [m, d]")
+        m, d, ld, x = self._rows(x)
+        if d < 1 or group < 1:
+            raise ValueError("d and group must be positive")
+        n = packed.shape[0]
+        if packed.dtype != torch.uint8 or packed.shape != (n, 16 * ((d + 31) // 32)) or not packed.is_contiguous():
+            raise ValueError(f"packed must be contiguous uint8 [rows, {16 * ((d + 31) // 32)}] for d = {d}")
+        if scales.dtype != torch.bfloat16 or scales.shape != (n, (d + group - 1) // group) or not scales.is_contiguous():
+            raise ValueError("scales must be contiguous bfloat16 [rows, ceil(d / group)]")
+        out = torch.empty(m, n, dtype=torch.float32, device=x.device)
+        w2v_fourbit_scores(self.h, x.data_ptr(), m, ld, packed.data_ptr(), scales.data_ptr(), n, d, group, out.data_ptr(), max(n, 1))
+        return out
 
     def set_step(self, s):
         w2v_set_step(self.h, s)
