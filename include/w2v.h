@@ -585,24 +585,23 @@ int32_t w2v_bucket_starts(uint32_t buckets, uint32_t reach, uint32_t two_sided, 
  *               position (a multiple of 8; one packed projection can hold q, k and v), 16-byte aligned.
  *   bias        [buckets][heads] floats, NULL when buckets is 0.
  *               A bias of -infinity hides a bucket, as one of the lowest float does where another bucket is seen.
- *   o_full      [n][heads][head_dim] floats, dense, or NULL: o before it is rounded; lse [heads][n] floats, or
- *               NULL: both for the backward call (o_full only for dbias, whose sums cancel so far that the
- *               rounding of o would show in them).
+ *   lse         [heads][n] floats for the backward call, or NULL: base-2 logarithm of the softmax sum, +infinity
+ *               for a position that sees nothing.
  * Errors: W2V_ERR_ARG, W2V_ERR_NOMEM, W2V_ERR_CUDA.  A block that waits too long on its own pipeline gives
  * up; w2v_sync then returns W2V_ERR_CUDA.
  */
 int32_t w2v_attend(w2v_handle *h, const w2v_window *w, uint64_t n, const int32_t *spans, const void *q, uint64_t q_stride,
                    const void *k, uint64_t k_stride, const void *v, uint64_t v_stride, const float *bias, void *o,
-                   uint64_t o_stride, float *o_full, float *lse);
+                   uint64_t o_stride, float *lse);
 
 /*
  * Its gradient.  d_o is laid out as o; dq as q, dk and dv as k and v (their own strides); gradients of
  * shared key/value heads are summed over the query heads.  All are written in full (zeros where nothing is seen).
- *   dbias  [buckets][heads] floats, written; NULL if not wanted.  Needs o_full.
+ *   dbias  [buckets][heads] floats, written; NULL if not wanted. 
  */
 int32_t w2v_attend_backward(w2v_handle *h, const w2v_window *w, uint64_t n, const int32_t *spans, const void *q, uint64_t q_stride,
                             const void *k, uint64_t k_stride, const void *v, uint64_t v_stride, const float *bias, const void *o,
-                            uint64_t o_stride, const float *o_full, const float *lse, const void *d_o, uint64_t do_stride, void *dq,
+                            uint64_t o_stride, const float *lse, const void *d_o, uint64_t do_stride, void *dq,
                             uint64_t dq_stride, void *dk, uint64_t dk_stride, void *dv, uint64_t dv_stride, float *dbias);
 
 /*

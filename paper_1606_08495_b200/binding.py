@@ -106,8 +106,8 @@ def load():
         "w2v_layer_norm_backward": [vp, u64, u32, vp, u64, u32, vp, u64, u32, vp, vp, vp, vp, u64, vp, vp],
         "w2v_sentence_spans": [vp, vp, u64, vp],
         "w2v_bucket_starts": [u32, u32, u32, vp],
-        "w2v_attend": [vp, C.POINTER(Window), u64, vp, vp, u64, vp, u64, vp, u64, vp, vp, u64, vp, vp],
-        "w2v_attend_backward": [vp, C.POINTER(Window), u64, vp, vp, u64, vp, u64, vp, u64, vp, vp, u64, vp, vp,
+        "w2v_attend": [vp, C.POINTER(Window), u64, vp, vp, u64, vp, u64, vp, u64, vp, vp, u64, vp],
+        "w2v_attend_backward": [vp, C.POINTER(Window), u64, vp, vp, u64, vp, u64, vp, u64, vp, vp, u64, vp,
                                 vp, u64, vp, u64, vp, u64, vp, u64, vp],
         "w2v_attend_token": [vp, C.POINTER(Window), u32, vp, vp, vp, vp, vp, vp, u64, vp, vp],
         "w2v_fourbit_pack": [vp, vp, u64, u32, u64, u32, vp, vp],
@@ -342,14 +342,14 @@ def w2v_bucket_starts(buckets, reach, two_sided):
     return starts
 
 
-def w2v_attend(h, window, n, spans, q, q_stride, k, k_stride, v, v_stride, bias, o, o_stride, o_full, lse):
-    return _check(h, load().w2v_attend(h, window, n, spans, q, q_stride, k, k_stride, v, v_stride, bias, o, o_stride, o_full, lse))
+def w2v_attend(h, window, n, spans, q, q_stride, k, k_stride, v, v_stride, bias, o, o_stride, lse):
+    return _check(h, load().w2v_attend(h, window, n, spans, q, q_stride, k, k_stride, v, v_stride, bias, o, o_stride, lse))
 
 
-def w2v_attend_backward(h, window, n, spans, q, q_stride, k, k_stride, v, v_stride, bias, o, o_stride, o_full, lse,
+def w2v_attend_backward(h, window, n, spans, q, q_stride, k, k_stride, v, v_stride, bias, o, o_stride, lse,
                         d_o, do_stride, dq, dq_stride, dk, dk_stride, dv, dv_stride, dbias):
     return _check(h, load().w2v_attend_backward(h, window, n, spans, q, q_stride, k, k_stride, v, v_stride, bias, o, o_stride,
-                                                o_full, lse, d_o, do_stride, dq, dq_stride, dk, dk_stride, dv, dv_stride, dbias))
+                                                lse, d_o, do_stride, dq, dq_stride, dk, dk_stride, dv, dv_stride, dbias))
 
 
 def w2v_attend_token(h, window, batch, pos, q, k, v, cache_k, cache_v, places, bias, o):
@@ -625,15 +625,14 @@ class W2V:
         (q, ldq), (k, ldk), (v, ldv) = self._heads(q, "q"), self._heads(k, "k"), self._heads(v, "v")
         o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         lse = torch.empty(q.shape[1], n, dtype=torch.float32, device=q.device) if train else None
-        full = torch.empty(q.shape, dtype=torch.float32, device=q.device) if train and bias is not None else None
         w2v_attend(self.h, w, n, spans.data_ptr(), q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv,
                    None if bias is None else bias.data_ptr(), o.data_ptr(), w.heads * w.head_dim,
-                   None if full is None else full.data_ptr(), None if lse is None else lse.data_ptr())
-        return (o, (w, spans, q, k, v, bias, o, full, lse)) if train else o
+                   None if lse is None else lse.data_ptr())
+        return (o, (w, spans, q, k, v, bias, o, lse)) if train else o
 
     def attend_backward(self, d_o, saved):
         """(dq, dk, dv, dbias) from d_o and what attend(train=True) returned; dbias is None without a bias."""
-        w, spans, q, k, v, bias, o, full, lse = saved
+        w, spans, q, k, v, bias, o, lse = saved
         self._on(d_o)
         if d_o.dtype != q.dtype or d_o.shape != q.shape:
             raise ValueError(f"d_o must be {q.dtype} of shape {tuple(q.shape)}")
@@ -643,8 +642,7 @@ class W2V:
         dbias = None if bias is None else torch.empty_like(bias)
         wq, wk = w.heads * w.head_dim, w.kv_heads * w.head_dim
         w2v_attend_backward(self.h, w, q.shape[0], spans.data_ptr(), q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv,
-                            None if bias is None else bias.data_ptr(), o.data_ptr(), wq, None if full is None else full.data_ptr(),
-                            lse.data_ptr(), d_o.data_ptr(), ld_do, dq.data_ptr(), wq, dk.data_ptr(), wk, dv.data_ptr(), wk,
+                            None if bias is None else bias.data_ptr(), o.data_ptr(), wq, lse.data_ptr(), d_o.data_ptr(), ld_do, dq.data_ptr(), wq, dk.data_ptr(), wk, dv.data_ptr(), wk,
                             None if dbias is None else dbias.data_ptr())
         return dq, dk, dv, dbias
 

@@ -1,304 +1,331 @@
-// Attention over a window of the word's sentence, forwards and backwards, and the sentence bounds.
-#include "w2v_device.cuh"
-#include "w2v_reader.h"
-#include "w2v_types.cuh"
+// Attention over a window of the sentence on the tensor cores.
+#include <type_traits>
+
+#include "w2v_attend.cuh"
 
 namespace w2v {
 
-// ---- sentence bounds ----------------------------------------------------------------------------
-// spans[t] = (first position of t's sentence, one past its last); a separator or a word that the
-// vocabulary does not have gets the empty span (t, t).  Two passes: the last and the first separator
-// of every tile, then every tile looks back and ahead for the nearest tile that has one.
-constexpr int kSpanThreads = 256, kSpanPer = 8, kSpanTile = kSpanThreads * kSpanPer;
+constexpr int kFwdThreads = 256;                 // warps 0-3: one softmax row per thread; warp 4: MMA; warps 5-7: copies
+constexpr int kFwdLoaders = 96;
+constexpr int kSoftmaxRegs = 200, kOtherRegs = 56;      // of 128 per thread at launch: 4 x 200 + 4 x 56 warps' shares = 8 x 128
+constexpr float kRescale = 8.f;                  // base-2: how far a row's scores may outgrow its reference before the output is rescaled
 
-uint64_t spans_tiles(uint64_t n) { return (n + kSpanTile - 1) / kSpanTile; }
+// NB = 64-column blocks of a head (1: head_dim <= 64, 2: up to 128).
+template <int NB>
+struct FwdShape {
+    static constexpr int kStages = NB == 1 ? 2 : 1;                 // of keys and of values each
+    static constexpr int kTileBytes = NB * kAttendTile * 128;
+    static constexpr bool kOwnP = NB == 1;                          // the weights have tensor memory of their own
+    static constexpr uint32_t kS = 0, kP = NB == 1 ? 128 : 0, kO = NB == 1 ? 192 : 128;   // columns
+    static constexpr int kSmem = kTileBytes * (1 + 2 * kStages) + 1024;
+};
 
-__global__ void __launch_bounds__(kSpanThreads)
-span_tiles_kernel(const int32_t *tokens, uint64_t n, int2 *tile_ends)
+struct FwdShared {
+    uint64_t q_full, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full, s_free, p_full, pv_done;
+    uint32_t tmem;
+    int abort_flag;
+    int32_t limits[4][6];                        // per warp: least lo, largest hi, least s, largest lo, least hi, any row
+    uint32_t vis[2][4];                          // per key stage: which keys are words
+};
+
+template <typename T, int NB>
+__global__ void __launch_bounds__(kFwdThreads, 2)
+attend_tc_kernel(AttendParams p, int *error)
 {
-    __shared__ int first, last;
-    if (threadIdx.x == 0) { first = INT32_MAX; last = -1; }
-    __syncthreads();
-    const uint64_t t0 = (uint64_t)blockIdx.x * kSpanTile;
-    for (int i = 0; i < kSpanPer; ++i) {
-        const uint64_t t = t0 + i * kSpanThreads + threadIdx.x;
-        if (t < n && tokens[t] == -1) { atomicMin(&first, (int)t); atomicMax(&last, (int)t); }
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) tile_ends[blockIdx.x] = make_int2(first, last);
-}
+    using Sh = FwdShape<NB>;
+    constexpr bool kBf16 = sizeof(T) == 2 && std::is_same<T, __nv_bfloat16>::value;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ FwdShared sh;
+    unsigned char *smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
+    const uint32_t qs = smem_addr(smem), ks = qs + Sh::kTileBytes, vs = ks + Sh::kStages * Sh::kTileBytes;
+    float *lut = reinterpret_cast<float *>(smem + Sh::kTileBytes * (1 + 2 * Sh::kStages));
 
-__global__ void __launch_bounds__(kSpanThreads)
-span_fill_kernel(const int32_t *tokens, uint64_t n, uint32_t vocab, const int2 *tile_ends, uint32_t tiles, int2 *spans)
-{
-    __shared__ int before, after, sh[kSpanThreads];
-    const uint32_t tid = threadIdx.x;
-    if (tid == 0) { before = -1; after = (int)n; }
-    __syncthreads();
-    for (int64_t c = (int64_t)blockIdx.x; c > 0; c -= kSpanThreads) {           // nearest separator before the tile
-        const int64_t j = c - 1 - (int64_t)tid;
-        if (j >= 0 && tile_ends[j].y >= 0) atomicMax(&before, tile_ends[j].y);
-        __syncthreads();
-        if (before >= 0) break;
-        __syncthreads();
-    }
-    for (int64_t c = (int64_t)blockIdx.x + 1; c < (int64_t)tiles; c += kSpanThreads) {
-        const int64_t j = c + (int64_t)tid;
-        if (j < (int64_t)tiles && tile_ends[j].x < (int)n) atomicMin(&after, tile_ends[j].x);
-        __syncthreads();
-        if (after < (int)n) break;
-        __syncthreads();
-    }
-    __syncthreads();
-    const uint64_t t0 = (uint64_t)blockIdx.x * kSpanTile + (uint64_t)tid * kSpanPer;
-    int tok[kSpanPer], lo[kSpanPer], hi[kSpanPer];
-    int run = -1;
-#pragma unroll
-    for (int i = 0; i < kSpanPer; ++i) {
-        tok[i] = t0 + i < n ? tokens[t0 + i] : -2;
-        if (tok[i] == -1) run = (int)(t0 + i);
-        lo[i] = run;
-    }
-    sh[tid] = run;                                                               // last separator of the thread's tokens
-    __syncthreads();
-    for (int o = 1; o < kSpanThreads; o <<= 1) {
-        const int x = tid >= (uint32_t)o ? sh[tid - o] : -1;
-        __syncthreads();
-        sh[tid] = max(sh[tid], x);
-        __syncthreads();
-    }
-    const int back = max(before, tid ? sh[tid - 1] : -1);
-    __syncthreads();
-    run = INT32_MAX;
-#pragma unroll
-    for (int i = kSpanPer - 1; i >= 0; --i) {
-        if (tok[i] == -1) run = (int)(t0 + i);
-        hi[i] = run;
-    }
-    sh[tid] = run;
-    __syncthreads();
-    for (int o = 1; o < kSpanThreads; o <<= 1) {
-        const int x = tid + o < kSpanThreads ? sh[tid + o] : INT32_MAX;
-        __syncthreads();
-        sh[tid] = min(sh[tid], x);
-        __syncthreads();
-    }
-    const int ahead = min(after, tid + 1 < kSpanThreads ? sh[tid + 1] : INT32_MAX);
-#pragma unroll
-    for (int i = 0; i < kSpanPer; ++i)
-        if (t0 + i < n) {
-            const int t = (int)(t0 + i);
-            const bool word = tok[i] >= 0 && (uint32_t)tok[i] < vocab;
-            spans[t0 + i] = word ? make_int2(max(lo[i], back) + 1, min(hi[i], ahead)) : make_int2(t, t);
+    const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t h = blockIdx.x % p.heads, kvh = h / (p.heads / p.kv_heads);
+    const int32_t t0 = (int32_t)(blockIdx.x / p.heads) * kAttendTile;
+    const uint32_t dim16 = (p.dim + 15u) & ~15u;
+
+    if (tid == 0) {
+        mbar_init(&sh.q_full, kFwdLoaders);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&sh.k_full[i], kFwdLoaders); mbar_init(&sh.k_empty[i], 1 + kAttendTile);
+            mbar_init(&sh.v_full[i], kFwdLoaders); mbar_init(&sh.v_empty[i], 1);
         }
-}
-
-int launch_spans(const int32_t *tokens, uint64_t n, uint32_t vocab, int32_t *tile_ends, int2 *spans, cudaStream_t s)
-{
-    if (n == 0) return 0;
-    const uint32_t tiles = (uint32_t)spans_tiles(n);
-    int2 *ends = reinterpret_cast<int2 *>(tile_ends);
-    span_tiles_kernel<<<tiles, kSpanThreads, 0, s>>>(tokens, n, ends);
-    span_fill_kernel<<<tiles, kSpanThreads, 0, s>>>(tokens, n, vocab, ends, tiles, spans);
-    return cudaPeekAtLastError() == cudaSuccess ? 2 : -1;
-}
-
-// ---- attention, the simple form: one warp per row --------------------------------------------------
-constexpr float kLog2e = 1.4426950408889634f;
-
-__device__ __forceinline__ uint32_t bucket_of(const BucketStarts &b, int32_t rel)
-{
-    const int32_t far = b.two_sided ? abs(rel) : max(-rel, 0);
-    uint32_t lo = 0, hi = b.n - 1;
-    while (lo < hi) {
-        const uint32_t mid = (lo + hi + 1) >> 1;
-        if (b.start[mid] <= far) lo = mid; else hi = mid - 1;
+        mbar_init(&sh.s_full, 1); mbar_init(&sh.s_free, kAttendTile);
+        mbar_init(&sh.p_full, kAttendTile); mbar_init(&sh.pv_done, 1);
+        sh.abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    return lo + (b.two_sided && rel > 0 ? b.n : 0u);
-}
-
-// A score in base-2 units; a bias of the lowest float stays finite there.
-__device__ __forceinline__ float log2_score(float s) { return s == -INFINITY ? s : fmaxf(s, -1e30f) * kLog2e; }
-template <typename T>
-__device__ __forceinline__ void row_read(float (&x)[4], const T *p, uint32_t dim, uint32_t lane)
-{
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = lane + 32u * i < dim ? to_f32(p[lane + 32 * i]) : 0.f;
-}
-__device__ __forceinline__ float row_dot(const float (&a)[4], const float (&b)[4])
-{
-    return warp_sum(a[0] * b[0] + a[1] * b[1] + a[2] * b[2] + a[3] * b[3]);
-}
-template <typename T>
-__device__ __forceinline__ void row_write(T *p, const float (&x)[4], uint32_t dim, uint32_t lane)
-{
-#pragma unroll
-    for (int i = 0; i < 4; ++i) if (lane + 32u * i < dim) p[lane + 32 * i] = from_f32<T>(x[i]);
-}
-
-// Calls f(j) for every key that query i sees.
-template <typename F>
-__device__ __forceinline__ void each_key(const AttendParams &p, int64_t i, F f)
-{
-    const int2 sp = p.spans[i];
-    if (sp.y <= sp.x) return;
-    const int64_t lo = max((int64_t)sp.x, i - p.left), hi = min((int64_t)sp.y, i + p.right + 1);
-    for (int64_t j = sp.x; j < min((int64_t)sp.x + p.sinks, lo); ++j)
-        if (p.spans[j].y > p.spans[j].x) f(j);
-    for (int64_t j = lo; j < hi; ++j)
-        if (p.spans[j].y > p.spans[j].x) f(j);
-}
-
-template <typename T>
-__global__ void attend_kernel(AttendParams p)
-{
-    const uint32_t lane = threadIdx.x & 31, h = blockIdx.y, kvh = h / (p.heads / p.kv_heads);
-    const int64_t i = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
-    if (i >= p.n) return;
-    float q[4], acc[4] = {0.f, 0.f, 0.f, 0.f};
-    row_read(q, static_cast<const T *>(p.q) + i * p.ldq + h * p.dim, p.dim, lane);
-    float top = -INFINITY, sum = 0.f;
-    each_key(p, i, [&](int64_t j) {
-        float k[4], v[4];
-        row_read(k, static_cast<const T *>(p.k) + j * p.ldk + kvh * p.dim, p.dim, lane);
-        row_read(v, static_cast<const T *>(p.v) + j * p.ldv + kvh * p.dim, p.dim, lane);
-        float s = row_dot(q, k) * p.scale;
-        if (p.b.n) s += p.bias[(size_t)bucket_of(p.b, (int32_t)(j - i)) * p.heads + h];
-        s = log2_score(s);
-        const float m = fmaxf(top, s), from = m == -INFINITY ? 0.f : m, keep = exp2f(top - from), w = exp2f(s - from);
-        top = m;
-        sum = sum * keep + w;
-        for (int e = 0; e < 4; ++e) acc[e] = acc[e] * keep + w * v[e];
-    });
-    for (int e = 0; e < 4; ++e) acc[e] = sum > 0.f ? acc[e] / sum : 0.f;
-    row_write(static_cast<T *>(p.out) + i * p.ldo + h * p.dim, acc, p.dim, lane);
-    if (p.out_full) row_write(p.out_full + (i * p.heads + h) * p.dim, acc, p.dim, lane);
-    if (p.lse && lane == 0) p.lse[(int64_t)h * p.n + i] = sum > 0.f ? top + log2f(sum) : INFINITY;
-}
-
-// dQ, delta and the bias' gradient: one block per (128 queries, head).
-template <typename T>
-__global__ void attend_dq_kernel(AttendParams p)
-{
-    __shared__ float db[4][kMaxBuckets];
-    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, h = blockIdx.y, kvh = h / (p.heads / p.kv_heads);
-    for (uint32_t b = lane; b < kMaxBuckets; b += 32) db[warp][b] = 0.f;
-    __syncwarp();
-    const uint32_t buckets = p.b.n * (p.b.two_sided ? 2 : 1);
-    for (int r = warp; r < kAttendTile; r += 4) {
-        const int64_t i = (int64_t)blockIdx.x * kAttendTile + r;
-        if (i >= p.n) break;
-        float q[4], o[4], go[4], dq[4] = {0.f, 0.f, 0.f, 0.f};
-        row_read(q, static_cast<const T *>(p.q) + i * p.ldq + h * p.dim, p.dim, lane);
-        if (p.o_full) row_read(o, p.o_full + (i * p.heads + h) * p.dim, p.dim, lane);
-        else row_read(o, static_cast<const T *>(p.o) + i * p.ldo + h * p.dim, p.dim, lane);
-        row_read(go, static_cast<const T *>(p.d_o) + i * p.ld_do + h * p.dim, p.dim, lane);
-        const float delta = row_dot(o, go), lse = p.lse[(int64_t)h * p.n + i];
-        if (lane == 0) p.delta[(int64_t)h * p.n + i] = delta;
-        each_key(p, i, [&](int64_t j) {
-            float k[4], v[4];
-            row_read(k, static_cast<const T *>(p.k) + j * p.ldk + kvh * p.dim, p.dim, lane);
-            row_read(v, static_cast<const T *>(p.v) + j * p.ldv + kvh * p.dim, p.dim, lane);
-            float s = row_dot(q, k) * p.scale;
-            uint32_t b = 0;
-            if (p.b.n) { b = bucket_of(p.b, (int32_t)(j - i)); s += p.bias[(size_t)b * p.heads + h]; }
-            const float ds = exp2f(log2_score(s) - lse) * (row_dot(go, v) - delta);
-            if (p.b.n && lane == 0) db[warp][b] += ds;
-            for (int e = 0; e < 4; ++e) dq[e] += ds * p.scale * k[e];
-        });
-        row_write(static_cast<T *>(p.dq) + i * p.ld_dq + h * p.dim, dq, p.dim, lane);
+    RowLimits row = {0, 0, 0, 0};
+    if (warp < 4) {
+        row = row_limits(p, (int64_t)t0 + tid);
+        const bool any = row.hi > row.lo;
+        const int32_t lo = __reduce_min_sync(kFullMask, any ? row.lo : INT32_MAX), hi = __reduce_max_sync(kFullMask, row.hi);
+        const int32_t s = __reduce_min_sync(kFullMask, any ? row.s : INT32_MAX);
+        if (lane == 0) { sh.limits[warp][0] = lo; sh.limits[warp][1] = hi; sh.limits[warp][2] = s; }
     }
+    if (warp == 4) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&sh.tmem)), "r"(256));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    if (p.b.n) fill_bias(p, h, lut, tid, kFwdThreads);
+    tc_fence_before();
     __syncthreads();
-    if (p.dbias_part && threadIdx.x < buckets)
-        p.dbias_part[((size_t)blockIdx.x * p.heads + h) * buckets + threadIdx.x] =
-            db[0][threadIdx.x] + db[1][threadIdx.x] + db[2][threadIdx.x] + db[3][threadIdx.x];
-}
+    tc_fence_after();
+    const uint32_t tmem = sh.tmem;
+    volatile int *abort_flag = &sh.abort_flag;
+    // the run of keys [lo, hi) and the sinks [s, s_end) before it
+    int32_t lo = INT32_MAX, hi = 0, s = INT32_MAX;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        lo = min(lo, sh.limits[w][0]);
+        hi = max(hi, sh.limits[w][1]);
+        s = min(s, sh.limits[w][2]);
+    }
+    const int32_t s_end = hi ? min(s + p.sinks, lo) : 0;
+    const int32_t extra = s < s_end ? 1 : 0;
+    const int32_t tiles = hi ? extra + (hi - lo + kAttendTile - 1) / kAttendTile : 0;
+    auto tile_at = [&](int32_t t) { return extra && t == 0 ? s : lo + (t - extra) * kAttendTile; };
+    auto tile_keys = [&](int32_t t) { return extra && t == 0 ? s_end - s : min(kAttendTile, hi - tile_at(t)); };
 
-template <typename T>
-__global__ void attend_dkv_kernel(AttendParams p)
-{
-    const uint32_t lane = threadIdx.x & 31, kvh = blockIdx.y, group = p.heads / p.kv_heads;
-    const int64_t j = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
-    if (j >= p.n) return;
-    const int2 sp = p.spans[j];
-    float k[4], v[4], dk[4] = {0.f, 0.f, 0.f, 0.f}, dv[4] = {0.f, 0.f, 0.f, 0.f};
-    row_read(k, static_cast<const T *>(p.k) + j * p.ldk + kvh * p.dim, p.dim, lane);
-    row_read(v, static_cast<const T *>(p.v) + j * p.ldv + kvh * p.dim, p.dim, lane);
-    if (sp.y > sp.x) {
-        const int64_t lo = max((int64_t)sp.x, j - p.right);
-        const int64_t hi = j - sp.x < p.sinks ? sp.y : min((int64_t)sp.y, j + p.left + 1);
-        for (int64_t i = lo; i < hi; ++i) {
-            const int2 si = p.spans[i];
-            if (si.y <= si.x) continue;
-            for (uint32_t h = kvh * group; h < (kvh + 1) * group; ++h) {
-                float q[4], go[4];
-                row_read(q, static_cast<const T *>(p.q) + i * p.ldq + h * p.dim, p.dim, lane);
-                row_read(go, static_cast<const T *>(p.d_o) + i * p.ld_do + h * p.dim, p.dim, lane);
-                float s = row_dot(q, k) * p.scale;
-                if (p.b.n) s += p.bias[(size_t)bucket_of(p.b, (int32_t)(j - i)) * p.heads + h];
-                const float w = exp2f(log2_score(s) - p.lse[(int64_t)h * p.n + i]);
-                const float ds = w * (row_dot(go, v) - p.delta[(int64_t)h * p.n + i]) * p.scale;
-                for (int e = 0; e < 4; ++e) { dv[e] += w * go[e]; dk[e] += ds * q[e]; }
+    if (warp < 4) {
+        // ============ softmax: one row per thread ============
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+        const int64_t i = (int64_t)t0 + tid;
+        const uint32_t lanes = (warp * 32u) << 16;
+        const float scale = p.scale * kLog2e;
+        const int32_t last = bias_last(p.b);
+        const float *near_row = lut - i + last + kBiasPad;         // + key position
+        float ref = -INFINITY, sum = 0.f;
+        bool ok = true;
+        for (int32_t t = 0; t < tiles; ++t) {
+            const int32_t k0 = tile_at(t), keys = tile_keys(t), cols = (keys + 15) & ~15;
+            if (!__all_sync(kFullMask, mbar_wait(&sh.s_full, t & 1, abort_flag))) { ok = false; break; }
+            tc_fence_after();
+            const uint32_t stage = t % Sh::kStages;
+            if (!__all_sync(kFullMask, mbar_wait(&sh.k_full[stage], (t / Sh::kStages) & 1, abort_flag))) { ok = false; break; }   // the bits of the keys
+            float x[4][32];
+            float top = -INFINITY;
+            // far from the rows every key of the tile has the bias of the side's last bucket
+            const bool far = p.b.n == 0 || k0 + cols - 1 - t0 <= -last || k0 - (t0 + kAttendTile - 1) >= last;
+            const float flat = p.b.n ? lut[k0 < t0 ? 0 : bias_entries(p.b) - 1] : 0.f;
+            const float *near = near_row + k0;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                if (c * 32 < cols) {
+                    uint32_t v[32];
+                    tmem_ld32(tmem + lanes + Sh::kS + c * 32, v);
+                    tmem_wait_ld(v);
+                    if (far) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) x[c][e] = fmaf(__uint_as_float(v[e]), scale, flat);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) x[c][e] = fmaf(__uint_as_float(v[e]), scale, near[c * 32 + e]);
+                    }
+                    const int32_t at = k0 + c * 32;
+                    const uint32_t m = (range_bits(row.lo, row.hi, at) | range_bits(row.s, row.se, at)) & sh.vis[stage][c];
+                    if (!__all_sync(kFullMask, m == 0xFFFFFFFFu)) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) x[c][e] = (m >> e) & 1u ? x[c][e] : -INFINITY;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) top = fmaxf(top, x[c][e]);
+                }
+            }
+            mbar_arrive(&sh.k_empty[stage]);                         // this thread is done with the stage's bits
+            if (Sh::kOwnP) {                                         // the next scores may be computed
+                tc_fence_before();
+                mbar_arrive(&sh.s_free);
+            }
+            const bool grown = top > ref + kRescale || (ref == -INFINITY && top > ref);
+            if (t > 0 && !__all_sync(kFullMask, mbar_wait(&sh.pv_done, (t - 1) & 1, abort_flag))) { ok = false; break; }
+            if (__any_sync(kFullMask, grown)) {
+                const float to = grown ? top : ref;
+                const float keep = ref == -INFINITY ? 0.f : fast_exp2(ref - to);
+                ref = to;
+                sum *= keep;
+                if (t > 0) {
+                    tc_fence_after();
+                    for (uint32_t c = 0; c < dim16; c += 16) {
+                        uint32_t o[16];
+                        tmem_ld16(tmem + lanes + Sh::kO + c, o);
+                        tmem_wait_ld(o);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * keep);
+                        tmem_st16(tmem + lanes + Sh::kO + c, o);
+                    }
+                }
+            }
+            const float from = ref == -INFINITY ? 0.f : ref;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                if (c * 32 < cols) {
+                    uint32_t w[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const float a = fast_exp2(x[c][2 * e] - from), b = fast_exp2(x[c][2 * e + 1] - from);
+                        sum += a + b;
+                        w[e] = pack2<T>(a, b);
+                    }
+                    tmem_st16(tmem + lanes + Sh::kP + c * 16, w);
+                }
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            mbar_arrive(&sh.p_full);
+        }
+        ok = __all_sync(kFullMask, ok && (tiles == 0 || mbar_wait(&sh.pv_done, (tiles - 1) & 1, abort_flag)));
+        tc_fence_after();
+        // the output leaves through shared memory (every tile is read by now), a row of 16-byte chunks at a time
+        const float inv = ok && sum > 0.f ? 1.f / sum : 0.f;
+        if (p.lse && i < p.n) p.lse[(int64_t)h * p.n + i] = sum > 0.f ? ref + log2f(sum) : INFINITY;
+        const uint32_t row_bytes = p.dim * 2u;
+        unsigned char *mine = smem + warp * 32u * row_bytes, *line = mine + lane * row_bytes;
+        const int32_t rows = (int32_t)min((int64_t)32, p.n - (t0 + (int64_t)warp * 32));
+        for (uint32_t c = 0; c < dim16; c += 16) {
+            uint32_t o[16];
+            if (tiles) { tmem_ld16(tmem + lanes + Sh::kO + c, o); tmem_wait_ld(o); }
+            else {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[e] = 0u;
+            }
+#pragma unroll
+            for (int g = 0; g < 2; ++g)
+                if (c + g * 8 < p.dim) {
+                    uint4 w;
+                    w.x = pack2<T>(__uint_as_float(o[g * 8 + 0]) * inv, __uint_as_float(o[g * 8 + 1]) * inv);
+                    w.y = pack2<T>(__uint_as_float(o[g * 8 + 2]) * inv, __uint_as_float(o[g * 8 + 3]) * inv);
+                    w.z = pack2<T>(__uint_as_float(o[g * 8 + 4]) * inv, __uint_as_float(o[g * 8 + 5]) * inv);
+                    w.w = pack2<T>(__uint_as_float(o[g * 8 + 6]) * inv, __uint_as_float(o[g * 8 + 7]) * inv);
+                    const uint32_t ch = (c >> 3) + g, chunks = p.dim >> 3;
+                    *reinterpret_cast<uint4 *>(line + ((ch + lane) % chunks) * 16u) = w;       // turned by the row: fewer bank conflicts
+                }
+        }
+        __syncwarp();
+        {
+            const uint32_t chunks = p.dim >> 3;
+            char *out = static_cast<char *>(p.out) + ((uint64_t)(t0 + warp * 32) * p.ldo + (uint64_t)h * p.dim) * 2u;
+            for (int32_t e = (int32_t)lane; e < rows * (int32_t)chunks; e += 32) {
+                const uint32_t r = (uint32_t)e / chunks, ch = (uint32_t)e - r * chunks;
+                *reinterpret_cast<uint4 *>(out + (uint64_t)r * p.ldo * 2u + ch * 16u) =
+                    *reinterpret_cast<const uint4 *>(mine + r * row_bytes + ((ch + r) % chunks) * 16u);
             }
         }
+        tc_fence_before();
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        if (warp == 4) {
+            // ============ MMA issue: one lane ============
+            if (lane == 0 && tiles) {
+                const uint32_t idesc_o = umma_idesc_f16(kBf16, kAttendTile, dim16, true);
+                auto scores = [&](int32_t t) {
+                    const uint32_t stage = t % Sh::kStages, cols = (uint32_t)(tile_keys(t) + 15) & ~15u;
+                    const uint32_t idesc = umma_idesc_f16(kBf16, kAttendTile, cols, false);
+                    for (uint32_t c = 0; c < dim16; c += 16) {
+                        const uint32_t off = (c >> 6) * (kAttendTile * 128) + (c & 63u) * 2u;
+                        umma_f16_ss(tmem + Sh::kS, umma_desc_sw128(qs + off, 0), umma_desc_sw128(ks + stage * Sh::kTileBytes + off, 0), idesc, c > 0);
+                    }
+                    umma_commit(&sh.s_full);
+                    umma_commit(&sh.k_empty[stage]);
+                };
+                bool ok = mbar_wait(&sh.q_full, 0, abort_flag) && mbar_wait(&sh.k_full[0], 0, abort_flag);
+                if (ok) { tc_fence_after(); scores(0); }
+                for (int32_t t = 0; t < tiles && ok; ++t) {
+                    const uint32_t stage = t % Sh::kStages;
+                    const int32_t n1 = t + 1;
+                    if (Sh::kOwnP && n1 < tiles) {
+                        ok = mbar_wait(&sh.k_full[n1 % Sh::kStages], (n1 / Sh::kStages) & 1, abort_flag) && mbar_wait(&sh.s_free, t & 1, abort_flag);
+                        if (!ok) break;
+                        tc_fence_after();
+                        scores(n1);
+                    }
+                    ok = mbar_wait(&sh.v_full[stage], (t / Sh::kStages) & 1, abort_flag) && mbar_wait(&sh.p_full, t & 1, abort_flag);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t cols = (uint32_t)(tile_keys(t) + 15) & ~15u;
+                    for (uint32_t k = 0; k < cols; k += 16)
+                        umma_f16_ts(tmem + Sh::kO, tmem + Sh::kP + k / 2, umma_desc_sw128(vs + stage * Sh::kTileBytes + k * 128u, kAttendTile * 128),
+                                    idesc_o, t > 0 || k > 0);
+                    umma_commit(&sh.pv_done);
+                    umma_commit(&sh.v_empty[stage]);
+                    if (!Sh::kOwnP && n1 < tiles) {
+                        ok = mbar_wait(&sh.k_full[n1 % Sh::kStages], (n1 / Sh::kStages) & 1, abort_flag);
+                        if (!ok) break;
+                        tc_fence_after();
+                        scores(n1);
+                    }
+                }
+            }
+            __syncwarp();
+        } else if (tiles) {
+            // ============ copies: keys and values of one tile after the other ============
+            const uint32_t lt = tid - 160u;
+            constexpr int CH = NB * 8;
+            const uint32_t used = dim16 >> 3, dch = p.dim >> 3;
+            const T *q = static_cast<const T *>(p.q) + (uint64_t)h * p.dim, *k = static_cast<const T *>(p.k) + (uint64_t)kvh * p.dim,
+                    *v = static_cast<const T *>(p.v) + (uint64_t)kvh * p.dim;
+            uint64_t *pending = nullptr;
+            bool ok = true;
+            // waits for the slot; the copies already under way are handed over first if it is not free yet
+            auto slot = [&](uint64_t *empty, uint32_t parity) {
+                if (mbar_try(empty, parity)) return true;
+                if (pending) { copy_wait<0>(); fence_async_proxy(); mbar_arrive(pending); pending = nullptr; }
+                return mbar_wait(empty, parity, abort_flag);
+            };
+            auto issued = [&](uint64_t *full) {
+                copy_commit();
+                if (pending) { copy_wait<1>(); fence_async_proxy(); mbar_arrive(pending); }
+                pending = full;
+            };
+            uint32_t vis[4];
+            visible_bits(p, t0, kAttendTile, lane, vis);
+            copy_rows_sw128<CH>(qs, kAttendTile * 128, q, p.ldq * 2, t0, kAttendTile, vis, dch, used, lt, kFwdLoaders);
+            issued(&sh.q_full);
+            for (int32_t t = 0; t < tiles && ok; ++t) {
+                const uint32_t stage = t % Sh::kStages, round = t / Sh::kStages;
+                const int32_t at = tile_at(t), keys = tile_keys(t);
+                const uint32_t cols = (uint32_t)(keys + 15) & ~15u;
+                visible_bits(p, at, (uint32_t)keys, lane, vis);
+                if (round > 0) ok = slot(&sh.k_empty[stage], (round - 1) & 1);
+                if (!ok) break;
+                if (lt == 0) { sh.vis[stage][0] = vis[0]; sh.vis[stage][1] = vis[1]; sh.vis[stage][2] = vis[2]; sh.vis[stage][3] = vis[3]; }
+                copy_rows_sw128<CH>(ks + stage * Sh::kTileBytes, kAttendTile * 128, k, p.ldk * 2, at, cols, vis, dch, used, lt, kFwdLoaders);
+                issued(&sh.k_full[stage]);
+                if (round > 0) ok = slot(&sh.v_empty[stage], (round - 1) & 1);
+                if (!ok) break;
+                copy_rows_sw128<CH>(vs + stage * Sh::kTileBytes, kAttendTile * 128, v, p.ldv * 2, at, cols, vis, dch, used, lt, kFwdLoaders);
+                issued(&sh.v_full[stage]);
+            }
+            copy_wait<0>();
+            if (pending && ok) { fence_async_proxy(); mbar_arrive(pending); }
+        }
     }
-    row_write(static_cast<T *>(p.dk) + j * p.ld_dk + kvh * p.dim, dk, p.dim, lane);
-    row_write(static_cast<T *>(p.dv) + j * p.ld_dv + kvh * p.dim, dv, p.dim, lane);
-}
-
-__global__ void attend_dbias_kernel(const float *part, uint64_t tiles, uint32_t columns, uint32_t heads, uint32_t buckets, float *dbias)
-{
-    __shared__ float t[8];
-    const uint32_t c = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    float a = 0.f;
-    for (uint64_t r = threadIdx.x; r < tiles; r += blockDim.x) a += part[r * columns + c];
-    a = warp_sum(a);
-    if (lane == 0) t[warp] = a;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < 8; ++w) a += t[w];
-        dbias[(c % buckets) * heads + c / buckets] = a;
-    }
+    tc_fence_after();
+    if (warp == 4) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(256));
+    if (tid == 0 && sh.abort_flag) atomicOr(error, kErrAttend);
 }
 
-int launch_attend(const AttendParams &p, uint32_t type, int *, int, cudaStream_t s)
+template <typename T, int NB>
+int launch_attend_shape(const AttendParams &p, int *error, cudaStream_t s)
 {
-    if (p.n == 0) return 0;
-    const dim3 grid((uint32_t)((p.n + 3) / 4), p.heads);
-    if (type == kBF16) attend_kernel<__nv_bfloat16><<<grid, 128, 0, s>>>(p);
-    else attend_kernel<__half><<<grid, 128, 0, s>>>(p);
+    auto kernel = attend_tc_kernel<T, NB>;
+    const int smem = FwdShape<NB>::kSmem + (int)(bias_entries(p.b) * sizeof(float));
+    cudaFuncAttributes at;
+    // the softmax warps take registers that the others give up: the block must have been launched with all of them
+    if (cudaFuncGetAttributes(&at, kernel) != cudaSuccess || at.numRegs * 8 < 4 * (kSoftmaxRegs + kOtherRegs)) return -1;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return -1;
+    const uint64_t tiles = ((uint64_t)p.n + kAttendTile - 1) / kAttendTile;
+    kernel<<<(uint32_t)(tiles * p.heads), kFwdThreads, smem, s>>>(p, error);
     return cudaPeekAtLastError() == cudaSuccess ? 1 : -1;
 }
 
-uint64_t attend_backward_ws(const AttendParams &p, bool want_dbias)
+int launch_attend(const AttendParams &p, uint32_t type, int *error, int, cudaStream_t s)
 {
-    const uint64_t tiles = ((uint64_t)p.n + kAttendTile - 1) / kAttendTile;
-    return 4 * (uint64_t)p.n * p.heads + (want_dbias ? 4 * tiles * p.heads * p.b.n * 2 : 0) + 256;
-}
-
-int launch_attend_backward(AttendParams &p, uint32_t type, unsigned char *ws, int *, int, cudaStream_t s)
-{
-    const uint32_t buckets = p.b.n * (p.b.two_sided ? 2 : 1);
-    const uint32_t tiles = (uint32_t)((p.n + kAttendTile - 1) / kAttendTile);
-    int k = 0;
-    if (p.n) {
-        p.delta = reinterpret_cast<float *>(ws);
-        p.dbias_part = p.dbias ? p.delta + (uint64_t)p.n * p.heads : nullptr;
-        const dim3 gq(tiles, p.heads), gk((uint32_t)((p.n + 3) / 4), p.kv_heads);
-        if (type == kBF16) {
-            attend_dq_kernel<__nv_bfloat16><<<gq, 128, 0, s>>>(p);
-            attend_dkv_kernel<__nv_bfloat16><<<gk, 128, 0, s>>>(p);
-        } else {
-            attend_dq_kernel<__half><<<gq, 128, 0, s>>>(p);
-            attend_dkv_kernel<__half><<<gk, 128, 0, s>>>(p);
-        }
-        k = 2;
-    }
-    if (p.dbias) {
-        attend_dbias_kernel<<<p.heads * buckets, 256, 0, s>>>(p.dbias_part, tiles, p.heads * buckets, p.heads, buckets, p.dbias);
-        ++k;
-    }
-    return cudaPeekAtLastError() == cudaSuccess ? k : -1;
+    if (p.n == 0) return 0;
+    if (type == kBF16) return p.dim <= 64 ? launch_attend_shape<__nv_bfloat16, 1>(p, error, s) : launch_attend_shape<__nv_bfloat16, 2>(p, error, s);
+    return p.dim <= 64 ? launch_attend_shape<__half, 1>(p, error, s) : launch_attend_shape<__half, 2>(p, error, s);
 }
 
 }  // namespace w2v

@@ -1,0 +1,751 @@
+// Attention backwards on the tensor cores.
+//
+// With P = exp2(S - lse) and dP = dO V^T:  dS = P (dP - delta), delta = rowsum(P dP) = rowsum(dO o),
+//   dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO,  dbias[b] = sum of dS over the pairs of bucket b.
+// Two passes over the scores, so that nothing is added up with atomics and the same inputs give the same bits:
+//   role 0, a block per 128 queries: dQ and delta.  The rounded o gives a first delta; the row's sum of dS, which is
+//           zero for an exact one, says how far it is off, and dQ is put right with the product P K that is formed
+//           beside dS K.  The delta kept for role 1 is so good to fp32: dbias sums cancel so far that they need it.
+//   role 1, a block per 128 keys and key/value head: dK, dV (all query heads that share them) and dbias.
+// Both keep two operands of their 128 rows in tensor memory (A sides), stream the other two through shared memory
+// and form both score products of a tile; a warpgroup turns them into P and dS, one row per thread, and puts those
+// back into tensor memory as the A sides of the gradient products, whose B sides are the streamed tiles again, read
+// with rows as the summed side.  Keys that are sinks of queries far behind them are summed by a kernel of their own.
+#include <type_traits>
+
+#include "w2v_attend.cuh"
+
+namespace w2v {
+
+template <int NB>
+struct BackShape {
+    static constexpr int kBuf = 2;                                   // score buffers, each with a warpgroup of its own
+    static constexpr int kRows = NB == 2 ? 32 : 64;                  // streamed rows per tile
+    static constexpr int kStages = 4;
+    static constexpr uint32_t kA0 = 0, kA1 = NB * 32, kG0 = NB * 64, kG1 = NB * 128;     // tensor-memory columns
+    static constexpr uint32_t kScores = NB * 192, kAlloc = 512;
+    static_assert(kScores + kBuf * 2 * kRows <= kAlloc, "tensor memory");
+    static constexpr int kOperand = NB * kRows * 128, kStage = 2 * kOperand, kRing = kStages * kStage;
+    static constexpr int kSoft = 128 * kBuf, kThreads = kSoft + 128;
+    static_assert(kRing >= 2 * NB * 128 * 128, "the outputs are staged where the ring was");
+};
+constexpr int kBackLoaders = 96;
+
+struct BackShared {
+    uint64_t a_full, full[4], empty[4], s_full[2], p_full[2], done;
+    uint32_t tmem;
+    int abort_flag;
+    int32_t limits[4][3];
+    uint32_t vis[4][2];                              // role 0: which keys of the stage are words
+    int32_t run_lo[4];                               // role 1: where the run of the stage's query tile begins
+    __align__(16) float lse[4][64], delta[4][64];    // role 1: of the stage's queries
+    float eps[128];
+    float far_sum[8][2];
+};
+
+__device__ __forceinline__ void soft_barrier(int threads) { asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory"); }
+
+// Sums the per-distance sums of `arrays` copies (`entries` floats each) and the far sums over the distances of
+// each bucket; warp w of `warps` takes buckets w, w + warps, ...
+__device__ __forceinline__ void write_bucket_sums(const AttendParams &p, const float *sums, uint32_t arrays, uint32_t entries, int32_t off,
+                                                  const float (*far_sum)[2], uint32_t far_rows, uint32_t warp, uint32_t warps,
+                                                  uint32_t lane, float *out)
+{
+    const uint32_t n = p.b.n, buckets = n * (p.b.two_sided ? 2u : 1u);
+    for (uint32_t b = warp; b < buckets; b += warps) {
+        const uint32_t side = b >= n ? 1u : 0u, k = b - side * n;
+        // distances [d0, d1) of this bucket on its side; those from the last start on include what is beyond the arrays
+        int32_t d0 = p.b.start[k], d1 = k + 1 < n ? p.b.start[k + 1] : off + 1;
+        int32_t r0, r1;                              // relative positions [r0, r1)
+        if (side) { r0 = max(d0, 1); r1 = d1; }
+        else { r0 = 1 - d1; r1 = 1 - d0; if (k == 0 && !p.b.two_sided) r1 = off + 1; }
+        r0 = max(r0, -off);
+        r1 = min(r1, off + 1);
+        float a = 0.f;
+        for (uint32_t w = 0; w < arrays; ++w)
+            for (int32_t r = r0 + (int32_t)lane; r < r1; r += 32) {
+                const int32_t at = r + off;
+                if (at >= 0 && at < (int32_t)entries) a += sums[w * entries + at];
+            }
+        const bool left = side == 0 && k == n - 1, right = p.b.two_sided ? side == 1 && k == n - 1 : k == 0;
+        if (lane < far_rows) a += (left ? far_sum[lane][0] : 0.f) + (right ? far_sum[lane][1] : 0.f);
+        a = warp_sum(a);
+        if (lane == 0) out[b] = a;
+    }
+}
+
+template <typename T, int NB, int ROLE>
+__global__ void __launch_bounds__(BackShape<NB>::kThreads, 1)
+attend_back_kernel(AttendParams p, int *error)
+{
+    using Sh = BackShape<NB>;
+    constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
+    constexpr int kChunks = Sh::kRows / 32;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ BackShared sh;
+    unsigned char *smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
+    const uint32_t ring = smem_addr(smem);
+    float *lut = reinterpret_cast<float *>(smem + Sh::kRing);
+    const uint32_t entries = bias_entries(p.b);
+    float *rel_sums = lut + ((entries + 3u) & ~3u);                  // role 1: [softmax warps][entries]
+
+    const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t group = p.heads / p.kv_heads, across = ROLE == 0 ? p.heads : p.kv_heads;
+    const uint32_t h_own = blockIdx.x % across, kvh = ROLE == 0 ? h_own / group : h_own;
+    const int32_t tile = (int32_t)(blockIdx.x / across), t0 = tile * kAttendTile;
+    const uint32_t heads_here = ROLE == 0 ? 1u : group, h0 = ROLE == 0 ? h_own : kvh * group;
+    const uint32_t dim16 = (p.dim + 15u) & ~15u;
+    constexpr uint32_t kSoftWarps = Sh::kSoft / 32, kMmaWarp = kSoftWarps;
+
+    if (tid == 0) {
+        mbar_init(&sh.a_full, 128);
+        for (int i = 0; i < Sh::kStages; ++i) { mbar_init(&sh.full[i], kBackLoaders); mbar_init(&sh.empty[i], 1 + 128); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&sh.s_full[i], 1); mbar_init(&sh.p_full[i], 128); }
+        mbar_init(&sh.done, 1);
+        sh.abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    const uint32_t r = tid & 127u;                                   // this thread's row (softmax warps)
+    const int64_t own = (int64_t)t0 + r;
+    RowLimits row = {0, 0, 0, 0};                                    // role 0: what the query sees
+    int32_t q_lo = 0, q_hi = 0, far_lo = 0, far_hi = 0, sent = 0;    // role 1: queries that see the key; far: as a sink
+    if (warp < kSoftWarps) {
+        int32_t least = INT32_MAX, most = 0, s = INT32_MAX;
+        if (ROLE == 0) {
+            row = row_limits(p, own);
+            if (row.hi > row.lo) { least = row.lo; most = row.hi; s = row.s; }
+        } else if (own < p.n) {
+            const int2 sp = __ldg(p.spans + own);
+            if (sp.y > sp.x) {
+                sent = sp.x;
+                q_lo = (int32_t)max((int64_t)sp.x, own - p.right);
+                q_hi = (int32_t)min((int64_t)sp.y, own + p.left + 1);
+                least = q_lo; most = q_hi;
+                if (own - sp.x < p.sinks) {
+                    // as a sink it is also seen from beyond the window; of those queries, this block takes the ones whose
+                    // tile's run reaches back to the key, all in the tile of the last query of the window
+                    far_lo = q_hi;
+                    far_hi = (int32_t)min((int64_t)sp.y, ((own + p.left) / kAttendTile + 1) * kAttendTile);
+                    far_hi = max(far_hi, far_lo);
+                    most = far_hi;
+                }
+            }
+        }
+        if (warp < 4) {
+            least = __reduce_min_sync(kFullMask, least);
+            most = __reduce_max_sync(kFullMask, most);
+            s = __reduce_min_sync(kFullMask, s);
+            if (lane == 0) { sh.limits[warp][0] = least; sh.limits[warp][1] = most; sh.limits[warp][2] = s; }
+        }
+    }
+    if (warp == kMmaWarp) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&sh.tmem)), "r"(Sh::kAlloc));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    if (p.b.n) {
+        fill_bias(p, h0, lut, tid, Sh::kThreads);
+        if (ROLE == 1)
+            for (uint32_t e = tid; e < kSoftWarps * entries; e += Sh::kThreads) rel_sums[e] = 0.f;
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = sh.tmem;
+    volatile int *abort_flag = &sh.abort_flag;
+    int32_t lo = INT32_MAX, hi = 0, s_lo = INT32_MAX;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        lo = min(lo, sh.limits[w][0]);
+        hi = max(hi, sh.limits[w][1]);
+        s_lo = min(s_lo, sh.limits[w][2]);
+    }
+    // tiles of one head: role 0 the run of keys and then the sinks before it, role 1 the queries, on a grid of kRows
+    if (ROLE == 1) lo = hi ? lo / Sh::kRows * Sh::kRows : 0;
+    const int32_t s_end = ROLE == 0 && hi ? min(s_lo + p.sinks, lo) : 0, extra = ROLE == 0 && hi && s_lo < s_end ? (s_end - s_lo + Sh::kRows - 1) / Sh::kRows : 0;
+    const int32_t run = hi ? (hi - lo + Sh::kRows - 1) / Sh::kRows : 0, per_head = run + extra;
+    const int32_t total = per_head * (int32_t)heads_here;
+    auto tile_at = [&](int32_t k) { return ROLE == 0 && k >= run ? s_lo + (k - run) * Sh::kRows : lo + k * Sh::kRows; };
+    auto tile_rows = [&](int32_t k) { return ROLE == 1 ? Sh::kRows : min((int32_t)Sh::kRows, (k >= run ? s_end : hi) - tile_at(k)); };
+
+    if (warp < kSoftWarps) {
+        // ============ softmax warpgroups ============
+        const uint32_t wg = tid >> 7, lanes = ((warp & 3u) * 32u) << 16;
+        const float scale = p.scale * kLog2e;
+        const int32_t last = bias_last(p.b), off = last + kBiasPad;
+        const int32_t w0 = t0 + (int32_t)(warp & 3u) * 32;           // first row of the warp
+        const bool word = ROLE == 0 ? row.hi > row.lo : q_hi > q_lo;
+        float lse = INFINITY, delta = 0.f;
+        if (ROLE == 0 && word) lse = __ldg(p.lse + (int64_t)h_own * p.n + own);
+        // the two operands of the block's rows go to tensor memory, zeros for rows that are not words
+        {
+            const T *a0 = ROLE == 0 ? static_cast<const T *>(p.q) + own * (int64_t)p.ldq + (int64_t)h_own * p.dim
+                                    : static_cast<const T *>(p.k) + own * (int64_t)p.ldk + (int64_t)kvh * p.dim;
+            const T *a1 = ROLE == 0 ? static_cast<const T *>(p.d_o) + own * (int64_t)p.ld_do + (int64_t)h_own * p.dim
+                                    : static_cast<const T *>(p.v) + own * (int64_t)p.ldv + (int64_t)kvh * p.dim;
+            const T *o = ROLE == 0 ? static_cast<const T *>(p.o) + own * (int64_t)p.ldo + (int64_t)h_own * p.dim : nullptr;
+#pragma unroll
+            for (int g = 0; g < NB * 2; ++g) {
+                uint32_t x[16], y[16];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const uint32_t at = g * 32 + c * 8;
+                    uint4 u = make_uint4(0, 0, 0, 0), w = u;
+                    if (word && at < p.dim) {
+                        u = __ldg(reinterpret_cast<const uint4 *>(a0 + at));
+                        w = __ldg(reinterpret_cast<const uint4 *>(a1 + at));
+                        if (ROLE == 0) {
+                            const Pack<T, 8> oo = load_pack<T, 8>(o + at), dd = load_pack<T, 8>(a1 + at);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) delta = fmaf(to_f32(oo.e[e]), to_f32(dd.e[e]), delta);
+                        }
+                    }
+                    x[c * 4] = u.x; x[c * 4 + 1] = u.y; x[c * 4 + 2] = u.z; x[c * 4 + 3] = u.w;
+                    y[c * 4] = w.x; y[c * 4 + 1] = w.y; y[c * 4 + 2] = w.z; y[c * 4 + 3] = w.w;
+                }
+                if (wg == 0) {
+                    tmem_st16(tmem + lanes + Sh::kA0 + g * 16, x);
+                    tmem_st16(tmem + lanes + Sh::kA1 + g * 16, y);
+                }
+            }
+            if (wg == 0) {
+                tmem_wait_st();
+                tc_fence_before();
+                mbar_arrive(&sh.a_full);
+            }
+        }
+        float eps = 0.f;
+        bool ok = true;
+        for (uint32_t g = 0; g < heads_here; ++g) {
+            if (ROLE == 1 && p.b.n && g > 0) {
+                soft_barrier(Sh::kSoft);                             // the sums of the head before are written
+                fill_bias(p, h0 + g, lut, tid, Sh::kSoft);
+                for (uint32_t e = tid; e < kSoftWarps * entries; e += Sh::kSoft) rel_sums[e] = 0.f;
+                soft_barrier(Sh::kSoft);
+            }
+            float far_l = 0.f, far_r = 0.f;
+            for (int32_t k = 0; k < per_head && ok; ++k) {
+                const int32_t t = (int32_t)g * per_head + k;
+                const uint32_t b = t % Sh::kBuf, stage = t % Sh::kStages;
+                if (b != wg) continue;
+                const int32_t at0 = tile_at(k), cols = (tile_rows(k) + 15) & ~15;
+                ok = __all_sync(kFullMask, mbar_wait(&sh.full[stage], (t / Sh::kStages) & 1, abort_flag) &&
+                                               mbar_wait(&sh.s_full[b], (t / Sh::kBuf) & 1, abort_flag));
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t cs = tmem + lanes + Sh::kScores + b * 2 * Sh::kRows, cd = cs + Sh::kRows;
+                // which side of the diagonal the warp's part of the tile lies on: distances key - query
+                const int32_t rel0 = ROLE == 0 ? at0 - (w0 + 31) : w0 - (at0 + Sh::kRows - 1);
+                const int32_t rel1 = ROLE == 0 ? at0 + Sh::kRows - 1 - w0 : w0 + 31 - at0;
+                const bool far_left = rel1 <= -last, far = p.b.n == 0 || far_left || rel0 >= last;
+                const float flat = p.b.n ? lut[far_left ? 0 : entries - 1] : 0.f;
+                float acc_p = 0.f, acc_n = 0.f;
+                const bool reach = ROLE == 1 && p.sinks && sh.run_lo[stage] <= own;
+#pragma unroll
+                for (int c = 0; c < kChunks; ++c) {
+                    if (c * 32 < cols) {
+                        uint32_t sv[32], dv[32];
+                        tmem_ld32(cs + c * 32, sv);
+                        tmem_ld32(cd + c * 32, dv);
+                        tmem_wait_ld(sv);
+                        tmem_held(dv);
+                        const int32_t at = at0 + c * 32;
+                        uint32_t m;
+                        if (ROLE == 0) m = (range_bits(row.lo, row.hi, at) | range_bits(row.s, row.se, at)) & sh.vis[stage][c];
+                        else {
+                            m = range_bits(q_lo, q_hi, at);
+                            if (reach) m |= range_bits(far_lo, far_hi, at);
+                        }
+                        float x[32];
+                        if (far) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) x[e] = fmaf(__uint_as_float(sv[e]), scale, flat);
+                        } else {
+                            // key - query grows with the column in role 0 and falls with it in role 1
+                            const float *near = ROLE == 0 ? lut + (at - (int32_t)own + off) : lut + ((int32_t)own - at + off);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) x[e] = fmaf(__uint_as_float(sv[e]), scale, ROLE == 0 ? near[e] : near[-e]);
+                        }
+                        if (!__all_sync(kFullMask, m == 0xFFFFFFFFu)) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) x[e] = (m >> e) & 1u ? x[e] : -INFINITY;
+                        }
+                        uint32_t ws[16], wp[16];
+                        if (ROLE == 0) {
+#pragma unroll
+                            for (int e = 0; e < 32; e += 2) {
+                                const float p0 = fast_exp2(x[e] - lse), p1 = fast_exp2(x[e + 1] - lse);
+                                const float d0 = p0 * (__uint_as_float(dv[e]) - delta), d1 = p1 * (__uint_as_float(dv[e + 1]) - delta);
+                                eps += d0 + d1;
+                                wp[e / 2] = pack2<T>(p0, p1);
+                                ws[e / 2] = pack2<T>(d0, d1);
+                            }
+                            tmem_st16(cs + c * 16, wp);
+                            tmem_st16(cd + c * 16, ws);
+                        } else {
+                            float ds[32];
+#pragma unroll
+                            for (int e = 0; e < 32; e += 4) {
+                                const float4 l4 = *reinterpret_cast<const float4 *>(&sh.lse[stage][c * 32 + e]);
+                                const float4 d4 = *reinterpret_cast<const float4 *>(&sh.delta[stage][c * 32 + e]);
+                                const float p0 = fast_exp2(x[e] - l4.x), p1 = fast_exp2(x[e + 1] - l4.y);
+                                const float p2 = fast_exp2(x[e + 2] - l4.z), p3 = fast_exp2(x[e + 3] - l4.w);
+                                wp[e / 2] = pack2<T>(p0, p1);
+                                wp[e / 2 + 1] = pack2<T>(p2, p3);
+                                ds[e] = p0 * (__uint_as_float(dv[e]) - d4.x);
+                                ds[e + 1] = p1 * (__uint_as_float(dv[e + 1]) - d4.y);
+                                ds[e + 2] = p2 * (__uint_as_float(dv[e + 2]) - d4.z);
+                                ds[e + 3] = p3 * (__uint_as_float(dv[e + 3]) - d4.w);
+                                ws[e / 2] = pack2<T>(ds[e], ds[e + 1]);
+                                ws[e / 2 + 1] = pack2<T>(ds[e + 2], ds[e + 3]);
+                            }
+                            tmem_st16(cs + c * 16, wp);
+                            tmem_st16(cd + c * 16, ws);
+                            if (p.dbias) {
+                                if (far) {
+                                    float a = 0.f;
+#pragma unroll
+                                    for (int e = 0; e < 32; ++e) a += ds[e];
+                                    if (far_left) far_l += a; else far_r += a;
+                                } else {
+                                    // lane l gathers the diagonal key - query = base + l (acc_p) and the one 32 below (acc_n)
+                                    const int32_t base = w0 - at;
+#pragma unroll
+                                    for (int e = 0; e < 32; ++e) {
+                                        const float y = __shfl_sync(kFullMask, ds[e], (lane + e) & 31u);
+                                        if (lane + e < 32u) acc_p += y; else acc_n += y;
+                                    }
+                                    float *mine = rel_sums + warp * entries + base + off + (int32_t)lane;
+                                    mine[0] += acc_p;
+                                    __syncwarp();
+                                    if (c + 1 == kChunks) mine[-32] += acc_n;
+                                    __syncwarp();
+                                    acc_p = acc_n;
+                                    acc_n = 0.f;
+                                }
+                            }
+                        }
+                    }
+                }
+                tmem_wait_st();
+                tc_fence_before();
+                mbar_arrive(&sh.p_full[b]);
+                mbar_arrive(&sh.empty[stage]);
+            }
+            if (ROLE == 1 && p.dbias) {
+                far_l = warp_sum(far_l);
+                far_r = warp_sum(far_r);
+                if (lane == 0) { sh.far_sum[warp][0] = far_l; sh.far_sum[warp][1] = far_r; }
+                soft_barrier(Sh::kSoft);
+                const uint32_t buckets = p.b.n * (p.b.two_sided ? 2u : 1u);
+                write_bucket_sums(p, rel_sums, kSoftWarps, entries, off, sh.far_sum, kSoftWarps, warp, kSoftWarps, lane,
+                                  p.dbias_part + ((size_t)tile * p.heads + h0 + g) * buckets);
+            }
+        }
+        if (ROLE == 0) {
+            if (wg == 1) sh.eps[r] = eps;
+            soft_barrier(Sh::kSoft);
+            if (wg == 0) eps += sh.eps[r];
+            if (wg == 0 && own < p.n) p.delta[(int64_t)h_own * p.n + own] = word ? delta + eps : 0.f;
+        }
+        ok = __all_sync(kFullMask, ok && (total == 0 || mbar_wait(&sh.done, 0, abort_flag)));
+        tc_fence_after();
+        // outputs leave through shared memory: role 0 dQ (warpgroup 0), role 1 dK and dV (a warpgroup each)
+        if (ROLE == 1 || wg == 0) {
+            const uint32_t from = tmem + lanes + (wg == 0 ? Sh::kG0 : Sh::kG1);
+            const float by = wg == 0 ? p.scale : 1.f;
+            const float *sink = nullptr;
+            if (ROLE == 1 && p.sink_used && word && own - sent < p.sinks && p.sink_used[sent / kAttendTile] == sent)
+                sink = p.sink_sum + ((((size_t)(sent / kAttendTile) * p.kv_heads + kvh) * p.sinks + (size_t)(own - sent)) * 2 + wg) * p.dim;
+            const uint32_t row_bytes = p.dim * 2u, chunks = p.dim >> 3;
+            unsigned char *mine = smem + warp * 32u * row_bytes, *line = mine + lane * row_bytes;
+            const int32_t rows = (int32_t)min((int64_t)32, p.n - (int64_t)w0);
+            for (uint32_t c = 0; c < dim16; c += 16) {
+                uint32_t o[16];
+                if (total) { tmem_ld16(from + c, o); tmem_wait_ld(o); }
+                else {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[e] = 0u;
+                }
+                if (ROLE == 0 && total) {                            // the correction of the first delta
+                    uint32_t pk[16];
+                    tmem_ld16(tmem + lanes + Sh::kG1 + c, pk);
+                    tmem_wait_ld(pk);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(fmaf(-eps, __uint_as_float(pk[e]), __uint_as_float(o[e])));
+                }
+#pragma unroll
+                for (int q = 0; q < 2; ++q)
+                    if (c + q * 8 < p.dim) {
+                        float f[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(o[q * 8 + e]);
+                        if (sink) {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) f[e] += sink[c + q * 8 + e];
+                        }
+                        uint4 w;
+                        w.x = pack2<T>(f[0] * by, f[1] * by); w.y = pack2<T>(f[2] * by, f[3] * by);
+                        w.z = pack2<T>(f[4] * by, f[5] * by); w.w = pack2<T>(f[6] * by, f[7] * by);
+                        const uint32_t ch = (c >> 3) + q;
+                        *reinterpret_cast<uint4 *>(line + ((ch + lane) % chunks) * 16u) = w;
+                    }
+            }
+            __syncwarp();
+            const uint64_t ld = ROLE == 0 ? p.ld_dq : wg == 0 ? p.ld_dk : p.ld_dv;
+            char *out = static_cast<char *>(ROLE == 0 ? p.dq : wg == 0 ? p.dk : p.dv) + ((uint64_t)w0 * ld + (uint64_t)(ROLE == 0 ? h_own : kvh) * p.dim) * 2u;
+            for (int32_t e = (int32_t)lane; e < rows * (int32_t)chunks; e += 32) {
+                const uint32_t rr = (uint32_t)e / chunks, ch = (uint32_t)e - rr * chunks;
+                *reinterpret_cast<uint4 *>(out + (uint64_t)rr * ld * 2u + ch * 16u) =
+                    *reinterpret_cast<const uint4 *>(mine + rr * row_bytes + ((ch + rr) % chunks) * 16u);
+            }
+        }
+        tc_fence_before();
+    } else if (warp == kMmaWarp) {
+        // ============ MMA issue: one lane ============
+        if (lane == 0 && total) {
+            const uint32_t idesc_g = umma_idesc_f16(kBf16, kAttendTile, dim16, true);
+            constexpr uint32_t kBlock = Sh::kRows * 128;
+            auto cols_of = [&](int32_t t) { return (uint32_t)(tile_rows(t % per_head) + 15) & ~15u; };
+            auto scores = [&](int32_t t) {
+                const uint32_t x = ring + (t % Sh::kStages) * Sh::kStage, y = x + Sh::kOperand;
+                const uint32_t d = tmem + Sh::kScores + (t % Sh::kBuf) * 2 * Sh::kRows, idesc = umma_idesc_f16(kBf16, kAttendTile, cols_of(t), false);
+                for (uint32_t c = 0; c < dim16; c += 16)
+                    umma_f16_ts(d, tmem + Sh::kA0 + c / 2, umma_desc_sw128(x + (c >> 6) * kBlock + (c & 63u) * 2u, 0), idesc, c > 0);
+                for (uint32_t c = 0; c < dim16; c += 16)
+                    umma_f16_ts(d + Sh::kRows, tmem + Sh::kA1 + c / 2, umma_desc_sw128(y + (c >> 6) * kBlock + (c & 63u) * 2u, 0), idesc, c > 0);
+                umma_commit(&sh.s_full[t % Sh::kBuf]);
+            };
+            bool ok = mbar_wait(&sh.a_full, 0, abort_flag);
+            for (int32_t t = 0; t < Sh::kBuf && t < total && ok; ++t) {
+                ok = mbar_wait(&sh.full[t % Sh::kStages], 0, abort_flag);
+                if (ok) { tc_fence_after(); scores(t); }
+            }
+            for (int32_t t = 0; t < total && ok; ++t) {
+                ok = mbar_wait(&sh.p_full[t % Sh::kBuf], (t / Sh::kBuf) & 1, abort_flag);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t x = ring + (t % Sh::kStages) * Sh::kStage, y = x + Sh::kOperand;
+                const uint32_t d = tmem + Sh::kScores + (t % Sh::kBuf) * 2 * Sh::kRows, cols = cols_of(t);
+                for (uint32_t k = 0; k < cols; k += 16)
+                    umma_f16_ts(tmem + Sh::kG1, d + k / 2, umma_desc_sw128((ROLE == 0 ? x : y) + k * 128u, kBlock), idesc_g, t > 0 || k > 0);
+                for (uint32_t k = 0; k < cols; k += 16)
+                    umma_f16_ts(tmem + Sh::kG0, d + Sh::kRows + k / 2, umma_desc_sw128(x + k * 128u, kBlock), idesc_g, t > 0 || k > 0);
+                umma_commit(&sh.empty[t % Sh::kStages]);
+                if (t + 1 == total) umma_commit(&sh.done);
+                const int32_t n1 = t + Sh::kBuf;
+                if (n1 < total) {
+                    ok = mbar_wait(&sh.full[n1 % Sh::kStages], (n1 / Sh::kStages) & 1, abort_flag);
+                    if (ok) { tc_fence_after(); scores(n1); }
+                }
+            }
+        }
+        __syncwarp();
+    } else if (total) {
+        // ============ copies ============
+        const uint32_t lt = tid - (kMmaWarp + 1) * 32u;
+        constexpr int CH = NB * 8;
+        const uint32_t used = dim16 >> 3, dch = p.dim >> 3;
+        uint64_t *pending = nullptr;
+        bool ok = true;
+        for (int32_t t = 0; t < total; ++t) {
+            const int32_t k = t % per_head;
+            const uint32_t h = h0 + (uint32_t)(t / per_head), stage = t % Sh::kStages, round = t / Sh::kStages;
+            const int32_t at = tile_at(k), rows = tile_rows(k);
+            uint32_t vis[4];
+            visible_bits(p, at, (uint32_t)rows, lane, vis);
+            int32_t run_lo = 0;
+            if (ROLE == 1 && p.sinks) {                              // where the run of keys of this query tile begins
+                uint32_t all[4];
+                const int32_t q0 = at / kAttendTile * kAttendTile;
+                visible_bits(p, q0, kAttendTile, lane, all);
+                const int32_t first = all[0] ? __ffs(all[0]) - 1 : all[1] ? 31 + __ffs(all[1]) : all[2] ? 63 + __ffs(all[2]) : 95 + __ffs(all[3]);
+                run_lo = (all[0] | all[1] | all[2] | all[3]) ? row_limits(p, q0 + first).lo : INT32_MAX;
+            }
+            if (round > 0) {
+                if (!mbar_try(&sh.empty[stage], (round - 1) & 1)) {
+                    if (pending) { copy_wait<0>(); fence_async_proxy(); mbar_arrive(pending); pending = nullptr; }
+                    ok = mbar_wait(&sh.empty[stage], (round - 1) & 1, abort_flag);
+                    if (!ok) break;
+                }
+            }
+            const T *x = ROLE == 0 ? static_cast<const T *>(p.k) + (uint64_t)kvh * p.dim : static_cast<const T *>(p.q) + (uint64_t)h * p.dim;
+            const T *y = ROLE == 0 ? static_cast<const T *>(p.v) + (uint64_t)kvh * p.dim : static_cast<const T *>(p.d_o) + (uint64_t)h * p.dim;
+            const uint32_t cols = (uint32_t)(rows + 15) & ~15u, xs = ring + stage * Sh::kStage;
+            copy_rows_sw128<CH>(xs, Sh::kRows * 128, x, (ROLE == 0 ? p.ldk : p.ldq) * 2, at, cols, vis, dch, used, lt, kBackLoaders);
+            copy_rows_sw128<CH>(xs + Sh::kOperand, Sh::kRows * 128, y, (ROLE == 0 ? p.ldv : p.ld_do) * 2, at, cols, vis, dch, used, lt, kBackLoaders);
+            copy_commit();
+            if (ROLE == 0) {
+                if (lt < 2) sh.vis[stage][lt] = lt ? vis[1] : vis[0];
+            } else {
+                if (lt == 0) sh.run_lo[stage] = run_lo;
+                if (lt < (uint32_t)Sh::kRows) {
+                    const int64_t i = (int64_t)at + lt;
+                    sh.lse[stage][lt] = i < p.n ? __ldg(p.lse + (int64_t)h * p.n + i) : INFINITY;
+                    sh.delta[stage][lt] = i < p.n ? p.delta[(int64_t)h * p.n + i] : 0.f;
+                }
+            }
+            if (pending) { copy_wait<1>(); fence_async_proxy(); mbar_arrive(pending); }
+            pending = &sh.full[stage];
+        }
+        copy_wait<0>();
+        if (pending && ok) { fence_async_proxy(); mbar_arrive(pending); }
+    }
+    __syncthreads();
+    tc_fence_after();
+    if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(Sh::kAlloc));
+    if (tid == 0 && sh.abort_flag) atomicOr(error, kErrAttend);
+}
+
+// ---- sinks seen from beyond the window -----------------------------------------------------------
+// One block per (query tile, head): the sums over the tile's queries for the sinks before the tile's run of keys.
+// A tile has at most one sentence whose sinks lie there, the one that reaches into it from the left; it is
+// written to sink_rec (-1: the tile has no word, -2: its first word's sentence begins inside the tile).
+constexpr int kSinkBatch = 4;
+template <typename T>
+__global__ void __launch_bounds__(128)
+attend_sink_kernel(AttendParams p, uint32_t part_row0)
+{
+    extern __shared__ float sink_smem[];
+    __shared__ int32_t limits[4][2];
+    __shared__ float kv[kSinkBatch][2][kMaxHeadDim];
+    const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, h = blockIdx.x % p.heads, kvh = h / (p.heads / p.kv_heads);
+    const int32_t tile = (int32_t)(blockIdx.x / p.heads), t0 = tile * kAttendTile;
+    const int64_t i = (int64_t)t0 + tid;
+    const RowLimits row = row_limits(p, i);
+    const bool word = row.hi > row.lo;
+    const int32_t wl = __reduce_min_sync(kFullMask, word ? row.lo : INT32_MAX), ws = __reduce_min_sync(kFullMask, word ? row.s : INT32_MAX);
+    if (lane == 0) { limits[warp][0] = wl; limits[warp][1] = ws; }
+    __syncthreads();
+    const int32_t lo = min(min(limits[0][0], limits[1][0]), min(limits[2][0], limits[3][0]));
+    const int32_t s = min(min(limits[0][1], limits[1][1]), min(limits[2][1], limits[3][1]));
+    const bool any = lo != INT32_MAX;
+    const int32_t ns = any ? max(0, min(s + p.sinks, lo) - s) : 0;
+    if (h == 0 && tid == 0) p.sink_rec[tile] = !any ? -1 : s < t0 ? s : -2;
+    const uint32_t buckets = p.b.n * (p.b.two_sided ? 2u : 1u);
+    float *bias_out = p.dbias ? p.dbias_part + ((size_t)(part_row0 + tile) * p.heads + h) * buckets : nullptr;
+    float *out = p.sink_part + ((size_t)tile * p.heads + h) * p.sinks * 2 * p.dim;
+    for (uint32_t e = tid + (uint32_t)ns * 2 * p.dim; e < (uint32_t)p.sinks * 2 * p.dim; e += 128) out[e] = 0.f;
+    if (ns == 0) {
+        if (bias_out) for (uint32_t b = tid; b < buckets; b += 128) bias_out[b] = 0.f;
+        return;
+    }
+    float *ps = sink_smem, *ds = ps + p.sinks * 128;                  // [sink][query]
+    const T *q = static_cast<const T *>(p.q) + i * (int64_t)p.ldq + (int64_t)h * p.dim;
+    const T *go = static_cast<const T *>(p.d_o) + i * (int64_t)p.ld_do + (int64_t)h * p.dim;
+    const float lse = word ? p.lse[(int64_t)h * p.n + i] : INFINITY, delta = word ? p.delta[(int64_t)h * p.n + i] : 0.f;
+    for (int32_t r0 = 0; r0 < ns; r0 += kSinkBatch) {
+        __syncthreads();
+        for (uint32_t e = tid; e < kSinkBatch * p.dim; e += 128) {
+            const uint32_t r = e / p.dim, c = e - r * p.dim;
+            const int64_t j = (int64_t)s + r0 + r;
+            const bool real = r0 + (int32_t)r < ns && p.spans[j].y > p.spans[j].x;
+            kv[r][0][c] = real ? to_f32(static_cast<const T *>(p.k)[j * (int64_t)p.ldk + (int64_t)kvh * p.dim + c]) : 0.f;
+            kv[r][1][c] = real ? to_f32(static_cast<const T *>(p.v)[j * (int64_t)p.ldv + (int64_t)kvh * p.dim + c]) : 0.f;
+        }
+        __syncthreads();
+        float a[kSinkBatch], b[kSinkBatch];
+#pragma unroll
+        for (int r = 0; r < kSinkBatch; ++r) a[r] = b[r] = 0.f;
+        if (word)
+            for (uint32_t c = 0; c < p.dim; c += 8) {
+                const Pack<T, 8> x = load_pack<T, 8>(q + c), y = load_pack<T, 8>(go + c);
+#pragma unroll
+                for (int r = 0; r < kSinkBatch; ++r)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        a[r] = fmaf(to_f32(x.e[e]), kv[r][0][c + e], a[r]);
+                        b[r] = fmaf(to_f32(y.e[e]), kv[r][1][c + e], b[r]);
+                    }
+            }
+#pragma unroll
+        for (int r = 0; r < kSinkBatch; ++r)
+            if (r0 + r < ns) {
+                const int32_t j = s + r0 + r;
+                const bool seen = word && j >= row.s && j < row.se && p.spans[j].y > p.spans[j].x;
+                float w = 0.f;
+                if (seen) {
+                    const float bias = p.b.n ? log2_bias(p.bias[(size_t)bucket_of(p.b, j - (int32_t)i) * p.heads + h]) : 0.f;
+                    w = fast_exp2(fmaf(a[r], p.scale * kLog2e, bias) - lse);
+                }
+                ps[(r0 + r) * 128 + tid] = w;
+                ds[(r0 + r) * 128 + tid] = seen ? w * (b[r] - delta) : 0.f;
+            }
+    }
+    __syncthreads();
+    // dK and dV of the sinks: one column per thread
+    if (tid < p.dim) {
+        const int32_t rows = (int32_t)min((int64_t)kAttendTile, p.n - t0);
+        for (int32_t r0 = 0; r0 < ns; r0 += kSinkBatch) {
+            float a[kSinkBatch], b[kSinkBatch];
+#pragma unroll
+            for (int r = 0; r < kSinkBatch; ++r) a[r] = b[r] = 0.f;
+            for (int32_t x = 0; x < rows; ++x) {
+                const int64_t at = (int64_t)t0 + x;
+                const bool real = p.spans[at].y > p.spans[at].x;
+                const float qv = real ? to_f32(static_cast<const T *>(p.q)[at * (int64_t)p.ldq + (int64_t)h * p.dim + tid]) : 0.f;
+                const float gv = real ? to_f32(static_cast<const T *>(p.d_o)[at * (int64_t)p.ld_do + (int64_t)h * p.dim + tid]) : 0.f;
+#pragma unroll
+                for (int r = 0; r < kSinkBatch; ++r) {
+                    const int32_t rr = min(r0 + r, ns - 1);
+                    a[r] = fmaf(ds[rr * 128 + x], qv, a[r]);
+                    b[r] = fmaf(ps[rr * 128 + x], gv, b[r]);
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < kSinkBatch; ++r)
+                if (r0 + r < ns) {
+                    out[((r0 + r) * 2) * p.dim + tid] = a[r];
+                    out[((r0 + r) * 2 + 1) * p.dim + tid] = b[r];
+                }
+        }
+    }
+    if (bias_out) {
+        // sums by distance first: key - query runs over ns + 127 values; then by bucket
+        float *rel = ds + p.sinks * 128;                              // [sinks + 128]
+        const int32_t least = s - (t0 + 127), count = ns + 127;
+        __syncthreads();
+        for (int32_t e = (int32_t)tid; e < count; e += 128) {
+            float a = 0.f;
+            for (int32_t r = 0; r < ns; ++r) {
+                const int32_t x = s + r - (least + e) - t0;           // the query of this key at this distance
+                if (x >= 0 && x < 128) a += ds[r * 128 + x];
+            }
+            rel[e] = a;
+        }
+        __syncthreads();
+        for (uint32_t b = warp; b < buckets; b += 4) {
+            float a = 0.f;
+            for (int32_t e = (int32_t)lane; e < count; e += 32)
+                if (bucket_of(p.b, least + e) == b) a += rel[e];
+            a = warp_sum(a);
+            if (lane == 0) bias_out[b] = a;
+        }
+    }
+}
+
+// Slot a holds the sums for the sentence that begins in tile a and reaches into a later one (there is at most one):
+// over its query tiles and the query heads of a key/value head, in a fixed order.
+__global__ void __launch_bounds__(256)
+attend_sink_sum_kernel(AttendParams p, int32_t tiles)
+{
+    const int32_t a = (int32_t)(blockIdx.x / p.kv_heads);
+    const uint32_t kvh = blockIdx.x % p.kv_heads, group = p.heads / p.kv_heads;
+    int32_t first = a + 1;
+    while (first < tiles && p.sink_rec[first] == -1) ++first;
+    const int32_t s = first < tiles ? p.sink_rec[first] : -2;
+    const bool here = s >= 0 && s / kAttendTile == a;
+    if (kvh == 0 && threadIdx.x == 0) p.sink_used[a] = here ? s : -1;
+    if (!here) return;
+    int32_t end = first;
+    while (end < tiles && (p.sink_rec[end] == s || p.sink_rec[end] == -1)) ++end;
+    const size_t width = (size_t)p.sinks * 2 * p.dim;
+    float *out = p.sink_sum + ((size_t)a * p.kv_heads + kvh) * width;
+    for (size_t e = threadIdx.x; e < width; e += blockDim.x) {
+        float x = 0.f;
+        for (int32_t t = first; t < end; ++t)
+            for (uint32_t g = 0; g < group; ++g) x += p.sink_part[((size_t)t * p.heads + kvh * group + g) * width + e];
+        out[e] = x;
+    }
+}
+
+__global__ void __launch_bounds__(256)
+attend_dbias_kernel(const float *part, uint64_t rows, uint32_t columns, uint32_t heads, uint32_t buckets, float *dbias)
+{
+    __shared__ float t[8];
+    const uint32_t c = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    float a = 0.f;
+    for (uint64_t r = threadIdx.x; r < rows; r += blockDim.x) a += part[r * columns + c];
+    a = warp_sum(a);
+    if (lane == 0) t[warp] = a;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < 8; ++w) a += t[w];
+        dbias[(c % buckets) * heads + c / buckets] = a;
+    }
+}
+
+namespace {
+
+struct BackWs {
+    uint64_t delta, part, sink_part, sink_sum, rec, used, bytes;
+};
+
+bool far_sinks(const AttendParams &p) { return p.sinks > 0 && p.n > (int64_t)p.left + 1; }
+
+BackWs back_ws(const AttendParams &p, bool want_dbias)
+{
+    const uint64_t tiles = ((uint64_t)p.n + kAttendTile - 1) / kAttendTile, buckets = p.b.n * (p.b.two_sided ? 2u : 1u);
+    const bool sinks = far_sinks(p);
+    BackWs w;
+    uint64_t at = 0;
+    auto take = [&](uint64_t floats) { const uint64_t x = at; at += (floats * 4 + 15) & ~15ull; return x; };
+    w.delta = take((uint64_t)p.n * p.heads);
+    w.part = take(want_dbias ? (sinks ? 2 : 1) * tiles * p.heads * buckets : 0);
+    w.sink_part = take(sinks ? tiles * p.heads * p.sinks * 2 * p.dim : 0);
+    w.sink_sum = take(sinks ? tiles * p.kv_heads * p.sinks * 2 * p.dim : 0);
+    w.rec = take(sinks ? tiles : 0);
+    w.used = take(sinks ? tiles : 0);
+    w.bytes = at + 16;
+    return w;
+}
+
+template <typename T, int NB, int ROLE>
+int launch_role(const AttendParams &p, uint32_t tiles, int *error, cudaStream_t s)
+{
+    using Sh = BackShape<NB>;
+    auto kernel = attend_back_kernel<T, NB, ROLE>;
+    const uint32_t entries = bias_entries(p.b);
+    int smem = Sh::kRing + 1024 + (int)(4 * (((entries + 3u) & ~3u) + (ROLE == 1 ? Sh::kSoft / 32 * entries : 0u)));
+    if (smem < 116 * 1024) smem = 116 * 1024;     // a second block would only wait for tensor memory
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return -1;
+    kernel<<<tiles * (ROLE == 0 ? p.heads : p.kv_heads), Sh::kThreads, smem, s>>>(p, error);
+    return cudaPeekAtLastError() == cudaSuccess ? 1 : -1;
+}
+
+template <typename T>
+int launch_back_typed(const AttendParams &p, uint32_t tiles, int *error, cudaStream_t s)
+{
+    int k = p.dim <= 64 ? launch_role<T, 1, 0>(p, tiles, error, s) : launch_role<T, 2, 0>(p, tiles, error, s);
+    if (k < 0) return -1;
+    if (far_sinks(p)) {
+        const int smem = (int)sizeof(float) * (2 * 128 * p.sinks + p.sinks + 128);
+        if (cudaFuncSetAttribute(attend_sink_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return -1;
+        attend_sink_kernel<T><<<tiles * p.heads, 128, smem, s>>>(p, tiles);
+        attend_sink_sum_kernel<<<tiles * p.kv_heads, 256, 0, s>>>(p, (int32_t)tiles);
+        k += 2;
+    }
+    const int j = p.dim <= 64 ? launch_role<T, 1, 1>(p, tiles, error, s) : launch_role<T, 2, 1>(p, tiles, error, s);
+    return j < 0 ? -1 : k + j;
+}
+
+}  // namespace
+
+uint64_t attend_backward_ws(const AttendParams &p, bool want_dbias) { return back_ws(p, want_dbias).bytes; }
+
+int launch_attend_backward(AttendParams &p, uint32_t type, unsigned char *ws, int *error, int, cudaStream_t s)
+{
+    const uint32_t buckets = p.b.n * (p.b.two_sided ? 2 : 1);
+    const uint32_t tiles = (uint32_t)((p.n + kAttendTile - 1) / kAttendTile);
+    const BackWs w = back_ws(p, p.dbias != nullptr);
+    int k = 0;
+    if (p.n) {
+        p.delta = reinterpret_cast<float *>(ws + w.delta);
+        p.dbias_part = reinterpret_cast<float *>(ws + w.part);
+        if (far_sinks(p)) {
+            p.sink_part = reinterpret_cast<float *>(ws + w.sink_part);
+            p.sink_sum = reinterpret_cast<float *>(ws + w.sink_sum);
+            p.sink_rec = reinterpret_cast<int32_t *>(ws + w.rec);
+            p.sink_used = reinterpret_cast<int32_t *>(ws + w.used);
+        }
+        k = type == kBF16 ? launch_back_typed<__nv_bfloat16>(p, tiles, error, s) : launch_back_typed<__half>(p, tiles, error, s);
+        if (k < 0) return -1;
+    }
+    if (p.dbias) {
+        attend_dbias_kernel<<<p.heads * buckets, 256, 0, s>>>(reinterpret_cast<const float *>(ws + w.part), (far_sinks(p) ? 2ull : 1ull) * tiles,
+                                                             p.heads * buckets, p.heads, buckets, p.dbias);
+        ++k;
+    }
+    return cudaPeekAtLastError() == cudaSuccess ? k : -1;
+}
+
+}  // namespace w2v

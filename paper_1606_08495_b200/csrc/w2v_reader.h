@@ -42,13 +42,15 @@ struct BucketStarts {
 struct AttendParams {
     const int2 *spans;              // [n] first position of the sentence, one past its last; empty = the row sees nothing
     const void *q, *k, *v, *o, *d_o;
-    const float *o_full;
     void *out, *dq, *dk, *dv;
     const float *bias;              // [buckets][heads]
-    float *out_full;                // forward: o before it is rounded, or NULL
     float *lse;                     // [heads][n] base-2 logarithm of the softmax sum (scores scaled by log2 e), +inf for an empty row
     float *delta;                   // [heads][n] backward: rowsum(dO o)
-    float *dbias, *dbias_part;      // [buckets][heads]; [query tiles][heads][buckets]
+    float *dbias, *dbias_part;      // [buckets][heads]; [key tiles, then query tiles with sinks][heads][buckets]
+    float *sink_part;               // [query tiles][heads][sinks][dk, dv][dim] sums over one query tile
+    int32_t *sink_rec;              // [query tiles] start of the sentence that reaches into the tile, -1: no word, -2: none
+    int32_t *sink_used;             // [query tiles] start of the sentence whose sums lie in the slot, -1: none
+    float *sink_sum;                // [query tiles][kv heads][sinks][dk, dv][dim]
     uint64_t ldq, ldk, ldv, ldo, ld_do, ld_dq, ld_dk, ld_dv;   // elements between tokens
     int64_t n;
     uint32_t heads, kv_heads, dim;

@@ -90,6 +90,7 @@ int32_t fill_attend(w2v_handle *h, const w2v_window *w, uint64_t n, const int32_
     if (rc != W2V_OK) return rc;
     if (n >= (1ull << 31) - 256) return fail(h, W2V_ERR_ARG, "n must be below 2^31 - 256");
     if (n && (!spans || !aligned(spans, 8))) return fail(h, W2V_ERR_ARG, "spans must be 8-byte aligned and not NULL");
+    if (((n + kAttendTile - 1) / kAttendTile) * w->heads >= (1ull << 31)) return fail(h, W2V_ERR_ARG, "n times heads must be below 2^38");
     p->spans = reinterpret_cast<const int2 *>(spans);
     p->bias = bias;
     p->n = (int64_t)n;
@@ -170,7 +171,7 @@ int32_t w2v_bucket_starts(uint32_t buckets, uint32_t reach, uint32_t two_sided, 
 
 int32_t w2v_attend(w2v_handle *h, const w2v_window *w, uint64_t n, const int32_t *spans, const void *q, uint64_t q_stride,
                    const void *k, uint64_t k_stride, const void *v, uint64_t v_stride, const float *bias, void *o,
-                   uint64_t o_stride, float *o_full, float *lse)
+                   uint64_t o_stride, float *lse)
 {
     if (!h) return W2V_ERR_ARG;
     AttendParams p;
@@ -182,18 +183,16 @@ int32_t w2v_attend(w2v_handle *h, const w2v_window *w, uint64_t n, const int32_t
     if ((rc = check_rows(h, q, q_stride, wq, bad)) != W2V_OK || (rc = check_rows(h, k, k_stride, wk, bad)) != W2V_OK ||
         (rc = check_rows(h, v, v_stride, wk, bad)) != W2V_OK || (rc = check_rows(h, o, o_stride, wq, bad)) != W2V_OK)
         return rc;
-    if (o_full && !aligned(o_full, 16)) return fail(h, W2V_ERR_ARG, "o_full must be 16-byte aligned");
-    if (o_full && !lse) return fail(h, W2V_ERR_ARG, "o_full is of use only with lse");
     DeviceGuard g(h->device);
     if ((rc = ensure_error_word(h)) != W2V_OK) return rc;
-    p.q = q; p.k = k; p.v = v; p.out = o; p.out_full = o_full; p.lse = lse;
+    p.q = q; p.k = k; p.v = v; p.out = o; p.lse = lse;
     p.ldq = q_stride; p.ldk = k_stride; p.ldv = v_stride; p.ldo = o_stride;
     return launched(h, launch_attend(p, w->type, h->tc_error, h->sms, h->stream), "attention launch");
 }
 
 int32_t w2v_attend_backward(w2v_handle *h, const w2v_window *w, uint64_t n, const int32_t *spans, const void *q, uint64_t q_stride,
                             const void *k, uint64_t k_stride, const void *v, uint64_t v_stride, const float *bias, const void *o,
-                            uint64_t o_stride, const float *o_full, const float *lse, const void *d_o, uint64_t do_stride, void *dq,
+                            uint64_t o_stride, const float *lse, const void *d_o, uint64_t do_stride, void *dq,
                             uint64_t dq_stride, void *dk, uint64_t dk_stride, void *dv, uint64_t dv_stride, float *dbias)
 {
     if (!h) return W2V_ERR_ARG;
@@ -210,12 +209,10 @@ int32_t w2v_attend_backward(w2v_handle *h, const w2v_window *w, uint64_t n, cons
             (rc = check_rows(h, dk, dk_stride, wk, bad)) != W2V_OK || (rc = check_rows(h, dv, dv_stride, wk, bad)) != W2V_OK)
             return rc;
         if (!lse) return fail(h, W2V_ERR_ARG, "lse is NULL");
-        if (dbias && !o_full) return fail(h, W2V_ERR_ARG, "dbias needs o_full");
-        if (o_full && !aligned(o_full, 16)) return fail(h, W2V_ERR_ARG, "o_full must be 16-byte aligned");
     }
     DeviceGuard g(h->device);
     if ((rc = ensure_error_word(h)) != W2V_OK) return rc;
-    p.q = q; p.k = k; p.v = v; p.o = o; p.o_full = o_full; p.d_o = d_o; p.lse = const_cast<float *>(lse);
+    p.q = q; p.k = k; p.v = v; p.o = o; p.d_o = d_o; p.lse = const_cast<float *>(lse);
     p.dq = dq; p.dk = dk; p.dv = dv; p.dbias = dbias;
     p.ldq = q_stride; p.ldk = k_stride; p.ldv = v_stride; p.ldo = o_stride; p.ld_do = do_stride;
     p.ld_dq = dq_stride; p.ld_dk = dk_stride; p.ld_dv = dv_stride;

@@ -22,6 +22,7 @@
 // exit that frees the tensor memory.
 #include "w2v_device.cuh"
 #include "w2v_internal.h"
+#include "w2v_tc.cuh"
 
 namespace w2v {
 
@@ -39,50 +40,6 @@ constexpr int kTcGroups = 2;                    // loader groups; group j fills 
 constexpr int kTcThreads = 5 * 32 + kTcGroups * kTcLoaders;
 constexpr uint32_t kTcSpinLimit = 1u << 20;
 
-__device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
-__device__ __forceinline__ void mbar_init(uint64_t *bar, uint32_t count)
-{
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(bar)), "r"(count));
-}
-__device__ __forceinline__ void mbar_arrive(uint64_t *bar)
-{
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory");
-}
-__device__ __forceinline__ bool mbar_try(uint64_t *bar, uint32_t parity)
-{
-    uint32_t done;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                 : "=r"(done) : "r"(smem_addr(bar)), "r"(parity) : "memory");
-    return done != 0;
-}
-// Bounded wait.  Returns false (and raises the block's abort flag) when the limit is reached or
-// another thread has already given up.  The limit is a time, not a count: how long a partner may
-// legitimately take depends on the data (an epilogue warp computes an exact cosine for every pair
-// that passes the screen, which for rows that are all alike is every pair).
-constexpr unsigned long long kTcWaitNs = 4000000000ull;           // 4 s
-__device__ __forceinline__ unsigned long long global_ns()
-{
-    unsigned long long t;
-    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-    return t;
-}
-__device__ __forceinline__ bool mbar_wait(uint64_t *bar, uint32_t parity, volatile int *abort_flag,
-                                          unsigned long long limit_ns = kTcWaitNs)
-{
-    unsigned long long t0 = 0;                                      // the clock is read only by a wait that lasts
-    for (uint32_t spin = 0; spin < (1u << 30); ++spin) {
-        if (mbar_try(bar, parity)) return true;
-        if ((spin & 1023u) == 1023u) {
-            if (*abort_flag) return false;
-            if (!t0) t0 = global_ns();
-            else if (global_ns() - t0 > limit_ns) break;
-        }
-    }
-    *abort_flag = 1;
-    return false;
-}
-
 // Shared-memory matrix descriptor: K-major, no swizzle; 8 rows x 16 B core matrices, `lbo` bytes
 // between the two 16-byte column chunks of one MMA, `sbo` bytes between groups of 8 rows.
 __device__ __forceinline__ uint64_t umma_desc(uint32_t saddr, uint32_t lbo, uint32_t sbo)
@@ -98,11 +55,6 @@ __device__ __forceinline__ void umma_tf32(uint32_t tmem_d, uint64_t adesc, uint6
         "tcgen05.mma.cta_group::1.kind::tf32 [%0], %1, %2, %3, {%5, %6, %7, %8}, p;\n\t}\n"
         ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(0), "r"(0), "r"(0), "r"(0) : "memory");
 }
-__device__ __forceinline__ void umma_commit(uint64_t *bar)
-{
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
-}
-
 // Does (score a, id ia) rank ahead of (score b, id ib)?  Larger cosine first, then smaller id.
 __device__ __forceinline__ bool ranks_ahead_tc(float a, long long ia, float b, long long ib)
 {

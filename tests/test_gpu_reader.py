@@ -159,7 +159,7 @@ def attend_by_hand(q, k, v, toks, bias, left, right, sinks, reach, two, d_o, res
     keys = ok.sum(1).double()
     out = {"o": o}
     bound = {"o": u * o.abs() + (u + F32) * torch.einsum("hij,jhd->ihd", P, V.abs()) + small * keys[:, None, None] * V.abs().amax() + 1e-6}
-    # a score gradient: fp32 products, and the row's delta (from the unrounded output where there is a bias, from the rounded one otherwise)
+    # a score gradient: fp32 products, and the row's delta (exact for dbias, from the rounded output otherwise)
     eS = P * (F32 * (aP + aD[..., None]) + (0 if rest else u) * aD[..., None])
     shared = lambda x: x.view(n, h // group, group, dim).sum(2)  # noqa: E731
     out["dq"] = torch.einsum("hij,jhd->ihd", dS, K) * scale
@@ -497,7 +497,7 @@ def test_refusals(model):
     refused(lambda: model.fourbit_scores(f(9, 10), packed, scales), "m must")
     refused(lambda: model.fourbit_scores(f(1, 33), packed, scales), "packed")
     refused(lambda: binding.w2v_attend(model.h, binding.Window(1, 4, 4, 64, 0, 0, 0, 0, 0, 0, 1.0), 4, spans.data_ptr(), q.data_ptr() + 2, 256,
-                                       q.data_ptr(), 256, q.data_ptr(), 256, None, q.data_ptr(), 256, None, None), "16-byte")
+                                       q.data_ptr(), 256, q.data_ptr(), 256, None, q.data_ptr(), 256, None), "16-byte")
     refused(lambda: binding.w2v_attend(model.h, binding.Window(1, 4, 4, 64, 0, 0, 0, 0, 0, 0, 1.0), 4, spans.data_ptr(), q.data_ptr(), 255,
-                                       q.data_ptr(), 256, q.data_ptr(), 256, None, q.data_ptr(), 256, None, None), "16-byte")
+                                       q.data_ptr(), 256, q.data_ptr(), 256, None, q.data_ptr(), 256, None), "16-byte")
     model.sync()

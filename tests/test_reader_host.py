@@ -41,7 +41,7 @@ def test_calls_without_a_handle_are_refused():
     w = binding.Window()
     assert lib.w2v_layer_norm(None, 0, 4, None, 4, 0, None, None, 1e-5, None, 4, 0, None, None) == binding.W2V_ERR_ARG
     assert lib.w2v_sentence_spans(None, None, 0, None) == binding.W2V_ERR_ARG
-    assert lib.w2v_attend(None, C.byref(w), 0, None, None, 0, None, 0, None, 0, None, None, 0, None, None) == binding.W2V_ERR_ARG
+    assert lib.w2v_attend(None, C.byref(w), 0, None, None, 0, None, 0, None, 0, None, None, 0, None) == binding.W2V_ERR_ARG
     assert lib.w2v_attend_token(None, C.byref(w), 0, None, None, None, None, None, None, 0, None, None) == binding.W2V_ERR_ARG
     assert lib.w2v_fourbit_scores(None, None, 0, 0, None, None, 0, 4, 32, None, 0) == binding.W2V_ERR_ARG
     assert C.sizeof(binding.Window) == 44
