@@ -114,8 +114,9 @@ fourbit_scores_kernel(const float *x, uint32_t m, uint64_t ldx, const unsigned c
     uint2 *frag = reinterpret_cast<uint2 *>(smem);
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     const uint32_t words = (d + 31) / 32, groups = (words + PER - 1) / PER;
-    const uint32_t pitch = unit | 1u, row_part = kQRows * pitch * 16, stage_bytes = row_part + kQRows * kQWords * 4;
-    unsigned char *mine = smem + piece * 512 * NT + warp * 2 * stage_bytes;
+    const uint32_t pitch = unit | 1u, stage_bytes = kQRows * pitch * 16;
+    unsigned char *mine = smem + piece * 512 * NT + warp * (2 * stage_bytes + kQRows * kQWords * 4);
+    float *sc = reinterpret_cast<float *>(mine + 2 * stage_bytes) ;     // [group of the unit][row]: of the unit worked on
     const uint64_t tiles = (rows + kQRows - 1) / kQRows;
     if (warp < m) {
         float top = 0.f;
@@ -144,14 +145,13 @@ fourbit_scores_kernel(const float *x, uint32_t m, uint64_t ldx, const unsigned c
     const bool once = piece >= words;
     // A unit: words [w, w + n) of the rows of a tile.  Which chunk of 16 bytes and which scales a lane copies is the same for
     // every full unit of a full tile.
-    uint32_t from_off[kQWords], to_off[kQWords], scale_off[kQWords];
+    uint32_t from_off[kQWords], to_off[kQWords];
     const uint32_t ng_full = (unit + PER - 1) / PER;
 #pragma unroll
     for (int i = 0; i < kQWords; ++i) {
-        const uint32_t e = lane + i * 32, r = e / unit, c = e - r * unit, rs = e / ng_full;
+        const uint32_t e = lane + i * 32, r = e / unit, c = e - r * unit;
         from_off[i] = (r * words + c) * 16;
         to_off[i] = (r * pitch + c) * 16;
-        scale_off[i] = rs * groups + (e - rs * ng_full);
     }
     uint16_t sreg[kQWords];                                             // scales of the unit under way
     const uint16_t *scale_bits = reinterpret_cast<const uint16_t *>(scales);
@@ -160,19 +160,19 @@ fourbit_scores_kernel(const float *x, uint32_t m, uint64_t ldx, const unsigned c
         const uint32_t dst = smem_addr(mine + stage * stage_bytes), gr = w / PER;
         if (n == unit && r0 + kQRows <= rows) {
             const unsigned char *src = packed + (r0 * words + w) * 16;
-            const uint16_t *ss = scale_bits + r0 * groups + gr;
+            const uint16_t *ss = scale_bits + (r0 + lane) * groups + gr;
 #pragma unroll
             for (int i = 0; i < kQWords; ++i) {
                 if ((uint32_t)i < unit) copy16(dst + to_off[i], src + from_off[i], true);
-                if ((uint32_t)i < ng_full) sreg[i] = __ldg(ss + scale_off[i]);
+                if ((uint32_t)i < ng_full) sreg[i] = __ldg(ss + i);
             }
         } else {
             const uint32_t ng = (n + PER - 1) / PER;
 #pragma unroll
             for (int i = 0; i < kQWords; ++i) {                         // rows past the end are read again, not written
-                const uint32_t e = lane + i * 32, r = e / n, c = e - r * n, rs = e / ng;
+                const uint32_t e = lane + i * 32, r = e / n, c = e - r * n;
                 if (r < kQRows) copy16(dst + (r * pitch + c) * 16, packed + (min(r0 + r, rows - 1) * words + w + c) * 16, true);
-                if (rs < kQRows) sreg[i] = __ldg(scale_bits + min(r0 + rs, rows - 1) * groups + gr + (e - rs * ng));
+                if ((uint32_t)i < ng) sreg[i] = __ldg(scale_bits + min(r0 + lane, rows - 1) * groups + gr + i);
             }
         }
         copy_commit();
@@ -205,7 +205,6 @@ fourbit_scores_kernel(const float *x, uint32_t m, uint64_t ldx, const unsigned c
             for (uint32_t w = w0; w < w_end; w += unit) {
                 const uint32_t n = min(unit, w_end - w), ng = (n + PER - 1) / PER;
                 unsigned char *st = mine + stage * stage_bytes;
-                float *sc = reinterpret_cast<float *>(st + row_part);
 #pragma unroll
                 for (int i = 0; i < kQWords; ++i) if ((uint32_t)i < ng) sc[lane + i * 32] = __uint_as_float((uint32_t)sreg[i] << 16);
                 const bool more = w + unit < w_end, cross = once && !more && tile + stride < tiles;
@@ -215,8 +214,9 @@ fourbit_scores_kernel(const float *x, uint32_t m, uint64_t ldx, const unsigned c
                 __syncwarp();
                 uint32_t from = smem_addr(st) + lane * pitch * 16;
                 const uint2 *f = frag + (size_t)(w - w0) * 2 * NT * 32 + lane;
-                const float *sg = sc + g * ng;
-                for (uint32_t a = 0; a < n; a += PER, ++sg) {
+                const float *sg = sc + g;
+                #pragma unroll(PER == 1 ? 2 : 1)
+                for (uint32_t a = 0; a < n; a += PER, sg += kQRows) {
 #pragma unroll
                     for (int sub = 0; sub < PER; ++sub, from += 16, f += 2 * NT * 32) {
                         if (sub > 0 && a + sub >= n) break;                         // the last group of a row may be shorter
@@ -240,7 +240,7 @@ fourbit_scores_kernel(const float *x, uint32_t m, uint64_t ldx, const unsigned c
                     }
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        const float s0 = sg[i * 16 * ng], s1 = sg[(i * 16 + 8) * ng];
+                        const float s0 = sg[i * 16], s1 = sg[i * 16 + 8];
 #pragma unroll
                         for (int k = 0; k < NT; ++k) {
                             tot[i][k][0] = fmaf(s0, c[i][k][0], tot[i][k][0]);
@@ -277,7 +277,7 @@ int launch_scores(const float *x, uint32_t m, uint64_t ldx, const unsigned char 
     const uint32_t longest = kQWords / PER * PER, parts = (words + longest - 1) / longest;
     const uint32_t unit = ((words + parts - 1) / parts + PER - 1) / PER * PER;
     const uint32_t most = kQFragBytes / (512 * NT) / unit * unit, piece = words <= most ? words : most;
-    const int smem = (int)(piece * 512 * NT + kQWarps * 2 * (kQRows * (unit | 1u) * 16 + kQRows * kQWords * 4));
+    const int smem = (int)(piece * 512 * NT + kQWarps * 2 * kQRows * (unit | 1u) * 16 + kQWarps * kQRows * kQWords * 4);
     if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return -1;
     const uint64_t want = (rows + kQRows * kQWarps - 1) / (kQRows * kQWarps), full = (uint64_t)sms * (smem <= 112 * 1024 ? 2 : 1);
     kernel<<<(uint32_t)(want < full ? want : full), kQWarps * 32, smem, s>>>(x, m, ldx, packed, scales, rows, d, out, ld_out, piece, unit);
