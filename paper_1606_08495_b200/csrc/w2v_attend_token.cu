@@ -3,191 +3,247 @@
 // writes the new key and value into their place and attends over the positions that the window and
 // the sinks leave visible, the new one included.
 //
-// Bound by reading the cache once.  A block takes one key/value head of one sequence (all query heads
+// Bound by reading the cache once.  A block takes one key/value head of one sequence (up to 16 of the query heads
 // that share it) and a part of the visible positions; the parts of one head are the blocks of a
 // cluster, which join their running maxima, sums and outputs through distributed shared memory: one
-// launch, a fixed order of additions.  Inside a block a key is read by LPK lanes, 16 bytes each, and
-// every LPK lanes run over keys of their own in steps of kTokU (that many keys and values in flight
-// per lane before the first is used).
+// launch, a fixed order of additions.
+//
+// A warp takes 16 keys a step and lets the matrix units form the products (query heads as the 16 rows): on the
+// other units the products, conversions and lane sums of four heads took 21 instructions per cache element, against
+// the three that the copy rate leaves time for.  Which dimension lands in which k (and which column) is free as long
+// as both sides agree, so that keys and values go from global memory to the operand registers in accesses of 16 bytes:
+//   scores:  lane (g, t) holds chunk 4 j + t (8 dimensions) of key g, the same of query head g;
+//   output:  lane (g, t) holds chunk g of keys 2t, 2t + 1, 2t + 8, 2t + 9; a byte permutation pairs the keys, and
+//            column g of product e is dimension 8 g + e.
+// The softmax weights enter the second product as the sum of two numbers of the cache's type, so that what is lost is
+// 2^-18 and not 2^-9 of them.  Values of one step are on their way while its scores are formed, the next step's
+// keys while its softmax is.
 #include <cooperative_groups.h>
 
-#include "w2v_device.cuh"
-#include "w2v_reader.h"
-#include "w2v_types.cuh"
+#include "w2v_attend.cuh"
 
 namespace cg = cooperative_groups;
 
 namespace w2v {
 
-constexpr int kTokThreads = 256;
-constexpr int kTokU = 4;
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kTokWarps = 4, kTokThreads = kTokWarps * 32, kTokRows = 16;
 
-template <typename T, int LPK, int GC>
-__global__ void __launch_bounds__(kTokThreads)
+template <typename T>
+__device__ __forceinline__ void mma_token(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1);
+template <>
+__device__ __forceinline__ void mma_token<__nv_bfloat16>(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+template <>
+__device__ __forceinline__ void mma_token<__half>(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// A weight pair as the sum of two pairs of T.
+template <typename T>
+__device__ __forceinline__ void split_pair(float a, float b, uint32_t &head, uint32_t &tail)
+{
+    const T ha = from_f32<T>(a), hb = from_f32<T>(b);
+    head = pack2<T>(a, b);
+    tail = pack2<T>(a - to_f32(ha), b - to_f32(hb));
+}
+
+// NB = 64-column blocks of a head; HI: more than 8 query heads share the key/value head.
+template <typename T, int NB, bool HI>
+__global__ void __launch_bounds__(kTokThreads, NB == 1 ? 4 : 2)
 attend_token_kernel(TokenParams p, uint32_t splits, uint32_t passes)
 {
     extern __shared__ float sm[];
-    const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    constexpr int kWarps = kTokThreads / 32, kSub = 32 / LPK;          // keys a warp reads at once
-    const uint32_t group = p.heads / p.kv_heads;
+    constexpr int kR = HI ? 2 : 1;                                      // rows g and g + 8 of a lane
+    const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+    const uint32_t group = p.heads / p.kv_heads, chunks = p.dim >> 3;
     const uint32_t split = blockIdx.x % splits, item = blockIdx.x / splits;
     const uint32_t pass = item % passes, kvh = (item / passes) % p.kv_heads, b = item / (passes * p.kv_heads);
-    const uint32_t h0 = kvh * group + pass * GC, nh = min((uint32_t)GC, group - pass * GC);
-    float *stat = sm;                                                   // [GC][2] maximum and sum of this block
-    float *acc_s = stat + 2 * GC;                                       // [GC][dim] output of this block
-    float *wstat = acc_s + GC * p.dim;                                  // [warps][GC][2]
-    float *wacc = wstat + kWarps * GC * 2;                              // [warps][GC][dim]
-    float *bias_s = wacc + kWarps * GC * p.dim;                         // [reach + 1][GC] bias by distance
+    const uint32_t h0 = kvh * group + pass * kTokRows, nh = min((uint32_t)kTokRows, group - pass * kTokRows);
+    constexpr uint32_t kKeep = 8 * kR;                                  // rows of a block's results
+    float *stat = sm;                                                   // [rows][2] maximum and sum of this block
+    float *acc_s = stat + 2 * kKeep;                                    // [rows][dim] output of this block
+    float *wstat = acc_s + kKeep * p.dim;                               // [warps][rows][2]
+    float *wacc = wstat + kTokWarps * kKeep * 2;                        // [warps][rows][dim]
+    float *bias_s = wacc + kTokWarps * kKeep * p.dim;                   // [rows][reach + 1] bias by distance
     const int32_t pos = p.pos[b];
     const int32_t reach = p.b.n ? p.b.start[p.b.n - 1] : 0;             // from here on one bucket
-    if (p.b.n) {
-        for (uint32_t i = tid; i < (uint32_t)(reach + 1) * GC; i += kTokThreads) {
-            const int32_t dist = (int32_t)(i / GC);
-            const uint32_t g = i % GC;
-            uint32_t lo = 0, hi = p.b.n - 1;                            // last bucket that starts at or before dist
-            while (lo < hi) {
-                const uint32_t mid = (lo + hi + 1) >> 1;
-                if (p.b.start[mid] <= dist) lo = mid; else hi = mid - 1;
-            }
-            const float v = g < nh ? p.bias[(size_t)lo * p.heads + h0 + g] : 0.f;
-            bias_s[i] = v == -INFINITY ? v : fmaxf(v, -1e30f) * kLog2e;   // the lowest float stays finite
+    if (p.b.n)
+        for (uint32_t i = tid; i < (uint32_t)(reach + 1) * nh; i += kTokThreads) {
+            const uint32_t r = i / (uint32_t)(reach + 1), dist = i - r * (uint32_t)(reach + 1);
+            bias_s[i] = log2_bias(__ldg(p.bias + (size_t)bucket_of(p.b, -(int32_t)dist) * p.heads + h0 + r));
         }
-    }
     __syncthreads();
-    const uint32_t li = lane % LPK, sub = warp * kSub + lane / LPK;
-    const bool mine = li * 8 < p.dim;
-    const T *q = static_cast<const T *>(p.q) + ((size_t)b * p.heads + h0) * p.dim + li * 8;
-    float qf[GC][8], acc[GC][8], mx[GC], sum[GC];
+    float acc[NB * 8][4], mx[kR], sum[kR];
 #pragma unroll
-    for (int g = 0; g < GC; ++g) {
-        mx[g] = -INFINITY;
-        sum[g] = 0.f;
+    for (int i = 0; i < NB * 8; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            acc[g][e] = 0.f;
-            qf[g][e] = mine && (uint32_t)g < nh ? to_f32(q[(size_t)g * p.dim + e]) * (p.scale * kLog2e) : 0.f;
-        }
-    }
+    for (int r = 0; r < kR; ++r) { mx[r] = -INFINITY; sum[r] = 0.f; }
     if (pos >= 0) {
+        uint4 q[kR][NB * 2];                                            // chunk 4 j + t of query heads g and g + 8
+#pragma unroll
+        for (int r = 0; r < kR; ++r)
+#pragma unroll
+            for (int j = 0; j < NB * 2; ++j) {
+                const uint32_t c = 4 * j + t;
+                q[r][j] = g + 8 * r < nh && c < chunks ? __ldg(reinterpret_cast<const uint4 *>(static_cast<const T *>(p.q) + ((size_t)b * p.heads + h0 + g + 8 * r) * p.dim) + c)
+                                                       : make_uint4(0, 0, 0, 0);
+            }
         const int32_t win = pos > p.left ? pos - p.left : 0;            // first position of the window
         const int32_t ns = min(p.sinks, win);                           // sinks before it
-        const int64_t total = (int64_t)pos - win + 1 + ns;
-        const int64_t t0 = total * split / splits, t1 = total * (split + 1) / splits;
-        const uint64_t ring = p.places - (uint64_t)p.sinks;
+        const int32_t total = pos - win + 1 + ns;                       // visible positions, numbered sinks first
+        const int32_t t0 = (int32_t)((int64_t)total * split / splits), t1 = (int32_t)((int64_t)total * (split + 1) / splits);
+        const uint32_t ring = (uint32_t)(p.places - (uint64_t)p.sinks);
+        // place of visible position number ns: the window lies in the ring with one wrap at most
+        const int64_t place0 = win < p.sinks ? win : p.sinks + (int64_t)((uint32_t)(win - p.sinks) % ring);
         const size_t row = (size_t)p.kv_heads * p.dim;
-        const size_t base = (size_t)b * p.places * row + (size_t)kvh * p.dim + li * 8;
-        T *ck = static_cast<T *>(p.ck) + base, *cv = static_cast<T *>(p.cv) + base;
-        const T *nk = static_cast<const T *>(p.k) + ((size_t)b * p.kv_heads + kvh) * p.dim + li * 8;
-        const T *nv = static_cast<const T *>(p.v) + ((size_t)b * p.kv_heads + kvh) * p.dim + li * 8;
-        constexpr int kStep = kWarps * kSub;                            // keys the block reads side by side
-        for (int64_t t = t0 + sub; t - sub < t1; t += kStep * kTokU) {  // all lanes of a warp take part to the end
-            Pack<T, 8> kk[kTokU], vv[kTokU];
-            int32_t at[kTokU];
-            int64_t place[kTokU];
+        T *ck = static_cast<T *>(p.ck) + (size_t)b * p.places * row + (size_t)kvh * p.dim, *cv = static_cast<T *>(p.cv) + (size_t)b * p.places * row + (size_t)kvh * p.dim;
+        const T *nk = static_cast<const T *>(p.k) + ((size_t)b * p.kv_heads + kvh) * p.dim, *nv = static_cast<const T *>(p.v) + ((size_t)b * p.kv_heads + kvh) * p.dim;
+        if (t1 == total && pass == 0 && t0 < t1 && tid < 2 * chunks) {  // the part that ends with the new token stores it; nobody reads its place
+            const int64_t at = pos < p.sinks ? pos : p.sinks + (int64_t)((uint32_t)(pos - p.sinks) % ring);
+            const bool value = tid >= chunks;
+            const uint32_t c = value ? tid - chunks : tid;
+            reinterpret_cast<uint4 *>((value ? cv : ck) + (size_t)at * row)[c] = __ldg(reinterpret_cast<const uint4 *>(value ? nv : nk) + c);
+        }
+        // row of visible position number x in the cache `c`, or the new one
+        auto source = [&](int32_t x, const T *c, const T *fresh) -> const uint4 * {
+            if (x >= total - 1) return reinterpret_cast<const uint4 *>(fresh);
+            int64_t at = x;
+            if (x >= ns) {
+                at = place0 + (x - ns);
+                if (at >= (int64_t)p.places) at -= ring;
+            }
+            return reinterpret_cast<const uint4 *>(c + (size_t)at * row);
+        };
+        auto load_keys = [&](uint4 (&k)[2][NB * 2], int32_t x0) {
 #pragma unroll
-            for (int u = 0; u < kTokU; ++u) {
-                const int64_t tu = t + (int64_t)u * kStep;
-                at[u] = -1;
-                place[u] = 0;
-                if (tu < t1) {
-                    at[u] = tu < ns ? (int32_t)tu : (int32_t)(win + (tu - ns));
-                    place[u] = at[u] < p.sinks ? at[u] : p.sinks + (int64_t)((uint32_t)(at[u] - p.sinks) % (uint32_t)ring);
-                }
+            for (int i = 0; i < 2; ++i) {
+                const int32_t x = x0 + i * 8 + (int32_t)g;
+                const uint4 *s = source(x, ck, nk);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) kk[u].e[e] = vv[u].e[e] = from_f32<T>(0.f);
-                if (tu < t1 && mine) {
-                    const bool fresh = at[u] == pos;
-                    kk[u] = load_pack<T, 8>(fresh ? nk : ck + (size_t)place[u] * row);
-                    vv[u] = load_pack<T, 8>(fresh ? nv : cv + (size_t)place[u] * row);
+                for (int j = 0; j < NB * 2; ++j) k[i][j] = x < t1 && 4 * j + t < chunks ? __ldg(s + 4 * j + t) : make_uint4(0, 0, 0, 0);
+            }
+        };
+        const int32_t first = t0 + (int32_t)warp * 16;
+        uint4 key[2][NB * 2];
+        if (first < t1) load_keys(key, first);
+        for (int32_t x0 = first; x0 < t1; x0 += kTokWarps * 16) {
+            uint4 val[NB][4];                                           // chunk g + 8 s of keys 2t, 2t + 1, 2t + 8, 2t + 9
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int32_t x = x0 + (i >> 1) * 8 + 2 * (int32_t)t + (i & 1);
+                const uint4 *s = source(x, cv, nv);
+#pragma unroll
+                for (int n = 0; n < NB; ++n) val[n][i] = x < t1 && g + 8 * n < chunks ? __ldg(s + g + 8 * n) : make_uint4(0, 0, 0, 0);
+            }
+            float sc[2][4];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                sc[i][0] = sc[i][1] = sc[i][2] = sc[i][3] = 0.f;
+#pragma unroll
+                for (int j = 0; j < NB * 2; ++j) {
+                    mma_token<T>(sc[i], q[0][j].x, HI ? q[kR - 1][j].x : 0u, q[0][j].y, HI ? q[kR - 1][j].y : 0u, key[i][j].x, key[i][j].y);
+                    mma_token<T>(sc[i], q[0][j].z, HI ? q[kR - 1][j].z : 0u, q[0][j].w, HI ? q[kR - 1][j].w : 0u, key[i][j].z, key[i][j].w);
                 }
             }
+            if (x0 + kTokWarps * 16 < t1) load_keys(key, x0 + kTokWarps * 16);
+            uint32_t head[2][kR], tail[2][kR];
 #pragma unroll
-            for (int u = 0; u < kTokU; ++u)
-                if (at[u] == pos && mine && pass == 0) {
-                    store_pack<T, 8>(ck + (size_t)place[u] * row, kk[u]);
-                    store_pack<T, 8>(cv + (size_t)place[u] * row, vv[u]);
+            for (int r = 0; r < kR; ++r) {
+                float s[4], top = mx[r];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int32_t x = x0 + (i >> 1) * 8 + 2 * (int32_t)t + (i & 1);
+                    s[i] = sc[i >> 1][2 * r + (i & 1)] * (p.scale * kLog2e);
+                    if (p.b.n) {
+                        const int32_t dist = x < ns ? pos - x : total - 1 - x;
+                        s[i] += x < t1 && g + 8 * r < nh ? bias_s[(g + 8 * r) * (uint32_t)(reach + 1) + (uint32_t)min(dist, reach)] : 0.f;
+                    }
+                    if (x >= t1) s[i] = -INFINITY;
+                    top = fmaxf(top, s[i]);
+                }
+                top = fmaxf(top, __shfl_xor_sync(kFullMask, top, 1));
+                top = fmaxf(top, __shfl_xor_sync(kFullMask, top, 2));
+                const float from = top == -INFINITY ? 0.f : top;
+                if (__any_sync(kFullMask, top > mx[r])) {
+                    const float keep = fast_exp2(mx[r] - from);         // 0 for the first keys
+                    sum[r] *= keep;
+#pragma unroll
+                    for (int i = 0; i < NB * 8; ++i) { acc[i][2 * r] *= keep; acc[i][2 * r + 1] *= keep; }
+                    mx[r] = top;
                 }
 #pragma unroll
-            for (int g = 0; g < GC; ++g) {
-                float sc[kTokU], top = mx[g];
+                for (int i = 0; i < 4; ++i) { s[i] = fast_exp2(s[i] - from); sum[r] += s[i]; }
+                split_pair<T>(s[0], s[1], head[0][r], tail[0][r]);
+                split_pair<T>(s[2], s[3], head[1][r], tail[1][r]);
+            }
 #pragma unroll
-                for (int u = 0; u < kTokU; ++u) {
-                    float s = 0.f;
+            for (int n = 0; n < NB; ++n) {
+                const uint32_t *v0 = reinterpret_cast<const uint32_t *>(&val[n][0]), *v1 = reinterpret_cast<const uint32_t *>(&val[n][1]);
+                const uint32_t *v2 = reinterpret_cast<const uint32_t *>(&val[n][2]), *v3 = reinterpret_cast<const uint32_t *>(&val[n][3]);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) s = fmaf(qf[g][e], to_f32(kk[u].e[e]), s);
-#pragma unroll
-                    for (int o = LPK / 2; o > 0; o >>= 1) s += __shfl_xor_sync(kFullMask, s, o);
-                    if (p.b.n) s += bias_s[(at[u] < 0 ? 0 : min(pos - at[u], reach)) * GC + g];
-                    sc[u] = at[u] < 0 ? -INFINITY : s;
-                    top = fmaxf(top, sc[u]);
-                }
-                const float keep = top == -INFINITY ? 1.f : exp2f(mx[g] - top);
-                mx[g] = top;
-                sum[g] *= keep;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) acc[g][e] *= keep;
-#pragma unroll
-                for (int u = 0; u < kTokU; ++u) {
-                    const float w = sc[u] == -INFINITY ? 0.f : exp2f(sc[u] - top);
-                    sum[g] += w;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) acc[g][e] = fmaf(w, to_f32(vv[u].e[e]), acc[g][e]);
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t pick = e & 1 ? 0x7632u : 0x5410u;    // dimension e of two keys in one register
+                    const uint32_t b0 = __byte_perm(v0[e >> 1], v1[e >> 1], pick), b1 = __byte_perm(v2[e >> 1], v3[e >> 1], pick);
+                    mma_token<T>(acc[n * 8 + e], tail[0][0], HI ? tail[0][kR - 1] : 0u, tail[1][0], HI ? tail[1][kR - 1] : 0u, b0, b1);
+                    mma_token<T>(acc[n * 8 + e], head[0][0], HI ? head[0][kR - 1] : 0u, head[1][0], HI ? head[1][kR - 1] : 0u, b0, b1);
                 }
             }
         }
     }
-    // join the keys that the lanes of a warp ran over, then the warps
+    // join the warps; a lane has columns 2t, 2t + 1 of every product: dimensions 64 n + 8 (2t) + e and 64 n + 8 (2t + 1) + e
 #pragma unroll
-    for (int g = 0; g < GC; ++g) {
-        float top = mx[g];
+    for (int r = 0; r < kR; ++r) {
+        sum[r] += __shfl_xor_sync(kFullMask, sum[r], 1);
+        sum[r] += __shfl_xor_sync(kFullMask, sum[r], 2);
+        const uint32_t at = warp * kKeep + g + 8 * r;
+        if (t == 0) { wstat[at * 2] = mx[r]; wstat[at * 2 + 1] = sum[r]; }
 #pragma unroll
-        for (int o = LPK; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(kFullMask, top, o));
-        const float keep = mx[g] == -INFINITY ? 0.f : exp2f(mx[g] - top);
-        sum[g] *= keep;
+        for (int n = 0; n < NB; ++n)
 #pragma unroll
-        for (int o = LPK; o < 32; o <<= 1) sum[g] += __shfl_xor_sync(kFullMask, sum[g], o);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            acc[g][e] *= keep;
-#pragma unroll
-            for (int o = LPK; o < 32; o <<= 1) acc[g][e] += __shfl_xor_sync(kFullMask, acc[g][e], o);
-        }
-        if (lane < LPK) {
-            if (li == 0) { wstat[(warp * GC + g) * 2] = top; wstat[(warp * GC + g) * 2 + 1] = sum[g]; }
-            if (mine)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) wacc[(warp * GC + g) * p.dim + li * 8 + e] = acc[g][e];
-        }
+            for (int c = 0; c < 2; ++c) {
+                const uint32_t d = 64 * n + 8 * (2 * t + c);
+                if (d < p.dim) {
+                    float4 *o = reinterpret_cast<float4 *>(wacc + at * p.dim + d);
+                    o[0] = make_float4(acc[n * 8][2 * r + c], acc[n * 8 + 1][2 * r + c], acc[n * 8 + 2][2 * r + c], acc[n * 8 + 3][2 * r + c]);
+                    o[1] = make_float4(acc[n * 8 + 4][2 * r + c], acc[n * 8 + 5][2 * r + c], acc[n * 8 + 6][2 * r + c], acc[n * 8 + 7][2 * r + c]);
+                }
+            }
     }
     __syncthreads();
-    for (uint32_t i = tid; i < GC * p.dim; i += kTokThreads) {
-        const uint32_t g = i / p.dim, c = i - g * p.dim;
+    for (uint32_t i = tid; i < nh * p.dim; i += kTokThreads) {
+        const uint32_t r = i / p.dim, c = i - r * p.dim;
         float top = -INFINITY, s = 0.f, a = 0.f;
-        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, wstat[(w * GC + g) * 2]);
+#pragma unroll
+        for (int w = 0; w < kTokWarps; ++w) top = fmaxf(top, wstat[(w * kKeep + r) * 2]);
         if (top != -INFINITY)
-            for (int w = 0; w < kWarps; ++w) {
-                const float m = wstat[(w * GC + g) * 2], f = m == -INFINITY ? 0.f : exp2f(m - top);
-                s = fmaf(f, wstat[(w * GC + g) * 2 + 1], s);
-                a = fmaf(f, wacc[(w * GC + g) * p.dim + c], a);
+#pragma unroll
+            for (int w = 0; w < kTokWarps; ++w) {
+                const float f = fast_exp2(wstat[(w * kKeep + r) * 2] - top);
+                s = fmaf(f, wstat[(w * kKeep + r) * 2 + 1], s);
+                a = fmaf(f, wacc[(w * kKeep + r) * p.dim + c], a);
             }
         acc_s[i] = a;
-        if (c == 0) { stat[2 * g] = top; stat[2 * g + 1] = s; }
+        if (c == 0) { stat[2 * r] = top; stat[2 * r + 1] = s; }
     }
     // join the blocks of the cluster: each writes a share of the outputs
     cg::cluster_group cluster = cg::this_cluster();
     if (splits > 1) cluster.sync(); else __syncthreads();
     T *out = static_cast<T *>(p.out) + ((size_t)b * p.heads + h0) * p.dim;
     for (uint32_t i = split * kTokThreads + tid; i < nh * p.dim; i += splits * kTokThreads) {
-        const uint32_t g = i / p.dim;
+        const uint32_t r = i / p.dim;
         float top = -INFINITY, s = 0.f, a = 0.f;
-        for (uint32_t r = 0; r < splits; ++r) top = fmaxf(top, splits > 1 ? cluster.map_shared_rank(stat, r)[2 * g] : stat[2 * g]);
+        for (uint32_t x = 0; x < splits; ++x) top = fmaxf(top, splits > 1 ? cluster.map_shared_rank(stat, x)[2 * r] : stat[2 * r]);
         if (top != -INFINITY)
-            for (uint32_t r = 0; r < splits; ++r) {
-                const float *st = splits > 1 ? cluster.map_shared_rank(stat, r) : stat;
-                const float *ac = splits > 1 ? cluster.map_shared_rank(acc_s, r) : acc_s;
-                const float f = st[2 * g] == -INFINITY ? 0.f : exp2f(st[2 * g] - top);
-                s = fmaf(f, st[2 * g + 1], s);
+            for (uint32_t x = 0; x < splits; ++x) {
+                const float *st = splits > 1 ? cluster.map_shared_rank(stat, x) : stat;
+                const float *ac = splits > 1 ? cluster.map_shared_rank(acc_s, x) : acc_s;
+                const float f = fast_exp2(st[2 * r] - top);
+                s = fmaf(f, st[2 * r + 1], s);
                 a = fmaf(f, ac[i], a);
             }
         out[i] = from_f32<T>(s > 0.f ? a / s : 0.f);
@@ -195,18 +251,19 @@ attend_token_kernel(TokenParams p, uint32_t splits, uint32_t passes)
     if (splits > 1) cluster.sync();                                     // nobody leaves while its memory is read
 }
 
-template <typename T, int LPK, int GC>
+template <typename T, int NB, bool HI>
 int launch_token_shape(const TokenParams &p, int sms, cudaStream_t s)
 {
-    const uint32_t group = p.heads / p.kv_heads, passes = (group + GC - 1) / GC;
+    const uint32_t group = p.heads / p.kv_heads, passes = (group + kTokRows - 1) / kTokRows, rows = HI ? 16 : 8;
     const uint64_t items = (uint64_t)p.batch * p.kv_heads * passes;
-    // parts of a head: enough blocks for two on every SM, as long as a part keeps some 64 keys
+    // parts of a head: enough blocks for several on every SM, as long as a part keeps some 64 keys (one step of its
+    // warps) when blocks are few, 512 when there are plenty
     const uint64_t keys = (uint64_t)p.left + 1 + (uint64_t)p.sinks;
     uint32_t splits = 1;
-    while (splits < 8 && items * splits < 2ull * (uint64_t)sms && keys / (2 * splits) >= 64) splits *= 2;
+    while (splits < 8 && keys / (2 * splits) >= (items * splits < 2ull * (uint64_t)sms ? 64u : 512u) && items * splits < 8ull * (uint64_t)sms) splits *= 2;
     const uint32_t reach = p.b.n ? (uint32_t)p.b.start[p.b.n - 1] + 1 : 0;
-    const size_t smem = sizeof(float) * (2 * GC + (size_t)GC * p.dim + (kTokThreads / 32) * GC * (2 + (size_t)p.dim) + (size_t)reach * GC);
-    auto kernel = attend_token_kernel<T, LPK, GC>;
+    const size_t smem = sizeof(float) * (2 * rows + (size_t)rows * p.dim + kTokWarps * rows * (2 + (size_t)p.dim) + (size_t)reach * kTokRows);
+    auto kernel = attend_token_kernel<T, NB, HI>;
     if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return -1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((uint32_t)(items * splits));
@@ -222,24 +279,18 @@ int launch_token_shape(const TokenParams &p, int sms, cudaStream_t s)
     return cudaLaunchKernelEx(&cfg, kernel, p, splits, passes) == cudaSuccess ? 1 : -1;
 }
 
-template <typename T, int LPK>
-int launch_token_lanes(const TokenParams &p, int sms, cudaStream_t s)
+template <typename T>
+int launch_token_typed(const TokenParams &p, int sms, cudaStream_t s)
 {
-    const uint32_t group = p.heads / p.kv_heads;
-    if (group == 1) return launch_token_shape<T, LPK, 1>(p, sms, s);
-    if (group == 2) return launch_token_shape<T, LPK, 2>(p, sms, s);
-    if (group <= 4) return launch_token_shape<T, LPK, 4>(p, sms, s);
-    return launch_token_shape<T, LPK, 8>(p, sms, s);
+    const bool hi = p.heads / p.kv_heads > 8;
+    if (p.dim <= 64) return hi ? launch_token_shape<T, 1, true>(p, sms, s) : launch_token_shape<T, 1, false>(p, sms, s);
+    return hi ? launch_token_shape<T, 2, true>(p, sms, s) : launch_token_shape<T, 2, false>(p, sms, s);
 }
 
 int launch_attend_token(const TokenParams &p, uint32_t type, int sms, cudaStream_t s)
 {
     if (p.batch == 0) return 0;
-    if (type == kBF16)
-        return p.dim <= 32 ? launch_token_lanes<__nv_bfloat16, 4>(p, sms, s)
-               : p.dim <= 64 ? launch_token_lanes<__nv_bfloat16, 8>(p, sms, s) : launch_token_lanes<__nv_bfloat16, 16>(p, sms, s);
-    return p.dim <= 32 ? launch_token_lanes<__half, 4>(p, sms, s)
-           : p.dim <= 64 ? launch_token_lanes<__half, 8>(p, sms, s) : launch_token_lanes<__half, 16>(p, sms, s);
+    return type == kBF16 ? launch_token_typed<__nv_bfloat16>(p, sms, s) : launch_token_typed<__half>(p, sms, s);
 }
 
 }  // namespace w2v

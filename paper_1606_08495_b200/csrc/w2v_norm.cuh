@@ -12,24 +12,64 @@ namespace w2v {
 
 constexpr uint32_t kNormPer = 16;
 
-// Sums two values over the `gw` warps of a row's group; `slot` is the group's shared memory, two
-// floats per warp, and `flip` alternates from call to call so that one barrier per call is enough.
-__device__ __forceinline__ float2 group_sum2(float a, float b, uint32_t gw, uint32_t wig, uint32_t group, uint32_t lane,
-                                             float2 *slot, uint32_t flip)
+// Sums K values over the `gw` warps of a row's group; `slot` is shared memory for K floats per warp, twice: `flip`
+// alternates from call to call so that one barrier per call is enough.
+template <int K>
+__device__ __forceinline__ void group_sum(float (&a)[K], uint32_t gw, uint32_t wig, uint32_t group, uint32_t lane, float *slot,
+                                          uint32_t flip)
 {
-    a = warp_sum(a);
-    b = warp_sum(b);
-    if (gw == 1) return make_float2(a, b);
-    float2 *s = slot + flip * 32u;
-    if (lane == 0) s[group * gw + wig] = make_float2(a, b);
-    asm volatile("bar.sync %0, %1;" ::"r"(group + 1u), "r"(gw * 32u) : "memory");
-    float2 t = make_float2(0.f, 0.f);
-    for (uint32_t w = 0; w < gw; ++w) {
-        const float2 x = s[group * gw + w];
-        t.x += x.x;
-        t.y += x.y;
+#pragma unroll
+    for (int k = 0; k < K; ++k) a[k] = warp_sum(a[k]);
+    if (gw == 1) return;
+    float *s = slot + flip * 32u * K + group * gw * K;
+    if (lane == 0) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) s[wig * K + k] = a[k];
     }
-    return t;
+    asm volatile("bar.sync %0, %1;" ::"r"(group + 1u), "r"(gw * 32u) : "memory");
+    const uint32_t wide = 1u << (32 - __clz(gw - 1u)), from = lane & (wide - 1u);     // gw rounded up to a power of two
+#pragma unroll
+    for (int k = 0; k < K; ++k) a[k] = from < gw ? s[from * K + k] : 0.f;
+    for (uint32_t o = wide >> 1; o > 0; o >>= 1) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) a[k] += __shfl_xor_sync(kFullMask, a[k], o);
+    }
+}
+
+// A lane's chunks of one row, zeros past its end.
+template <typename T, int E, int NV>
+__device__ __forceinline__ void norm_row_load(Pack<T, E> (&v)[NV], const T *row, uint32_t gl, uint32_t gw, uint32_t d)
+{
+#pragma unroll
+    for (int c = 0; c < NV; ++c) {
+        const uint32_t at = (gl + c * 32u * gw) * E;
+        if (at < d) v[c] = load_pack<T, E>(row + at);
+        else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[c].e[e] = from_f32<T>(0.f);
+        }
+    }
+}
+
+// A lane's weights (zeros past the row's end), 16 bytes at a time where they are aligned.
+template <int E, int NV>
+__device__ __forceinline__ void norm_weights_load(float (&w)[NV * E], const float *from, uint32_t gl, uint32_t gw, uint32_t d)
+{
+    const bool wide = E % 4 == 0 && (reinterpret_cast<uintptr_t>(from) & 15u) == 0;
+#pragma unroll
+    for (int c = 0; c < NV; ++c) {
+        const uint32_t at = (gl + c * 32u * gw) * E;
+        if (wide) {
+#pragma unroll
+            for (int e = 0; e + 3 < E; e += 4) {
+                const float4 t = at < d ? __ldg(reinterpret_cast<const float4 *>(from + at + e)) : make_float4(0.f, 0.f, 0.f, 0.f);
+                w[c * E + e] = t.x; w[c * E + e + 1] = t.y; w[c * E + e + 2] = t.z; w[c * E + e + 3] = t.w;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) w[c * E + e] = at < d ? __ldg(from + at + e) : 0.f;
+        }
+    }
 }
 
 struct NormShape {

@@ -12,7 +12,7 @@ template <typename TX, typename TY, int E, int NV>
 __global__ void __launch_bounds__(512)
 norm_backward_kernel(NormParams p, uint32_t gw, uint32_t groups)
 {
-    __shared__ float2 slot[64];
+    __shared__ float slot[128];
     extern __shared__ float sums[];                     // [groups - 1][2][d], only with more than one row per block
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const uint32_t group = warp / gw, wig = warp - group * gw, gl = wig * 32 + lane;
@@ -20,44 +20,56 @@ norm_backward_kernel(NormParams p, uint32_t gw, uint32_t groups)
     const TY *dy = static_cast<const TY *>(p.dy);
     TX *dx = static_cast<TX *>(p.dx);
     const float inv_d = 1.0f / (float)p.d;
-    float dg[NV * E], db[NV * E];
+    const uint64_t step = (uint64_t)gridDim.x * groups;
+    uint64_t r = (uint64_t)blockIdx.x * groups + group;
+    // the next row's x, dy and statistics are under way while one row is worked on
+    Pack<TX, E> xn[NV];
+    Pack<TY, E> yn[NV];
+    float mean_n = 0.f, rstd_n = 0.f;
+    auto fetch = [&](uint64_t row) {
+        norm_row_load<TX, E, NV>(xn, x + row * p.ldx, gl, gw, p.d);
+        norm_row_load<TY, E, NV>(yn, dy + row * p.ldy, gl, gw, p.d);
+        mean_n = p.mean[row];
+        rstd_n = p.rstd[row];
+    };
+    if (r < p.rows) fetch(r);
+    float gamma[NV * E], dg[NV * E], db[NV * E];
+    norm_weights_load<E, NV>(gamma, p.gamma, gl, gw, p.d);
 #pragma unroll
     for (int i = 0; i < NV * E; ++i) dg[i] = db[i] = 0.f;
     uint32_t flip = 0;
-    for (uint64_t r = (uint64_t)blockIdx.x * groups + group; r < p.rows; r += (uint64_t)gridDim.x * groups) {
-        const float mean = p.mean[r], rstd = p.rstd[r];
-        float xh[NV * E], g[NV * E];
-        float a = 0.f, b = 0.f;
+    for (; r < p.rows; r += step) {
+        const float mean = mean_n, rstd = rstd_n;
+        Pack<TX, E> xc[NV];
+        Pack<TY, E> yc[NV];
+        float t[2] = {0.f, 0.f};
 #pragma unroll
         for (int c = 0; c < NV; ++c) {
-            const uint32_t at = (gl + c * 32u * gw) * E;
+            xc[c] = xn[c];
+            yc[c] = yn[c];
 #pragma unroll
-            for (int e = 0; e < E; ++e) xh[c * E + e] = g[c * E + e] = 0.f;
-            if (at < p.d) {
-                const Pack<TX, E> t = load_pack<TX, E>(x + r * p.ldx + at);
-                const Pack<TY, E> u = load_pack<TY, E>(dy + r * p.ldy + at);
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const float h = (to_f32(t.e[e]) - mean) * rstd, w = to_f32(u.e[e]);
-                    dg[c * E + e] = fmaf(w, h, dg[c * E + e]);
-                    db[c * E + e] += w;
-                    xh[c * E + e] = h;
-                    g[c * E + e] = w * __ldg(p.gamma + at + e);
-                    a += g[c * E + e];
-                    b = fmaf(g[c * E + e], h, b);
-                }
+            for (int e = 0; e < E; ++e) {               // past the row's end dy and gamma are zero
+                const float h = (to_f32(xc[c].e[e]) - mean) * rstd, w = to_f32(yc[c].e[e]), g = w * gamma[c * E + e];
+                dg[c * E + e] = fmaf(w, h, dg[c * E + e]);
+                db[c * E + e] += w;
+                t[0] += g;
+                t[1] = fmaf(g, h, t[1]);
             }
         }
-        const float2 t = group_sum2(a, b, gw, wig, group, lane, slot, flip);
+        if (r + step < p.rows) fetch(r + step);
+        group_sum<2>(t, gw, wig, group, lane, slot, flip);
         flip ^= 1u;
-        const float ma = t.x * inv_d, mb = t.y * inv_d;
+        const float ma = t[0] * inv_d, mb = t[1] * inv_d;
 #pragma unroll
         for (int c = 0; c < NV; ++c) {
             const uint32_t at = (gl + c * 32u * gw) * E;
             if (at < p.d) {
                 Pack<TX, E> o;
 #pragma unroll
-                for (int e = 0; e < E; ++e) o.e[e] = from_f32<TX>(rstd * (g[c * E + e] - ma - xh[c * E + e] * mb));
+                for (int e = 0; e < E; ++e) {           // formed again from the packed row: fewer registers than keeping them
+                    const float h = (to_f32(xc[c].e[e]) - mean) * rstd, g = to_f32(yc[c].e[e]) * gamma[c * E + e];
+                    o.e[e] = from_f32<TX>(rstd * (g - ma - h * mb));
+                }
                 store_pack<TX, E>(dx + r * p.ld_dx + at, o);
             }
         }
@@ -114,9 +126,9 @@ norm_weights_kernel(const float *part, uint32_t blocks, uint32_t d, float *dgamm
 
 uint32_t norm_backward_blocks(uint64_t rows, uint32_t d, int sms)
 {
-    // resident blocks of the widest and of the narrowest access differ little: sized by the row length alone
+    // at 128 registers a thread 16 warps are resident per SM
     const uint32_t gw = (d + 32 * kNormPer - 1) / (32 * kNormPer), groups = gw >= 8 ? 1 : 8 / gw;
-    const uint32_t per_sm = 24 / (gw * groups) ? 24 / (gw * groups) : 1;
+    const uint32_t per_sm = 16 / (gw * groups) ? 16 / (gw * groups) : 1;
     const uint64_t want = (rows + groups - 1) / groups, most = (uint64_t)sms * per_sm;
     return (uint32_t)(want < most ? want : most);
 }
