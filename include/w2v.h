@@ -564,7 +564,7 @@ typedef struct {
     uint32_t buckets;    /* rows of the bias table, 0 = no bias */
     uint32_t reach;      /* distance from which on every key falls in the last bucket, or nearly; at most 1024 */
     uint32_t two_sided;  /* 1: the second half of the buckets is for keys after the query */
-    float scale;         /* of the products q.k */
+    float scale;         /* of the products q.k, positive */
 } w2v_window;
 
 /*

@@ -1,80 +1,111 @@
 // Attention over a window of the sentence on the tensor cores.
+//
+// A block takes 128 queries of a head and streams the keys and values of its run in tiles of 64 through a ring in
+// shared memory.  Two warpgroups take the tiles in turn, one row per thread; each has a score buffer, a running
+// reference, a sum and an output accumulator of its own in tensor memory, so that neither waits for the other; the two
+// are joined at the end.  The softmax weights go back to tensor memory, over the scores, as the A side of P V.
+// A tile's scores are read twice from tensor memory instead of being held: the first pass finds the largest (and,
+// where a tile has masks or differing biases, writes the scores back with both applied), the second exponentiates.
+// The output is rescaled only when a row's largest score outgrows the reference by 2^8.
+//
+// What bounds it: 64 x 128 exponentials take the special-function units 512 cycles, the products of a head of 64
+// take the tensor cores 128; the rest of the second pass is two fp32 operations per instruction.
 #include <type_traits>
 
 #include "w2v_attend.cuh"
 
 namespace w2v {
 
-constexpr int kFwdThreads = 256;                 // warps 0-3: one softmax row per thread; warp 4: MMA; warps 5-7: copies
-constexpr int kFwdLoaders = 96;
-constexpr int kSoftmaxRegs = 200, kOtherRegs = 56;      // of 128 per thread at launch: 4 x 200 + 4 x 56 warps' shares = 8 x 128
+constexpr int kFwdRows = 64;                     // keys per tile
+constexpr int kFwdThreads = 384;                 // warps 0-7: two softmax warpgroups; warp 8: MMA; warp 9: copies; warps 10-11: rows that are not words
+// Heads of at most 64: of the 80 registers a thread has at launch with two blocks per SM, the third warpgroup gives
+// its share beyond 48 to the two of the softmax (96 + 96 + 48 = 3 x 80).
+constexpr int kLaunchRegs = 80, kSoftmaxRegs = 96, kOtherRegs = 48;
 constexpr float kRescale = 8.f;                  // base-2: how far a row's scores may outgrow its reference before the output is rescaled
 
 // NB = 64-column blocks of a head (1: head_dim <= 64, 2: up to 128).
 template <int NB>
 struct FwdShape {
-    static constexpr int kStages = NB == 1 ? 2 : 1;                 // of keys and of values each
-    static constexpr int kTileBytes = NB * kAttendTile * 128;
-    static constexpr bool kOwnP = NB == 1;                          // the weights have tensor memory of their own
-    static constexpr uint32_t kS = 0, kP = NB == 1 ? 128 : 0, kO = NB == 1 ? 192 : 128;   // columns
-    static constexpr int kSmem = kTileBytes * (1 + 2 * kStages) + 1024;
+    static constexpr int kBlocks = NB == 1 ? 2 : 1;                 // resident per SM: tensor memory is the limit
+    static constexpr bool kQTmem = NB == 2;                         // queries as an A side in tensor memory (read from shared memory
+                                                                    // for every tile they would cost as much as keys and values)
+    static constexpr int kStages = NB == 1 ? 4 : 3;
+    static constexpr int kOperand = NB * kFwdRows * 128, kStage = 2 * kOperand, kQBytes = kQTmem ? 0 : NB * 128 * 128;
+    static constexpr uint32_t kQ = 0, kS = NB == 1 ? 0 : 64, kO = NB == 1 ? 128 : 192, kAlloc = NB == 1 ? 256 : 512;   // columns
+    static constexpr int kRing = kQBytes + kStages * kStage;
+    static_assert(kRing >= NB * 128 * 128, "the output is staged where the ring was");
 };
 
 struct FwdShared {
-    uint64_t q_full, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full, s_free, p_full, pv_done;
+    uint64_t q_full, landed[4], full[4], empty[4], s_full[2], p_full[2], done;
     uint32_t tmem;
-    int abort_flag;
-    int32_t limits[4][6];                        // per warp: least lo, largest hi, least s, largest lo, least hi, any row
-    uint32_t vis[2][4];                          // per key stage: which keys are words
+    int abort_flag, quiet;
+    int32_t limits[4][3];                        // per warp: least lo, largest hi, least sentence start
+    uint32_t vis[4][2];                          // per stage: which keys are words
+    float ref[2][128], sum[2][128];              // per warpgroup and row
 };
 
 template <typename T, int NB>
-__global__ void __launch_bounds__(kFwdThreads, 2)
-attend_tc_kernel(AttendParams p, int *error)
+__global__ void __launch_bounds__(kFwdThreads, FwdShape<NB>::kBlocks)
+attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                 const __grid_constant__ CUtensorMap map_v, AttendParams p, int *error)
 {
     using Sh = FwdShape<NB>;
-    constexpr bool kBf16 = sizeof(T) == 2 && std::is_same<T, __nv_bfloat16>::value;
+    constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
     extern __shared__ unsigned char smem_raw[];
     __shared__ FwdShared sh;
     unsigned char *smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
-    const uint32_t qs = smem_addr(smem), ks = qs + Sh::kTileBytes, vs = ks + Sh::kStages * Sh::kTileBytes;
-    float *lut = reinterpret_cast<float *>(smem + Sh::kTileBytes * (1 + 2 * Sh::kStages));
+    const uint32_t qs = smem_addr(smem), ring = qs + Sh::kQBytes;
+    float *lut = reinterpret_cast<float *>(smem + Sh::kRing);
 
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t h = blockIdx.x % p.heads, kvh = h / (p.heads / p.kv_heads);
     const int32_t t0 = (int32_t)(blockIdx.x / p.heads) * kAttendTile;
-    const uint32_t dim16 = (p.dim + 15u) & ~15u;
-
-    if (tid == 0) {
-        mbar_init(&sh.q_full, kFwdLoaders);
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(&sh.k_full[i], kFwdLoaders); mbar_init(&sh.k_empty[i], 1 + kAttendTile);
-            mbar_init(&sh.v_full[i], kFwdLoaders); mbar_init(&sh.v_empty[i], 1);
-        }
-        mbar_init(&sh.s_full, 1); mbar_init(&sh.s_free, kAttendTile);
-        mbar_init(&sh.p_full, kAttendTile); mbar_init(&sh.pv_done, 1);
-        sh.abort_flag = 0;
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
+    const uint32_t dim16 = (p.dim + 15u) & ~15u, dch = p.dim >> 3;
+    const uint32_t r = tid & 127u;                                   // this thread's row (softmax warps)
+    const int64_t own = (int64_t)t0 + r;
+    const T *q_head = static_cast<const T *>(p.q) + (uint64_t)h * p.dim;
     RowLimits row = {0, 0, 0, 0};
-    if (warp < 4) {
-        row = row_limits(p, (int64_t)t0 + tid);
-        const bool any = row.hi > row.lo;
-        const int32_t lo = __reduce_min_sync(kFullMask, any ? row.lo : INT32_MAX), hi = __reduce_max_sync(kFullMask, row.hi);
-        const int32_t s = __reduce_min_sync(kFullMask, any ? row.s : INT32_MAX);
-        if (lane == 0) { sh.limits[warp][0] = lo; sh.limits[warp][1] = hi; sh.limits[warp][2] = s; }
-    }
-    if (warp == 4) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&sh.tmem)), "r"(256));
+    uint4 q_row[Sh::kQTmem ? NB * 8 : 1];
+
+    if (warp < 8) {
+        row = row_limits(p, own);
+        if (warp < 4) {
+            if (Sh::kQTmem) {
+#pragma unroll
+                for (int c = 0; c < NB * 8; ++c)
+                    q_row[c] = own < p.n && (uint32_t)c < dch ? __ldg(reinterpret_cast<const uint4 *>(q_head + own * (int64_t)p.ldq) + c) : make_uint4(0, 0, 0, 0);
+            }
+            const bool any = row.hi > row.lo;
+            const int32_t lo = __reduce_min_sync(kFullMask, any ? row.lo : INT32_MAX), hi = __reduce_max_sync(kFullMask, row.hi);
+            const int32_t s = __reduce_min_sync(kFullMask, any ? row.s : INT32_MAX);
+            if (lane == 0) { sh.limits[warp][0] = lo; sh.limits[warp][1] = hi; sh.limits[warp][2] = s; }
+        } else if (p.b.n) {
+            fill_bias(p, h, lut, warp - 4, 4, lane);
+        }
+    } else if (warp == 8) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&sh.tmem)), "r"(Sh::kAlloc));
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    } else if (warp == 9 && lane == 0) {
+        mbar_init(&sh.q_full, Sh::kQTmem ? 128 : 1);
+        for (int i = 0; i < Sh::kStages; ++i) { mbar_init(&sh.landed[i], 1); mbar_init(&sh.full[i], 32); mbar_init(&sh.empty[i], 1 + 128); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&sh.s_full[i], 1); mbar_init(&sh.p_full[i], 128); }
+        mbar_init(&sh.done, 1);
+        sh.abort_flag = sh.quiet = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_async_proxy();
+        // a query that is not a word may hold anything: it spoils its own scores only, which are never used
+        if (!Sh::kQTmem) {
+            mbar_expect(&sh.q_full, Sh::kQBytes);
+            copy_box(qs, &map_q, 0, (int32_t)h, t0, &sh.q_full);
+        }
     }
-    if (p.b.n) fill_bias(p, h, lut, tid, kFwdThreads);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = sh.tmem;
     volatile int *abort_flag = &sh.abort_flag;
-    // the run of keys [lo, hi) and the sinks [s, s_end) before it
+    // the run of keys [lo, hi) and the sinks [s, s_end) before it, which are the first tile
     int32_t lo = INT32_MAX, hi = 0, s = INT32_MAX;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
@@ -84,226 +115,261 @@ attend_tc_kernel(AttendParams p, int *error)
     }
     const int32_t s_end = hi ? min(s + p.sinks, lo) : 0;
     const int32_t extra = s < s_end ? 1 : 0;
-    const int32_t tiles = hi ? extra + (hi - lo + kAttendTile - 1) / kAttendTile : 0;
-    auto tile_at = [&](int32_t t) { return extra && t == 0 ? s : lo + (t - extra) * kAttendTile; };
-    auto tile_keys = [&](int32_t t) { return extra && t == 0 ? s_end - s : min(kAttendTile, hi - tile_at(t)); };
+    const int32_t tiles = hi ? extra + (hi - lo + kFwdRows - 1) / kFwdRows : 0;
+    auto tile_at = [&](int32_t t) { return extra && t == 0 ? s : lo + (t - extra) * kFwdRows; };
+    auto tile_keys = [&](int32_t t) { return extra && t == 0 ? s_end - s : min(kFwdRows, hi - tile_at(t)); };
 
-    if (warp < 4) {
-        // ============ softmax: one row per thread ============
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
-        const int64_t i = (int64_t)t0 + tid;
-        const uint32_t lanes = (warp * 32u) << 16;
-        const float scale = p.scale * kLog2e;
-        const int32_t last = bias_last(p.b);
-        const float *near_row = lut - i + last + kBiasPad;         // + key position
-        float ref = -INFINITY, sum = 0.f;
-        bool ok = true;
-        for (int32_t t = 0; t < tiles; ++t) {
-            const int32_t k0 = tile_at(t), keys = tile_keys(t), cols = (keys + 15) & ~15;
-            if (!__all_sync(kFullMask, mbar_wait(&sh.s_full, t & 1, abort_flag))) { ok = false; break; }
-            tc_fence_after();
-            const uint32_t stage = t % Sh::kStages;
-            if (!__all_sync(kFullMask, mbar_wait(&sh.k_full[stage], (t / Sh::kStages) & 1, abort_flag))) { ok = false; break; }   // the bits of the keys
-            float x[4][32];
-            float top = -INFINITY;
-            // far from the rows every key of the tile has the bias of the side's last bucket
-            const bool far = p.b.n == 0 || k0 + cols - 1 - t0 <= -last || k0 - (t0 + kAttendTile - 1) >= last;
-            const float flat = p.b.n ? lut[k0 < t0 ? 0 : bias_entries(p.b) - 1] : 0.f;
-            const float *near = near_row + k0;
+    if (warp < 8) {
+        // ============ softmax: one row per thread, tiles in turn ============
+        if (NB == 1) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+        const uint32_t wg = warp >> 2, lanes = ((warp & 3u) * 32u) << 16;
+        const uint32_t cs = tmem + lanes + Sh::kS + wg * kFwdRows, co = tmem + lanes + Sh::kO + wg * NB * 64;
+        if (Sh::kQTmem && wg == 0) {
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                if (c * 32 < cols) {
+            for (int g = 0; g < NB * 2; ++g) {
+                uint32_t x[16];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const uint4 u = q_row[Sh::kQTmem ? g * 4 + c : 0];
+                    x[c * 4] = u.x; x[c * 4 + 1] = u.y; x[c * 4 + 2] = u.z; x[c * 4 + 3] = u.w;
+                }
+                tmem_st16(tmem + lanes + Sh::kQ + g * 16, x);
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            mbar_arrive(&sh.q_full);
+        }
+        const float scale = p.scale * kLog2e;
+        const int32_t last = bias_last(p.b), w0 = t0 + (int32_t)(warp & 3u) * 32;
+        const bool word = row.hi > row.lo;
+        // keys that every row of the warp sees (rows that are not words do not matter)
+        const int32_t all_lo = __reduce_max_sync(kFullMask, word ? row.lo : 0), all_hi = __reduce_min_sync(kFullMask, word ? row.hi : INT32_MAX);
+        float ref = -INFINITY;
+        float2 sum2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+        bool ok = true;
+        for (int32_t t = (int32_t)wg; t < tiles; t += 2) {
+            const int32_t k0 = tile_at(t), keys = tile_keys(t), cols = (keys + 15) & ~15;
+            const uint32_t stage = t % Sh::kStages;
+            ok = __all_sync(kFullMask, mbar_wait(&sh.full[stage], (t / Sh::kStages) & 1, abort_flag) &&        // the bits of the keys
+                                           mbar_wait(&sh.s_full[wg], (t >> 1) & 1, abort_flag));
+            if (!ok) break;
+            tc_fence_after();
+            // far from the warp's rows every key of the tile has the bias of the side's last bucket
+            const bool far_left = k0 + kFwdRows - 1 - w0 <= -last, far = p.b.n == 0 || far_left || k0 - (w0 + 31) >= last;
+            const float flat = p.b.n ? lut[far_left ? 0 : bias_entries(p.b) - 1] : 0.f;
+            const uint32_t vis0 = sh.vis[stage][0], vis1 = sh.vis[stage][1];
+            const bool plain = far && k0 >= all_lo && k0 + kFwdRows <= all_hi && (vis0 & vis1) == 0xFFFFFFFFu;
+            float top = -INFINITY, by = 1.f, add = 0.f;
+            if (plain) {
+                float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                uint32_t v[2][32];
+                tmem_ld32(cs, v[0]);
+                tmem_ld32(cs + 32, v[1]);
+                tmem_wait_ld(v[0]);
+                tmem_held(v[1]);
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) {
+                        float &x = m[(e >> 1) & 3];
+                        x = fmaxf(x, fmaxf(__uint_as_float(v[c][e]), __uint_as_float(v[c][e + 1])));
+                    }
+                top = fmaf(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])), scale, flat);
+                by = scale;
+                add = flat;
+            } else {
+#pragma unroll 1
+                for (int c = 0; c < 2; ++c) {
+                    if (c * 32 >= cols) break;
                     uint32_t v[32];
-                    tmem_ld32(tmem + lanes + Sh::kS + c * 32, v);
+                    tmem_ld32(cs + c * 32, v);
                     tmem_wait_ld(v);
+                    const int32_t at = k0 + c * 32;
+                    const uint32_t m = (range_bits(row.lo, row.hi, at) | range_bits(row.s, row.se, at)) & (c ? vis1 : vis0);
                     if (far) {
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) x[c][e] = fmaf(__uint_as_float(v[e]), scale, flat);
+                        for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(fmaf(__uint_as_float(v[e]), scale, flat));
                     } else {
+                        const float *near = lut + (at - (int32_t)own + last + kBiasPad);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) x[c][e] = fmaf(__uint_as_float(v[e]), scale, near[c * 32 + e]);
+                        for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(fmaf(__uint_as_float(v[e]), scale, near[e]));
                     }
-                    const int32_t at = k0 + c * 32;
-                    const uint32_t m = (range_bits(row.lo, row.hi, at) | range_bits(row.s, row.se, at)) & sh.vis[stage][c];
                     if (!__all_sync(kFullMask, m == 0xFFFFFFFFu)) {
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) x[c][e] = (m >> e) & 1u ? x[c][e] : -INFINITY;
+                        for (int e = 0; e < 32; ++e) v[e] = m & (1u << e) ? v[e] : 0xFF800000u;      // -infinity
                     }
+                    float n[4] = {top, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) top = fmaxf(top, x[c][e]);
+                    for (int e = 0; e < 32; e += 2) n[(e >> 1) & 3] = fmaxf(n[(e >> 1) & 3], fmaxf(__uint_as_float(v[e]), __uint_as_float(v[e + 1])));
+                    top = fmaxf(fmaxf(n[0], n[1]), fmaxf(n[2], n[3]));
+                    tmem_st32(cs + c * 32, v);
                 }
-            }
-            mbar_arrive(&sh.k_empty[stage]);                         // this thread is done with the stage's bits
-            if (Sh::kOwnP) {                                         // the next scores may be computed
-                tc_fence_before();
-                mbar_arrive(&sh.s_free);
+                tmem_wait_st();
             }
             const bool grown = top > ref + kRescale || (ref == -INFINITY && top > ref);
-            if (t > 0 && !__all_sync(kFullMask, mbar_wait(&sh.pv_done, (t - 1) & 1, abort_flag))) { ok = false; break; }
             if (__any_sync(kFullMask, grown)) {
-                const float to = grown ? top : ref;
-                const float keep = ref == -INFINITY ? 0.f : fast_exp2(ref - to);
+                const float to = grown ? top : ref, keep = ref == -INFINITY ? 0.f : fast_exp2(ref - to);
                 ref = to;
-                sum *= keep;
-                if (t > 0) {
-                    tc_fence_after();
+                sum2[0].x *= keep; sum2[0].y *= keep; sum2[1].x *= keep; sum2[1].y *= keep;
+                if (t >= 2) {                                        // the scores came after the warpgroup's last product with values: the output is still
                     for (uint32_t c = 0; c < dim16; c += 16) {
                         uint32_t o[16];
-                        tmem_ld16(tmem + lanes + Sh::kO + c, o);
+                        tmem_ld16(co + c, o);
                         tmem_wait_ld(o);
 #pragma unroll
                         for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * keep);
-                        tmem_st16(tmem + lanes + Sh::kO + c, o);
+                        tmem_st16(co + c, o);
                     }
                 }
             }
-            const float from = ref == -INFINITY ? 0.f : ref;
+            add -= ref == -INFINITY ? 0.f : ref;
+            const float2 by2 = make_float2(by, by), add_2 = make_float2(add, add);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
+            for (int c = 0; c < 2; ++c) {
                 if (c * 32 < cols) {
-                    uint32_t w[16];
+                    uint32_t v[32], w[16];
+                    tmem_ld32(cs + c * 32, v);
+                    tmem_wait_ld(v);
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        const float a = fast_exp2(x[c][2 * e] - from), b = fast_exp2(x[c][2 * e + 1] - from);
-                        sum += a + b;
-                        w[e] = pack2<T>(a, b);
+                        float2 x = fma2(pair_of(v[2 * e], v[2 * e + 1]), by2, add_2);
+                        x.x = fast_exp2(x.x);
+                        x.y = fast_exp2(x.y);
+                        sum2[e & 1] = add2(sum2[e & 1], x);
+                        w[e] = pack2<T>(x.x, x.y);
                     }
-                    tmem_st16(tmem + lanes + Sh::kP + c * 16, w);
+                    tmem_st16(cs + c * 16, w);                       // over scores that have been read
                 }
             }
             tmem_wait_st();
             tc_fence_before();
-            mbar_arrive(&sh.p_full);
+            mbar_arrive(&sh.p_full[wg]);
+            mbar_arrive(&sh.empty[stage]);                           // this thread is done with the stage's bits
         }
-        ok = __all_sync(kFullMask, ok && (tiles == 0 || mbar_wait(&sh.pv_done, (tiles - 1) & 1, abort_flag)));
+        // the two warpgroups' rows are joined: each takes half of the columns of every row
+        const float mine = (sum2[0].x + sum2[0].y) + (sum2[1].x + sum2[1].y);
+        sh.ref[wg][r] = ref;
+        sh.sum[wg][r] = word ? mine : 0.f;
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        const float r0 = sh.ref[0][r], r1 = sh.ref[1][r], to = fmaxf(r0, r1);
+        ok = __all_sync(kFullMask, ok && (tiles == 0 || mbar_wait(&sh.done, 0, abort_flag)));
         tc_fence_after();
-        // the output leaves through shared memory (every tile is read by now), a row of 16-byte chunks at a time
-        const float inv = ok && sum > 0.f ? 1.f / sum : 0.f;
-        if (p.lse && i < p.n) p.lse[(int64_t)h * p.n + i] = sum > 0.f ? ref + log2f(sum) : INFINITY;
-        const uint32_t row_bytes = p.dim * 2u;
-        unsigned char *mine = smem + warp * 32u * row_bytes, *line = mine + lane * row_bytes;
-        const int32_t rows = (int32_t)min((int64_t)32, p.n - (t0 + (int64_t)warp * 32));
-        for (uint32_t c = 0; c < dim16; c += 16) {
-            uint32_t o[16];
-            if (tiles) { tmem_ld16(tmem + lanes + Sh::kO + c, o); tmem_wait_ld(o); }
-            else {
+        float f0 = to == -INFINITY ? 0.f : fast_exp2(r0 - to), f1 = to == -INFINITY ? 0.f : fast_exp2(r1 - to);
+        const float total = sh.sum[0][r] * f0 + sh.sum[1][r] * f1, inv = total > 0.f ? 1.f / total : 0.f;
+        if (p.lse && wg == 0 && own < p.n) p.lse[(int64_t)h * p.n + own] = total > 0.f ? to + log2f(total) : INFINITY;
+        f0 *= inv;
+        f1 *= inv;
+        // out through shared memory (every tile is read by now), a row of 16-byte chunks at a time
+        const uint32_t row_bytes = p.dim * 2u, part = (warp & 3u) * 32u;
+        unsigned char *stripe = smem + part * row_bytes, *line = stripe + lane * row_bytes;
+        for (uint32_t c = wg * 16; c < dim16; c += 32) {
+            uint32_t a[16], b[16];
+            tmem_ld16(tmem + lanes + Sh::kO + c, a);
+            tmem_ld16(tmem + lanes + Sh::kO + NB * 64 + c, b);
+            tmem_wait_ld(a);
+            tmem_wait_ld(b);
+            float o[16];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) o[e] = 0u;
+            for (int e = 0; e < 16; ++e) {                           // an accumulator that no tile was added to holds anything
+                const float x = f0 > 0.f ? __uint_as_float(a[e]) * f0 : 0.f;
+                o[e] = f1 > 0.f ? fmaf(__uint_as_float(b[e]), f1, x) : x;
             }
 #pragma unroll
             for (int g = 0; g < 2; ++g)
                 if (c + g * 8 < p.dim) {
                     uint4 w;
-                    w.x = pack2<T>(__uint_as_float(o[g * 8 + 0]) * inv, __uint_as_float(o[g * 8 + 1]) * inv);
-                    w.y = pack2<T>(__uint_as_float(o[g * 8 + 2]) * inv, __uint_as_float(o[g * 8 + 3]) * inv);
-                    w.z = pack2<T>(__uint_as_float(o[g * 8 + 4]) * inv, __uint_as_float(o[g * 8 + 5]) * inv);
-                    w.w = pack2<T>(__uint_as_float(o[g * 8 + 6]) * inv, __uint_as_float(o[g * 8 + 7]) * inv);
-                    const uint32_t ch = (c >> 3) + g, chunks = p.dim >> 3;
-                    *reinterpret_cast<uint4 *>(line + ((ch + lane) % chunks) * 16u) = w;       // turned by the row: fewer bank conflicts
+                    w.x = pack2<T>(o[g * 8], o[g * 8 + 1]); w.y = pack2<T>(o[g * 8 + 2], o[g * 8 + 3]);
+                    w.z = pack2<T>(o[g * 8 + 4], o[g * 8 + 5]); w.w = pack2<T>(o[g * 8 + 6], o[g * 8 + 7]);
+                    uint32_t ch = (c >> 3) + g + lane;               // turned by the row: fewer bank conflicts
+                    while (ch >= dch) ch -= dch;
+                    *reinterpret_cast<uint4 *>(line + ch * 16u) = w;
                 }
+        }
+        asm volatile("bar.sync %0, 64;" ::"r"(2u + (warp & 3u)) : "memory");        // the two warps of these rows
+        store_rows(static_cast<char *>(p.out) + ((uint64_t)(t0 + part) * p.ldo + (uint64_t)h * p.dim) * 2u, p.ldo * 2u, stripe, dch,
+                   (int32_t)min((int64_t)32, p.n - (int64_t)(t0 + part)), wg * 32u + lane, 64u);
+        tc_fence_before();
+    } else if (warp == 8) {
+        // ============ MMA issue: one lane ============
+        if (NB == 1) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        if (lane == 0 && tiles) {
+            const uint32_t idesc_o = umma_idesc_f16(kBf16, kAttendTile, dim16, true);
+            constexpr uint32_t kBlock = kFwdRows * 128;
+            auto scores = [&](int32_t t) {
+                const uint32_t k = ring + (t % Sh::kStages) * Sh::kStage, d = tmem + Sh::kS + (t & 1) * kFwdRows;
+                const uint32_t idesc = umma_idesc_f16(kBf16, kAttendTile, (uint32_t)(tile_keys(t) + 15) & ~15u, false);
+                for (uint32_t c = 0; c < dim16; c += 16) {
+                    const uint64_t kd = umma_desc_sw128(k + (c >> 6) * kBlock + (c & 63u) * 2u, 0);
+                    if (Sh::kQTmem) umma_f16_ts(d, tmem + Sh::kQ + c / 2, kd, idesc, c > 0);
+                    else umma_f16_ss(d, umma_desc_sw128(qs + (c >> 6) * (kAttendTile * 128) + (c & 63u) * 2u, 0), kd, idesc, c > 0);
+                }
+                umma_commit(&sh.s_full[t & 1]);
+            };
+            bool ok = mbar_wait(&sh.q_full, 0, abort_flag);
+            for (int32_t t = 0; t < 2 && t < tiles && ok; ++t) {
+                ok = mbar_wait(&sh.full[t % Sh::kStages], 0, abort_flag);
+                if (ok) { tc_fence_after(); scores(t); }
+            }
+            for (int32_t t = 0; t < tiles && ok; ++t) {
+                ok = mbar_wait(&sh.p_full[t & 1], (t >> 1) & 1, abort_flag);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t v = ring + (t % Sh::kStages) * Sh::kStage + Sh::kOperand, cols = (uint32_t)(tile_keys(t) + 15) & ~15u;
+                for (uint32_t k = 0; k < cols; k += 16)
+                    umma_f16_ts(tmem + Sh::kO + (t & 1) * NB * 64, tmem + Sh::kS + (t & 1) * kFwdRows + k / 2,
+                                umma_desc_sw128(v + k * 128u, kBlock), idesc_o, t > 1 || k > 0);
+                umma_commit(&sh.empty[t % Sh::kStages]);
+                if (t + 1 == tiles) umma_commit(&sh.done);
+                const int32_t n1 = t + 2;
+                if (n1 < tiles) {
+                    ok = mbar_wait(&sh.full[n1 % Sh::kStages], (n1 / Sh::kStages) & 1, abort_flag);
+                    if (ok) { tc_fence_after(); scores(n1); }
+                }
+            }
         }
         __syncwarp();
-        {
-            const uint32_t chunks = p.dim >> 3;
-            char *out = static_cast<char *>(p.out) + ((uint64_t)(t0 + warp * 32) * p.ldo + (uint64_t)h * p.dim) * 2u;
-            for (int32_t e = (int32_t)lane; e < rows * (int32_t)chunks; e += 32) {
-                const uint32_t r = (uint32_t)e / chunks, ch = (uint32_t)e - r * chunks;
-                *reinterpret_cast<uint4 *>(out + (uint64_t)r * p.ldo * 2u + ch * 16u) =
-                    *reinterpret_cast<const uint4 *>(mine + r * row_bytes + ((ch + r) % chunks) * 16u);
-            }
-        }
-        tc_fence_before();
-    } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-        if (warp == 4) {
-            // ============ MMA issue: one lane ============
-            if (lane == 0 && tiles) {
-                const uint32_t idesc_o = umma_idesc_f16(kBf16, kAttendTile, dim16, true);
-                auto scores = [&](int32_t t) {
-                    const uint32_t stage = t % Sh::kStages, cols = (uint32_t)(tile_keys(t) + 15) & ~15u;
-                    const uint32_t idesc = umma_idesc_f16(kBf16, kAttendTile, cols, false);
-                    for (uint32_t c = 0; c < dim16; c += 16) {
-                        const uint32_t off = (c >> 6) * (kAttendTile * 128) + (c & 63u) * 2u;
-                        umma_f16_ss(tmem + Sh::kS, umma_desc_sw128(qs + off, 0), umma_desc_sw128(ks + stage * Sh::kTileBytes + off, 0), idesc, c > 0);
-                    }
-                    umma_commit(&sh.s_full);
-                    umma_commit(&sh.k_empty[stage]);
-                };
-                bool ok = mbar_wait(&sh.q_full, 0, abort_flag) && mbar_wait(&sh.k_full[0], 0, abort_flag);
-                if (ok) { tc_fence_after(); scores(0); }
-                for (int32_t t = 0; t < tiles && ok; ++t) {
-                    const uint32_t stage = t % Sh::kStages;
-                    const int32_t n1 = t + 1;
-                    if (Sh::kOwnP && n1 < tiles) {
-                        ok = mbar_wait(&sh.k_full[n1 % Sh::kStages], (n1 / Sh::kStages) & 1, abort_flag) && mbar_wait(&sh.s_free, t & 1, abort_flag);
-                        if (!ok) break;
-                        tc_fence_after();
-                        scores(n1);
-                    }
-                    ok = mbar_wait(&sh.v_full[stage], (t / Sh::kStages) & 1, abort_flag) && mbar_wait(&sh.p_full, t & 1, abort_flag);
-                    if (!ok) break;
-                    tc_fence_after();
-                    const uint32_t cols = (uint32_t)(tile_keys(t) + 15) & ~15u;
-                    for (uint32_t k = 0; k < cols; k += 16)
-                        umma_f16_ts(tmem + Sh::kO, tmem + Sh::kP + k / 2, umma_desc_sw128(vs + stage * Sh::kTileBytes + k * 128u, kAttendTile * 128),
-                                    idesc_o, t > 0 || k > 0);
-                    umma_commit(&sh.pv_done);
-                    umma_commit(&sh.v_empty[stage]);
-                    if (!Sh::kOwnP && n1 < tiles) {
-                        ok = mbar_wait(&sh.k_full[n1 % Sh::kStages], (n1 / Sh::kStages) & 1, abort_flag);
-                        if (!ok) break;
-                        tc_fence_after();
-                        scores(n1);
-                    }
+    } else if (warp == 9) {
+        // ============ copies: one lane ============
+        if (NB == 1) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        if (lane == 0) {
+            int32_t t = 0;
+            for (; t < tiles; ++t) {
+                const uint32_t stage = t % Sh::kStages, round = t / Sh::kStages, base = ring + stage * Sh::kStage;
+                if (round > 0 && !mbar_wait(&sh.empty[stage], (round - 1) & 1, abort_flag)) break;
+                mbar_expect(&sh.landed[stage], Sh::kStage);
+#pragma unroll
+                for (int c = 0; c < NB; ++c) {
+                    copy_box(base + c * kFwdRows * 128, &map_k, c * 64, (int32_t)kvh, tile_at(t), &sh.landed[stage]);
+                    copy_box(base + Sh::kOperand + c * kFwdRows * 128, &map_v, c * 64, (int32_t)kvh, tile_at(t), &sh.landed[stage]);
                 }
             }
-            __syncwarp();
-        } else if (tiles) {
-            // ============ copies: keys and values of one tile after the other ============
-            const uint32_t lt = tid - 160u;
-            constexpr int CH = NB * 8;
-            const uint32_t used = dim16 >> 3, dch = p.dim >> 3;
-            const T *q = static_cast<const T *>(p.q) + (uint64_t)h * p.dim, *k = static_cast<const T *>(p.k) + (uint64_t)kvh * p.dim,
-                    *v = static_cast<const T *>(p.v) + (uint64_t)kvh * p.dim;
-            uint64_t *pending = nullptr;
-            bool ok = true;
-            // waits for the slot; the copies already under way are handed over first if it is not free yet
-            auto slot = [&](uint64_t *empty, uint32_t parity) {
-                if (mbar_try(empty, parity)) return true;
-                if (pending) { copy_wait<0>(); fence_async_proxy(); mbar_arrive(pending); pending = nullptr; }
-                return mbar_wait(empty, parity, abort_flag);
-            };
-            auto issued = [&](uint64_t *full) {
-                copy_commit();
-                if (pending) { copy_wait<1>(); fence_async_proxy(); mbar_arrive(pending); }
-                pending = full;
-            };
-            uint32_t vis[4];
-            visible_bits(p, t0, kAttendTile, lane, vis);
-            copy_rows_sw128<CH>(qs, kAttendTile * 128, q, p.ldq * 2, t0, kAttendTile, vis, dch, used, lt, kFwdLoaders);
-            issued(&sh.q_full);
-            for (int32_t t = 0; t < tiles && ok; ++t) {
-                const uint32_t stage = t % Sh::kStages, round = t / Sh::kStages;
-                const int32_t at = tile_at(t), keys = tile_keys(t);
-                const uint32_t cols = (uint32_t)(keys + 15) & ~15u;
-                visible_bits(p, at, (uint32_t)keys, lane, vis);
-                if (round > 0) ok = slot(&sh.k_empty[stage], (round - 1) & 1);
-                if (!ok) break;
-                if (lt == 0) { sh.vis[stage][0] = vis[0]; sh.vis[stage][1] = vis[1]; sh.vis[stage][2] = vis[2]; sh.vis[stage][3] = vis[3]; }
-                copy_rows_sw128<CH>(ks + stage * Sh::kTileBytes, kAttendTile * 128, k, p.ldk * 2, at, cols, vis, dch, used, lt, kFwdLoaders);
-                issued(&sh.k_full[stage]);
-                if (round > 0) ok = slot(&sh.v_empty[stage], (round - 1) & 1);
-                if (!ok) break;
-                copy_rows_sw128<CH>(vs + stage * Sh::kTileBytes, kAttendTile * 128, v, p.ldv * 2, at, cols, vis, dch, used, lt, kFwdLoaders);
-                issued(&sh.v_full[stage]);
-            }
-            copy_wait<0>();
-            if (pending && ok) { fence_async_proxy(); mbar_arrive(pending); }
+            // after a wait that ran out: what is under way lands before the block leaves
+            if (*abort_flag)
+                for (int32_t u = max(0, t - Sh::kStages); u < t; ++u) mbar_wait(&sh.landed[u % Sh::kStages], (u / Sh::kStages) & 1, &sh.quiet);
+        }
+        __syncwarp();
+    } else {
+        // ============ rows that are not words: a warp per tile, in turn ============
+        if (NB == 1) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        int32_t t = (int32_t)warp - 10;
+        uint32_t vis[2], next[2] = {0u, 0u};
+        if (t < tiles) word_bits(p, tile_at(t), (uint32_t)tile_keys(t), lane, next);
+        for (; t < tiles; t += 2) {
+            const uint32_t stage = t % Sh::kStages;
+            vis[0] = next[0];
+            vis[1] = next[1];
+            if (t + 2 < tiles) word_bits(p, tile_at(t + 2), (uint32_t)tile_keys(t + 2), lane, next);
+            if (!__all_sync(kFullMask, mbar_wait(&sh.landed[stage], (t / Sh::kStages) & 1, abort_flag))) break;
+            if (lane < 2) sh.vis[stage][lane] = lane ? vis[1] : vis[0];
+            // values only: the scores of such a key are masked
+            zero_rows<NB>(ring + stage * Sh::kStage + Sh::kOperand, kFwdRows * 128, (uint32_t)(tile_keys(t) + 15) & ~15u, vis, lane);
+            fence_async_proxy();
+            mbar_arrive(&sh.full[stage]);
         }
     }
     __syncthreads();
     tc_fence_after();
-    if (warp == 4) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(256));
+    if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(Sh::kAlloc));
     if (tid == 0 && sh.abort_flag) atomicOr(error, kErrAttend);
 }
 
@@ -311,13 +377,22 @@ template <typename T, int NB>
 int launch_attend_shape(const AttendParams &p, int *error, cudaStream_t s)
 {
     auto kernel = attend_tc_kernel<T, NB>;
-    const int smem = FwdShape<NB>::kSmem + (int)(bias_entries(p.b) * sizeof(float));
-    cudaFuncAttributes at;
-    // the softmax warps take registers that the others give up: the block must have been launched with all of them
-    if (cudaFuncGetAttributes(&at, kernel) != cudaSuccess || at.numRegs * 8 < 4 * (kSoftmaxRegs + kOtherRegs)) return -1;
+    int smem = FwdShape<NB>::kRing + 1024 + (int)(bias_entries(p.b) * sizeof(float));
+    if (FwdShape<NB>::kBlocks == 1 && smem < 116 * 1024) smem = 116 * 1024;      // a second block would only wait for tensor memory
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return -1;
+    if (NB == 1) {
+        // a block launched with fewer registers could never hand out the softmax's share
+        cudaFuncAttributes at;
+        if (cudaFuncGetAttributes(&at, kernel) != cudaSuccess || at.numRegs < kLaunchRegs) return -1;
+    }
     const uint64_t tiles = ((uint64_t)p.n + kAttendTile - 1) / kAttendTile;
-    kernel<<<(uint32_t)(tiles * p.heads), kFwdThreads, smem, s>>>(p, error);
+    CUtensorMap q, k, v;
+    const bool bf16 = std::is_same<T, __nv_bfloat16>::value;
+    if (!make_rows_map(&q, bf16, p.q, p.dim, p.heads, (uint64_t)p.n, p.ldq, kAttendTile) ||
+        !make_rows_map(&k, bf16, p.k, p.dim, p.kv_heads, (uint64_t)p.n, p.ldk, kFwdRows) ||
+        !make_rows_map(&v, bf16, p.v, p.dim, p.kv_heads, (uint64_t)p.n, p.ldv, kFwdRows))
+        return -1;
+    kernel<<<(uint32_t)(tiles * p.heads), kFwdThreads, smem, s>>>(q, k, v, p, error);
     return cudaPeekAtLastError() == cudaSuccess ? 1 : -1;
 }
 

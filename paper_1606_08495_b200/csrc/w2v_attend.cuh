@@ -9,6 +9,7 @@
 #include "w2v_device.cuh"
 #include "w2v_reader.h"
 #include "w2v_tc.cuh"
+#include "w2v_tma.h"
 #include "w2v_types.cuh"
 
 namespace w2v {
@@ -63,43 +64,74 @@ __device__ __forceinline__ uint32_t bucket_of(const BucketStarts &b, int32_t rel
 // A bias in base-2 units; one of the lowest float stays finite, so that a row of nothing else is still a row.
 __device__ __forceinline__ float log2_bias(float b) { return b == -INFINITY ? b : fmaxf(b, -1e30f) * kLog2e; }
 
-__device__ __forceinline__ void fill_bias(const AttendParams &p, uint32_t h, float *lut, uint32_t tid, uint32_t threads)
+// Relative positions [r0, r1) (key - query, within -off .. off) whose bias is bucket b's.
+__device__ __forceinline__ void bucket_range(const BucketStarts &s, uint32_t b, int32_t off, int32_t &r0, int32_t &r1)
+{
+    const uint32_t side = b >= s.n ? 1u : 0u, k = b - side * s.n;
+    const int32_t d0 = s.start[k], d1 = k + 1 < s.n ? s.start[k + 1] : off + 1;       // distances [d0, d1) on its side
+    if (side) { r0 = max(d0, 1); r1 = d1; }
+    else { r0 = 1 - d1; r1 = k == 0 && !s.two_sided ? off + 1 : 1 - d0; }
+}
+
+// The table of a head by `warps` warps (this one is number `warp`), a bucket at a time.
+__device__ __forceinline__ void fill_bias(const AttendParams &p, uint32_t h, float *lut, uint32_t warp, uint32_t warps, uint32_t lane)
 {
     const int32_t off = bias_last(p.b) + kBiasPad;
-    for (uint32_t e = tid; e < bias_entries(p.b); e += threads)
-        lut[e] = log2_bias(__ldg(p.bias + (size_t)bucket_of(p.b, (int32_t)e - off) * p.heads + h));
-}
-
-// Rows [at, at + rows) of an operand into a tile of the 128-byte swizzle by the `threads` calling threads
-// (thread number lt): zeros for rows whose bit in `vis` (one word per 32 rows) is clear and for columns past the
-// head.  CH = 16-byte chunks a row has room for (8 or 16), `used` of them are written.
-template <int CH>
-__device__ __forceinline__ void copy_rows_sw128(uint32_t tile, uint32_t block_bytes, const void *base, uint64_t ld_bytes, int64_t at,
-                                                uint32_t rows, const uint32_t (&vis)[4], uint32_t dim_chunks, uint32_t used,
-                                                uint32_t lt, uint32_t threads)
-{
-    const uint32_t ch = lt % CH;
-    if (ch >= used) return;
-    const uint32_t dst0 = tile + (ch >> 3) * block_bytes;
-    const char *src0 = static_cast<const char *>(base) + ch * 16u;
-    for (uint32_t r = lt / CH; r < rows; r += threads / CH) {
-        const uint32_t word = r < 32 ? vis[0] : r < 64 ? vis[1] : r < 96 ? vis[2] : vis[3];
-        const bool real = ch < dim_chunks && ((word >> (r & 31u)) & 1u);
-        copy16(dst0 + r * 128u + (((ch & 7u) ^ (r & 7u)) << 4), real ? src0 + (uint64_t)(at + r) * ld_bytes : src0, real);
+    const uint32_t buckets = p.b.n * (p.b.two_sided ? 2u : 1u);
+    float v[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) v[i] = lane + 32u * i < buckets ? log2_bias(__ldg(p.bias + (size_t)(lane + 32 * i) * p.heads + h)) : 0.f;
+    for (uint32_t b = warp; b < buckets; b += warps) {
+        int32_t r0, r1;
+        bucket_range(p.b, b, off, r0, r1);
+        const float x = __shfl_sync(kFullMask, b < 32 ? v[0] : v[1], b & 31u);
+        for (int32_t r = r0 + (int32_t)lane; r < r1; r += 32) lut[r + off] = x;
     }
 }
 
-// Which of the 128 positions from `at` on are words: one word of bits per 32, the same in every lane of the warp.
-__device__ __forceinline__ void visible_bits(const AttendParams &p, int64_t at, uint32_t rows, uint32_t lane, uint32_t (&vis)[4])
+// Which of `rows` <= 64 positions from `at` on are words: a bit each in two words, the same in every lane of the warp.
+__device__ __forceinline__ void word_bits(const AttendParams &p, int64_t at, uint32_t rows, uint32_t lane, uint32_t (&vis)[2])
 {
-    int2 sp[4];
+    int2 sp[2];
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < 2; ++w) {
         const int64_t j = at + w * 32 + lane;
-        sp[w] = w * 32u + lane < rows && j >= 0 && j < p.n ? __ldg(p.spans + j) : make_int2(0, 0);
+        sp[w] = w * 32u + lane < rows && j < p.n ? __ldg(p.spans + j) : make_int2(0, 0);
     }
 #pragma unroll
-    for (int w = 0; w < 4; ++w) vis[w] = __ballot_sync(kFullMask, sp[w].y > sp[w].x);
+    for (int w = 0; w < 2; ++w) vis[w] = __ballot_sync(kFullMask, sp[w].y > sp[w].x);
+}
+
+// Rows of a tile that are not words are zeroed once it has landed (by one warp): their weights are zero, but what
+// they hold may not be finite.  A row is NB blocks of 128 bytes, `block` bytes apart.
+template <int NB>
+__device__ __forceinline__ void zero_rows(uint32_t tile, uint32_t block, uint32_t rows, const uint32_t (&vis)[2], uint32_t lane)
+{
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        uint32_t bad = ~vis[w] & (rows >= (w + 1) * 32u ? 0xFFFFFFFFu : rows > w * 32u ? (1u << (rows - w * 32u)) - 1u : 0u);
+        while (bad) {
+            const uint32_t r = w * 32u + (uint32_t)__ffs(bad) - 1u;
+            bad &= bad - 1u;
+            if (lane < NB * 8u)
+                asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(tile + (lane >> 3) * block + r * 128u + (lane & 7u) * 16u), "r"(0u) : "memory");
+        }
+    }
+}
+
+// Rows of `chunks` 16-byte chunks from a stripe of shared memory (chunk c of row r at chunk (c + r) mod chunks) to
+// global memory, by `threads` threads of which this is number `at`.
+__device__ __forceinline__ void store_rows(char *out, uint64_t ld_bytes, const unsigned char *stripe, uint32_t chunks, int32_t rows,
+                                           uint32_t at, uint32_t threads)
+{
+    const uint32_t inv = (65536u + chunks - 1) / chunks;             // exact for the up to 512 chunks of 32 rows
+    for (int32_t e = (int32_t)at; e < rows * (int32_t)chunks; e += (int32_t)threads) {
+        const uint32_t r = ((uint32_t)e * inv) >> 16, c = (uint32_t)e - r * chunks;
+        uint32_t from = c + r;
+        while (from >= chunks) from -= chunks;
+        *reinterpret_cast<uint4 *>(out + (uint64_t)r * ld_bytes + c * 16u) =
+            *reinterpret_cast<const uint4 *>(stripe + (r * chunks + from) * 16u);
+    }
 }
 
 }  // namespace w2v

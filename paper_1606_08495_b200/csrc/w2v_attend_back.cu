@@ -29,12 +29,11 @@ struct BackShape {
     static constexpr int kSoft = 128 * kBuf, kThreads = kSoft + 128;
     static_assert(kRing >= 2 * NB * 128 * 128, "the outputs are staged where the ring was");
 };
-constexpr int kBackLoaders = 96;
 
 struct BackShared {
-    uint64_t a_full, full[4], empty[4], s_full[2], p_full[2], done;
+    uint64_t a_full, landed[4], full[4], empty[4], s_full[2], p_full[2], done;
     uint32_t tmem;
-    int abort_flag;
+    int abort_flag, quiet;
     int32_t limits[4][3];
     uint32_t vis[4][2];                              // role 0: which keys of the stage are words
     int32_t run_lo[4];                               // role 1: where the run of the stage's query tile begins
@@ -54,19 +53,11 @@ __device__ __forceinline__ void write_bucket_sums(const AttendParams &p, const f
     const uint32_t n = p.b.n, buckets = n * (p.b.two_sided ? 2u : 1u);
     for (uint32_t b = warp; b < buckets; b += warps) {
         const uint32_t side = b >= n ? 1u : 0u, k = b - side * n;
-        // distances [d0, d1) of this bucket on its side; those from the last start on include what is beyond the arrays
-        int32_t d0 = p.b.start[k], d1 = k + 1 < n ? p.b.start[k + 1] : off + 1;
-        int32_t r0, r1;                              // relative positions [r0, r1)
-        if (side) { r0 = max(d0, 1); r1 = d1; }
-        else { r0 = 1 - d1; r1 = 1 - d0; if (k == 0 && !p.b.two_sided) r1 = off + 1; }
-        r0 = max(r0, -off);
-        r1 = min(r1, off + 1);
+        int32_t r0, r1;
+        bucket_range(p.b, b, off, r0, r1);
         float a = 0.f;
         for (uint32_t w = 0; w < arrays; ++w)
-            for (int32_t r = r0 + (int32_t)lane; r < r1; r += 32) {
-                const int32_t at = r + off;
-                if (at >= 0 && at < (int32_t)entries) a += sums[w * entries + at];
-            }
+            for (int32_t r = r0 + (int32_t)lane; r < r1; r += 32) a += sums[w * entries + (uint32_t)(r + off)];
         const bool left = side == 0 && k == n - 1, right = p.b.two_sided ? side == 1 && k == n - 1 : k == 0;
         if (lane < far_rows) a += (left ? far_sum[lane][0] : 0.f) + (right ? far_sum[lane][1] : 0.f);
         a = warp_sum(a);
@@ -76,7 +67,7 @@ __device__ __forceinline__ void write_bucket_sums(const AttendParams &p, const f
 
 template <typename T, int NB, int ROLE>
 __global__ void __launch_bounds__(BackShape<NB>::kThreads, 1)
-attend_back_kernel(AttendParams p, int *error)
+attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_y, AttendParams p, int *error)
 {
     using Sh = BackShape<NB>;
     constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
@@ -99,11 +90,12 @@ attend_back_kernel(AttendParams p, int *error)
 
     if (tid == 0) {
         mbar_init(&sh.a_full, 128);
-        for (int i = 0; i < Sh::kStages; ++i) { mbar_init(&sh.full[i], kBackLoaders); mbar_init(&sh.empty[i], 1 + 128); }
+        for (int i = 0; i < Sh::kStages; ++i) { mbar_init(&sh.landed[i], 1); mbar_init(&sh.full[i], 32); mbar_init(&sh.empty[i], 1 + 128); }
         for (int i = 0; i < 2; ++i) { mbar_init(&sh.s_full[i], 1); mbar_init(&sh.p_full[i], 128); }
         mbar_init(&sh.done, 1);
-        sh.abort_flag = 0;
+        sh.abort_flag = sh.quiet = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_async_proxy();
     }
     const uint32_t r = tid & 127u;                                   // this thread's row (softmax warps)
     const int64_t own = (int64_t)t0 + r;
@@ -143,7 +135,7 @@ attend_back_kernel(AttendParams p, int *error)
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
     if (p.b.n) {
-        fill_bias(p, h0, lut, tid, Sh::kThreads);
+        fill_bias(p, h0, lut, warp, Sh::kThreads / 32, lane);
         if (ROLE == 1)
             for (uint32_t e = tid; e < kSoftWarps * entries; e += Sh::kThreads) rel_sums[e] = 0.f;
     }
@@ -218,7 +210,7 @@ attend_back_kernel(AttendParams p, int *error)
         for (uint32_t g = 0; g < heads_here; ++g) {
             if (ROLE == 1 && p.b.n && g > 0) {
                 soft_barrier(Sh::kSoft);                             // the sums of the head before are written
-                fill_bias(p, h0 + g, lut, tid, Sh::kSoft);
+                fill_bias(p, h0 + g, lut, warp, kSoftWarps, lane);
                 for (uint32_t e = tid; e < kSoftWarps * entries; e += Sh::kSoft) rel_sums[e] = 0.f;
                 soft_barrier(Sh::kSoft);
             }
@@ -440,55 +432,65 @@ attend_back_kernel(AttendParams p, int *error)
             }
         }
         __syncwarp();
-    } else if (total) {
-        // ============ copies ============
-        const uint32_t lt = tid - (kMmaWarp + 1) * 32u;
-        constexpr int CH = NB * 8;
-        const uint32_t used = dim16 >> 3, dch = p.dim >> 3;
-        uint64_t *pending = nullptr;
-        bool ok = true;
-        for (int32_t t = 0; t < total; ++t) {
-            const int32_t k = t % per_head;
-            const uint32_t h = h0 + (uint32_t)(t / per_head), stage = t % Sh::kStages, round = t / Sh::kStages;
-            const int32_t at = tile_at(k), rows = tile_rows(k);
-            uint32_t vis[4];
-            visible_bits(p, at, (uint32_t)rows, lane, vis);
-            int32_t run_lo = 0;
-            if (ROLE == 1 && p.sinks) {                              // where the run of keys of this query tile begins
-                uint32_t all[4];
-                const int32_t q0 = at / kAttendTile * kAttendTile;
-                visible_bits(p, q0, kAttendTile, lane, all);
-                const int32_t first = all[0] ? __ffs(all[0]) - 1 : all[1] ? 31 + __ffs(all[1]) : all[2] ? 63 + __ffs(all[2]) : 95 + __ffs(all[3]);
-                run_lo = (all[0] | all[1] | all[2] | all[3]) ? row_limits(p, q0 + first).lo : INT32_MAX;
-            }
-            if (round > 0) {
-                if (!mbar_try(&sh.empty[stage], (round - 1) & 1)) {
-                    if (pending) { copy_wait<0>(); fence_async_proxy(); mbar_arrive(pending); pending = nullptr; }
-                    ok = mbar_wait(&sh.empty[stage], (round - 1) & 1, abort_flag);
-                    if (!ok) break;
+    } else if (warp == kMmaWarp + 1) {
+        // ============ copies: one lane ============
+        if (lane == 0) {
+            int32_t t = 0;
+            for (; t < total; ++t) {
+                const uint32_t stage = t % Sh::kStages, round = t / Sh::kStages, base = ring + stage * Sh::kStage;
+                if (round > 0 && !mbar_wait(&sh.empty[stage], (round - 1) & 1, abort_flag)) break;
+                const int32_t head = ROLE == 0 ? (int32_t)kvh : (int32_t)h0 + t / per_head, at = tile_at(t % per_head);
+                mbar_expect(&sh.landed[stage], Sh::kStage);
+#pragma unroll
+                for (int c = 0; c < NB; ++c) {
+                    copy_box(base + c * Sh::kRows * 128, &map_x, c * 64, head, at, &sh.landed[stage]);
+                    copy_box(base + Sh::kOperand + c * Sh::kRows * 128, &map_y, c * 64, head, at, &sh.landed[stage]);
                 }
             }
-            const T *x = ROLE == 0 ? static_cast<const T *>(p.k) + (uint64_t)kvh * p.dim : static_cast<const T *>(p.q) + (uint64_t)h * p.dim;
-            const T *y = ROLE == 0 ? static_cast<const T *>(p.v) + (uint64_t)kvh * p.dim : static_cast<const T *>(p.d_o) + (uint64_t)h * p.dim;
-            const uint32_t cols = (uint32_t)(rows + 15) & ~15u, xs = ring + stage * Sh::kStage;
-            copy_rows_sw128<CH>(xs, Sh::kRows * 128, x, (ROLE == 0 ? p.ldk : p.ldq) * 2, at, cols, vis, dch, used, lt, kBackLoaders);
-            copy_rows_sw128<CH>(xs + Sh::kOperand, Sh::kRows * 128, y, (ROLE == 0 ? p.ldv : p.ld_do) * 2, at, cols, vis, dch, used, lt, kBackLoaders);
-            copy_commit();
-            if (ROLE == 0) {
-                if (lt < 2) sh.vis[stage][lt] = lt ? vis[1] : vis[0];
-            } else {
-                if (lt == 0) sh.run_lo[stage] = run_lo;
-                if (lt < (uint32_t)Sh::kRows) {
-                    const int64_t i = (int64_t)at + lt;
-                    sh.lse[stage][lt] = i < p.n ? __ldg(p.lse + (int64_t)h * p.n + i) : INFINITY;
-                    sh.delta[stage][lt] = i < p.n ? p.delta[(int64_t)h * p.n + i] : 0.f;
-                }
-            }
-            if (pending) { copy_wait<1>(); fence_async_proxy(); mbar_arrive(pending); }
-            pending = &sh.full[stage];
+            // after a wait that ran out: what is under way lands before the block leaves
+            if (*abort_flag)
+                for (int32_t u = max(0, t - Sh::kStages); u < t; ++u) mbar_wait(&sh.landed[u % Sh::kStages], (u / Sh::kStages) & 1, &sh.quiet);
         }
-        copy_wait<0>();
-        if (pending && ok) { fence_async_proxy(); mbar_arrive(pending); }
+        __syncwarp();
+    } else {
+        // ============ rows that are not words, and what goes with the rows: a warp per tile, in turn ============
+        for (int32_t t = (int32_t)(warp - kMmaWarp) - 2; t < total; t += 2) {
+            const uint32_t stage = t % Sh::kStages, h = h0 + (uint32_t)(t / per_head);
+            const int32_t k = t % per_head, at = tile_at(k), rows = tile_rows(k);
+            uint32_t vis[2];
+            word_bits(p, at, (uint32_t)rows, lane, vis);
+            float lse[2], delta[2];
+            int32_t run_lo = 0;
+            if (ROLE == 1) {
+#pragma unroll
+                for (int w = 0; w < Sh::kRows / 32; ++w) {
+                    const int64_t i = (int64_t)at + w * 32 + lane;
+                    lse[w] = i < p.n ? __ldg(p.lse + (int64_t)h * p.n + i) : INFINITY;
+                    delta[w] = i < p.n ? p.delta[(int64_t)h * p.n + i] : 0.f;
+                }
+                if (p.sinks) {                                       // where the run of keys of this query tile begins
+                    uint32_t a[2], b[2];
+                    const int32_t q0 = at / kAttendTile * kAttendTile;
+                    word_bits(p, q0, 64, lane, a);
+                    word_bits(p, (int64_t)q0 + 64, 64, lane, b);
+                    const int32_t first = a[0] ? __ffs(a[0]) - 1 : a[1] ? 31 + __ffs(a[1]) : b[0] ? 63 + __ffs(b[0]) : 95 + __ffs(b[1]);
+                    run_lo = (a[0] | a[1] | b[0] | b[1]) ? row_limits(p, q0 + first).lo : INT32_MAX;
+                }
+            }
+            if (!__all_sync(kFullMask, mbar_wait(&sh.landed[stage], (t / Sh::kStages) & 1, abort_flag))) break;
+            if (ROLE == 0) {
+                if (lane < 2) sh.vis[stage][lane] = lane ? vis[1] : vis[0];
+            } else {
+#pragma unroll
+                for (int w = 0; w < Sh::kRows / 32; ++w) { sh.lse[stage][w * 32 + lane] = lse[w]; sh.delta[stage][w * 32 + lane] = delta[w]; }
+                if (lane == 0) sh.run_lo[stage] = run_lo;
+            }
+            const uint32_t x = ring + stage * Sh::kStage, cols = (uint32_t)(rows + 15) & ~15u;
+            zero_rows<NB>(x, Sh::kRows * 128, cols, vis, lane);
+            zero_rows<NB>(x + Sh::kOperand, Sh::kRows * 128, cols, vis, lane);
+            fence_async_proxy();
+            mbar_arrive(&sh.full[stage]);
+        }
     }
     __syncthreads();
     tc_fence_after();
@@ -698,7 +700,14 @@ int launch_role(const AttendParams &p, uint32_t tiles, int *error, cudaStream_t 
     int smem = Sh::kRing + 1024 + (int)(4 * (((entries + 3u) & ~3u) + (ROLE == 1 ? Sh::kSoft / 32 * entries : 0u)));
     if (smem < 116 * 1024) smem = 116 * 1024;     // a second block would only wait for tensor memory
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return -1;
-    kernel<<<tiles * (ROLE == 0 ? p.heads : p.kv_heads), Sh::kThreads, smem, s>>>(p, error);
+    CUtensorMap x, y;
+    const bool bf16 = std::is_same<T, __nv_bfloat16>::value;
+    if (ROLE == 0 ? !make_rows_map(&x, bf16, p.k, p.dim, p.kv_heads, (uint64_t)p.n, p.ldk, Sh::kRows) ||
+                        !make_rows_map(&y, bf16, p.v, p.dim, p.kv_heads, (uint64_t)p.n, p.ldv, Sh::kRows)
+                  : !make_rows_map(&x, bf16, p.q, p.dim, p.heads, (uint64_t)p.n, p.ldq, Sh::kRows) ||
+                        !make_rows_map(&y, bf16, p.d_o, p.dim, p.heads, (uint64_t)p.n, p.ld_do, Sh::kRows))
+        return -1;
+    kernel<<<tiles * (ROLE == 0 ? p.heads : p.kv_heads), Sh::kThreads, smem, s>>>(x, y, p, error);
     return cudaPeekAtLastError() == cudaSuccess ? 1 : -1;
 }
 

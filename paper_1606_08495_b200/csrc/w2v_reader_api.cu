@@ -60,7 +60,7 @@ int32_t check_window(w2v_handle *h, const w2v_window *w, const float *bias, Buck
         return fail(h, W2V_ERR_ARG, "head_dim must be a multiple of 8 in 8..128");
     if (w->left >= (1u << 30) || w->right >= (1u << 30)) return fail(h, W2V_ERR_ARG, "left and right must be below 2^30");
     if (w->sinks > kMaxSinks) return fail(h, W2V_ERR_ARG, "sinks must be at most 64");
-    if (!std::isfinite(w->scale)) return fail(h, W2V_ERR_ARG, "scale must be finite");
+    if (!(w->scale > 0.f) || std::isinf(w->scale)) return fail(h, W2V_ERR_ARG, "scale must be positive and finite");
     std::memset(b, 0, sizeof(*b));
     if (w->buckets) {
         const int32_t rc = check_buckets(h, w->buckets, w->reach, w->two_sided);
