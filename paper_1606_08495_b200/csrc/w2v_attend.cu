@@ -148,7 +148,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         float2 sum2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
         bool ok = true;
         for (int32_t t = (int32_t)wg; t < tiles; t += 2) {
-            const int32_t k0 = tile_at(t), keys = tile_keys(t), cols = (keys + 15) & ~15;
+            const int32_t k0 = tile_at(t), cols = tile_keys(t);
             const uint32_t stage = t % Sh::kStages;
             ok = __all_sync(kFullMask, mbar_wait(&sh.full[stage], (t / Sh::kStages) & 1, abort_flag) &&        // the bits of the keys
                                            mbar_wait(&sh.s_full[wg], (t >> 1) & 1, abort_flag));
@@ -292,38 +292,49 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     } else if (warp == 8) {
         // ============ MMA issue: one lane ============
         if (NB == 1) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        // The lane that issues is what the block waits for when its code is long: everything that does not change is
+        // formed once, a product costs an addition per operand.
         if (lane == 0 && tiles) {
-            const uint32_t idesc_o = umma_idesc_f16(kBf16, kAttendTile, dim16, true);
-            constexpr uint32_t kBlock = kFwdRows * 128;
-            auto scores = [&](int32_t t) {
-                const uint32_t k = ring + (t % Sh::kStages) * Sh::kStage, d = tmem + Sh::kS + (t & 1) * kFwdRows;
-                const uint32_t idesc = umma_idesc_f16(kBf16, kAttendTile, (uint32_t)(tile_keys(t) + 15) & ~15u, false);
-                for (uint32_t c = 0; c < dim16; c += 16) {
-                    const uint64_t kd = umma_desc_sw128(k + (c >> 6) * kBlock + (c & 63u) * 2u, 0);
-                    if (Sh::kQTmem) umma_f16_ts(d, tmem + Sh::kQ + c / 2, kd, idesc, c > 0);
-                    else umma_f16_ss(d, umma_desc_sw128(qs + (c >> 6) * (kAttendTile * 128) + (c & 63u) * 2u, 0), kd, idesc, c > 0);
-                }
-                umma_commit(&sh.s_full[t & 1]);
+            constexpr uint32_t kBlock = kFwdRows * 128, kStep = Sh::kStage >> 4;
+            const uint32_t idesc_o = umma_idesc_f16(kBf16, kAttendTile, dim16, true), idesc_s = umma_idesc_f16(kBf16, kAttendTile, kFwdRows, false);
+            const uint32_t q_low = umma_desc_low(qs, 0), k_low = umma_desc_low(ring, 0), v_low = umma_desc_low(ring + Sh::kOperand, kBlock);
+            // keys past the tile's end are products of what lies there and are masked
+            auto scores = [&](uint32_t b, uint32_t stage) {
+                const uint32_t k = k_low + stage * kStep, d = tmem + Sh::kS + b * kFwdRows;
+#pragma unroll
+                for (int c = 0; c < NB * 4; ++c)
+                    if ((uint32_t)c * 16 < dim16) {
+                        const uint32_t k_at = k + (c >> 2) * (kBlock >> 4) + (c & 3) * 2;
+                        if (Sh::kQTmem) umma_f16_ts(d, tmem + Sh::kQ + c * 8, k_at, idesc_s, c > 0);
+                        else umma_f16_ss(d, q_low + (c >> 2) * (kAttendTile * 128 >> 4) + (c & 3) * 2, k_at, idesc_s, c > 0);
+                    }
+                umma_commit(&sh.s_full[b]);
             };
             bool ok = mbar_wait(&sh.q_full, 0, abort_flag);
+            uint32_t ahead = 0, ahead_phase = 0;                     // stage and phase of the next scores, two tiles ahead of the products with values
             for (int32_t t = 0; t < 2 && t < tiles && ok; ++t) {
-                ok = mbar_wait(&sh.full[t % Sh::kStages], 0, abort_flag);
-                if (ok) { tc_fence_after(); scores(t); }
+                ok = mbar_wait(&sh.full[ahead], 0, abort_flag);
+                if (ok) { tc_fence_after(); scores((uint32_t)t, ahead); ++ahead; }
             }
+            uint32_t stage = 0;
             for (int32_t t = 0; t < tiles && ok; ++t) {
-                ok = mbar_wait(&sh.p_full[t & 1], (t >> 1) & 1, abort_flag);
+                const uint32_t b = t & 1, v = v_low + stage * kStep, w = tmem + Sh::kS + b * kFwdRows, d = tmem + Sh::kO + b * NB * 64;
+                const int32_t keys = tile_keys(t);
+                ok = mbar_wait(&sh.p_full[b], (t >> 1) & 1, abort_flag);
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t v = ring + (t % Sh::kStages) * Sh::kStage + Sh::kOperand, cols = (uint32_t)(tile_keys(t) + 15) & ~15u;
-                for (uint32_t k = 0; k < cols; k += 16)
-                    umma_f16_ts(tmem + Sh::kO + (t & 1) * NB * 64, tmem + Sh::kS + (t & 1) * kFwdRows + k / 2,
-                                umma_desc_sw128(v + k * 128u, kBlock), idesc_o, t > 1 || k > 0);
-                umma_commit(&sh.empty[t % Sh::kStages]);
+#pragma unroll
+                for (int k = 0; k < kFwdRows / 16; ++k)
+                    if (k * 16 < keys) umma_f16_ts(d, w + k * 8, v + k * 128, idesc_o, t > 1 || k > 0);
+                umma_commit(&sh.empty[stage]);
                 if (t + 1 == tiles) umma_commit(&sh.done);
-                const int32_t n1 = t + 2;
-                if (n1 < tiles) {
-                    ok = mbar_wait(&sh.full[n1 % Sh::kStages], (n1 / Sh::kStages) & 1, abort_flag);
-                    if (ok) { tc_fence_after(); scores(n1); }
+                if (++stage == Sh::kStages) stage = 0;
+                if (t + 2 < tiles) {
+                    ok = mbar_wait(&sh.full[ahead], ahead_phase, abort_flag);
+                    if (!ok) break;
+                    tc_fence_after();
+                    scores(b, ahead);
+                    if (++ahead == Sh::kStages) { ahead = 0; ahead_phase ^= 1u; }
                 }
             }
         }

@@ -394,40 +394,53 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
         tc_fence_before();
     } else if (warp == kMmaWarp) {
         // ============ MMA issue: one lane ============
+        // everything that does not change is formed once: the block waits for this lane when its code is long
         if (lane == 0 && total) {
-            const uint32_t idesc_g = umma_idesc_f16(kBf16, kAttendTile, dim16, true);
-            constexpr uint32_t kBlock = Sh::kRows * 128;
-            auto cols_of = [&](int32_t t) { return (uint32_t)(tile_rows(t % per_head) + 15) & ~15u; };
-            auto scores = [&](int32_t t) {
-                const uint32_t x = ring + (t % Sh::kStages) * Sh::kStage, y = x + Sh::kOperand;
-                const uint32_t d = tmem + Sh::kScores + (t % Sh::kBuf) * 2 * Sh::kRows, idesc = umma_idesc_f16(kBf16, kAttendTile, cols_of(t), false);
-                for (uint32_t c = 0; c < dim16; c += 16)
-                    umma_f16_ts(d, tmem + Sh::kA0 + c / 2, umma_desc_sw128(x + (c >> 6) * kBlock + (c & 63u) * 2u, 0), idesc, c > 0);
-                for (uint32_t c = 0; c < dim16; c += 16)
-                    umma_f16_ts(d + Sh::kRows, tmem + Sh::kA1 + c / 2, umma_desc_sw128(y + (c >> 6) * kBlock + (c & 63u) * 2u, 0), idesc, c > 0);
-                umma_commit(&sh.s_full[t % Sh::kBuf]);
+            constexpr uint32_t kBlock = Sh::kRows * 128, kStep = Sh::kStage >> 4;
+            const uint32_t idesc_g = umma_idesc_f16(kBf16, kAttendTile, dim16, true), idesc_s = umma_idesc_f16(kBf16, kAttendTile, Sh::kRows, false);
+            // the streamed operands with columns as the summed side (scores) and with rows as the summed side (gradients)
+            const uint32_t xs = umma_desc_low(ring, 0), ys = umma_desc_low(ring + Sh::kOperand, 0);
+            const uint32_t xg = umma_desc_low(ring, kBlock), yg = umma_desc_low(ring + (ROLE == 0 ? 0 : Sh::kOperand), kBlock);
+            auto scores = [&](uint32_t b, uint32_t stage) {
+                const uint32_t x = xs + stage * kStep, y = ys + stage * kStep, d = tmem + Sh::kScores + b * 2 * Sh::kRows;
+#pragma unroll
+                for (int c = 0; c < NB * 4; ++c)
+                    if ((uint32_t)c * 16 < dim16) {
+                        const uint32_t at = (c >> 2) * (kBlock >> 4) + (c & 3) * 2;
+                        umma_f16_ts(d, tmem + Sh::kA0 + c * 8, x + at, idesc_s, c > 0);
+                        umma_f16_ts(d + Sh::kRows, tmem + Sh::kA1 + c * 8, y + at, idesc_s, c > 0);
+                    }
+                umma_commit(&sh.s_full[b]);
             };
             bool ok = mbar_wait(&sh.a_full, 0, abort_flag);
+            uint32_t ahead = 0, ahead_phase = 0, stage = 0;          // stage and phase of the next scores, two tiles ahead of the gradients
             for (int32_t t = 0; t < Sh::kBuf && t < total && ok; ++t) {
-                ok = mbar_wait(&sh.full[t % Sh::kStages], 0, abort_flag);
-                if (ok) { tc_fence_after(); scores(t); }
+                ok = mbar_wait(&sh.full[ahead], 0, abort_flag);
+                if (ok) { tc_fence_after(); scores((uint32_t)t, ahead); ++ahead; }
             }
+            int32_t k = 0;                                           // number of the tile within its head
             for (int32_t t = 0; t < total && ok; ++t) {
-                ok = mbar_wait(&sh.p_full[t % Sh::kBuf], (t / Sh::kBuf) & 1, abort_flag);
+                const uint32_t b = t % Sh::kBuf, x = xg + stage * kStep, y = yg + stage * kStep, d = tmem + Sh::kScores + b * 2 * Sh::kRows;
+                const int32_t rows = tile_rows(k);
+                if (++k == per_head) k = 0;
+                ok = mbar_wait(&sh.p_full[b], (t / Sh::kBuf) & 1, abort_flag);
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t x = ring + (t % Sh::kStages) * Sh::kStage, y = x + Sh::kOperand;
-                const uint32_t d = tmem + Sh::kScores + (t % Sh::kBuf) * 2 * Sh::kRows, cols = cols_of(t);
-                for (uint32_t k = 0; k < cols; k += 16)
-                    umma_f16_ts(tmem + Sh::kG1, d + k / 2, umma_desc_sw128((ROLE == 0 ? x : y) + k * 128u, kBlock), idesc_g, t > 0 || k > 0);
-                for (uint32_t k = 0; k < cols; k += 16)
-                    umma_f16_ts(tmem + Sh::kG0, d + Sh::kRows + k / 2, umma_desc_sw128(x + k * 128u, kBlock), idesc_g, t > 0 || k > 0);
-                umma_commit(&sh.empty[t % Sh::kStages]);
+#pragma unroll
+                for (int c = 0; c < Sh::kRows / 16; ++c)
+                    if (c * 16 < rows) {
+                        umma_f16_ts(tmem + Sh::kG1, d + c * 8, y + c * 128, idesc_g, t > 0 || c > 0);
+                        umma_f16_ts(tmem + Sh::kG0, d + Sh::kRows + c * 8, x + c * 128, idesc_g, t > 0 || c > 0);
+                    }
+                umma_commit(&sh.empty[stage]);
                 if (t + 1 == total) umma_commit(&sh.done);
-                const int32_t n1 = t + Sh::kBuf;
-                if (n1 < total) {
-                    ok = mbar_wait(&sh.full[n1 % Sh::kStages], (n1 / Sh::kStages) & 1, abort_flag);
-                    if (ok) { tc_fence_after(); scores(n1); }
+                if (++stage == Sh::kStages) stage = 0;
+                if (t + Sh::kBuf < total) {
+                    ok = mbar_wait(&sh.full[ahead], ahead_phase, abort_flag);
+                    if (!ok) break;
+                    tc_fence_after();
+                    scores(b, ahead);
+                    if (++ahead == Sh::kStages) { ahead = 0; ahead_phase ^= 1u; }
                 }
             }
         }

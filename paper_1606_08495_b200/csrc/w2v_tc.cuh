@@ -71,21 +71,25 @@ __device__ __forceinline__ uint32_t umma_idesc_f16(bool bf16, uint32_t m, uint32
     return (1u << 4) | ((bf16 ? 1u : 0u) << 7) | ((bf16 ? 1u : 0u) << 10) | ((b_rows ? 1u : 0u) << 16) | ((n >> 3) << 17) | ((m >> 4) << 24);
 }
 
-// D (tensor memory) = or += A B, A and B in shared memory.
-__device__ __forceinline__ void umma_f16_ss(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
+// The low words of such a descriptor move with the address (in units of 16 bytes); the high word is always this one.
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t umma_desc_low(uint32_t saddr, uint32_t lbo) { return (uint32_t)umma_desc_sw128(saddr, lbo); }
+
+// D (tensor memory) = or += A B with B in shared memory; A in shared memory or in tensor memory (two elements per 32-bit
+// column).  Shared operands by their descriptors' low words.
+__device__ __forceinline__ void umma_f16_ss(uint32_t d, uint32_t a_low, uint32_t b_low, uint32_t idesc, bool accumulate)
 {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, {%5, %6, %7, %8}, p;\n\t}\n"
-        ::"r"(d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(0), "r"(0), "r"(0), "r"(0) : "memory");
+        "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 a, {%1, %3};\n\tmov.b64 b, {%2, %3};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, {%6, %6, %6, %6}, p;\n\t}\n"
+        ::"r"(d), "r"(a_low), "r"(b_low), "r"(kDescHigh), "r"(idesc), "r"((uint32_t)accumulate), "r"(0) : "memory");
 }
-// The same with A in tensor memory (two elements per 32-bit column).
-__device__ __forceinline__ void umma_f16_ts(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
+__device__ __forceinline__ void umma_f16_ts(uint32_t d, uint32_t a, uint32_t b_low, uint32_t idesc, bool accumulate)
 {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %6, %7, %8}, p;\n\t}\n"
-        ::"r"(d), "r"(a), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(0), "r"(0), "r"(0), "r"(0) : "memory");
+        "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 b, {%2, %3};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, {%6, %6, %6, %6}, p;\n\t}\n"
+        ::"r"(d), "r"(a), "r"(b_low), "r"(kDescHigh), "r"(idesc), "r"((uint32_t)accumulate), "r"(0) : "memory");
 }
 
 // 32 or 16 consecutive fp32 columns of this thread's accumulator row; tmem_wait_ld before the first use.
