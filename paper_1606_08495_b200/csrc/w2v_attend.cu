@@ -103,7 +103,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = sh.tmem;
+    const uint32_t tmem = warp_value(sh.tmem);
     volatile int *abort_flag = &sh.abort_flag;
     // the run of keys [lo, hi) and the sinks [s, s_end) before it, which are the first tile
     int32_t lo = INT32_MAX, hi = 0, s = INT32_MAX;
@@ -113,6 +113,9 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         hi = max(hi, sh.limits[w][1]);
         s = min(s, sh.limits[w][2]);
     }
+    lo = warp_value(lo);
+    hi = warp_value(hi);
+    s = warp_value(s);
     const int32_t s_end = hi ? min(s + p.sinks, lo) : 0;
     const int32_t extra = s < s_end ? 1 : 0;
     const int32_t tiles = hi ? extra + (hi - lo + kFwdRows - 1) / kFwdRows : 0;
@@ -292,9 +295,11 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     } else if (warp == 8) {
         // ============ MMA issue: one lane ============
         if (NB == 1) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-        // The lane that issues is what the block waits for when its code is long: everything that does not change is
-        // formed once, a product costs an addition per operand.
-        if (lane == 0 && tiles) {
+        // The whole block waits for this warp when its code is long: everything that does not change is formed once, a
+        // product costs an addition per operand, and the warp stays together, so that addresses and descriptors are
+        // formed in uniform registers, where the instruction wants them; one lane issues.
+        if (tiles) {
+            const bool leader = elect_one();
             constexpr uint32_t kBlock = kFwdRows * 128, kStep = Sh::kStage >> 4;
             const uint32_t idesc_o = umma_idesc_f16(kBf16, kAttendTile, dim16, true), idesc_s = umma_idesc_f16(kBf16, kAttendTile, kFwdRows, false);
             const uint32_t q_low = umma_desc_low(qs, 0), k_low = umma_desc_low(ring, 0), v_low = umma_desc_low(ring + Sh::kOperand, kBlock);
@@ -310,30 +315,39 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     }
                 umma_commit(&sh.s_full[b]);
             };
-            bool ok = mbar_wait(&sh.q_full, 0, abort_flag);
+            auto wait = [&](uint64_t *bar, uint32_t parity) {
+                const bool got = __all_sync(kFullMask, mbar_wait(bar, parity, abort_flag));
+                tc_fence_after();
+                return got;
+            };
+            bool ok = wait(&sh.q_full, 0);
             uint32_t ahead = 0, ahead_phase = 0;                     // stage and phase of the next scores, two tiles ahead of the products with values
             for (int32_t t = 0; t < 2 && t < tiles && ok; ++t) {
-                ok = mbar_wait(&sh.full[ahead], 0, abort_flag);
-                if (ok) { tc_fence_after(); scores((uint32_t)t, ahead); ++ahead; }
+                ok = wait(&sh.full[ahead], 0);
+                if (ok && leader) scores((uint32_t)t, ahead);
+                __syncwarp();
+                ++ahead;
             }
             uint32_t stage = 0;
             for (int32_t t = 0; t < tiles && ok; ++t) {
                 const uint32_t b = t & 1, v = v_low + stage * kStep, w = tmem + Sh::kS + b * kFwdRows, d = tmem + Sh::kO + b * NB * 64;
                 const int32_t keys = tile_keys(t);
-                ok = mbar_wait(&sh.p_full[b], (t >> 1) & 1, abort_flag);
+                ok = wait(&sh.p_full[b], (t >> 1) & 1);
                 if (!ok) break;
-                tc_fence_after();
+                if (leader) {
 #pragma unroll
-                for (int k = 0; k < kFwdRows / 16; ++k)
-                    if (k * 16 < keys) umma_f16_ts(d, w + k * 8, v + k * 128, idesc_o, t > 1 || k > 0);
-                umma_commit(&sh.empty[stage]);
-                if (t + 1 == tiles) umma_commit(&sh.done);
+                    for (int k = 0; k < kFwdRows / 16; ++k)
+                        if (k * 16 < keys) umma_f16_ts(d, w + k * 8, v + k * 128, idesc_o, t > 1 || k > 0);
+                    umma_commit(&sh.empty[stage]);
+                    if (t + 1 == tiles) umma_commit(&sh.done);
+                }
+                __syncwarp();
                 if (++stage == Sh::kStages) stage = 0;
                 if (t + 2 < tiles) {
-                    ok = mbar_wait(&sh.full[ahead], ahead_phase, abort_flag);
+                    ok = wait(&sh.full[ahead], ahead_phase);
                     if (!ok) break;
-                    tc_fence_after();
-                    scores(b, ahead);
+                    if (leader) scores(b, ahead);
+                    __syncwarp();
                     if (++ahead == Sh::kStages) { ahead = 0; ahead_phase ^= 1u; }
                 }
             }

@@ -142,7 +142,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = sh.tmem;
+    const uint32_t tmem = warp_value(sh.tmem);
     volatile int *abort_flag = &sh.abort_flag;
     int32_t lo = INT32_MAX, hi = 0, s_lo = INT32_MAX;
 #pragma unroll
@@ -151,6 +151,9 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
         hi = max(hi, sh.limits[w][1]);
         s_lo = min(s_lo, sh.limits[w][2]);
     }
+    lo = warp_value(lo);
+    hi = warp_value(hi);
+    s_lo = warp_value(s_lo);
     // tiles of one head: role 0 the run of keys and then the sinks before it, role 1 the queries, on a grid of kRows
     if (ROLE == 1) lo = hi ? lo / Sh::kRows * Sh::kRows : 0;
     const int32_t s_end = ROLE == 0 && hi ? min(s_lo + p.sinks, lo) : 0, extra = ROLE == 0 && hi && s_lo < s_end ? (s_end - s_lo + Sh::kRows - 1) / Sh::kRows : 0;
@@ -394,8 +397,10 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
         tc_fence_before();
     } else if (warp == kMmaWarp) {
         // ============ MMA issue: one lane ============
-        // everything that does not change is formed once: the block waits for this lane when its code is long
-        if (lane == 0 && total) {
+        // everything that does not change is formed once, in a warp that stays together: the block waits for it when its
+        // code is long
+        if (total) {
+            const bool leader = elect_one();
             constexpr uint32_t kBlock = Sh::kRows * 128, kStep = Sh::kStage >> 4;
             const uint32_t idesc_g = umma_idesc_f16(kBf16, kAttendTile, dim16, true), idesc_s = umma_idesc_f16(kBf16, kAttendTile, Sh::kRows, false);
             // the streamed operands with columns as the summed side (scores) and with rows as the summed side (gradients)
@@ -412,34 +417,43 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                     }
                 umma_commit(&sh.s_full[b]);
             };
-            bool ok = mbar_wait(&sh.a_full, 0, abort_flag);
+            auto wait = [&](uint64_t *bar, uint32_t parity) {
+                const bool got = __all_sync(kFullMask, mbar_wait(bar, parity, abort_flag));
+                tc_fence_after();
+                return got;
+            };
+            bool ok = wait(&sh.a_full, 0);
             uint32_t ahead = 0, ahead_phase = 0, stage = 0;          // stage and phase of the next scores, two tiles ahead of the gradients
             for (int32_t t = 0; t < Sh::kBuf && t < total && ok; ++t) {
-                ok = mbar_wait(&sh.full[ahead], 0, abort_flag);
-                if (ok) { tc_fence_after(); scores((uint32_t)t, ahead); ++ahead; }
+                ok = wait(&sh.full[ahead], 0);
+                if (ok && leader) scores((uint32_t)t, ahead);
+                __syncwarp();
+                ++ahead;
             }
             int32_t k = 0;                                           // number of the tile within its head
             for (int32_t t = 0; t < total && ok; ++t) {
                 const uint32_t b = t % Sh::kBuf, x = xg + stage * kStep, y = yg + stage * kStep, d = tmem + Sh::kScores + b * 2 * Sh::kRows;
                 const int32_t rows = tile_rows(k);
                 if (++k == per_head) k = 0;
-                ok = mbar_wait(&sh.p_full[b], (t / Sh::kBuf) & 1, abort_flag);
+                ok = wait(&sh.p_full[b], (t / Sh::kBuf) & 1);
                 if (!ok) break;
-                tc_fence_after();
+                if (leader) {
 #pragma unroll
-                for (int c = 0; c < Sh::kRows / 16; ++c)
-                    if (c * 16 < rows) {
-                        umma_f16_ts(tmem + Sh::kG1, d + c * 8, y + c * 128, idesc_g, t > 0 || c > 0);
-                        umma_f16_ts(tmem + Sh::kG0, d + Sh::kRows + c * 8, x + c * 128, idesc_g, t > 0 || c > 0);
-                    }
-                umma_commit(&sh.empty[stage]);
-                if (t + 1 == total) umma_commit(&sh.done);
+                    for (int c = 0; c < Sh::kRows / 16; ++c)
+                        if (c * 16 < rows) {
+                            umma_f16_ts(tmem + Sh::kG1, d + c * 8, y + c * 128, idesc_g, t > 0 || c > 0);
+                            umma_f16_ts(tmem + Sh::kG0, d + Sh::kRows + c * 8, x + c * 128, idesc_g, t > 0 || c > 0);
+                        }
+                    umma_commit(&sh.empty[stage]);
+                    if (t + 1 == total) umma_commit(&sh.done);
+                }
+                __syncwarp();
                 if (++stage == Sh::kStages) stage = 0;
                 if (t + Sh::kBuf < total) {
-                    ok = mbar_wait(&sh.full[ahead], ahead_phase, abort_flag);
+                    ok = wait(&sh.full[ahead], ahead_phase);
                     if (!ok) break;
-                    tc_fence_after();
-                    scores(b, ahead);
+                    if (leader) scores(b, ahead);
+                    __syncwarp();
                     if (++ahead == Sh::kStages) { ahead = 0; ahead_phase ^= 1u; }
                 }
             }

@@ -71,6 +71,17 @@ __device__ __forceinline__ uint32_t umma_idesc_f16(bool bf16, uint32_t m, uint32
     return (1u << 4) | ((bf16 ? 1u : 0u) << 7) | ((bf16 ? 1u : 0u) << 10) | ((b_rows ? 1u : 0u) << 16) | ((n >> 3) << 17) | ((m >> 4) << 24);
 }
 
+// One lane of a converged warp, the same each time.
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t x;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(x));
+    return x != 0;
+}
+// A value that every lane of the warp has, as one the compiler knows to be the same in all.
+__device__ __forceinline__ uint32_t warp_value(uint32_t x) { return __reduce_or_sync(0xFFFFFFFFu, x); }
+__device__ __forceinline__ int32_t warp_value(int32_t x) { return (int32_t)__reduce_or_sync(0xFFFFFFFFu, (uint32_t)x); }
+
 // The low words of such a descriptor move with the address (in units of 16 bytes); the high word is always this one.
 constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
 __device__ __forceinline__ uint32_t umma_desc_low(uint32_t saddr, uint32_t lbo) { return (uint32_t)umma_desc_sw128(saddr, lbo); }
