@@ -265,7 +265,11 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         // out through shared memory (every tile is read by now), a row of 16-byte chunks at a time
         const uint32_t row_bytes = p.dim * 2u, part = (warp & 3u) * 32u;
         unsigned char *stripe = smem + part * row_bytes, *line = stripe + lane * row_bytes;
-        for (uint32_t c = wg * 16; c < dim16; c += 32) {
+        const uint32_t turn = lane % dch;                            // chunks are turned by the row: fewer bank conflicts
+#pragma unroll
+        for (int i = 0; i < NB * 2; ++i) {
+            const uint32_t c = i * 32 + wg * 16;
+            if (c >= dim16) break;
             uint32_t a[16], b[16];
             tmem_ld16(tmem + lanes + Sh::kO + c, a);
             tmem_ld16(tmem + lanes + Sh::kO + NB * 64 + c, b);
@@ -283,9 +287,8 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     uint4 w;
                     w.x = pack2<T>(o[g * 8], o[g * 8 + 1]); w.y = pack2<T>(o[g * 8 + 2], o[g * 8 + 3]);
                     w.z = pack2<T>(o[g * 8 + 4], o[g * 8 + 5]); w.w = pack2<T>(o[g * 8 + 6], o[g * 8 + 7]);
-                    uint32_t ch = (c >> 3) + g + lane;               // turned by the row: fewer bank conflicts
-                    while (ch >= dch) ch -= dch;
-                    *reinterpret_cast<uint4 *>(line + ch * 16u) = w;
+                    const uint32_t ch = (c >> 3) + g + turn;
+                    *reinterpret_cast<uint4 *>(line + (ch >= dch ? ch - dch : ch) * 16u) = w;
                 }
         }
         asm volatile("bar.sync %0, 64;" ::"r"(2u + (warp & 3u)) : "memory");        // the two warps of these rows
@@ -377,19 +380,17 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         // ============ rows that are not words: a warp per tile, in turn ============
         if (NB == 1) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         int32_t t = (int32_t)warp - 10;
-        uint32_t vis[2], next[2] = {0u, 0u};
-        if (t < tiles) word_bits(p, tile_at(t), (uint32_t)tile_keys(t), lane, next);
+        uint32_t vis[2] = {0u, 0u};
+        if (t < tiles) word_bits(p, tile_at(t), (uint32_t)tile_keys(t), lane, vis);
         for (; t < tiles; t += 2) {
             const uint32_t stage = t % Sh::kStages;
-            vis[0] = next[0];
-            vis[1] = next[1];
-            if (t + 2 < tiles) word_bits(p, tile_at(t + 2), (uint32_t)tile_keys(t + 2), lane, next);
             if (!__all_sync(kFullMask, mbar_wait(&sh.landed[stage], (t / Sh::kStages) & 1, abort_flag))) break;
             if (lane < 2) sh.vis[stage][lane] = lane ? vis[1] : vis[0];
             // values only: the scores of such a key are masked
             zero_rows<NB>(ring + stage * Sh::kStage + Sh::kOperand, kFwdRows * 128, (uint32_t)(tile_keys(t) + 15) & ~15u, vis, lane);
             fence_async_proxy();
             mbar_arrive(&sh.full[stage]);
+            if (t + 2 < tiles) word_bits(p, tile_at(t + 2), (uint32_t)tile_keys(t + 2), lane, vis);
         }
     }
     __syncthreads();

@@ -73,19 +73,42 @@ __device__ __forceinline__ void bucket_range(const BucketStarts &s, uint32_t b, 
     else { r0 = 1 - d1; r1 = k == 0 && !s.two_sided ? off + 1 : 1 - d0; }
 }
 
-// The table of a head by `warps` warps (this one is number `warp`), a bucket at a time.
+// The table of a head by `warps` warps (this one is number `warp`).  A lane takes one distance and counts the buckets
+// that start at or before it, a bucket's start per shuffle; the entries beyond the last start are the last bucket's.
 __device__ __forceinline__ void fill_bias(const AttendParams &p, uint32_t h, float *lut, uint32_t warp, uint32_t warps, uint32_t lane)
 {
-    const int32_t off = bias_last(p.b) + kBiasPad;
-    const uint32_t buckets = p.b.n * (p.b.two_sided ? 2u : 1u);
+    const int32_t last = bias_last(p.b), off = last + kBiasPad;
+    const uint32_t n = p.b.n, buckets = n * (p.b.two_sided ? 2u : 1u);
     float v[2];
+    int32_t start[2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) v[i] = lane + 32u * i < buckets ? log2_bias(__ldg(p.bias + (size_t)(lane + 32 * i) * p.heads + h)) : 0.f;
-    for (uint32_t b = warp; b < buckets; b += warps) {
-        int32_t r0, r1;
-        bucket_range(p.b, b, off, r0, r1);
-        const float x = __shfl_sync(kFullMask, b < 32 ? v[0] : v[1], b & 31u);
-        for (int32_t r = r0 + (int32_t)lane; r < r1; r += 32) lut[r + off] = x;
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t b = lane + 32u * i;
+        v[i] = b < buckets ? __ldg(p.bias + (size_t)b * p.heads + h) : 0.f;
+        start[i] = b < n ? p.b.start[b] : INT32_MAX;
+    }
+    v[0] = log2_bias(v[0]);
+    v[1] = log2_bias(v[1]);
+    auto value = [&](uint32_t b) {                                   // every lane its own bucket
+        const float x = __shfl_sync(kFullMask, v[0], b & 31u), y = buckets > 32 ? __shfl_sync(kFullMask, v[1], b & 31u) : 0.f;
+        return b < 32 ? x : y;
+    };
+    for (int32_t d0 = (int32_t)warp * 32; d0 <= last; d0 += (int32_t)warps * 32) {
+        const int32_t d = d0 + (int32_t)lane;
+        uint32_t b = 0;
+#pragma unroll 4
+        for (uint32_t k = 1; k < min(n, 32u); ++k) b += __shfl_sync(kFullMask, start[0], k) <= d ? 1u : 0u;
+        for (uint32_t k = 32; k < n; ++k) b += __shfl_sync(kFullMask, start[1], k & 31u) <= d ? 1u : 0u;
+        const float x = value(b), y = value(p.b.two_sided ? b + n : 0u);
+        if (d <= last) {
+            if (d > 0) lut[off + d] = y;
+            lut[off - d] = x;
+        }
+    }
+    const float x = value(n - 1), y = value(p.b.two_sided ? 2 * n - 1 : 0u);
+    for (int32_t i = last + 1 + (int32_t)(warp * 32 + lane); i <= off; i += (int32_t)warps * 32) {
+        lut[off - i] = x;
+        lut[off + i] = y;
     }
 }
 
@@ -127,10 +150,9 @@ __device__ __forceinline__ void store_rows(char *out, uint64_t ld_bytes, const u
     const uint32_t inv = (65536u + chunks - 1) / chunks;             // exact for the up to 512 chunks of 32 rows
     for (int32_t e = (int32_t)at; e < rows * (int32_t)chunks; e += (int32_t)threads) {
         const uint32_t r = ((uint32_t)e * inv) >> 16, c = (uint32_t)e - r * chunks;
-        uint32_t from = c + r;
-        while (from >= chunks) from -= chunks;
+        const uint32_t turned = c + r - ((r * inv) >> 16) * chunks;  // c + r mod chunks
         *reinterpret_cast<uint4 *>(out + (uint64_t)r * ld_bytes + c * 16u) =
-            *reinterpret_cast<const uint4 *>(stripe + (r * chunks + from) * 16u);
+            *reinterpret_cast<const uint4 *>(stripe + (r * chunks + (turned >= chunks ? turned - chunks : turned)) * 16u);
     }
 }
 
