@@ -26,48 +26,54 @@ struct BackShape {
     static constexpr uint32_t kScores = NB * 192, kAlloc = 512;
     static_assert(kScores + kBuf * 2 * kRows <= kAlloc, "tensor memory");
     static constexpr int kOperand = NB * kRows * 128, kStage = 2 * kOperand, kRing = kStages * kStage;
+    static constexpr int kOwn = NB * 128 * 128;                      // bytes of one operand of the block's own rows
     static constexpr int kSoft = 128 * kBuf, kThreads = kSoft + 128;
-    static_assert(kRing >= 2 * NB * 128 * 128, "the outputs are staged where the ring was");
+    static_assert(kRing >= 2 * kOwn, "the outputs are staged where the ring was");
 };
 
 struct BackShared {
-    uint64_t a_full, landed[4], full[4], empty[4], s_full[2], p_full[2], done;
+    uint64_t own_landed, a_full, landed[4], full[4], empty[4], s_full[2], p_full[2], done;
     uint32_t tmem;
     int abort_flag, quiet;
     int32_t limits[4][3];
     uint32_t vis[4][2];                              // role 0: which keys of the stage are words
     int32_t run_lo[4];                               // role 1: where the run of the stage's query tile begins
-    __align__(16) float lse[4][64], delta[4][64];    // role 1: of the stage's queries
-    float eps[128];
+    __align__(16) float lse[4][64], delta[4][64];    // role 1: of the stage's queries, negated
+    float eps[2][128];
     float far_sum[8][2];
 };
 
 __device__ __forceinline__ void soft_barrier(int threads) { asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory"); }
 
-// Sums the per-distance sums of `arrays` copies (`entries` floats each) and the far sums over the distances of
-// each bucket; warp w of `warps` takes buckets w, w + warps, ...
-__device__ __forceinline__ void write_bucket_sums(const AttendParams &p, const float *sums, uint32_t arrays, uint32_t entries, int32_t off,
-                                                  const float (*far_sum)[2], uint32_t far_rows, uint32_t warp, uint32_t warps,
-                                                  uint32_t lane, float *out)
+// Sums per distance (`off` on either side of 0) and the warps' far sums over the distances of each bucket; warp w of
+// `warps` takes buckets w, w + warps, ...
+__device__ __forceinline__ void write_bucket_sums(const AttendParams &p, const float *sums, int32_t off, const float (*far_sum)[2],
+                                                  uint32_t warp, uint32_t warps, uint32_t lane, float *out)
 {
     const uint32_t n = p.b.n, buckets = n * (p.b.two_sided ? 2u : 1u);
+    const float far_l = lane < warps ? far_sum[lane][0] : 0.f, far_r = lane < warps ? far_sum[lane][1] : 0.f;
     for (uint32_t b = warp; b < buckets; b += warps) {
         const uint32_t side = b >= n ? 1u : 0u, k = b - side * n;
         int32_t r0, r1;
         bucket_range(p.b, b, off, r0, r1);
-        float a = 0.f;
-        for (uint32_t w = 0; w < arrays; ++w)
-            for (int32_t r = r0 + (int32_t)lane; r < r1; r += 32) a += sums[w * entries + (uint32_t)(r + off)];
-        const bool left = side == 0 && k == n - 1, right = p.b.two_sided ? side == 1 && k == n - 1 : k == 0;
-        if (lane < far_rows) a += (left ? far_sum[lane][0] : 0.f) + (right ? far_sum[lane][1] : 0.f);
-        a = warp_sum(a);
-        if (lane == 0) out[b] = a;
+        float a[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int32_t r = r0 + (int32_t)lane; r < r1; r += 128) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) if (r + i * 32 < r1) a[i] += sums[r + i * 32 + off];
+        }
+        float t = (a[0] + a[1]) + (a[2] + a[3]);
+        if (side == 0 && k == n - 1) t += far_l;
+        if (p.b.two_sided ? side == 1 && k == n - 1 : k == 0) t += far_r;
+        t = warp_sum(t);
+        if (lane == 0) out[b] = t;
     }
 }
 
 template <typename T, int NB, int ROLE>
 __global__ void __launch_bounds__(BackShape<NB>::kThreads, 1)
-attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_y, AttendParams p, int *error)
+attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_y,
+                   const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ CUtensorMap map_a1,
+                   const __grid_constant__ CUtensorMap map_o, AttendParams p, int *error)
 {
     using Sh = BackShape<NB>;
     constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
@@ -76,7 +82,8 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
     __shared__ BackShared sh;
     unsigned char *smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
     const uint32_t ring = smem_addr(smem);
-    float *lut = reinterpret_cast<float *>(smem + Sh::kRing);
+    const unsigned char *own_rows = smem + Sh::kRing;                // the two A sides, and o in role 0, as they land
+    float *lut = reinterpret_cast<float *>(smem + Sh::kRing + (ROLE == 0 ? 3 : 2) * Sh::kOwn);
     const uint32_t entries = bias_entries(p.b);
     float *rel_sums = lut + ((entries + 3u) & ~3u);                  // role 1: [softmax warps][entries]
 
@@ -88,14 +95,23 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
     const uint32_t dim16 = (p.dim + 15u) & ~15u;
     constexpr uint32_t kSoftWarps = Sh::kSoft / 32, kMmaWarp = kSoftWarps;
 
-    if (tid == 0) {
-        mbar_init(&sh.a_full, 128);
+    if (warp == kMmaWarp + 1 && lane == 0) {
+        mbar_init(&sh.own_landed, 1);
+        mbar_init(&sh.a_full, 256);
         for (int i = 0; i < Sh::kStages; ++i) { mbar_init(&sh.landed[i], 1); mbar_init(&sh.full[i], 32); mbar_init(&sh.empty[i], 1 + 128); }
         for (int i = 0; i < 2; ++i) { mbar_init(&sh.s_full[i], 1); mbar_init(&sh.p_full[i], 128); }
         mbar_init(&sh.done, 1);
         sh.abort_flag = sh.quiet = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_proxy();
+        mbar_expect(&sh.own_landed, (ROLE == 0 ? 3 : 2) * Sh::kOwn);
+#pragma unroll
+        for (int c = 0; c < NB; ++c) {
+            const uint32_t to = ring + Sh::kRing + c * (128 * 128);
+            copy_box(to, &map_a0, c * 64, (int32_t)h_own, t0, &sh.own_landed);
+            copy_box(to + Sh::kOwn, &map_a1, c * 64, (int32_t)h_own, t0, &sh.own_landed);
+            if (ROLE == 0) copy_box(to + 2 * Sh::kOwn, &map_o, c * 64, (int32_t)h_own, t0, &sh.own_landed);
+        }
     }
     const uint32_t r = tid & 127u;                                   // this thread's row (softmax warps)
     const int64_t own = (int64_t)t0 + r;
@@ -171,45 +187,36 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
         const bool word = ROLE == 0 ? row.hi > row.lo : q_hi > q_lo;
         float lse = INFINITY, delta = 0.f;
         if (ROLE == 0 && word) lse = __ldg(p.lse + (int64_t)h_own * p.n + own);
-        // the two operands of the block's rows go to tensor memory, zeros for rows that are not words
+        // the two operands of the block's rows go to tensor memory (a warpgroup each), zeros for rows that are not words
+        bool ok = __all_sync(kFullMask, mbar_wait(&sh.own_landed, 0, abort_flag));
         {
-            const T *a0 = ROLE == 0 ? static_cast<const T *>(p.q) + own * (int64_t)p.ldq + (int64_t)h_own * p.dim
-                                    : static_cast<const T *>(p.k) + own * (int64_t)p.ldk + (int64_t)kvh * p.dim;
-            const T *a1 = ROLE == 0 ? static_cast<const T *>(p.d_o) + own * (int64_t)p.ld_do + (int64_t)h_own * p.dim
-                                    : static_cast<const T *>(p.v) + own * (int64_t)p.ldv + (int64_t)kvh * p.dim;
-            const T *o = ROLE == 0 ? static_cast<const T *>(p.o) + own * (int64_t)p.ldo + (int64_t)h_own * p.dim : nullptr;
+            auto chunk = [&](int operand, int c) {                   // 8 columns of this thread's row, from the 128-byte swizzle
+                return *reinterpret_cast<const uint4 *>(own_rows + operand * Sh::kOwn + (c >> 3) * (128 * 128) + r * 128u + (((c & 7) ^ (r & 7u)) << 4));
+            };
 #pragma unroll
             for (int g = 0; g < NB * 2; ++g) {
-                uint32_t x[16], y[16];
+                uint32_t x[16];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    const uint32_t at = g * 32 + c * 8;
-                    uint4 u = make_uint4(0, 0, 0, 0), w = u;
-                    if (word && at < p.dim) {
-                        u = __ldg(reinterpret_cast<const uint4 *>(a0 + at));
-                        w = __ldg(reinterpret_cast<const uint4 *>(a1 + at));
-                        if (ROLE == 0) {
-                            const Pack<T, 8> oo = load_pack<T, 8>(o + at), dd = load_pack<T, 8>(a1 + at);
+                    const int at = g * 4 + c;
+                    uint4 u = chunk((int)wg, at);
+                    if (!word) u = make_uint4(0, 0, 0, 0);
+                    if (ROLE == 0) {                                 // both warpgroups need the first delta
+                        const uint4 d4 = chunk(1, at), o4 = chunk(2, at);
+                        const Pack<T, 8> dd = reinterpret_cast<const Pack<T, 8> &>(d4), oo = reinterpret_cast<const Pack<T, 8> &>(o4);
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) delta = fmaf(to_f32(oo.e[e]), to_f32(dd.e[e]), delta);
-                        }
+                        for (int e = 0; e < 8; ++e) delta = fmaf(to_f32(oo.e[e]), to_f32(dd.e[e]), delta);
                     }
                     x[c * 4] = u.x; x[c * 4 + 1] = u.y; x[c * 4 + 2] = u.z; x[c * 4 + 3] = u.w;
-                    y[c * 4] = w.x; y[c * 4 + 1] = w.y; y[c * 4 + 2] = w.z; y[c * 4 + 3] = w.w;
                 }
-                if (wg == 0) {
-                    tmem_st16(tmem + lanes + Sh::kA0 + g * 16, x);
-                    tmem_st16(tmem + lanes + Sh::kA1 + g * 16, y);
-                }
+                tmem_st16(tmem + lanes + (wg == 0 ? Sh::kA0 : Sh::kA1) + g * 16, x);
             }
-            if (wg == 0) {
-                tmem_wait_st();
-                tc_fence_before();
-                mbar_arrive(&sh.a_full);
-            }
+            if (!word) delta = 0.f;
+            tmem_wait_st();
+            tc_fence_before();
+            mbar_arrive(&sh.a_full);
         }
-        float eps = 0.f;
-        bool ok = true;
+        float2 eps2 = make_float2(0.f, 0.f);
         for (uint32_t g = 0; g < heads_here; ++g) {
             if (ROLE == 1 && p.b.n && g > 0) {
                 soft_barrier(Sh::kSoft);                             // the sums of the head before are written
@@ -250,10 +257,16 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                             m = range_bits(q_lo, q_hi, at);
                             if (reach) m |= range_bits(far_lo, far_hi, at);
                         }
+                        // -infinity where the key is hidden; a row or column that sees nothing has lse +infinity
                         float x[32];
                         if (far) {
+                            const float2 scale2 = make_float2(scale, scale), flat2 = make_float2(flat, flat);
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) x[e] = fmaf(__uint_as_float(sv[e]), scale, flat);
+                            for (int e = 0; e < 32; e += 2) {
+                                const float2 y = fma2(pair_of(sv[e], sv[e + 1]), scale2, flat2);
+                                x[e] = y.x;
+                                x[e + 1] = y.y;
+                            }
                         } else {
                             // key - query grows with the column in role 0 and falls with it in role 1
                             const float *near = ROLE == 0 ? lut + (at - (int32_t)own + off) : lut + ((int32_t)own - at + off);
@@ -262,17 +275,20 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                         }
                         if (!__all_sync(kFullMask, m == 0xFFFFFFFFu)) {
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) x[e] = (m >> e) & 1u ? x[e] : -INFINITY;
+                            for (int e = 0; e < 32; ++e) x[e] = m & (1u << e) ? x[e] : -INFINITY;
                         }
                         uint32_t ws[16], wp[16];
                         if (ROLE == 0) {
+                            const float2 lse2 = make_float2(-lse, -lse), delta2 = make_float2(-delta, -delta);
 #pragma unroll
                             for (int e = 0; e < 32; e += 2) {
-                                const float p0 = fast_exp2(x[e] - lse), p1 = fast_exp2(x[e + 1] - lse);
-                                const float d0 = p0 * (__uint_as_float(dv[e]) - delta), d1 = p1 * (__uint_as_float(dv[e + 1]) - delta);
-                                eps += d0 + d1;
-                                wp[e / 2] = pack2<T>(p0, p1);
-                                ws[e / 2] = pack2<T>(d0, d1);
+                                float2 w = add2(make_float2(x[e], x[e + 1]), lse2);
+                                w.x = fast_exp2(w.x);
+                                w.y = fast_exp2(w.y);
+                                const float2 d = mul2(w, add2(pair_of(dv[e], dv[e + 1]), delta2));
+                                eps2 = add2(eps2, d);
+                                wp[e / 2] = pack2<T>(w.x, w.y);
+                                ws[e / 2] = pack2<T>(d.x, d.y);
                             }
                             tmem_st16(cs + c * 16, wp);
                             tmem_st16(cd + c * 16, ws);
@@ -280,18 +296,18 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                             float ds[32];
 #pragma unroll
                             for (int e = 0; e < 32; e += 4) {
-                                const float4 l4 = *reinterpret_cast<const float4 *>(&sh.lse[stage][c * 32 + e]);
+                                const float4 l4 = *reinterpret_cast<const float4 *>(&sh.lse[stage][c * 32 + e]);        // negated, as delta
                                 const float4 d4 = *reinterpret_cast<const float4 *>(&sh.delta[stage][c * 32 + e]);
-                                const float p0 = fast_exp2(x[e] - l4.x), p1 = fast_exp2(x[e + 1] - l4.y);
-                                const float p2 = fast_exp2(x[e + 2] - l4.z), p3 = fast_exp2(x[e + 3] - l4.w);
-                                wp[e / 2] = pack2<T>(p0, p1);
-                                wp[e / 2 + 1] = pack2<T>(p2, p3);
-                                ds[e] = p0 * (__uint_as_float(dv[e]) - d4.x);
-                                ds[e + 1] = p1 * (__uint_as_float(dv[e + 1]) - d4.y);
-                                ds[e + 2] = p2 * (__uint_as_float(dv[e + 2]) - d4.z);
-                                ds[e + 3] = p3 * (__uint_as_float(dv[e + 3]) - d4.w);
-                                ws[e / 2] = pack2<T>(ds[e], ds[e + 1]);
-                                ws[e / 2 + 1] = pack2<T>(ds[e + 2], ds[e + 3]);
+                                float2 p0 = add2(make_float2(x[e], x[e + 1]), make_float2(l4.x, l4.y));
+                                float2 p1 = add2(make_float2(x[e + 2], x[e + 3]), make_float2(l4.z, l4.w));
+                                p0.x = fast_exp2(p0.x); p0.y = fast_exp2(p0.y); p1.x = fast_exp2(p1.x); p1.y = fast_exp2(p1.y);
+                                wp[e / 2] = pack2<T>(p0.x, p0.y);
+                                wp[e / 2 + 1] = pack2<T>(p1.x, p1.y);
+                                p0 = mul2(p0, add2(pair_of(dv[e], dv[e + 1]), make_float2(d4.x, d4.y)));
+                                p1 = mul2(p1, add2(pair_of(dv[e + 2], dv[e + 3]), make_float2(d4.z, d4.w)));
+                                ws[e / 2] = pack2<T>(p0.x, p0.y);
+                                ws[e / 2 + 1] = pack2<T>(p1.x, p1.y);
+                                ds[e] = p0.x; ds[e + 1] = p0.y; ds[e + 2] = p1.x; ds[e + 3] = p1.y;
                             }
                             tmem_st16(cs + c * 16, wp);
                             tmem_st16(cd + c * 16, ws);
@@ -331,67 +347,82 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                 far_r = warp_sum(far_r);
                 if (lane == 0) { sh.far_sum[warp][0] = far_l; sh.far_sum[warp][1] = far_r; }
                 soft_barrier(Sh::kSoft);
+                for (uint32_t e = tid; e < entries; e += Sh::kSoft) {        // the warps' sums
+                    float a = 0.f;
+#pragma unroll
+                    for (uint32_t w = 0; w < kSoftWarps; ++w) a += rel_sums[w * entries + e];
+                    rel_sums[e] = a;
+                }
+                soft_barrier(Sh::kSoft);
                 const uint32_t buckets = p.b.n * (p.b.two_sided ? 2u : 1u);
-                write_bucket_sums(p, rel_sums, kSoftWarps, entries, off, sh.far_sum, kSoftWarps, warp, kSoftWarps, lane,
-                                  p.dbias_part + ((size_t)tile * p.heads + h0 + g) * buckets);
+                write_bucket_sums(p, rel_sums, off, sh.far_sum, warp, kSoftWarps, lane, p.dbias_part + ((size_t)tile * p.heads + h0 + g) * buckets);
             }
         }
+        float eps = 0.f;
         if (ROLE == 0) {
-            if (wg == 1) sh.eps[r] = eps;
+            sh.eps[wg][r] = eps2.x + eps2.y;
             soft_barrier(Sh::kSoft);
-            if (wg == 0) eps += sh.eps[r];
+            eps = sh.eps[0][r] + sh.eps[1][r];
             if (wg == 0 && own < p.n) p.delta[(int64_t)h_own * p.n + own] = word ? delta + eps : 0.f;
         }
         ok = __all_sync(kFullMask, ok && (total == 0 || mbar_wait(&sh.done, 0, abort_flag)));
         tc_fence_after();
-        // outputs leave through shared memory: role 0 dQ (warpgroup 0), role 1 dK and dV (a warpgroup each)
-        if (ROLE == 1 || wg == 0) {
-            const uint32_t from = tmem + lanes + (wg == 0 ? Sh::kG0 : Sh::kG1);
-            const float by = wg == 0 ? p.scale : 1.f;
+        // outputs leave through shared memory: role 0 half of dQ's columns by each warpgroup, role 1 dK and dV by one each
+        {
+            const float by = ROLE == 0 || wg == 0 ? p.scale : 1.f;
             const float *sink = nullptr;
             if (ROLE == 1 && p.sink_used && word && own - sent < p.sinks && p.sink_used[sent / kAttendTile] == sent)
                 sink = p.sink_sum + ((((size_t)(sent / kAttendTile) * p.kv_heads + kvh) * p.sinks + (size_t)(own - sent)) * 2 + wg) * p.dim;
-            const uint32_t row_bytes = p.dim * 2u, chunks = p.dim >> 3;
-            unsigned char *mine = smem + warp * 32u * row_bytes, *line = mine + lane * row_bytes;
-            const int32_t rows = (int32_t)min((int64_t)32, p.n - (int64_t)w0);
-            for (uint32_t c = 0; c < dim16; c += 16) {
-                uint32_t o[16];
-                if (total) { tmem_ld16(from + c, o); tmem_wait_ld(o); }
-                else {
+            const uint32_t row_bytes = p.dim * 2u, chunks = p.dim >> 3, turn = lane % chunks, part = (ROLE == 0 ? warp & 3u : warp) * 32u;
+            unsigned char *mine = smem + part * row_bytes, *line = mine + lane * row_bytes;
+            constexpr int kCols = ROLE == 0 ? NB * 2 : NB * 4;       // steps of 16 columns
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) o[e] = 0u;
-                }
-                if (ROLE == 0 && total) {                            // the correction of the first delta
-                    uint32_t pk[16];
-                    tmem_ld16(tmem + lanes + Sh::kG1 + c, pk);
-                    tmem_wait_ld(pk);
+            for (int i = 0; i < kCols; ++i) {
+                const uint32_t c = ROLE == 0 ? i * 32 + wg * 16 : i * 16;
+                if (c >= dim16) break;
+                float f[16];
+                if (total) {
+                    uint32_t o[16];
+                    tmem_ld16(tmem + lanes + (ROLE == 0 || wg == 0 ? Sh::kG0 : Sh::kG1) + c, o);
+                    if (ROLE == 0) {                                 // the correction of the first delta
+                        uint32_t pk[16];
+                        tmem_ld16(tmem + lanes + Sh::kG1 + c, pk);
+                        tmem_wait_ld(o);
+                        tmem_wait_ld(pk);
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(fmaf(-eps, __uint_as_float(pk[e]), __uint_as_float(o[e])));
+                        for (int e = 0; e < 16; ++e) f[e] = word ? fmaf(-eps, __uint_as_float(pk[e]), __uint_as_float(o[e])) : 0.f;
+                    } else {
+                        tmem_wait_ld(o);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) f[e] = __uint_as_float(o[e]);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) f[e] = 0.f;
                 }
 #pragma unroll
                 for (int q = 0; q < 2; ++q)
                     if (c + q * 8 < p.dim) {
-                        float f[8];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(o[q * 8 + e]);
                         if (sink) {
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) f[e] += sink[c + q * 8 + e];
+                            for (int e = 0; e < 8; ++e) f[q * 8 + e] += sink[c + q * 8 + e];
                         }
                         uint4 w;
-                        w.x = pack2<T>(f[0] * by, f[1] * by); w.y = pack2<T>(f[2] * by, f[3] * by);
-                        w.z = pack2<T>(f[4] * by, f[5] * by); w.w = pack2<T>(f[6] * by, f[7] * by);
-                        const uint32_t ch = (c >> 3) + q;
-                        *reinterpret_cast<uint4 *>(line + ((ch + lane) % chunks) * 16u) = w;
+                        w.x = pack2<T>(f[q * 8] * by, f[q * 8 + 1] * by); w.y = pack2<T>(f[q * 8 + 2] * by, f[q * 8 + 3] * by);
+                        w.z = pack2<T>(f[q * 8 + 4] * by, f[q * 8 + 5] * by); w.w = pack2<T>(f[q * 8 + 6] * by, f[q * 8 + 7] * by);
+                        const uint32_t ch = (c >> 3) + q + turn;
+                        *reinterpret_cast<uint4 *>(line + (ch >= chunks ? ch - chunks : ch) * 16u) = w;
                     }
             }
-            __syncwarp();
+            const int32_t rows = (int32_t)min((int64_t)32, p.n - (int64_t)w0);
             const uint64_t ld = ROLE == 0 ? p.ld_dq : wg == 0 ? p.ld_dk : p.ld_dv;
-            char *out = static_cast<char *>(ROLE == 0 ? p.dq : wg == 0 ? p.dk : p.dv) + ((uint64_t)w0 * ld + (uint64_t)(ROLE == 0 ? h_own : kvh) * p.dim) * 2u;
-            for (int32_t e = (int32_t)lane; e < rows * (int32_t)chunks; e += 32) {
-                const uint32_t rr = (uint32_t)e / chunks, ch = (uint32_t)e - rr * chunks;
-                *reinterpret_cast<uint4 *>(out + (uint64_t)rr * ld * 2u + ch * 16u) =
-                    *reinterpret_cast<const uint4 *>(mine + rr * row_bytes + ((ch + rr) % chunks) * 16u);
+            char *out = static_cast<char *>(ROLE == 0 ? p.dq : wg == 0 ? p.dk : p.dv) + ((uint64_t)w0 * ld + (uint64_t)h_own * p.dim) * 2u;
+            if (ROLE == 0) {
+                asm volatile("bar.sync %0, 64;" ::"r"(2u + (warp & 3u)) : "memory");    // the two warps of these rows
+                store_rows(out, ld * 2u, mine, chunks, rows, wg * 32u + lane, 64u);
+            } else {
+                __syncwarp();
+                store_rows(out, ld * 2u, mine, chunks, rows, lane, 32u);
             }
         }
         tc_fence_before();
@@ -509,7 +540,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                 if (lane < 2) sh.vis[stage][lane] = lane ? vis[1] : vis[0];
             } else {
 #pragma unroll
-                for (int w = 0; w < Sh::kRows / 32; ++w) { sh.lse[stage][w * 32 + lane] = lse[w]; sh.delta[stage][w * 32 + lane] = delta[w]; }
+                for (int w = 0; w < Sh::kRows / 32; ++w) { sh.lse[stage][w * 32 + lane] = -lse[w]; sh.delta[stage][w * 32 + lane] = -delta[w]; }
                 if (lane == 0) sh.run_lo[stage] = run_lo;
             }
             const uint32_t x = ring + stage * Sh::kStage, cols = (uint32_t)(rows + 15) & ~15u;
@@ -724,17 +755,24 @@ int launch_role(const AttendParams &p, uint32_t tiles, int *error, cudaStream_t 
     using Sh = BackShape<NB>;
     auto kernel = attend_back_kernel<T, NB, ROLE>;
     const uint32_t entries = bias_entries(p.b);
-    int smem = Sh::kRing + 1024 + (int)(4 * (((entries + 3u) & ~3u) + (ROLE == 1 ? Sh::kSoft / 32 * entries : 0u)));
+    int smem = Sh::kRing + (ROLE == 0 ? 3 : 2) * Sh::kOwn + 1024 + (int)(4 * (((entries + 3u) & ~3u) + (ROLE == 1 ? Sh::kSoft / 32 * entries : 0u)));
     if (smem < 116 * 1024) smem = 116 * 1024;     // a second block would only wait for tensor memory
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return -1;
-    CUtensorMap x, y;
+    CUtensorMap x, y, a0, a1, o;
     const bool bf16 = std::is_same<T, __nv_bfloat16>::value;
-    if (ROLE == 0 ? !make_rows_map(&x, bf16, p.k, p.dim, p.kv_heads, (uint64_t)p.n, p.ldk, Sh::kRows) ||
-                        !make_rows_map(&y, bf16, p.v, p.dim, p.kv_heads, (uint64_t)p.n, p.ldv, Sh::kRows)
-                  : !make_rows_map(&x, bf16, p.q, p.dim, p.heads, (uint64_t)p.n, p.ldq, Sh::kRows) ||
-                        !make_rows_map(&y, bf16, p.d_o, p.dim, p.heads, (uint64_t)p.n, p.ld_do, Sh::kRows))
-        return -1;
-    kernel<<<tiles * (ROLE == 0 ? p.heads : p.kv_heads), Sh::kThreads, smem, s>>>(x, y, p, error);
+    const uint64_t n = (uint64_t)p.n;
+    auto queries = [&](CUtensorMap *m, const void *at, uint64_t ld, uint32_t rows) { return make_rows_map(m, bf16, at, p.dim, p.heads, n, ld, rows); };
+    auto keys = [&](CUtensorMap *m, const void *at, uint64_t ld, uint32_t rows) { return make_rows_map(m, bf16, at, p.dim, p.kv_heads, n, ld, rows); };
+    if (ROLE == 0) {
+        if (!keys(&x, p.k, p.ldk, Sh::kRows) || !keys(&y, p.v, p.ldv, Sh::kRows) || !queries(&a0, p.q, p.ldq, 128) ||
+            !queries(&a1, p.d_o, p.ld_do, 128) || !queries(&o, p.o, p.ldo, 128))
+            return -1;
+    } else {
+        if (!queries(&x, p.q, p.ldq, Sh::kRows) || !queries(&y, p.d_o, p.ld_do, Sh::kRows) || !keys(&a0, p.k, p.ldk, 128) || !keys(&a1, p.v, p.ldv, 128))
+            return -1;
+        o = a0;
+    }
+    kernel<<<tiles * (ROLE == 0 ? p.heads : p.kv_heads), Sh::kThreads, smem, s>>>(x, y, a0, a1, o, p, error);
     return cudaPeekAtLastError() == cudaSuccess ? 1 : -1;
 }
 
