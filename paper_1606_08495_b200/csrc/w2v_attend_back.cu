@@ -10,7 +10,8 @@
 // Both keep two operands of their 128 rows in tensor memory (A sides), stream the other two through shared memory
 // and form both score products of a tile; a warpgroup turns them into P and dS, one row per thread, and puts those
 // back into tensor memory as the A sides of the gradient products, whose B sides are the streamed tiles again, read
-// with rows as the summed side.  Keys that are sinks of queries far behind them are summed by a kernel of their own.
+// with rows as the summed side.  Keys that are sinks of queries far behind them get what those add from role 0, as
+// sums over its 128 queries (the tile of the sinks is there anyway), which a small kernel adds up for role 1.
 #include <type_traits>
 
 #include "w2v_attend.cuh"
@@ -69,6 +70,83 @@ __device__ __forceinline__ void write_bucket_sums(const AttendParams &p, const f
     }
 }
 
+// What this block's queries add to the sinks before its run: dK (before the scale) and dV of each, and the bias' sums,
+// by the 256 softmax threads.  sink_d holds dS for the first delta, which eps puts right.  A thread takes two columns
+// and every 8th or 4th part of the rows, four sinks at a time; `red` is 16 KB for joining the parts.
+template <typename T, int NB>
+__device__ __forceinline__ void sink_sums(const AttendParams &p, const unsigned char *own_rows, const float *sink_p, float *sink_d,
+                                       const float (*eps)[128], float *red, int32_t sinks, int32_t s, int32_t t0, uint32_t wg, uint32_t r,
+                                       uint32_t tid, float *out, float *bias_out)
+{
+    constexpr int kSoft = 256, kPairs = 32 * NB, kParts = kSoft / kPairs, kPartRows = 128 / kParts, kOwn = NB * 128 * 128;
+    const float e = eps[0][r] + eps[1][r];
+    for (int32_t k = (int32_t)wg; k < sinks; k += 2) sink_d[k * 128 + (int32_t)r] -= e * sink_p[k * 128 + (int32_t)r];
+    soft_barrier(kSoft);
+    const uint32_t pair = tid % kPairs, part = tid / kPairs, width = 2 * p.dim;
+    for (int32_t k0 = 0; k0 < sinks; k0 += 4) {
+        float2 a[4], b[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] = b[i] = make_float2(0.f, 0.f);
+        if (2 * pair < p.dim) {
+#pragma unroll 2
+            for (uint32_t x0 = part * kPartRows; x0 < (part + 1) * kPartRows; x0 += 4) {
+                float2 q[4], g[4];
+#pragma unroll
+                for (uint32_t y = 0; y < 4; ++y) {
+                    const uint32_t x = x0 + y, at = (pair >> 5) * (128 * 128) + x * 128u + (((((pair & 31u) >> 2) ^ (x & 7u)) << 4) | ((pair & 3u) << 2));
+                    const Pack<T, 2> u = *reinterpret_cast<const Pack<T, 2> *>(own_rows + at), w = *reinterpret_cast<const Pack<T, 2> *>(own_rows + kOwn + at);
+                    q[y] = make_float2(to_f32(u.e[0]), to_f32(u.e[1]));
+                    g[y] = make_float2(to_f32(w.e[0]), to_f32(w.e[1]));
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (k0 + i < sinks) {
+                        const float4 d = *reinterpret_cast<const float4 *>(sink_d + (k0 + i) * 128 + x0), w = *reinterpret_cast<const float4 *>(sink_p + (k0 + i) * 128 + x0);
+                        a[i] = fma2(make_float2(d.x, d.x), q[0], a[i]); a[i] = fma2(make_float2(d.y, d.y), q[1], a[i]);
+                        a[i] = fma2(make_float2(d.z, d.z), q[2], a[i]); a[i] = fma2(make_float2(d.w, d.w), q[3], a[i]);
+                        b[i] = fma2(make_float2(w.x, w.x), g[0], b[i]); b[i] = fma2(make_float2(w.y, w.y), g[1], b[i]);
+                        b[i] = fma2(make_float2(w.z, w.z), g[2], b[i]); b[i] = fma2(make_float2(w.w, w.w), g[3], b[i]);
+                    }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                *reinterpret_cast<float2 *>(red + (part * 4 + i) * width + 2 * pair) = a[i];
+                *reinterpret_cast<float2 *>(red + (part * 4 + i) * width + p.dim + 2 * pair) = b[i];
+            }
+        }
+        soft_barrier(kSoft);
+        for (uint32_t i = tid; i < 4 * width; i += kSoft) {
+            float x = 0.f;
+#pragma unroll
+            for (int y = 0; y < kParts; ++y) x += red[y * 4 * width + i];
+            if (k0 * width + i < (uint32_t)p.sinks * width) out[k0 * width + i] = x;       // sinks that the tile does not have: zeros
+        }
+        soft_barrier(kSoft);
+    }
+    for (uint32_t i = tid + (((uint32_t)sinks + 3u) & ~3u) * width; i < (uint32_t)p.sinks * width; i += kSoft) out[i] = 0.f;
+    if (!bias_out) return;
+    // sums by distance first: key - query runs over sinks + 127 values; then by bucket
+    uint32_t *of = reinterpret_cast<uint32_t *>(red + 256);
+    const int32_t least = s - (t0 + 127), count = sinks + 127;
+    if ((int32_t)tid < count) {
+        float x = 0.f;
+        for (int32_t k = 0; k < sinks; ++k) {
+            const int32_t q = s + k - (least + (int32_t)tid) - t0;   // the query of this key at this distance
+            if (q >= 0 && q < 128) x += sink_d[k * 128 + q];
+        }
+        red[tid] = x;
+        of[tid] = bucket_of(p.b, least + (int32_t)tid);
+    }
+    soft_barrier(kSoft);
+    const uint32_t lane = tid & 31u, buckets = p.b.n * (p.b.two_sided ? 2u : 1u);
+    for (uint32_t b = tid >> 5; b < buckets; b += kSoft / 32) {
+        float x = 0.f;
+        for (int32_t i = (int32_t)lane; i < count; i += 32) if (of[i] == b) x += red[i];
+        x = warp_sum(x);
+        if (lane == 0) bias_out[b] = x;
+    }
+}
+
 template <typename T, int NB, int ROLE>
 __global__ void __launch_bounds__(BackShape<NB>::kThreads, 1)
 attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_y,
@@ -83,7 +161,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
     unsigned char *smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
     const uint32_t ring = smem_addr(smem);
     const unsigned char *own_rows = smem + Sh::kRing;                // the two A sides, and o in role 0, as they land
-    float *lut = reinterpret_cast<float *>(smem + Sh::kRing + (ROLE == 0 ? 3 : 2) * Sh::kOwn);
+    float *lut = reinterpret_cast<float *>(smem + Sh::kRing + 2 * Sh::kOwn + (ROLE == 0 ? max(Sh::kOwn, p.sinks * 1024) : 0));
     const uint32_t entries = bias_entries(p.b);
     float *rel_sums = lut + ((entries + 3u) & ~3u);                  // role 1: [softmax warps][entries]
 
@@ -173,6 +251,8 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
     // tiles of one head: role 0 the run of keys and then the sinks before it, role 1 the queries, on a grid of kRows
     if (ROLE == 1) lo = hi ? lo / Sh::kRows * Sh::kRows : 0;
     const int32_t s_end = ROLE == 0 && hi ? min(s_lo + p.sinks, lo) : 0, extra = ROLE == 0 && hi && s_lo < s_end ? (s_end - s_lo + Sh::kRows - 1) / Sh::kRows : 0;
+    const int32_t sinks = extra ? s_end - s_lo : 0;
+    float *sink_p = reinterpret_cast<float *>(smem + Sh::kRing + 2 * Sh::kOwn), *sink_d = sink_p + sinks * 128;      // [sink][row], where o was
     const int32_t run = hi ? (hi - lo + Sh::kRows - 1) / Sh::kRows : 0, per_head = run + extra;
     const int32_t total = per_head * (int32_t)heads_here;
     auto tile_at = [&](int32_t k) { return ROLE == 0 && k >= run ? s_lo + (k - run) * Sh::kRows : lo + k * Sh::kRows; };
@@ -211,7 +291,13 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                 }
                 tmem_st16(tmem + lanes + (wg == 0 ? Sh::kA0 : Sh::kA1) + g * 16, x);
             }
-            if (!word) delta = 0.f;
+            if (!word) {
+                delta = 0.f;
+                if (ROLE == 0 && p.sinks)                            // the sums for the sinks read the rows again
+#pragma unroll
+                    for (int c = 0; c < NB * 8; ++c)
+                        *reinterpret_cast<uint4 *>(smem + Sh::kRing + wg * Sh::kOwn + (c >> 3) * (128 * 128) + r * 128u + ((c & 7) << 4)) = make_uint4(0, 0, 0, 0);
+            }
             tmem_wait_st();
             tc_fence_before();
             mbar_arrive(&sh.a_full);
@@ -292,6 +378,17 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                             }
                             tmem_st16(cs + c * 16, wp);
                             tmem_st16(cd + c * 16, ws);
+                            if (k >= run) {                          // sinks: kept in fp32 for their own sums
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) {
+                                    const int32_t i = (k - run) * Sh::kRows + c * 32 + e;
+                                    if (i < sinks) {
+                                        const float w = fast_exp2(x[e] - lse);
+                                        sink_p[i * 128 + (int32_t)r] = w;
+                                        sink_d[i * 128 + (int32_t)r] = w * (__uint_as_float(dv[e]) - delta);
+                                    }
+                                }
+                            }
                         } else {
                             float ds[32];
 #pragma unroll
@@ -367,6 +464,14 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
         }
         ok = __all_sync(kFullMask, ok && (total == 0 || mbar_wait(&sh.done, 0, abort_flag)));
         tc_fence_after();
+        if (ROLE == 0 && p.sink_rec) {
+            if (h_own == 0 && tid == 0) p.sink_rec[tile] = !hi ? -1 : s_lo >= t0 ? -2 : sinks ? s_lo : -1;
+            const uint32_t buckets = p.b.n * (p.b.two_sided ? 2u : 1u);
+            float *bias_out = p.dbias ? p.dbias_part + ((size_t)((uint32_t)((p.n + kAttendTile - 1) / kAttendTile) + tile) * p.heads + h_own) * buckets : nullptr;
+            if (sinks) sink_sums<T, NB>(p, own_rows, sink_p, sink_d, sh.eps, reinterpret_cast<float *>(smem + 32 * 1024), sinks, s_lo, t0, wg, r, tid,
+                                        p.sink_part + ((size_t)tile * p.heads + h_own) * p.sinks * 2 * p.dim, bias_out);
+            else if (bias_out) for (uint32_t b = tid; b < buckets; b += Sh::kSoft) bias_out[b] = 0.f;
+        }
         // outputs leave through shared memory: role 0 half of dQ's columns by each warpgroup, role 1 dK and dV by one each
         {
             const float by = ROLE == 0 || wg == 0 ? p.scale : 1.f;
@@ -556,155 +661,48 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
     if (tid == 0 && sh.abort_flag) atomicOr(error, kErrAttend);
 }
 
-// ---- sinks seen from beyond the window -----------------------------------------------------------
-// One block per (query tile, head): the sums over the tile's queries for the sinks before the tile's run of keys.
-// A tile has at most one sentence whose sinks lie there, the one that reaches into it from the left; it is
-// written to sink_rec (-1: the tile has no word, -2: its first word's sentence begins inside the tile).
-constexpr int kSinkBatch = 4;
-template <typename T>
-__global__ void __launch_bounds__(128)
-attend_sink_kernel(AttendParams p, uint32_t part_row0)
+// The first word of a tile that has one.
+__device__ __forceinline__ int64_t first_word(const AttendParams &p, int32_t tile)
 {
-    extern __shared__ float sink_smem[];
-    __shared__ int32_t limits[4][2];
-    __shared__ float kv[kSinkBatch][2][kMaxHeadDim];
-    const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, h = blockIdx.x % p.heads, kvh = h / (p.heads / p.kv_heads);
-    const int32_t tile = (int32_t)(blockIdx.x / p.heads), t0 = tile * kAttendTile;
-    const int64_t i = (int64_t)t0 + tid;
-    const RowLimits row = row_limits(p, i);
-    const bool word = row.hi > row.lo;
-    const int32_t wl = __reduce_min_sync(kFullMask, word ? row.lo : INT32_MAX), ws = __reduce_min_sync(kFullMask, word ? row.s : INT32_MAX);
-    if (lane == 0) { limits[warp][0] = wl; limits[warp][1] = ws; }
-    __syncthreads();
-    const int32_t lo = min(min(limits[0][0], limits[1][0]), min(limits[2][0], limits[3][0]));
-    const int32_t s = min(min(limits[0][1], limits[1][1]), min(limits[2][1], limits[3][1]));
-    const bool any = lo != INT32_MAX;
-    const int32_t ns = any ? max(0, min(s + p.sinks, lo) - s) : 0;
-    if (h == 0 && tid == 0) p.sink_rec[tile] = !any ? -1 : s < t0 ? s : -2;
-    const uint32_t buckets = p.b.n * (p.b.two_sided ? 2u : 1u);
-    float *bias_out = p.dbias ? p.dbias_part + ((size_t)(part_row0 + tile) * p.heads + h) * buckets : nullptr;
-    float *out = p.sink_part + ((size_t)tile * p.heads + h) * p.sinks * 2 * p.dim;
-    for (uint32_t e = tid + (uint32_t)ns * 2 * p.dim; e < (uint32_t)p.sinks * 2 * p.dim; e += 128) out[e] = 0.f;
-    if (ns == 0) {
-        if (bias_out) for (uint32_t b = tid; b < buckets; b += 128) bias_out[b] = 0.f;
-        return;
-    }
-    float *ps = sink_smem, *ds = ps + p.sinks * 128;                  // [sink][query]
-    const T *q = static_cast<const T *>(p.q) + i * (int64_t)p.ldq + (int64_t)h * p.dim;
-    const T *go = static_cast<const T *>(p.d_o) + i * (int64_t)p.ld_do + (int64_t)h * p.dim;
-    const float lse = word ? p.lse[(int64_t)h * p.n + i] : INFINITY, delta = word ? p.delta[(int64_t)h * p.n + i] : 0.f;
-    for (int32_t r0 = 0; r0 < ns; r0 += kSinkBatch) {
-        __syncthreads();
-        for (uint32_t e = tid; e < kSinkBatch * p.dim; e += 128) {
-            const uint32_t r = e / p.dim, c = e - r * p.dim;
-            const int64_t j = (int64_t)s + r0 + r;
-            const bool real = r0 + (int32_t)r < ns && p.spans[j].y > p.spans[j].x;
-            kv[r][0][c] = real ? to_f32(static_cast<const T *>(p.k)[j * (int64_t)p.ldk + (int64_t)kvh * p.dim + c]) : 0.f;
-            kv[r][1][c] = real ? to_f32(static_cast<const T *>(p.v)[j * (int64_t)p.ldv + (int64_t)kvh * p.dim + c]) : 0.f;
-        }
-        __syncthreads();
-        float a[kSinkBatch], b[kSinkBatch];
-#pragma unroll
-        for (int r = 0; r < kSinkBatch; ++r) a[r] = b[r] = 0.f;
-        if (word)
-            for (uint32_t c = 0; c < p.dim; c += 8) {
-                const Pack<T, 8> x = load_pack<T, 8>(q + c), y = load_pack<T, 8>(go + c);
-#pragma unroll
-                for (int r = 0; r < kSinkBatch; ++r)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        a[r] = fmaf(to_f32(x.e[e]), kv[r][0][c + e], a[r]);
-                        b[r] = fmaf(to_f32(y.e[e]), kv[r][1][c + e], b[r]);
-                    }
-            }
-#pragma unroll
-        for (int r = 0; r < kSinkBatch; ++r)
-            if (r0 + r < ns) {
-                const int32_t j = s + r0 + r;
-                const bool seen = word && j >= row.s && j < row.se && p.spans[j].y > p.spans[j].x;
-                float w = 0.f;
-                if (seen) {
-                    const float bias = p.b.n ? log2_bias(p.bias[(size_t)bucket_of(p.b, j - (int32_t)i) * p.heads + h]) : 0.f;
-                    w = fast_exp2(fmaf(a[r], p.scale * kLog2e, bias) - lse);
-                }
-                ps[(r0 + r) * 128 + tid] = w;
-                ds[(r0 + r) * 128 + tid] = seen ? w * (b[r] - delta) : 0.f;
-            }
-    }
-    __syncthreads();
-    // dK and dV of the sinks: one column per thread
-    if (tid < p.dim) {
-        const int32_t rows = (int32_t)min((int64_t)kAttendTile, p.n - t0);
-        for (int32_t r0 = 0; r0 < ns; r0 += kSinkBatch) {
-            float a[kSinkBatch], b[kSinkBatch];
-#pragma unroll
-            for (int r = 0; r < kSinkBatch; ++r) a[r] = b[r] = 0.f;
-            for (int32_t x = 0; x < rows; ++x) {
-                const int64_t at = (int64_t)t0 + x;
-                const bool real = p.spans[at].y > p.spans[at].x;
-                const float qv = real ? to_f32(static_cast<const T *>(p.q)[at * (int64_t)p.ldq + (int64_t)h * p.dim + tid]) : 0.f;
-                const float gv = real ? to_f32(static_cast<const T *>(p.d_o)[at * (int64_t)p.ld_do + (int64_t)h * p.dim + tid]) : 0.f;
-#pragma unroll
-                for (int r = 0; r < kSinkBatch; ++r) {
-                    const int32_t rr = min(r0 + r, ns - 1);
-                    a[r] = fmaf(ds[rr * 128 + x], qv, a[r]);
-                    b[r] = fmaf(ps[rr * 128 + x], gv, b[r]);
-                }
-            }
-#pragma unroll
-            for (int r = 0; r < kSinkBatch; ++r)
-                if (r0 + r < ns) {
-                    out[((r0 + r) * 2) * p.dim + tid] = a[r];
-                    out[((r0 + r) * 2 + 1) * p.dim + tid] = b[r];
-                }
-        }
-    }
-    if (bias_out) {
-        // sums by distance first: key - query runs over ns + 127 values; then by bucket
-        float *rel = ds + p.sinks * 128;                              // [sinks + 128]
-        const int32_t least = s - (t0 + 127), count = ns + 127;
-        __syncthreads();
-        for (int32_t e = (int32_t)tid; e < count; e += 128) {
-            float a = 0.f;
-            for (int32_t r = 0; r < ns; ++r) {
-                const int32_t x = s + r - (least + e) - t0;           // the query of this key at this distance
-                if (x >= 0 && x < 128) a += ds[r * 128 + x];
-            }
-            rel[e] = a;
-        }
-        __syncthreads();
-        for (uint32_t b = warp; b < buckets; b += 4) {
-            float a = 0.f;
-            for (int32_t e = (int32_t)lane; e < count; e += 32)
-                if (bucket_of(p.b, least + e) == b) a += rel[e];
-            a = warp_sum(a);
-            if (lane == 0) bias_out[b] = a;
-        }
-    }
+    int64_t i = (int64_t)tile * kAttendTile;
+    while (i + 1 < p.n && p.spans[i].y <= p.spans[i].x) ++i;
+    return i;
 }
 
 // Slot a holds the sums for the sentence that begins in tile a and reaches into a later one (there is at most one):
-// over its query tiles and the query heads of a key/value head, in a fixed order.
+// over its query tiles and the query heads of a key/value head, in a fixed order, 32 elements per block.
 __global__ void __launch_bounds__(256)
 attend_sink_sum_kernel(AttendParams p, int32_t tiles)
 {
+    __shared__ float part[8][32];
     const int32_t a = (int32_t)(blockIdx.x / p.kv_heads);
-    const uint32_t kvh = blockIdx.x % p.kv_heads, group = p.heads / p.kv_heads;
+    const uint32_t kvh = blockIdx.x % p.kv_heads, group = p.heads / p.kv_heads, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int32_t first = a + 1;
     while (first < tiles && p.sink_rec[first] == -1) ++first;
     const int32_t s = first < tiles ? p.sink_rec[first] : -2;
     const bool here = s >= 0 && s / kAttendTile == a;
-    if (kvh == 0 && threadIdx.x == 0) p.sink_used[a] = here ? s : -1;
+    if (blockIdx.y == 0 && kvh == 0 && threadIdx.x == 0) p.sink_used[a] = here ? s : -1;
     if (!here) return;
-    int32_t end = first;
-    while (end < tiles && (p.sink_rec[end] == s || p.sink_rec[end] == -1)) ++end;
-    const size_t width = (size_t)p.sinks * 2 * p.dim;
-    float *out = p.sink_sum + ((size_t)a * p.kv_heads + kvh) * width;
-    for (size_t e = threadIdx.x; e < width; e += blockDim.x) {
-        float x = 0.f;
-        for (int32_t t = first; t < end; ++t)
-            for (uint32_t g = 0; g < group; ++g) x += p.sink_part[((size_t)t * p.heads + kvh * group + g) * width + e];
-        out[e] = x;
+    // the sentence's last tile is that of its last word; tiles without words in between have nothing
+    const int32_t end = min(tiles, (p.spans[first_word(p, first)].y - 1) / kAttendTile + 1);
+    const size_t width = (size_t)p.sinks * 2 * p.dim, e = (size_t)blockIdx.y * 32 + lane;
+    float x[4] = {0.f, 0.f, 0.f, 0.f};
+    const int32_t items = (end - first) * (int32_t)group;
+    if (e < width)
+        for (int32_t i = (int32_t)warp; i < items; i += 32) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int32_t j = i + u * 8, t = first + j / (int32_t)group;
+                if (j < items && p.sink_rec[t] == s) x[u] += p.sink_part[((size_t)t * p.heads + kvh * group + (uint32_t)j % group) * width + e];
+            }
+        }
+    part[warp][lane] = (x[0] + x[1]) + (x[2] + x[3]);
+    __syncthreads();
+    if (warp == 0 && e < width) {
+        float y = 0.f;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) y += part[w][lane];
+        p.sink_sum[((size_t)a * p.kv_heads + kvh) * width + e] = y;
     }
 }
 
@@ -755,7 +753,7 @@ int launch_role(const AttendParams &p, uint32_t tiles, int *error, cudaStream_t 
     using Sh = BackShape<NB>;
     auto kernel = attend_back_kernel<T, NB, ROLE>;
     const uint32_t entries = bias_entries(p.b);
-    int smem = Sh::kRing + (ROLE == 0 ? 3 : 2) * Sh::kOwn + 1024 + (int)(4 * (((entries + 3u) & ~3u) + (ROLE == 1 ? Sh::kSoft / 32 * entries : 0u)));
+    int smem = Sh::kRing + 2 * Sh::kOwn + (ROLE == 0 ? (p.sinks * 1024 > Sh::kOwn ? p.sinks * 1024 : Sh::kOwn) : 0) + 1024 + (int)(4 * (((entries + 3u) & ~3u) + (ROLE == 1 ? Sh::kSoft / 32 * entries : 0u)));
     if (smem < 116 * 1024) smem = 116 * 1024;     // a second block would only wait for tensor memory
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return -1;
     CUtensorMap x, y, a0, a1, o;
@@ -782,11 +780,8 @@ int launch_back_typed(const AttendParams &p, uint32_t tiles, int *error, cudaStr
     int k = p.dim <= 64 ? launch_role<T, 1, 0>(p, tiles, error, s) : launch_role<T, 2, 0>(p, tiles, error, s);
     if (k < 0) return -1;
     if (far_sinks(p)) {
-        const int smem = (int)sizeof(float) * (2 * 128 * p.sinks + p.sinks + 128);
-        if (cudaFuncSetAttribute(attend_sink_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return -1;
-        attend_sink_kernel<T><<<tiles * p.heads, 128, smem, s>>>(p, tiles);
-        attend_sink_sum_kernel<<<tiles * p.kv_heads, 256, 0, s>>>(p, (int32_t)tiles);
-        k += 2;
+        attend_sink_sum_kernel<<<dim3(tiles * p.kv_heads, (2 * (uint32_t)p.sinks * p.dim + 31) / 32), 256, 0, s>>>(p, (int32_t)tiles);
+        ++k;
     }
     const int j = p.dim <= 64 ? launch_role<T, 1, 1>(p, tiles, error, s) : launch_role<T, 2, 1>(p, tiles, error, s);
     return j < 0 ? -1 : k + j;
