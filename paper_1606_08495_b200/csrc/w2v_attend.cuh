@@ -74,19 +74,14 @@ __device__ __forceinline__ void bucket_range(const BucketStarts &s, uint32_t b, 
 }
 
 // The table of a head by `warps` warps (this one is number `warp`).  A lane takes one distance and counts the buckets
-// that start at or before it, a bucket's start per shuffle; the entries beyond the last start are the last bucket's.
+// that start at or before it; the entries beyond the last start are the last bucket's.
 __device__ __forceinline__ void fill_bias(const AttendParams &p, uint32_t h, float *lut, uint32_t warp, uint32_t warps, uint32_t lane)
 {
     const int32_t last = bias_last(p.b), off = last + kBiasPad;
     const uint32_t n = p.b.n, buckets = n * (p.b.two_sided ? 2u : 1u);
     float v[2];
-    int32_t start[2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const uint32_t b = lane + 32u * i;
-        v[i] = b < buckets ? __ldg(p.bias + (size_t)b * p.heads + h) : 0.f;
-        start[i] = b < n ? p.b.start[b] : INT32_MAX;
-    }
+    for (int i = 0; i < 2; ++i) v[i] = lane + 32u * i < buckets ? __ldg(p.bias + (size_t)(lane + 32 * i) * p.heads + h) : 0.f;
     v[0] = log2_bias(v[0]);
     v[1] = log2_bias(v[1]);
     auto value = [&](uint32_t b) {                                   // every lane its own bucket
@@ -96,9 +91,8 @@ __device__ __forceinline__ void fill_bias(const AttendParams &p, uint32_t h, flo
     for (int32_t d0 = (int32_t)warp * 32; d0 <= last; d0 += (int32_t)warps * 32) {
         const int32_t d = d0 + (int32_t)lane;
         uint32_t b = 0;
-#pragma unroll 4
-        for (uint32_t k = 1; k < min(n, 32u); ++k) b += __shfl_sync(kFullMask, start[0], k) <= d ? 1u : 0u;
-        for (uint32_t k = 32; k < n; ++k) b += __shfl_sync(kFullMask, start[1], k & 31u) <= d ? 1u : 0u;
+#pragma unroll 8
+        for (uint32_t k = 1; k < n; ++k) b += p.b.start[k] <= d ? 1u : 0u;
         const float x = value(b), y = value(p.b.two_sided ? b + n : 0u);
         if (d <= last) {
             if (d > 0) lut[off + d] = y;

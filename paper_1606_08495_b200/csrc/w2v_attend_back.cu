@@ -18,29 +18,40 @@
 
 namespace w2v {
 
-template <int NB>
+// Two layouts of a block.
+//   SMALL (heads of up to 96): 256 columns of tensor memory and half of the shared memory, so that two blocks share an SM
+//          and one's beginning and end lie under the other's middle; one softmax warpgroup; the A sides stay in shared
+//          memory; tiles of 32 rows.
+//   else:  all of the tensor memory; two softmax warpgroups that take the tiles in turn; the A sides in tensor memory
+//          (heads of up to 64: tiles of 64 rows).
+template <int NB, bool SMALL>
 struct BackShape {
-    static constexpr int kBuf = 2;                                   // score buffers, each with a warpgroup of its own
-    static constexpr int kRows = NB == 2 ? 32 : 64;                  // streamed rows per tile
-    static constexpr int kStages = 4;
-    static constexpr uint32_t kA0 = 0, kA1 = NB * 32, kG0 = NB * 64, kG1 = NB * 128;     // tensor-memory columns
-    static constexpr uint32_t kScores = NB * 192, kAlloc = 512;
+    static constexpr int kWg = SMALL ? 1 : 2;                        // softmax warpgroups
+    static constexpr int kBuf = SMALL && NB == 2 ? 1 : 2;            // score buffers
+    static constexpr int kRows = SMALL || NB == 2 ? 32 : 64;         // streamed rows per tile
+    static constexpr int kStages = SMALL && NB == 2 ? 2 : 4;
+    static constexpr uint32_t kWide = !SMALL ? NB * 64 : NB == 1 ? 64 : 96;              // columns of a gradient
+    static constexpr uint32_t kA0 = 0, kA1 = NB * 32, kG0 = SMALL ? 0 : NB * 64, kG1 = kG0 + kWide;      // tensor-memory columns
+    static constexpr uint32_t kScores = kG1 + kWide, kAlloc = SMALL ? 256 : 512;
     static_assert(kScores + kBuf * 2 * kRows <= kAlloc, "tensor memory");
     static constexpr int kOperand = NB * kRows * 128, kStage = 2 * kOperand, kRing = kStages * kStage;
     static constexpr int kOwn = NB * 128 * 128;                      // bytes of one operand of the block's own rows
-    static constexpr int kSoft = 128 * kBuf, kThreads = kSoft + 128;
-    static_assert(kRing >= 2 * kOwn, "the outputs are staged where the ring was");
+    static constexpr int kSoft = 128 * kWg, kThreads = kSoft + 128, kBlocks = 512 / (int)kAlloc;
+    static_assert(kRing + 2 * kOwn >= 2 * NB * 128 * 128, "the outputs are staged where the ring and the own rows were");
 };
+// SMALL: of the 128 registers a thread has at launch, the helpers give all beyond 56 to the softmax (200 + 56 = 2 x 128).
+constexpr int kBackLaunchRegs = 128, kBackSoftRegs = 200, kBackOtherRegs = 56;
 
+template <typename Sh>
 struct BackShared {
-    uint64_t own_landed, a_full, landed[4], full[4], empty[4], s_full[2], p_full[2], done;
+    uint64_t own_landed, own_full, landed[Sh::kStages], full[Sh::kStages], empty[Sh::kStages], s_full[2], p_full[2], done;
     uint32_t tmem;
     int abort_flag, quiet;
     int32_t limits[4][3];
-    uint32_t vis[4][2];                              // role 0: which keys of the stage are words
-    int32_t run_lo[4];                               // role 1: where the run of the stage's query tile begins
-    __align__(16) float lse[4][64], delta[4][64];    // role 1: of the stage's queries, negated
-    float eps[2][128];
+    uint32_t vis[Sh::kStages][2];                    // role 0: which keys of the stage are words
+    int32_t run_lo[Sh::kStages];                     // role 1: where the run of the stage's query tile begins
+    __align__(16) float lse[Sh::kStages][Sh::kRows], delta[Sh::kStages][Sh::kRows];      // role 1: of the stage's queries, negated
+    float eps[Sh::kWg][128];
     float far_sum[8][2];
 };
 
@@ -71,16 +82,15 @@ __device__ __forceinline__ void write_bucket_sums(const AttendParams &p, const f
 }
 
 // What this block's queries add to the sinks before its run: dK (before the scale) and dV of each, and the bias' sums,
-// by the 256 softmax threads.  sink_d holds dS for the first delta, which eps puts right.  A thread takes two columns
-// and every 8th or 4th part of the rows, four sinks at a time; `red` is 16 KB for joining the parts.
-template <typename T, int NB>
+// by the softmax threads.  sink_d holds dS for the first delta, which eps puts right.  A thread takes two columns
+// and a part of the rows, four sinks at a time; `red` is 16 KB for joining the parts.
+template <typename T, int NB, int kSoft>
 __device__ __forceinline__ void sink_sums(const AttendParams &p, const unsigned char *own_rows, const float *sink_p, float *sink_d,
-                                       const float (*eps)[128], float *red, int32_t sinks, int32_t s, int32_t t0, uint32_t wg, uint32_t r,
+                                       float eps, float *red, int32_t sinks, int32_t s, int32_t t0, uint32_t wg, uint32_t r,
                                        uint32_t tid, float *out, float *bias_out)
 {
-    constexpr int kSoft = 256, kPairs = 32 * NB, kParts = kSoft / kPairs, kPartRows = 128 / kParts, kOwn = NB * 128 * 128;
-    const float e = eps[0][r] + eps[1][r];
-    for (int32_t k = (int32_t)wg; k < sinks; k += 2) sink_d[k * 128 + (int32_t)r] -= e * sink_p[k * 128 + (int32_t)r];
+    constexpr int kPairs = 32 * NB, kParts = kSoft / kPairs, kPartRows = 128 / kParts, kOwn = NB * 128 * 128;
+    for (int32_t k = (int32_t)wg; k < sinks; k += kSoft / 128) sink_d[k * 128 + (int32_t)r] -= eps * sink_p[k * 128 + (int32_t)r];
     soft_barrier(kSoft);
     const uint32_t pair = tid % kPairs, part = tid / kPairs, width = 2 * p.dim;
     for (int32_t k0 = 0; k0 < sinks; k0 += 4) {
@@ -128,14 +138,14 @@ __device__ __forceinline__ void sink_sums(const AttendParams &p, const unsigned 
     // sums by distance first: key - query runs over sinks + 127 values; then by bucket
     uint32_t *of = reinterpret_cast<uint32_t *>(red + 256);
     const int32_t least = s - (t0 + 127), count = sinks + 127;
-    if ((int32_t)tid < count) {
+    for (int32_t i = (int32_t)tid; i < count; i += kSoft) {
         float x = 0.f;
         for (int32_t k = 0; k < sinks; ++k) {
-            const int32_t q = s + k - (least + (int32_t)tid) - t0;   // the query of this key at this distance
+            const int32_t q = s + k - (least + i) - t0;              // the query of this key at this distance
             if (q >= 0 && q < 128) x += sink_d[k * 128 + q];
         }
-        red[tid] = x;
-        of[tid] = bucket_of(p.b, least + (int32_t)tid);
+        red[i] = x;
+        of[i] = bucket_of(p.b, least + i);
     }
     soft_barrier(kSoft);
     const uint32_t lane = tid & 31u, buckets = p.b.n * (p.b.two_sided ? 2u : 1u);
@@ -147,21 +157,21 @@ __device__ __forceinline__ void sink_sums(const AttendParams &p, const unsigned 
     }
 }
 
-template <typename T, int NB, int ROLE>
-__global__ void __launch_bounds__(BackShape<NB>::kThreads, 1)
+template <typename T, int NB, int ROLE, bool SMALL>
+__global__ void __launch_bounds__(BackShape<NB, SMALL>::kThreads, BackShape<NB, SMALL>::kBlocks)
 attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_y,
                    const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ CUtensorMap map_a1,
                    const __grid_constant__ CUtensorMap map_o, AttendParams p, int *error)
 {
-    using Sh = BackShape<NB>;
+    using Sh = BackShape<NB, SMALL>;
     constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
     constexpr int kChunks = Sh::kRows / 32;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ BackShared sh;
+    __shared__ BackShared<Sh> sh;
     unsigned char *smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
     const uint32_t ring = smem_addr(smem);
-    const unsigned char *own_rows = smem + Sh::kRing;                // the two A sides, and o in role 0, as they land
-    float *lut = reinterpret_cast<float *>(smem + Sh::kRing + 2 * Sh::kOwn + (ROLE == 0 ? max(Sh::kOwn, p.sinks * 1024) : 0));
+    const unsigned char *own_rows = smem + Sh::kRing;                // the two A sides, and o in role 0 (not SMALL), as they land
+    float *lut = reinterpret_cast<float *>(smem + Sh::kRing + 2 * Sh::kOwn + (ROLE == 0 ? max(SMALL ? 0 : Sh::kOwn, p.sinks * 1024) : 0));
     const uint32_t entries = bias_entries(p.b);
     float *rel_sums = lut + ((entries + 3u) & ~3u);                  // role 1: [softmax warps][entries]
 
@@ -175,20 +185,20 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
 
     if (warp == kMmaWarp + 1 && lane == 0) {
         mbar_init(&sh.own_landed, 1);
-        mbar_init(&sh.a_full, 256);
+        mbar_init(&sh.own_full, SMALL ? 64 : 256);
         for (int i = 0; i < Sh::kStages; ++i) { mbar_init(&sh.landed[i], 1); mbar_init(&sh.full[i], 32); mbar_init(&sh.empty[i], 1 + 128); }
         for (int i = 0; i < 2; ++i) { mbar_init(&sh.s_full[i], 1); mbar_init(&sh.p_full[i], 128); }
         mbar_init(&sh.done, 1);
         sh.abort_flag = sh.quiet = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_proxy();
-        mbar_expect(&sh.own_landed, (ROLE == 0 ? 3 : 2) * Sh::kOwn);
+        mbar_expect(&sh.own_landed, (ROLE == 0 && !SMALL ? 3 : 2) * Sh::kOwn);
 #pragma unroll
         for (int c = 0; c < NB; ++c) {
             const uint32_t to = ring + Sh::kRing + c * (128 * 128);
             copy_box(to, &map_a0, c * 64, (int32_t)h_own, t0, &sh.own_landed);
             copy_box(to + Sh::kOwn, &map_a1, c * 64, (int32_t)h_own, t0, &sh.own_landed);
-            if (ROLE == 0) copy_box(to + 2 * Sh::kOwn, &map_o, c * 64, (int32_t)h_own, t0, &sh.own_landed);
+            if (ROLE == 0 && !SMALL) copy_box(to + 2 * Sh::kOwn, &map_o, c * 64, (int32_t)h_own, t0, &sh.own_landed);
         }
     }
     const uint32_t r = tid & 127u;                                   // this thread's row (softmax warps)
@@ -228,10 +238,21 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&sh.tmem)), "r"(Sh::kAlloc));
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
+    uint32_t own_words[4];
+    if (SMALL && warp >= kMmaWarp + 2) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const int64_t i = (int64_t)t0 + w * 32 + lane;
+            const int2 sp = i < p.n ? __ldg(p.spans + i) : make_int2(0, 0);
+            own_words[w] = __ballot_sync(kFullMask, sp.y > sp.x);
+        }
+    }
+    // the table by warps that have nothing else to begin with, the zeros by the others
     if (p.b.n) {
-        fill_bias(p, h0, lut, warp, Sh::kThreads / 32, lane);
-        if (ROLE == 1)
-            for (uint32_t e = tid; e < kSoftWarps * entries; e += Sh::kThreads) rel_sums[e] = 0.f;
+        if (!SMALL && warp >= 4 && warp < 8) fill_bias(p, h0, lut, warp - 4, 4, lane);
+        if (SMALL && warp >= kMmaWarp + 2) fill_bias(p, h0, lut, warp - kMmaWarp - 2, 2, lane);
+        if (ROLE == 1 && warp < 4)
+            for (uint32_t e = tid; e < kSoftWarps * entries; e += 128) rel_sums[e] = 0.f;
     }
     tc_fence_before();
     __syncthreads();
@@ -252,7 +273,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
     if (ROLE == 1) lo = hi ? lo / Sh::kRows * Sh::kRows : 0;
     const int32_t s_end = ROLE == 0 && hi ? min(s_lo + p.sinks, lo) : 0, extra = ROLE == 0 && hi && s_lo < s_end ? (s_end - s_lo + Sh::kRows - 1) / Sh::kRows : 0;
     const int32_t sinks = extra ? s_end - s_lo : 0;
-    float *sink_p = reinterpret_cast<float *>(smem + Sh::kRing + 2 * Sh::kOwn), *sink_d = sink_p + sinks * 128;      // [sink][row], where o was
+    float *sink_p = reinterpret_cast<float *>(smem + Sh::kRing + 2 * Sh::kOwn), *sink_d = sink_p + sinks * 128;      // [sink][row]; where o was, if it was
     const int32_t run = hi ? (hi - lo + Sh::kRows - 1) / Sh::kRows : 0, per_head = run + extra;
     const int32_t total = per_head * (int32_t)heads_here;
     auto tile_at = [&](int32_t k) { return ROLE == 0 && k >= run ? s_lo + (k - run) * Sh::kRows : lo + k * Sh::kRows; };
@@ -260,6 +281,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
 
     if (warp < kSoftWarps) {
         // ============ softmax warpgroups ============
+        if (SMALL) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kBackSoftRegs));
         const uint32_t wg = tid >> 7, lanes = ((warp & 3u) * 32u) << 16;
         const float scale = p.scale * kLog2e;
         const int32_t last = bias_last(p.b), off = last + kBiasPad;
@@ -267,40 +289,48 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
         const bool word = ROLE == 0 ? row.hi > row.lo : q_hi > q_lo;
         float lse = INFINITY, delta = 0.f;
         if (ROLE == 0 && word) lse = __ldg(p.lse + (int64_t)h_own * p.n + own);
-        // the two operands of the block's rows go to tensor memory (a warpgroup each), zeros for rows that are not words
         bool ok = __all_sync(kFullMask, mbar_wait(&sh.own_landed, 0, abort_flag));
         {
             auto chunk = [&](int operand, int c) {                   // 8 columns of this thread's row, from the 128-byte swizzle
                 return *reinterpret_cast<const uint4 *>(own_rows + operand * Sh::kOwn + (c >> 3) * (128 * 128) + r * 128u + (((c & 7) ^ (r & 7u)) << 4));
             };
+            auto first_delta = [&](uint4 d4, uint4 o4) {
+                const Pack<T, 8> dd = reinterpret_cast<const Pack<T, 8> &>(d4), oo = reinterpret_cast<const Pack<T, 8> &>(o4);
 #pragma unroll
-            for (int g = 0; g < NB * 2; ++g) {
-                uint32_t x[16];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const int at = g * 4 + c;
-                    uint4 u = chunk((int)wg, at);
-                    if (!word) u = make_uint4(0, 0, 0, 0);
-                    if (ROLE == 0) {                                 // both warpgroups need the first delta
-                        const uint4 d4 = chunk(1, at), o4 = chunk(2, at);
-                        const Pack<T, 8> dd = reinterpret_cast<const Pack<T, 8> &>(d4), oo = reinterpret_cast<const Pack<T, 8> &>(o4);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) delta = fmaf(to_f32(oo.e[e]), to_f32(dd.e[e]), delta);
-                    }
-                    x[c * 4] = u.x; x[c * 4 + 1] = u.y; x[c * 4 + 2] = u.z; x[c * 4 + 3] = u.w;
-                }
-                tmem_st16(tmem + lanes + (wg == 0 ? Sh::kA0 : Sh::kA1) + g * 16, x);
-            }
-            if (!word) {
-                delta = 0.f;
-                if (ROLE == 0 && p.sinks)                            // the sums for the sinks read the rows again
+                for (int e = 0; e < 8; ++e) delta = fmaf(to_f32(oo.e[e]), to_f32(dd.e[e]), delta);
+            };
+            if (SMALL) {
+                const uint4 *o = reinterpret_cast<const uint4 *>(static_cast<const T *>(p.o) + own * (int64_t)p.ldo + (int64_t)h_own * p.dim);
+                if (ROLE == 0 && word)
 #pragma unroll
                     for (int c = 0; c < NB * 8; ++c)
-                        *reinterpret_cast<uint4 *>(smem + Sh::kRing + wg * Sh::kOwn + (c >> 3) * (128 * 128) + r * 128u + ((c & 7) << 4)) = make_uint4(0, 0, 0, 0);
+                        if ((uint32_t)c * 8 < p.dim) first_delta(chunk(1, c), __ldg(o + c));
+            } else {
+                // the two operands of the block's rows go to tensor memory (a warpgroup each), zeros for rows that are not words
+#pragma unroll
+                for (int g = 0; g < NB * 2; ++g) {
+                    uint32_t x[16];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const int at = g * 4 + c;
+                        uint4 u = chunk((int)wg, at);
+                        if (!word) u = make_uint4(0, 0, 0, 0);
+                        if (ROLE == 0) first_delta(chunk(1, at), chunk(2, at));      // both warpgroups need it
+                        x[c * 4] = u.x; x[c * 4 + 1] = u.y; x[c * 4 + 2] = u.z; x[c * 4 + 3] = u.w;
+                    }
+                    tmem_st16(tmem + lanes + (wg == 0 ? Sh::kA0 : Sh::kA1) + g * 16, x);
+                }
+                if (!word) {
+                    delta = 0.f;
+                    if (ROLE == 0 && p.sinks)                        // the sums for the sinks read the rows again
+#pragma unroll
+                        for (int c = 0; c < NB * 8; ++c)
+                            *reinterpret_cast<uint4 *>(smem + Sh::kRing + wg * Sh::kOwn + (c >> 3) * (128 * 128) + r * 128u + ((c & 7) << 4)) = make_uint4(0, 0, 0, 0);
+                }
+                tmem_wait_st();
+                tc_fence_before();
+                mbar_arrive(&sh.own_full);
             }
-            tmem_wait_st();
-            tc_fence_before();
-            mbar_arrive(&sh.a_full);
         }
         float2 eps2 = make_float2(0.f, 0.f);
         for (uint32_t g = 0; g < heads_here; ++g) {
@@ -314,7 +344,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
             for (int32_t k = 0; k < per_head && ok; ++k) {
                 const int32_t t = (int32_t)g * per_head + k;
                 const uint32_t b = t % Sh::kBuf, stage = t % Sh::kStages;
-                if (b != wg) continue;
+                if (Sh::kWg == 2 && b != wg) continue;
                 const int32_t at0 = tile_at(k), cols = (tile_rows(k) + 15) & ~15;
                 ok = __all_sync(kFullMask, mbar_wait(&sh.full[stage], (t / Sh::kStages) & 1, abort_flag) &&
                                                mbar_wait(&sh.s_full[b], (t / Sh::kBuf) & 1, abort_flag));
@@ -457,9 +487,12 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
         }
         float eps = 0.f;
         if (ROLE == 0) {
-            sh.eps[wg][r] = eps2.x + eps2.y;
-            soft_barrier(Sh::kSoft);
-            eps = sh.eps[0][r] + sh.eps[1][r];
+            eps = eps2.x + eps2.y;
+            if (Sh::kWg == 2) {
+                sh.eps[wg][r] = eps;
+                soft_barrier(Sh::kSoft);
+                eps = sh.eps[0][r] + sh.eps[Sh::kWg - 1][r];
+            }
             if (wg == 0 && own < p.n) p.delta[(int64_t)h_own * p.n + own] = word ? delta + eps : 0.f;
         }
         ok = __all_sync(kFullMask, ok && (total == 0 || mbar_wait(&sh.done, 0, abort_flag)));
@@ -468,27 +501,32 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
             if (h_own == 0 && tid == 0) p.sink_rec[tile] = !hi ? -1 : s_lo >= t0 ? -2 : sinks ? s_lo : -1;
             const uint32_t buckets = p.b.n * (p.b.two_sided ? 2u : 1u);
             float *bias_out = p.dbias ? p.dbias_part + ((size_t)((uint32_t)((p.n + kAttendTile - 1) / kAttendTile) + tile) * p.heads + h_own) * buckets : nullptr;
-            if (sinks) sink_sums<T, NB>(p, own_rows, sink_p, sink_d, sh.eps, reinterpret_cast<float *>(smem + 32 * 1024), sinks, s_lo, t0, wg, r, tid,
-                                        p.sink_part + ((size_t)tile * p.heads + h_own) * p.sinks * 2 * p.dim, bias_out);
+            if (sinks) sink_sums<T, NB, Sh::kSoft>(p, own_rows, sink_p, sink_d, eps, reinterpret_cast<float *>(smem), sinks, s_lo, t0, wg, r, tid,
+                                                   p.sink_part + ((size_t)tile * p.heads + h_own) * p.sinks * 2 * p.dim, bias_out);
             else if (bias_out) for (uint32_t b = tid; b < buckets; b += Sh::kSoft) bias_out[b] = 0.f;
+            soft_barrier(Sh::kSoft);
         }
-        // outputs leave through shared memory: role 0 half of dQ's columns by each warpgroup, role 1 dK and dV by one each
-        {
-            const float by = ROLE == 0 || wg == 0 ? p.scale : 1.f;
+        // outputs leave through shared memory: dQ (with two warpgroups, half of its columns by each), or dK and dV (by one each)
+        constexpr int kTurns = ROLE == 1 && Sh::kWg == 1 ? 2 : 1;
+#pragma unroll
+        for (int turn_of = 0; turn_of < kTurns; ++turn_of) {
+            constexpr bool kHalf = ROLE == 0 && Sh::kWg == 2;
+            const uint32_t which = ROLE == 0 ? 0u : Sh::kWg == 2 ? wg : (uint32_t)turn_of;       // 0: dQ or dK, 1: dV
+            const float by = which == 0 ? p.scale : 1.f;
             const float *sink = nullptr;
             if (ROLE == 1 && p.sink_used && word && own - sent < p.sinks && p.sink_used[sent / kAttendTile] == sent)
-                sink = p.sink_sum + ((((size_t)(sent / kAttendTile) * p.kv_heads + kvh) * p.sinks + (size_t)(own - sent)) * 2 + wg) * p.dim;
-            const uint32_t row_bytes = p.dim * 2u, chunks = p.dim >> 3, turn = lane % chunks, part = (ROLE == 0 ? warp & 3u : warp) * 32u;
+                sink = p.sink_sum + ((((size_t)(sent / kAttendTile) * p.kv_heads + kvh) * p.sinks + (size_t)(own - sent)) * 2 + which) * p.dim;
+            const uint32_t row_bytes = p.dim * 2u, chunks = p.dim >> 3, turn = lane % chunks, part = ((warp & 3u) + which * 4u) * 32u;
             unsigned char *mine = smem + part * row_bytes, *line = mine + lane * row_bytes;
-            constexpr int kCols = ROLE == 0 ? NB * 2 : NB * 4;       // steps of 16 columns
+            constexpr int kCols = kHalf ? NB * 2 : NB * 4;           // steps of 16 columns
 #pragma unroll
             for (int i = 0; i < kCols; ++i) {
-                const uint32_t c = ROLE == 0 ? i * 32 + wg * 16 : i * 16;
+                const uint32_t c = kHalf ? i * 32 + wg * 16 : i * 16;
                 if (c >= dim16) break;
                 float f[16];
                 if (total) {
                     uint32_t o[16];
-                    tmem_ld16(tmem + lanes + (ROLE == 0 || wg == 0 ? Sh::kG0 : Sh::kG1) + c, o);
+                    tmem_ld16(tmem + lanes + (which == 0 ? Sh::kG0 : Sh::kG1) + c, o);
                     if (ROLE == 0) {                                 // the correction of the first delta
                         uint32_t pk[16];
                         tmem_ld16(tmem + lanes + Sh::kG1 + c, pk);
@@ -520,9 +558,9 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                     }
             }
             const int32_t rows = (int32_t)min((int64_t)32, p.n - (int64_t)w0);
-            const uint64_t ld = ROLE == 0 ? p.ld_dq : wg == 0 ? p.ld_dk : p.ld_dv;
-            char *out = static_cast<char *>(ROLE == 0 ? p.dq : wg == 0 ? p.dk : p.dv) + ((uint64_t)w0 * ld + (uint64_t)h_own * p.dim) * 2u;
-            if (ROLE == 0) {
+            const uint64_t ld = ROLE == 0 ? p.ld_dq : which == 0 ? p.ld_dk : p.ld_dv;
+            char *out = static_cast<char *>(ROLE == 0 ? p.dq : which == 0 ? p.dk : p.dv) + ((uint64_t)w0 * ld + (uint64_t)h_own * p.dim) * 2u;
+            if (kHalf) {
                 asm volatile("bar.sync %0, 64;" ::"r"(2u + (warp & 3u)) : "memory");    // the two warps of these rows
                 store_rows(out, ld * 2u, mine, chunks, rows, wg * 32u + lane, 64u);
             } else {
@@ -533,6 +571,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
         tc_fence_before();
     } else if (warp == kMmaWarp) {
         // ============ MMA issue: one lane ============
+        if (SMALL) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kBackOtherRegs));
         // everything that does not change is formed once, in a warp that stays together: the block waits for it when its
         // code is long
         if (total) {
@@ -542,14 +581,21 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
             // the streamed operands with columns as the summed side (scores) and with rows as the summed side (gradients)
             const uint32_t xs = umma_desc_low(ring, 0), ys = umma_desc_low(ring + Sh::kOperand, 0);
             const uint32_t xg = umma_desc_low(ring, kBlock), yg = umma_desc_low(ring + (ROLE == 0 ? 0 : Sh::kOperand), kBlock);
+            const uint32_t own_low = umma_desc_low(ring + Sh::kRing, 0);
             auto scores = [&](uint32_t b, uint32_t stage) {
                 const uint32_t x = xs + stage * kStep, y = ys + stage * kStep, d = tmem + Sh::kScores + b * 2 * Sh::kRows;
 #pragma unroll
                 for (int c = 0; c < NB * 4; ++c)
                     if ((uint32_t)c * 16 < dim16) {
                         const uint32_t at = (c >> 2) * (kBlock >> 4) + (c & 3) * 2;
-                        umma_f16_ts(d, tmem + Sh::kA0 + c * 8, x + at, idesc_s, c > 0);
-                        umma_f16_ts(d + Sh::kRows, tmem + Sh::kA1 + c * 8, y + at, idesc_s, c > 0);
+                        if (SMALL) {
+                            const uint32_t a_at = (c >> 2) * (128 * 128 >> 4) + (c & 3) * 2;
+                            umma_f16_ss(d, own_low + a_at, x + at, idesc_s, c > 0);
+                            umma_f16_ss(d + Sh::kRows, own_low + (Sh::kOwn >> 4) + a_at, y + at, idesc_s, c > 0);
+                        } else {
+                            umma_f16_ts(d, tmem + Sh::kA0 + c * 8, x + at, idesc_s, c > 0);
+                            umma_f16_ts(d + Sh::kRows, tmem + Sh::kA1 + c * 8, y + at, idesc_s, c > 0);
+                        }
                     }
                 umma_commit(&sh.s_full[b]);
             };
@@ -558,7 +604,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                 tc_fence_after();
                 return got;
             };
-            bool ok = wait(&sh.a_full, 0);
+            bool ok = wait(&sh.own_full, 0);
             uint32_t ahead = 0, ahead_phase = 0, stage = 0;          // stage and phase of the next scores, two tiles ahead of the gradients
             for (int32_t t = 0; t < Sh::kBuf && t < total && ok; ++t) {
                 ok = wait(&sh.full[ahead], 0);
@@ -597,6 +643,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
         __syncwarp();
     } else if (warp == kMmaWarp + 1) {
         // ============ copies: one lane ============
+        if (SMALL) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kBackOtherRegs));
         if (lane == 0) {
             int32_t t = 0;
             for (; t < total; ++t) {
@@ -617,6 +664,17 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
         __syncwarp();
     } else {
         // ============ rows that are not words, and what goes with the rows: a warp per tile, in turn ============
+        if (SMALL) {
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kBackOtherRegs));
+            // the block's own rows: one operand each
+            if (__all_sync(kFullMask, mbar_wait(&sh.own_landed, 0, abort_flag))) {
+                const uint32_t a = ring + Sh::kRing + (warp - kMmaWarp - 2) * Sh::kOwn, top[2] = {own_words[0], own_words[1]}, low[2] = {own_words[2], own_words[3]};
+                zero_rows<NB>(a, 128 * 128, 64, top, lane);
+                zero_rows<NB>(a + 64 * 128, 128 * 128, 64, low, lane);
+                fence_async_proxy();
+                mbar_arrive(&sh.own_full);
+            }
+        }
         for (int32_t t = (int32_t)(warp - kMmaWarp) - 2; t < total; t += 2) {
             const uint32_t stage = t % Sh::kStages, h = h0 + (uint32_t)(t / per_head);
             const int32_t k = t % per_head, at = tile_at(k), rows = tile_rows(k);
@@ -747,14 +805,21 @@ BackWs back_ws(const AttendParams &p, bool want_dbias)
     return w;
 }
 
-template <typename T, int NB, int ROLE>
+template <typename T, int NB, int ROLE, bool SMALL>
 int launch_role(const AttendParams &p, uint32_t tiles, int *error, cudaStream_t s)
 {
-    using Sh = BackShape<NB>;
-    auto kernel = attend_back_kernel<T, NB, ROLE>;
+    using Sh = BackShape<NB, SMALL>;
+    auto kernel = attend_back_kernel<T, NB, ROLE, SMALL>;
     const uint32_t entries = bias_entries(p.b);
-    int smem = Sh::kRing + 2 * Sh::kOwn + (ROLE == 0 ? (p.sinks * 1024 > Sh::kOwn ? p.sinks * 1024 : Sh::kOwn) : 0) + 1024 + (int)(4 * (((entries + 3u) & ~3u) + (ROLE == 1 ? Sh::kSoft / 32 * entries : 0u)));
-    if (smem < 116 * 1024) smem = 116 * 1024;     // a second block would only wait for tensor memory
+    const int o_bytes = SMALL ? 0 : Sh::kOwn, sink_bytes = p.sinks * 1024;
+    int smem = Sh::kRing + 2 * Sh::kOwn + (ROLE == 0 ? (sink_bytes > o_bytes ? sink_bytes : o_bytes) : 0) + 1024 +
+               (int)(4 * (((entries + 3u) & ~3u) + (ROLE == 1 ? Sh::kSoft / 32 * entries : 0u)));
+    if (!SMALL && smem < 116 * 1024) smem = 116 * 1024;              // a second block would only wait for tensor memory
+    if (SMALL) {
+        // a block launched with fewer registers could never hand out the softmax's share
+        cudaFuncAttributes at;
+        if (cudaFuncGetAttributes(&at, kernel) != cudaSuccess || at.numRegs < kBackLaunchRegs) return -1;
+    }
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return -1;
     CUtensorMap x, y, a0, a1, o;
     const bool bf16 = std::is_same<T, __nv_bfloat16>::value;
@@ -777,13 +842,18 @@ int launch_role(const AttendParams &p, uint32_t tiles, int *error, cudaStream_t 
 template <typename T>
 int launch_back_typed(const AttendParams &p, uint32_t tiles, int *error, cudaStream_t s)
 {
-    int k = p.dim <= 64 ? launch_role<T, 1, 0>(p, tiles, error, s) : launch_role<T, 2, 0>(p, tiles, error, s);
+    auto role = [&](auto which) {
+        constexpr int R = decltype(which)::value;
+        return p.dim <= 64 ? launch_role<T, 1, R, true>(p, tiles, error, s)
+               : p.dim <= 96 ? launch_role<T, 2, R, true>(p, tiles, error, s) : launch_role<T, 2, R, false>(p, tiles, error, s);
+    };
+    int k = role(std::integral_constant<int, 0>());
     if (k < 0) return -1;
     if (far_sinks(p)) {
         attend_sink_sum_kernel<<<dim3(tiles * p.kv_heads, (2 * (uint32_t)p.sinks * p.dim + 31) / 32), 256, 0, s>>>(p, (int32_t)tiles);
         ++k;
     }
-    const int j = p.dim <= 64 ? launch_role<T, 1, 1>(p, tiles, error, s) : launch_role<T, 2, 1>(p, tiles, error, s);
+    const int j = role(std::integral_constant<int, 1>());
     return j < 0 ? -1 : k + j;
 }
 
