@@ -16,22 +16,26 @@
 
 namespace w2v {
 
-constexpr int kFwdRows = 64;                     // keys per tile
 constexpr int kFwdThreads = 384;                 // warps 0-7: two softmax warpgroups; warp 8: MMA; warp 9: copies; warps 10-11: rows that are not words
-// Heads of at most 64: of the 80 registers a thread has at launch with two blocks per SM, the third warpgroup gives
+// Of the 80 registers a thread has at launch with two blocks per SM, the third warpgroup gives
 // its share beyond 48 to the two of the softmax (96 + 96 + 48 = 3 x 80).
 constexpr int kLaunchRegs = 80, kSoftmaxRegs = 96, kOtherRegs = 48;
 constexpr float kRescale = 8.f;                  // base-2: how far a row's scores may outgrow its reference before the output is rescaled
 
-// NB = 64-column blocks of a head (1: head_dim <= 64, 2: up to 128).
-template <int NB>
+// NB = 64-column blocks of a head (1: head_dim <= 64, 2: up to 128).  SMALL (up to 96): half of the tensor memory, so that
+// two blocks share an SM and one's beginning and end lie under the other's middle; tiles of 32 keys where two 96-column
+// outputs leave room for no more.
+template <int NB, bool SMALL>
 struct FwdShape {
-    static constexpr int kBlocks = NB == 1 ? 2 : 1;                 // resident per SM: tensor memory is the limit
-    static constexpr bool kQTmem = NB == 2;                         // queries as an A side in tensor memory (read from shared memory
+    static constexpr int kBlocks = SMALL ? 2 : 1;                   // resident per SM: tensor memory is the limit
+    static constexpr int kRows = SMALL && NB == 2 ? 32 : 64;        // keys per tile
+    static constexpr bool kQTmem = !SMALL;                          // queries as an A side in tensor memory (read from shared memory
                                                                     // for every tile they would cost as much as keys and values)
-    static constexpr int kStages = NB == 1 ? 4 : 3;
-    static constexpr int kOperand = NB * kFwdRows * 128, kStage = 2 * kOperand, kQBytes = kQTmem ? 0 : NB * 128 * 128;
-    static constexpr uint32_t kQ = 0, kS = NB == 1 ? 0 : 64, kO = NB == 1 ? 128 : 192, kAlloc = NB == 1 ? 256 : 512;   // columns
+    static constexpr int kStages = SMALL ? 4 : 3;
+    static constexpr int kOperand = NB * kRows * 128, kStage = 2 * kOperand, kQBytes = kQTmem ? 0 : NB * 128 * 128;
+    static constexpr uint32_t kWide = SMALL && NB == 2 ? 96 : NB * 64;                          // columns of an output
+    static constexpr uint32_t kQ = 0, kS = kQTmem ? NB * 32 : 0, kO = kS + 2 * kRows, kAlloc = SMALL ? 256 : 512;
+    static_assert(kO + 2 * kWide <= kAlloc, "tensor memory");
     static constexpr int kRing = kQBytes + kStages * kStage;
     static_assert(kRing >= NB * 128 * 128, "the output is staged where the ring was");
 };
@@ -45,12 +49,12 @@ struct FwdShared {
     float ref[2][128], sum[2][128];              // per warpgroup and row
 };
 
-template <typename T, int NB>
-__global__ void __launch_bounds__(kFwdThreads, FwdShape<NB>::kBlocks)
+template <typename T, int NB, bool SMALL>
+__global__ void __launch_bounds__(kFwdThreads, FwdShape<NB, SMALL>::kBlocks)
 attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                  const __grid_constant__ CUtensorMap map_v, AttendParams p, int *error)
 {
-    using Sh = FwdShape<NB>;
+    using Sh = FwdShape<NB, SMALL>;
     constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
     extern __shared__ unsigned char smem_raw[];
     __shared__ FwdShared sh;
@@ -97,7 +101,8 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         // a query that is not a word may hold anything: it spoils its own scores only, which are never used
         if (!Sh::kQTmem) {
             mbar_expect(&sh.q_full, Sh::kQBytes);
-            copy_box(qs, &map_q, 0, (int32_t)h, t0, &sh.q_full);
+#pragma unroll
+            for (int c = 0; c < NB; ++c) copy_box(qs + c * (128 * 128), &map_q, c * 64, (int32_t)h, t0, &sh.q_full);
         }
     }
     tc_fence_before();
@@ -118,15 +123,15 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     s = warp_value(s);
     const int32_t s_end = hi ? min(s + p.sinks, lo) : 0;
     const int32_t extra = s < s_end ? 1 : 0;
-    const int32_t tiles = hi ? extra + (hi - lo + kFwdRows - 1) / kFwdRows : 0;
-    auto tile_at = [&](int32_t t) { return extra && t == 0 ? s : lo + (t - extra) * kFwdRows; };
-    auto tile_keys = [&](int32_t t) { return extra && t == 0 ? s_end - s : min(kFwdRows, hi - tile_at(t)); };
+    const int32_t tiles = hi ? extra + (hi - lo + Sh::kRows - 1) / Sh::kRows : 0;
+    auto tile_at = [&](int32_t t) { return extra && t == 0 ? s : lo + (t - extra) * Sh::kRows; };
+    auto tile_keys = [&](int32_t t) { return extra && t == 0 ? s_end - s : min(Sh::kRows, hi - tile_at(t)); };
 
     if (warp < 8) {
         // ============ softmax: one row per thread, tiles in turn ============
-        if (NB == 1) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+        if (SMALL) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
         const uint32_t wg = warp >> 2, lanes = ((warp & 3u) * 32u) << 16;
-        const uint32_t cs = tmem + lanes + Sh::kS + wg * kFwdRows, co = tmem + lanes + Sh::kO + wg * NB * 64;
+        const uint32_t cs = tmem + lanes + Sh::kS + wg * Sh::kRows, co = tmem + lanes + Sh::kO + wg * Sh::kWide;
         if (Sh::kQTmem && wg == 0) {
 #pragma unroll
             for (int g = 0; g < NB * 2; ++g) {
@@ -158,20 +163,21 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             if (!ok) break;
             tc_fence_after();
             // far from the warp's rows every key of the tile has the bias of the side's last bucket
-            const bool far_left = k0 + kFwdRows - 1 - w0 <= -last, far = p.b.n == 0 || far_left || k0 - (w0 + 31) >= last;
+            const bool far_left = k0 + Sh::kRows - 1 - w0 <= -last, far = p.b.n == 0 || far_left || k0 - (w0 + 31) >= last;
             const float flat = p.b.n ? lut[far_left ? 0 : bias_entries(p.b) - 1] : 0.f;
-            const uint32_t vis0 = sh.vis[stage][0], vis1 = sh.vis[stage][1];
-            const bool plain = far && k0 >= all_lo && k0 + kFwdRows <= all_hi && (vis0 & vis1) == 0xFFFFFFFFu;
+            const uint32_t vis0 = sh.vis[stage][0], vis1 = Sh::kRows == 64 ? sh.vis[stage][1] : 0xFFFFFFFFu;
+            const bool plain = far && k0 >= all_lo && k0 + Sh::kRows <= all_hi && (vis0 & vis1) == 0xFFFFFFFFu;
             float top = -INFINITY, by = 1.f, add = 0.f;
             if (plain) {
                 float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-                uint32_t v[2][32];
-                tmem_ld32(cs, v[0]);
-                tmem_ld32(cs + 32, v[1]);
-                tmem_wait_ld(v[0]);
-                tmem_held(v[1]);
+                constexpr int kC = Sh::kRows / 32;
+                uint32_t v[kC][32];
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
+                for (int c = 0; c < kC; ++c) tmem_ld32(cs + c * 32, v[c]);
+                tmem_wait_ld(v[0]);
+                if (kC == 2) tmem_held(v[kC - 1]);
+#pragma unroll
+                for (int c = 0; c < kC; ++c)
 #pragma unroll
                     for (int e = 0; e < 32; e += 2) {
                         float &x = m[(e >> 1) & 3];
@@ -182,7 +188,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 add = flat;
             } else {
 #pragma unroll 1
-                for (int c = 0; c < 2; ++c) {
+                for (int c = 0; c < Sh::kRows / 32; ++c) {
                     if (c * 32 >= cols) break;
                     uint32_t v[32];
                     tmem_ld32(cs + c * 32, v);
@@ -228,7 +234,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             add -= ref == -INFINITY ? 0.f : ref;
             const float2 by2 = make_float2(by, by), add_2 = make_float2(add, add);
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
+            for (int c = 0; c < Sh::kRows / 32; ++c) {
                 if (c * 32 < cols) {
                     uint32_t v[32], w[16];
                     tmem_ld32(cs + c * 32, v);
@@ -272,7 +278,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             if (c >= dim16) break;
             uint32_t a[16], b[16];
             tmem_ld16(tmem + lanes + Sh::kO + c, a);
-            tmem_ld16(tmem + lanes + Sh::kO + NB * 64 + c, b);
+            tmem_ld16(tmem + lanes + Sh::kO + Sh::kWide + c, b);
             tmem_wait_ld(a);
             tmem_wait_ld(b);
             float o[16];
@@ -297,18 +303,18 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         tc_fence_before();
     } else if (warp == 8) {
         // ============ MMA issue: one lane ============
-        if (NB == 1) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        if (SMALL) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         // The whole block waits for this warp when its code is long: everything that does not change is formed once, a
         // product costs an addition per operand, and the warp stays together, so that addresses and descriptors are
         // formed in uniform registers, where the instruction wants them; one lane issues.
         if (tiles) {
             const bool leader = elect_one();
-            constexpr uint32_t kBlock = kFwdRows * 128, kStep = Sh::kStage >> 4;
-            const uint32_t idesc_o = umma_idesc_f16(kBf16, kAttendTile, dim16, true), idesc_s = umma_idesc_f16(kBf16, kAttendTile, kFwdRows, false);
+            constexpr uint32_t kBlock = Sh::kRows * 128, kStep = Sh::kStage >> 4;
+            const uint32_t idesc_o = umma_idesc_f16(kBf16, kAttendTile, dim16, true), idesc_s = umma_idesc_f16(kBf16, kAttendTile, Sh::kRows, false);
             const uint32_t q_low = umma_desc_low(qs, 0), k_low = umma_desc_low(ring, 0), v_low = umma_desc_low(ring + Sh::kOperand, kBlock);
             // keys past the tile's end are products of what lies there and are masked
             auto scores = [&](uint32_t b, uint32_t stage) {
-                const uint32_t k = k_low + stage * kStep, d = tmem + Sh::kS + b * kFwdRows;
+                const uint32_t k = k_low + stage * kStep, d = tmem + Sh::kS + b * Sh::kRows;
 #pragma unroll
                 for (int c = 0; c < NB * 4; ++c)
                     if ((uint32_t)c * 16 < dim16) {
@@ -333,13 +339,13 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             }
             uint32_t stage = 0;
             for (int32_t t = 0; t < tiles && ok; ++t) {
-                const uint32_t b = t & 1, v = v_low + stage * kStep, w = tmem + Sh::kS + b * kFwdRows, d = tmem + Sh::kO + b * NB * 64;
+                const uint32_t b = t & 1, v = v_low + stage * kStep, w = tmem + Sh::kS + b * Sh::kRows, d = tmem + Sh::kO + b * Sh::kWide;
                 const int32_t keys = tile_keys(t);
                 ok = wait(&sh.p_full[b], (t >> 1) & 1);
                 if (!ok) break;
                 if (leader) {
 #pragma unroll
-                    for (int k = 0; k < kFwdRows / 16; ++k)
+                    for (int k = 0; k < Sh::kRows / 16; ++k)
                         if (k * 16 < keys) umma_f16_ts(d, w + k * 8, v + k * 128, idesc_o, t > 1 || k > 0);
                     umma_commit(&sh.empty[stage]);
                     if (t + 1 == tiles) umma_commit(&sh.done);
@@ -358,7 +364,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         __syncwarp();
     } else if (warp == 9) {
         // ============ copies: one lane ============
-        if (NB == 1) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        if (SMALL) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         if (lane == 0) {
             int32_t t = 0;
             for (; t < tiles; ++t) {
@@ -367,8 +373,8 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 mbar_expect(&sh.landed[stage], Sh::kStage);
 #pragma unroll
                 for (int c = 0; c < NB; ++c) {
-                    copy_box(base + c * kFwdRows * 128, &map_k, c * 64, (int32_t)kvh, tile_at(t), &sh.landed[stage]);
-                    copy_box(base + Sh::kOperand + c * kFwdRows * 128, &map_v, c * 64, (int32_t)kvh, tile_at(t), &sh.landed[stage]);
+                    copy_box(base + c * Sh::kRows * 128, &map_k, c * 64, (int32_t)kvh, tile_at(t), &sh.landed[stage]);
+                    copy_box(base + Sh::kOperand + c * Sh::kRows * 128, &map_v, c * 64, (int32_t)kvh, tile_at(t), &sh.landed[stage]);
                 }
             }
             // after a wait that ran out: what is under way lands before the block leaves
@@ -378,7 +384,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         __syncwarp();
     } else {
         // ============ rows that are not words: a warp per tile, in turn ============
-        if (NB == 1) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        if (SMALL) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         int32_t t = (int32_t)warp - 10;
         uint32_t vis[2] = {0u, 0u};
         if (t < tiles) word_bits(p, tile_at(t), (uint32_t)tile_keys(t), lane, vis);
@@ -387,7 +393,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             if (!__all_sync(kFullMask, mbar_wait(&sh.landed[stage], (t / Sh::kStages) & 1, abort_flag))) break;
             if (lane < 2) sh.vis[stage][lane] = lane ? vis[1] : vis[0];
             // values only: the scores of such a key are masked
-            zero_rows<NB>(ring + stage * Sh::kStage + Sh::kOperand, kFwdRows * 128, (uint32_t)(tile_keys(t) + 15) & ~15u, vis, lane);
+            zero_rows<NB>(ring + stage * Sh::kStage + Sh::kOperand, Sh::kRows * 128, (uint32_t)(tile_keys(t) + 15) & ~15u, vis, lane);
             fence_async_proxy();
             mbar_arrive(&sh.full[stage]);
             if (t + 2 < tiles) word_bits(p, tile_at(t + 2), (uint32_t)tile_keys(t + 2), lane, vis);
@@ -399,14 +405,15 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     if (tid == 0 && sh.abort_flag) atomicOr(error, kErrAttend);
 }
 
-template <typename T, int NB>
+template <typename T, int NB, bool SMALL>
 int launch_attend_shape(const AttendParams &p, int *error, cudaStream_t s)
 {
-    auto kernel = attend_tc_kernel<T, NB>;
-    int smem = FwdShape<NB>::kRing + 1024 + (int)(bias_entries(p.b) * sizeof(float));
-    if (FwdShape<NB>::kBlocks == 1 && smem < 116 * 1024) smem = 116 * 1024;      // a second block would only wait for tensor memory
+    auto kernel = attend_tc_kernel<T, NB, SMALL>;
+    using Sh = FwdShape<NB, SMALL>;
+    int smem = Sh::kRing + 1024 + (int)(bias_entries(p.b) * sizeof(float));
+    if (Sh::kBlocks == 1 && smem < 116 * 1024) smem = 116 * 1024;      // a second block would only wait for tensor memory
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return -1;
-    if (NB == 1) {
+    if (SMALL) {
         // a block launched with fewer registers could never hand out the softmax's share
         cudaFuncAttributes at;
         if (cudaFuncGetAttributes(&at, kernel) != cudaSuccess || at.numRegs < kLaunchRegs) return -1;
@@ -415,8 +422,8 @@ int launch_attend_shape(const AttendParams &p, int *error, cudaStream_t s)
     CUtensorMap q, k, v;
     const bool bf16 = std::is_same<T, __nv_bfloat16>::value;
     if (!make_rows_map(&q, bf16, p.q, p.dim, p.heads, (uint64_t)p.n, p.ldq, kAttendTile) ||
-        !make_rows_map(&k, bf16, p.k, p.dim, p.kv_heads, (uint64_t)p.n, p.ldk, kFwdRows) ||
-        !make_rows_map(&v, bf16, p.v, p.dim, p.kv_heads, (uint64_t)p.n, p.ldv, kFwdRows))
+        !make_rows_map(&k, bf16, p.k, p.dim, p.kv_heads, (uint64_t)p.n, p.ldk, Sh::kRows) ||
+        !make_rows_map(&v, bf16, p.v, p.dim, p.kv_heads, (uint64_t)p.n, p.ldv, Sh::kRows))
         return -1;
     kernel<<<(uint32_t)(tiles * p.heads), kFwdThreads, smem, s>>>(q, k, v, p, error);
     return cudaPeekAtLastError() == cudaSuccess ? 1 : -1;
@@ -425,8 +432,12 @@ int launch_attend_shape(const AttendParams &p, int *error, cudaStream_t s)
 int launch_attend(const AttendParams &p, uint32_t type, int *error, int, cudaStream_t s)
 {
     if (p.n == 0) return 0;
-    if (type == kBF16) return p.dim <= 64 ? launch_attend_shape<__nv_bfloat16, 1>(p, error, s) : launch_attend_shape<__nv_bfloat16, 2>(p, error, s);
-    return p.dim <= 64 ? launch_attend_shape<__half, 1>(p, error, s) : launch_attend_shape<__half, 2>(p, error, s);
+    auto shape = [&](auto element) {
+        using T = decltype(element);
+        return p.dim <= 64 ? launch_attend_shape<T, 1, true>(p, error, s)
+               : p.dim <= 96 ? launch_attend_shape<T, 2, true>(p, error, s) : launch_attend_shape<T, 2, false>(p, error, s);
+    };
+    return type == kBF16 ? shape(__nv_bfloat16()) : shape(__half());
 }
 
 }  // namespace w2v

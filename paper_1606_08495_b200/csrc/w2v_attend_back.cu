@@ -728,7 +728,7 @@ __device__ __forceinline__ int64_t first_word(const AttendParams &p, int32_t til
 }
 
 // Slot a holds the sums for the sentence that begins in tile a and reaches into a later one (there is at most one):
-// over its query tiles and the query heads of a key/value head, in a fixed order, 32 elements per block.
+// over its query tiles and the query heads of a key/value head, in a fixed order, 32 elements at a time.
 __global__ void __launch_bounds__(256)
 attend_sink_sum_kernel(AttendParams p, int32_t tiles)
 {
@@ -743,24 +743,28 @@ attend_sink_sum_kernel(AttendParams p, int32_t tiles)
     if (!here) return;
     // the sentence's last tile is that of its last word; tiles without words in between have nothing
     const int32_t end = min(tiles, (p.spans[first_word(p, first)].y - 1) / kAttendTile + 1);
-    const size_t width = (size_t)p.sinks * 2 * p.dim, e = (size_t)blockIdx.y * 32 + lane;
-    float x[4] = {0.f, 0.f, 0.f, 0.f};
+    const size_t width = (size_t)p.sinks * 2 * p.dim;
     const int32_t items = (end - first) * (int32_t)group;
-    if (e < width)
-        for (int32_t i = (int32_t)warp; i < items; i += 32) {
+    for (size_t e0 = (size_t)blockIdx.y * 32; e0 < width; e0 += (size_t)gridDim.y * 32) {
+        const size_t e = e0 + lane;
+        float x[4] = {0.f, 0.f, 0.f, 0.f};
+        if (e < width)
+            for (int32_t i = (int32_t)warp; i < items; i += 32) {
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int32_t j = i + u * 8, t = first + j / (int32_t)group;
-                if (j < items && p.sink_rec[t] == s) x[u] += p.sink_part[((size_t)t * p.heads + kvh * group + (uint32_t)j % group) * width + e];
+                for (int u = 0; u < 4; ++u) {
+                    const int32_t j = i + u * 8, t = first + j / (int32_t)group;
+                    if (j < items && p.sink_rec[t] == s) x[u] += p.sink_part[((size_t)t * p.heads + kvh * group + (uint32_t)j % group) * width + e];
+                }
             }
-        }
-    part[warp][lane] = (x[0] + x[1]) + (x[2] + x[3]);
-    __syncthreads();
-    if (warp == 0 && e < width) {
-        float y = 0.f;
+        part[warp][lane] = (x[0] + x[1]) + (x[2] + x[3]);
+        __syncthreads();
+        if (warp == 0 && e < width) {
+            float y = 0.f;
 #pragma unroll
-        for (int w = 0; w < 8; ++w) y += part[w][lane];
-        p.sink_sum[((size_t)a * p.kv_heads + kvh) * width + e] = y;
+            for (int w = 0; w < 8; ++w) y += part[w][lane];
+            p.sink_sum[((size_t)a * p.kv_heads + kvh) * width + e] = y;
+        }
+        __syncthreads();
     }
 }
 
@@ -850,7 +854,9 @@ int launch_back_typed(const AttendParams &p, uint32_t tiles, int *error, cudaStr
     int k = role(std::integral_constant<int, 0>());
     if (k < 0) return -1;
     if (far_sinks(p)) {
-        attend_sink_sum_kernel<<<dim3(tiles * p.kv_heads, (2 * (uint32_t)p.sinks * p.dim + 31) / 32), 256, 0, s>>>(p, (int32_t)tiles);
+        // most blocks find that no sentence crosses their tile's end: few blocks per slot, unless slots are few
+        const uint32_t parts = (2 * (uint32_t)p.sinks * p.dim + 31) / 32, some = 4096 / (tiles * p.kv_heads) + 1;
+        attend_sink_sum_kernel<<<dim3(tiles * p.kv_heads, parts < some ? parts : some), 256, 0, s>>>(p, (int32_t)tiles);
         ++k;
     }
     const int j = role(std::integral_constant<int, 1>());

@@ -96,9 +96,9 @@ int launch_spans(const int32_t *tokens, uint64_t n, uint32_t vocab, int32_t *til
     if (n == 0) return 0;
     const uint32_t tiles = (uint32_t)spans_tiles(n);
     int2 *ends = reinterpret_cast<int2 *>(tile_ends);
-    span_tiles_kernel<<<tiles, kSpanThreads, 0, s>>>(tokens, n, ends);
+    if (tiles > 1) span_tiles_kernel<<<tiles, kSpanThreads, 0, s>>>(tokens, n, ends);       // a single tile looks at no other
     span_fill_kernel<<<tiles, kSpanThreads, 0, s>>>(tokens, n, vocab, ends, tiles, spans);
-    return cudaPeekAtLastError() == cudaSuccess ? 2 : -1;
+    return cudaPeekAtLastError() == cudaSuccess ? (tiles > 1 ? 2 : 1) : -1;
 }
 
 }  // namespace w2v
