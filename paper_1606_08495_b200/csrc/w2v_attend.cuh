@@ -44,10 +44,11 @@ __device__ __forceinline__ uint32_t range_bits(int32_t a, int32_t b, int32_t at)
     return (y == 32 ? 0xFFFFFFFFu : (1u << y) - 1u) & ~((1u << x) - 1u);   // x < 32 here
 }
 
-// The bias by distance, in base-2 units, for every distance that a tile can hold which is not beyond the last
-// bucket's start on one side: entries -(last + 255) .. last + 255.
+// The bias by distance, in base-2 units, for every distance that the part of a tile which a warp works on (32 rows, up
+// to 64 columns: distances that span 94) can hold unless all of it lies beyond the last bucket's start: entries
+// -(last + kBiasPad) .. last + kBiasPad.
 __host__ __device__ inline int32_t bias_last(const BucketStarts &b) { return b.n ? b.start[b.n - 1] : 0; }
-constexpr int32_t kBiasPad = 255;
+constexpr int32_t kBiasPad = 96;
 __host__ __device__ inline uint32_t bias_entries(const BucketStarts &b) { return b.n ? 2u * (uint32_t)(bias_last(b) + kBiasPad) + 1u : 0u; }
 
 __device__ __forceinline__ uint32_t bucket_of(const BucketStarts &b, int32_t rel)

@@ -20,13 +20,14 @@ namespace w2v {
 
 // Two layouts of a block.
 //   SMALL (heads of up to 96): 256 columns of tensor memory and half of the shared memory, so that two blocks share an SM
-//          and one's beginning and end lie under the other's middle; one softmax warpgroup; the A sides stay in shared
-//          memory; tiles of 32 rows.
-//   else:  all of the tensor memory; two softmax warpgroups that take the tiles in turn; the A sides in tensor memory
-//          (heads of up to 64: tiles of 64 rows).
+//          and one's beginning and end lie under the other's middle; the A sides stay in shared memory; the two softmax
+//          warpgroups take half of the columns of every tile.
+//   else:  all of the tensor memory; the A sides in tensor memory; the warpgroups take the tiles in turn.
 template <int NB, bool SMALL>
 struct BackShape {
-    static constexpr int kWg = SMALL ? 1 : 2;                        // softmax warpgroups
+    static constexpr int kWg = 2;                                    // softmax warpgroups
+    static constexpr int kTile = SMALL ? 256 : 128;                  // softmax threads that share a tile
+    static constexpr int kChunk = SMALL ? 16 : 32;                   // columns a thread takes at once
     static constexpr int kBuf = SMALL && NB == 2 ? 1 : 2;            // score buffers
     static constexpr int kRows = SMALL || NB == 2 ? 32 : 64;         // streamed rows per tile
     static constexpr int kStages = SMALL && NB == 2 ? 2 : 4;
@@ -39,8 +40,9 @@ struct BackShape {
     static constexpr int kSoft = 128 * kWg, kThreads = kSoft + 128, kBlocks = 512 / (int)kAlloc;
     static_assert(kRing + 2 * kOwn >= 2 * NB * 128 * 128, "the outputs are staged where the ring and the own rows were");
 };
-// SMALL: of the 128 registers a thread has at launch, the helpers give all beyond 56 to the softmax (200 + 56 = 2 x 128).
-constexpr int kBackLaunchRegs = 128, kBackSoftRegs = 200, kBackOtherRegs = 56;
+// SMALL: of the 80 registers a thread has at launch, the helpers' warpgroup gives what it has beyond 48 to the two of
+// the softmax (96 + 96 + 48 = 3 x 80).
+constexpr int kBackLaunchRegs = 80, kBackSoftRegs = 96, kBackOtherRegs = 48;
 
 template <typename Sh>
 struct BackShared {
@@ -165,7 +167,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
 {
     using Sh = BackShape<NB, SMALL>;
     constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
-    constexpr int kChunks = Sh::kRows / 32;
+    constexpr int kChunks = SMALL ? 1 : Sh::kRows / Sh::kChunk;      // of a thread per tile
     extern __shared__ unsigned char smem_raw[];
     __shared__ BackShared<Sh> sh;
     unsigned char *smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
@@ -173,7 +175,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
     const unsigned char *own_rows = smem + Sh::kRing;                // the two A sides, and o in role 0 (not SMALL), as they land
     float *lut = reinterpret_cast<float *>(smem + Sh::kRing + 2 * Sh::kOwn + (ROLE == 0 ? max(SMALL ? 0 : Sh::kOwn, p.sinks * 1024) : 0));
     const uint32_t entries = bias_entries(p.b);
-    float *rel_sums = lut + ((entries + 3u) & ~3u);                  // role 1: [softmax warps][entries]
+    float *rel_sums = lut + ((entries + 3u) & ~3u);                  // role 1: [softmax warps][entries]; role 0, SMALL: halves of the first delta
 
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t group = p.heads / p.kv_heads, across = ROLE == 0 ? p.heads : p.kv_heads;
@@ -186,8 +188,8 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
     if (warp == kMmaWarp + 1 && lane == 0) {
         mbar_init(&sh.own_landed, 1);
         mbar_init(&sh.own_full, SMALL ? 64 : 256);
-        for (int i = 0; i < Sh::kStages; ++i) { mbar_init(&sh.landed[i], 1); mbar_init(&sh.full[i], 32); mbar_init(&sh.empty[i], 1 + 128); }
-        for (int i = 0; i < 2; ++i) { mbar_init(&sh.s_full[i], 1); mbar_init(&sh.p_full[i], 128); }
+        for (int i = 0; i < Sh::kStages; ++i) { mbar_init(&sh.landed[i], 1); mbar_init(&sh.full[i], 32); mbar_init(&sh.empty[i], 1 + Sh::kTile); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&sh.s_full[i], 1); mbar_init(&sh.p_full[i], Sh::kTile); }
         mbar_init(&sh.done, 1);
         sh.abort_flag = sh.quiet = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -249,8 +251,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
     }
     // the table by warps that have nothing else to begin with, the zeros by the others
     if (p.b.n) {
-        if (!SMALL && warp >= 4 && warp < 8) fill_bias(p, h0, lut, warp - 4, 4, lane);
-        if (SMALL && warp >= kMmaWarp + 2) fill_bias(p, h0, lut, warp - kMmaWarp - 2, 2, lane);
+        if (warp >= 4 && warp < 8) fill_bias(p, h0, lut, warp - 4, 4, lane);
         if (ROLE == 1 && warp < 4)
             for (uint32_t e = tid; e < kSoftWarps * entries; e += 128) rel_sums[e] = 0.f;
     }
@@ -301,10 +302,17 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
             };
             if (SMALL) {
                 const uint4 *o = reinterpret_cast<const uint4 *>(static_cast<const T *>(p.o) + own * (int64_t)p.ldo + (int64_t)h_own * p.dim);
-                if (ROLE == 0 && word)
+                if (ROLE == 0) {                                     // each warpgroup half of the row
+                    if (word)
 #pragma unroll
-                    for (int c = 0; c < NB * 8; ++c)
-                        if ((uint32_t)c * 8 < p.dim) first_delta(chunk(1, c), __ldg(o + c));
+                        for (int c = 0; c < NB * 4; ++c) {
+                            const uint32_t x = 2 * c + wg;
+                            if (x * 8 < p.dim) first_delta(chunk(1, (int)x), __ldg(o + x));
+                        }
+                    rel_sums[wg * 128 + r] = delta;
+                    soft_barrier(Sh::kSoft);
+                    delta = rel_sums[r] + rel_sums[128 + r];
+                }
             } else {
                 // the two operands of the block's rows go to tensor memory (a warpgroup each), zeros for rows that are not words
 #pragma unroll
@@ -344,7 +352,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
             for (int32_t k = 0; k < per_head && ok; ++k) {
                 const int32_t t = (int32_t)g * per_head + k;
                 const uint32_t b = t % Sh::kBuf, stage = t % Sh::kStages;
-                if (Sh::kWg == 2 && b != wg) continue;
+                if (!SMALL && b != wg) continue;
                 const int32_t at0 = tile_at(k), cols = (tile_rows(k) + 15) & ~15;
                 ok = __all_sync(kFullMask, mbar_wait(&sh.full[stage], (t / Sh::kStages) & 1, abort_flag) &&
                                                mbar_wait(&sh.s_full[b], (t / Sh::kBuf) & 1, abort_flag));
@@ -360,25 +368,28 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                 const bool reach = ROLE == 1 && p.sinks && sh.run_lo[stage] <= own;
 #pragma unroll
                 for (int c = 0; c < kChunks; ++c) {
-                    if (c * 32 < cols) {
-                        uint32_t sv[32], dv[32];
-                        tmem_ld32(cs + c * 32, sv);
-                        tmem_ld32(cd + c * 32, dv);
-                        tmem_wait_ld(sv);
-                        tmem_held(dv);
-                        const int32_t at = at0 + c * 32;
+                    constexpr int kC = Sh::kChunk;
+                    constexpr uint32_t kAll = kC == 32 ? 0xFFFFFFFFu : (1u << kC) - 1u;
+                    const int32_t c0 = SMALL ? (int32_t)wg * kC : c * kC;    // first column
+                    if (c0 < cols) {
+                        uint32_t sv[kC], dv[kC];
+                        tmem_ld(cs + c0, sv);
+                        tmem_ld(cd + c0, dv);
+                        const int32_t at = at0 + c0;
                         uint32_t m;
-                        if (ROLE == 0) m = (range_bits(row.lo, row.hi, at) | range_bits(row.s, row.se, at)) & sh.vis[stage][c];
+                        if (ROLE == 0) m = (range_bits(row.lo, row.hi, at) | range_bits(row.s, row.se, at)) & (SMALL ? sh.vis[stage][0] >> c0 : sh.vis[stage][c]);
                         else {
                             m = range_bits(q_lo, q_hi, at);
                             if (reach) m |= range_bits(far_lo, far_hi, at);
                         }
+                        tmem_wait_ld(sv);
+                        tmem_held(dv);
                         // -infinity where the key is hidden; a row or column that sees nothing has lse +infinity
-                        float x[32];
+                        float x[kC];
                         if (far) {
                             const float2 scale2 = make_float2(scale, scale), flat2 = make_float2(flat, flat);
 #pragma unroll
-                            for (int e = 0; e < 32; e += 2) {
+                            for (int e = 0; e < kC; e += 2) {
                                 const float2 y = fma2(pair_of(sv[e], sv[e + 1]), scale2, flat2);
                                 x[e] = y.x;
                                 x[e + 1] = y.y;
@@ -387,17 +398,17 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                             // key - query grows with the column in role 0 and falls with it in role 1
                             const float *near = ROLE == 0 ? lut + (at - (int32_t)own + off) : lut + ((int32_t)own - at + off);
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) x[e] = fmaf(__uint_as_float(sv[e]), scale, ROLE == 0 ? near[e] : near[-e]);
+                            for (int e = 0; e < kC; ++e) x[e] = fmaf(__uint_as_float(sv[e]), scale, ROLE == 0 ? near[e] : near[-e]);
                         }
-                        if (!__all_sync(kFullMask, m == 0xFFFFFFFFu)) {
+                        if (!__all_sync(kFullMask, (m | ~kAll) == 0xFFFFFFFFu)) {
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) x[e] = m & (1u << e) ? x[e] : -INFINITY;
+                            for (int e = 0; e < kC; ++e) x[e] = m & (1u << e) ? x[e] : -INFINITY;
                         }
-                        uint32_t ws[16], wp[16];
+                        uint32_t ws[kC / 2], wp[kC / 2];
                         if (ROLE == 0) {
                             const float2 lse2 = make_float2(-lse, -lse), delta2 = make_float2(-delta, -delta);
 #pragma unroll
-                            for (int e = 0; e < 32; e += 2) {
+                            for (int e = 0; e < kC; e += 2) {
                                 float2 w = add2(make_float2(x[e], x[e + 1]), lse2);
                                 w.x = fast_exp2(w.x);
                                 w.y = fast_exp2(w.y);
@@ -406,12 +417,12 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                                 wp[e / 2] = pack2<T>(w.x, w.y);
                                 ws[e / 2] = pack2<T>(d.x, d.y);
                             }
-                            tmem_st16(cs + c * 16, wp);
-                            tmem_st16(cd + c * 16, ws);
+                            tmem_st(cs + (SMALL ? c0 : c0 / 2), wp);
+                            tmem_st(cd + (SMALL ? c0 : c0 / 2), ws);
                             if (k >= run) {                          // sinks: kept in fp32 for their own sums
 #pragma unroll
-                                for (int e = 0; e < 32; ++e) {
-                                    const int32_t i = (k - run) * Sh::kRows + c * 32 + e;
+                                for (int e = 0; e < kC; ++e) {
+                                    const int32_t i = (k - run) * Sh::kRows + c0 + e;
                                     if (i < sinks) {
                                         const float w = fast_exp2(x[e] - lse);
                                         sink_p[i * 128 + (int32_t)r] = w;
@@ -420,11 +431,11 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                                 }
                             }
                         } else {
-                            float ds[32];
+                            float ds[kC];
 #pragma unroll
-                            for (int e = 0; e < 32; e += 4) {
-                                const float4 l4 = *reinterpret_cast<const float4 *>(&sh.lse[stage][c * 32 + e]);        // negated, as delta
-                                const float4 d4 = *reinterpret_cast<const float4 *>(&sh.delta[stage][c * 32 + e]);
+                            for (int e = 0; e < kC; e += 4) {
+                                const float4 l4 = *reinterpret_cast<const float4 *>(&sh.lse[stage][c0 + e]);        // negated, as delta
+                                const float4 d4 = *reinterpret_cast<const float4 *>(&sh.delta[stage][c0 + e]);
                                 float2 p0 = add2(make_float2(x[e], x[e + 1]), make_float2(l4.x, l4.y));
                                 float2 p1 = add2(make_float2(x[e + 2], x[e + 3]), make_float2(l4.z, l4.w));
                                 p0.x = fast_exp2(p0.x); p0.y = fast_exp2(p0.y); p1.x = fast_exp2(p1.x); p1.y = fast_exp2(p1.y);
@@ -436,21 +447,22 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                                 ws[e / 2 + 1] = pack2<T>(p1.x, p1.y);
                                 ds[e] = p0.x; ds[e + 1] = p0.y; ds[e + 2] = p1.x; ds[e + 3] = p1.y;
                             }
-                            tmem_st16(cs + c * 16, wp);
-                            tmem_st16(cd + c * 16, ws);
+                            tmem_st(cs + (SMALL ? c0 : c0 / 2), wp);
+                            tmem_st(cd + (SMALL ? c0 : c0 / 2), ws);
                             if (p.dbias) {
                                 if (far) {
-                                    float a = 0.f;
+                                    float a[4] = {ds[0], ds[1], ds[2], ds[3]};
 #pragma unroll
-                                    for (int e = 0; e < 32; ++e) a += ds[e];
-                                    if (far_left) far_l += a; else far_r += a;
+                                    for (int e = 4; e < kC; ++e) a[e & 3] += ds[e];
+                                    if (far_left) far_l += (a[0] + a[1]) + (a[2] + a[3]); else far_r += (a[0] + a[1]) + (a[2] + a[3]);
                                 } else {
-                                    // lane l gathers the diagonal key - query = base + l (acc_p) and the one 32 below (acc_n)
-                                    const int32_t base = w0 - at;
+                                    // over 32 columns lane l gathers the diagonal key - query = base + l (acc_p) and the one 32 below (acc_n)
+                                    const int32_t base = w0 - (SMALL ? at0 : at);
 #pragma unroll
-                                    for (int e = 0; e < 32; ++e) {
-                                        const float y = __shfl_sync(kFullMask, ds[e], (lane + e) & 31u);
-                                        if (lane + e < 32u) acc_p += y; else acc_n += y;
+                                    for (int e = 0; e < kC; ++e) {
+                                        const uint32_t from = lane + (SMALL ? (uint32_t)c0 : 0u) + e;
+                                        const float y = __shfl_sync(kFullMask, ds[e], from & 31u);
+                                        if (from < 32u) acc_p += y; else acc_n += y;
                                     }
                                     float *mine = rel_sums + warp * entries + base + off + (int32_t)lane;
                                     mine[0] += acc_p;
@@ -623,8 +635,9 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
 #pragma unroll
                     for (int c = 0; c < Sh::kRows / 16; ++c)
                         if (c * 16 < rows) {
-                            umma_f16_ts(tmem + Sh::kG1, d + c * 8, y + c * 128, idesc_g, t > 0 || c > 0);
-                            umma_f16_ts(tmem + Sh::kG0, d + Sh::kRows + c * 8, x + c * 128, idesc_g, t > 0 || c > 0);
+                            // each thread has put its weights over its own scores: SMALL, the second half of a tile's lie 16 columns on
+                            umma_f16_ts(tmem + Sh::kG1, d + c * (SMALL ? 16 : 8), y + c * 128, idesc_g, t > 0 || c > 0);
+                            umma_f16_ts(tmem + Sh::kG0, d + Sh::kRows + c * (SMALL ? 16 : 8), x + c * 128, idesc_g, t > 0 || c > 0);
                         }
                     umma_commit(&sh.empty[stage]);
                     if (t + 1 == total) umma_commit(&sh.done);
@@ -817,7 +830,7 @@ int launch_role(const AttendParams &p, uint32_t tiles, int *error, cudaStream_t 
     const uint32_t entries = bias_entries(p.b);
     const int o_bytes = SMALL ? 0 : Sh::kOwn, sink_bytes = p.sinks * 1024;
     int smem = Sh::kRing + 2 * Sh::kOwn + (ROLE == 0 ? (sink_bytes > o_bytes ? sink_bytes : o_bytes) : 0) + 1024 +
-               (int)(4 * (((entries + 3u) & ~3u) + (ROLE == 1 ? Sh::kSoft / 32 * entries : 0u)));
+               (int)(4 * (((entries + 3u) & ~3u) + (ROLE == 1 ? Sh::kSoft / 32 * entries : 256u)));
     if (!SMALL && smem < 116 * 1024) smem = 116 * 1024;              // a second block would only wait for tensor memory
     if (SMALL) {
         // a block launched with fewer registers could never hand out the softmax's share
