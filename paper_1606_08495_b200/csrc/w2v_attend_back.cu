@@ -746,20 +746,19 @@ __global__ void __launch_bounds__(256)
 attend_sink_sum_kernel(AttendParams p, int32_t tiles)
 {
     __shared__ float part[8][32];
-    const int32_t a = (int32_t)(blockIdx.x / p.kv_heads);
     const uint32_t kvh = blockIdx.x % p.kv_heads, group = p.heads / p.kv_heads, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int32_t first = a + 1;
-    while (first < tiles && p.sink_rec[first] == -1) ++first;
-    const int32_t s = first < tiles ? p.sink_rec[first] : -2;
-    const bool here = s >= 0 && s / kAttendTile == a;
-    if (blockIdx.y == 0 && kvh == 0 && threadIdx.x == 0) p.sink_used[a] = here ? s : -1;
-    if (!here) return;
-    // the sentence's last tile is that of its last word; tiles without words in between have nothing
-    const int32_t end = min(tiles, (p.spans[first_word(p, first)].y - 1) / kAttendTile + 1);
-    const size_t width = (size_t)p.sinks * 2 * p.dim;
-    const int32_t items = (end - first) * (int32_t)group;
-    for (size_t e0 = (size_t)blockIdx.y * 32; e0 < width; e0 += (size_t)gridDim.y * 32) {
-        const size_t e = e0 + lane;
+    const size_t width = (size_t)p.sinks * 2 * p.dim, e = (size_t)(blockIdx.x / p.kv_heads) * 32 + lane;
+    // most slots are empty, which takes one look to see: a block goes over many
+    for (int32_t a = (int32_t)blockIdx.y; a < tiles; a += (int32_t)gridDim.y) {
+        int32_t first = a + 1;
+        while (first < tiles && p.sink_rec[first] == -1) ++first;
+        const int32_t s = first < tiles ? p.sink_rec[first] : -2;
+        const bool here = s >= 0 && s / kAttendTile == a;
+        if (blockIdx.x == 0 && threadIdx.x == 0) p.sink_used[a] = here ? s : -1;
+        if (!here) continue;
+        // the sentence's last tile is that of its last word; tiles without words in between have nothing
+        const int32_t end = min(tiles, (p.spans[first_word(p, first)].y - 1) / kAttendTile + 1);
+        const int32_t items = (end - first) * (int32_t)group;
         float x[4] = {0.f, 0.f, 0.f, 0.f};
         if (e < width)
             for (int32_t i = (int32_t)warp; i < items; i += 32) {
@@ -867,9 +866,8 @@ int launch_back_typed(const AttendParams &p, uint32_t tiles, int *error, cudaStr
     int k = role(std::integral_constant<int, 0>());
     if (k < 0) return -1;
     if (far_sinks(p)) {
-        // most blocks find that no sentence crosses their tile's end: few blocks per slot, unless slots are few
-        const uint32_t parts = (2 * (uint32_t)p.sinks * p.dim + 31) / 32, some = 4096 / (tiles * p.kv_heads) + 1;
-        attend_sink_sum_kernel<<<dim3(tiles * p.kv_heads, parts < some ? parts : some), 256, 0, s>>>(p, (int32_t)tiles);
+        const uint32_t columns = (2 * (uint32_t)p.sinks * p.dim + 31) / 32 * p.kv_heads, some = 2048 / columns + 1;
+        attend_sink_sum_kernel<<<dim3(columns, tiles < some ? tiles : some), 256, 0, s>>>(p, (int32_t)tiles);
         ++k;
     }
     const int j = role(std::integral_constant<int, 1>());
