@@ -320,17 +320,17 @@ _TYPES = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16, torch.float16: TYP
 
 
 def w2v_layer_norm(h, rows, d, x, x_stride, x_type, gamma, beta, eps, y, y_stride, y_type, mean, rstd):
-    return _check(h, load().w2v_layer_norm(h, rows, d, x, x_stride, x_type, gamma, beta, eps, y, y_stride, y_type, mean, rstd))
+    return _check(h, (_lib or load()).w2v_layer_norm(h, rows, d, x, x_stride, x_type, gamma, beta, eps, y, y_stride, y_type, mean, rstd))
 
 
 def w2v_layer_norm_backward(h, rows, d, dy, dy_stride, y_type, x, x_stride, x_type, gamma, mean, rstd, dx, dx_stride,
                             dgamma, dbeta):
-    return _check(h, load().w2v_layer_norm_backward(h, rows, d, dy, dy_stride, y_type, x, x_stride, x_type, gamma, mean, rstd,
+    return _check(h, (_lib or load()).w2v_layer_norm_backward(h, rows, d, dy, dy_stride, y_type, x, x_stride, x_type, gamma, mean, rstd,
                                                     dx, dx_stride, dgamma, dbeta))
 
 
 def w2v_sentence_spans(h, tokens, n, spans):
-    return _check(h, load().w2v_sentence_spans(h, tokens, n, spans))
+    return _check(h, (_lib or load()).w2v_sentence_spans(h, tokens, n, spans))
 
 
 def w2v_bucket_starts(buckets, reach, two_sided):
@@ -343,25 +343,25 @@ def w2v_bucket_starts(buckets, reach, two_sided):
 
 
 def w2v_attend(h, window, n, spans, q, q_stride, k, k_stride, v, v_stride, bias, o, o_stride, lse):
-    return _check(h, load().w2v_attend(h, window, n, spans, q, q_stride, k, k_stride, v, v_stride, bias, o, o_stride, lse))
+    return _check(h, (_lib or load()).w2v_attend(h, window, n, spans, q, q_stride, k, k_stride, v, v_stride, bias, o, o_stride, lse))
 
 
 def w2v_attend_backward(h, window, n, spans, q, q_stride, k, k_stride, v, v_stride, bias, o, o_stride, lse,
                         d_o, do_stride, dq, dq_stride, dk, dk_stride, dv, dv_stride, dbias):
-    return _check(h, load().w2v_attend_backward(h, window, n, spans, q, q_stride, k, k_stride, v, v_stride, bias, o, o_stride,
+    return _check(h, (_lib or load()).w2v_attend_backward(h, window, n, spans, q, q_stride, k, k_stride, v, v_stride, bias, o, o_stride,
                                                 lse, d_o, do_stride, dq, dq_stride, dk, dk_stride, dv, dv_stride, dbias))
 
 
 def w2v_attend_token(h, window, batch, pos, q, k, v, cache_k, cache_v, places, bias, o):
-    return _check(h, load().w2v_attend_token(h, window, batch, pos, q, k, v, cache_k, cache_v, places, bias, o))
+    return _check(h, (_lib or load()).w2v_attend_token(h, window, batch, pos, q, k, v, cache_k, cache_v, places, bias, o))
 
 
 def w2v_fourbit_pack(h, rows, n, d, row_stride, group, packed, scales):
-    return _check(h, load().w2v_fourbit_pack(h, rows, n, d, row_stride, group, packed, scales))
+    return _check(h, (_lib or load()).w2v_fourbit_pack(h, rows, n, d, row_stride, group, packed, scales))
 
 
 def w2v_fourbit_scores(h, x, m, x_stride, packed, scales, rows, d, group, out, out_stride):
-    return _check(h, load().w2v_fourbit_scores(h, x, m, x_stride, packed, scales, rows, d, group, out, out_stride))
+    return _check(h, (_lib or load()).w2v_fourbit_scores(h, x, m, x_stride, packed, scales, rows, d, group, out, out_stride))
 
 
 def w2v_set_step(h, step_id):
@@ -428,6 +428,8 @@ class W2V:
         with torch.cuda.device(self.device):
             self.U = torch.empty(self.vocab * self.row_stride, dtype=torch.float32, device=self.device)
             self.V = torch.empty(self.vocab * self.row_stride, dtype=torch.float32, device=self.device)
+            self._index = self.U.get_device()
+            self._windows = {}
             self.stream = torch.cuda.current_stream(self.device)
             self.h = w2v_create_shard(self.vocab, self.d_full, self.col_lo, self.col_hi, self.row_stride,
                                       self.seed, self.U, self.V, self.stream.cuda_stream)
@@ -529,28 +531,34 @@ class W2V:
         return ids.view(-1, K).cpu().numpy(), cs.view(-1, K).cpu().numpy()
 
     # ---- reader operators: tensors on this model's device, results on its stream ----
+    # (written for short calls: a small operator's time is what happens here)
     def _on(self, *tensors):
         for t in tensors:
-            if t is not None and t.device != self.U.device:
+            if t is not None and t.get_device() != self._index:
                 raise ValueError(f"tensor on {t.device}, this model is on {self.U.device}")
 
     @staticmethod
     def _type(t):
-        if t.dtype not in _TYPES:
+        code = _TYPES.get(t.dtype)
+        if code is None:
             raise TypeError(f"{t.dtype} is not one of float32, bfloat16, float16")
-        return _TYPES[t.dtype]
+        return code
 
-    def _weights(self, d, *tensors):
+    @staticmethod
+    def _weights(d, *tensors):
         for t in tensors:
-            if t.dtype != torch.float32 or t.shape != (d,) or not t.is_contiguous():
+            if t.dtype is not torch.float32 or t.dim() != 1 or t.numel() != d or not t.is_contiguous():
                 raise ValueError(f"weights must be contiguous float32 of shape ({d},)")
 
     @staticmethod
     def _rows(t):
         """A tensor whose last dimension is dense, as (rows, d, stride between rows, tensor)."""
+        if t.dim() == 2:
+            rows, d = t.shape
+            ld, one = t.stride()
+            if (one == 1 or d == 1) and (ld >= d or rows <= 1):
+                return rows, d, ld if ld >= d else d, t
         d = t.shape[-1]
-        if t.dim() == 2 and (t.stride(1) == 1 or d == 1) and (t.stride(0) >= d or t.shape[0] <= 1):
-            return t.shape[0], d, max(t.stride(0), d), t
         t = t.contiguous()
         return t.numel() // max(d, 1), d, d, t
 
@@ -559,33 +567,35 @@ class W2V:
         self._on(x, gamma, beta)
         rows, d, ld, xv = self._rows(x)
         self._weights(d, gamma, beta)
-        y = torch.empty(x.shape, dtype=out_dtype or x.dtype, device=x.device)
-        stats = torch.empty(2, rows, dtype=torch.float32, device=x.device)
+        y = x.new_empty(x.shape, dtype=out_dtype or x.dtype)
+        stats = gamma.new_empty((2, rows))
+        at = stats.data_ptr()
         w2v_layer_norm(self.h, rows, d, xv.data_ptr(), ld, self._type(x), gamma.data_ptr(), beta.data_ptr(), eps, y.data_ptr(), d,
-                       self._type(y), stats.data_ptr(), stats.data_ptr() + 4 * rows)
+                       self._type(y), at, at + 4 * rows)
         return y, (xv, gamma, stats, y.dtype, x.shape)
 
     def layer_norm_backward(self, dy, saved):
         """(dx, dgamma, dbeta) from dy and what layer_norm returned."""
         x, gamma, stats, y_dtype, shape = saved
         self._on(dy)
-        if dy.dtype != y_dtype or dy.shape != shape:
+        if dy.dtype is not y_dtype or dy.shape != shape:
             raise ValueError(f"dy must be {y_dtype} of shape {tuple(shape)}")
         rows, d, ld, dy = self._rows(dy)
         _, _, ldx, _ = self._rows(x)
-        dx = torch.empty(shape, dtype=x.dtype, device=x.device)
-        dw = torch.empty(2, d, dtype=torch.float32, device=x.device)
+        dx = x.new_empty(shape)
+        dw = gamma.new_empty((2, d))
+        at, to = stats.data_ptr(), dw.data_ptr()
         w2v_layer_norm_backward(self.h, rows, d, dy.data_ptr(), ld, _TYPES[y_dtype], x.data_ptr(), ldx, self._type(x),
-                                gamma.data_ptr(), stats.data_ptr(), stats.data_ptr() + 4 * rows, dx.data_ptr(), d,
-                                dw.data_ptr(), dw.data_ptr() + 4 * d)
+                                gamma.data_ptr(), at, at + 4 * rows, dx.data_ptr(), d, to, to + 4 * d)
         return dx, dw[0], dw[1]
 
     def sentence_spans(self, tokens):
         """[n, 2] int32: sentence bounds of every position of a token stream (-1 ends a sentence)."""
         self._on(tokens)
-        t = tokens if tokens.dtype == torch.int32 and tokens.is_contiguous() else tokens.to(torch.int32).contiguous()
-        spans = torch.empty(t.numel(), 2, dtype=torch.int32, device=t.device)
-        w2v_sentence_spans(self.h, t.data_ptr(), t.numel(), spans.data_ptr())
+        t = tokens if tokens.dtype is torch.int32 and tokens.is_contiguous() else tokens.to(torch.int32).contiguous()
+        n = t.numel()
+        spans = t.new_empty((n, 2))
+        w2v_sentence_spans(self.h, t.data_ptr(), n, spans.data_ptr())
         return spans
 
     @staticmethod
@@ -595,55 +605,68 @@ class W2V:
             raise ValueError(f"{what} must be [n, heads, head_dim]")
         n, heads, dim = t.shape
         width = heads * dim
-        if t.stride(2) == 1 and (heads == 1 or t.stride(1) == dim) and t.data_ptr() % 16 == 0:
+        ld, between, one = t.stride()
+        if one == 1 and (heads == 1 or between == dim) and t.data_ptr() % 16 == 0:
             if n <= 1:
                 return t, width
-            if t.stride(0) >= width and t.stride(0) % 8 == 0:
-                return t, t.stride(0)
+            if ld >= width and ld % 8 == 0:
+                return t, ld
         t = t.contiguous()
         return (t if t.data_ptr() % 16 == 0 else t.clone()), width
 
     def _window(self, q, k, v, bias, left, right, sinks, reach, two_sided, scale):
+        """The w2v_window of a call, made once for a set of values."""
         self._on(q, k, v, bias)
-        if not (q.dtype == k.dtype == v.dtype) or q.dtype not in (torch.bfloat16, torch.float16):
+        dtype = q.dtype
+        if k.dtype is not dtype or v.dtype is not dtype or dtype not in (torch.bfloat16, torch.float16):
             raise TypeError("q, k and v must all be bfloat16 or all float16")
-        if k.shape != v.shape or k.shape[0] != q.shape[0] or k.shape[-1] != q.shape[-1]:
+        qs, ks = q.shape, k.shape
+        if len(qs) != 3 or len(ks) != 3 or v.shape != ks or ks[0] != qs[0] or ks[2] != qs[2]:
             raise ValueError("q [n, heads, dim], k and v [n, kv_heads, dim] do not fit together")
-        if bias is not None and (bias.dtype != torch.float32 or bias.dim() != 2 or bias.shape[1] != q.shape[1] or not bias.is_contiguous()):
-            raise ValueError("bias must be contiguous float32 [buckets, heads]")
-        return Window(_TYPES[q.dtype], q.shape[1], k.shape[1], q.shape[2], left, right, sinks, 0 if bias is None else bias.shape[0],
-                      reach, int(two_sided), q.shape[2] ** -0.5 if scale is None else scale)
+        buckets = 0
+        if bias is not None:
+            if bias.dtype is not torch.float32 or bias.dim() != 2 or bias.shape[1] != qs[1] or not bias.is_contiguous():
+                raise ValueError("bias must be contiguous float32 [buckets, heads]")
+            buckets = bias.shape[0]
+        key = (dtype, qs[1], ks[1], qs[2], left, right, sinks, buckets, reach, two_sided, scale)
+        w = self._windows.get(key)
+        if w is None:
+            w = Window(_TYPES[dtype], qs[1], ks[1], qs[2], left, right, sinks, buckets, reach, int(two_sided),
+                       qs[2] ** -0.5 if scale is None else scale)
+            if len(self._windows) > 256:
+                self._windows.clear()
+            self._windows[key] = w
+        return w
 
     def attend(self, q, k, v, spans, bias=None, left=0, right=0, sinks=0, reach=128, two_sided=False, scale=None, train=False):
         """o [n, heads, dim] of attention over a window of the sentence (w2v_attend); with train=True
         (o, what attend_backward needs)."""
         w = self._window(q, k, v, bias, left, right, sinks, reach, two_sided, scale)
         n = q.shape[0]
-        if spans.dtype != torch.int32 or spans.shape != (n, 2) or not spans.is_contiguous():
+        if spans.dtype is not torch.int32 or spans.shape != (n, 2) or not spans.is_contiguous():
             raise ValueError(f"spans must be the contiguous int32 [{n}, 2] of sentence_spans")
         self._on(spans)
         (q, ldq), (k, ldk), (v, ldv) = self._heads(q, "q"), self._heads(k, "k"), self._heads(v, "v")
-        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        lse = torch.empty(q.shape[1], n, dtype=torch.float32, device=q.device) if train else None
+        o = q.new_empty(q.shape)
+        lse = q.new_empty((w.heads, n), dtype=torch.float32) if train else None
         w2v_attend(self.h, w, n, spans.data_ptr(), q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv,
-                   None if bias is None else bias.data_ptr(), o.data_ptr(), w.heads * w.head_dim,
-                   None if lse is None else lse.data_ptr())
+                   None if bias is None else bias.data_ptr(), o.data_ptr(), w.heads * w.head_dim, None if lse is None else lse.data_ptr())
         return (o, (w, spans, q, k, v, bias, o, lse)) if train else o
 
     def attend_backward(self, d_o, saved):
         """(dq, dk, dv, dbias) from d_o and what attend(train=True) returned; dbias is None without a bias."""
         w, spans, q, k, v, bias, o, lse = saved
         self._on(d_o)
-        if d_o.dtype != q.dtype or d_o.shape != q.shape:
+        if d_o.dtype is not q.dtype or d_o.shape != q.shape:
             raise ValueError(f"d_o must be {q.dtype} of shape {tuple(q.shape)}")
         d_o, ld_do = self._heads(d_o, "d_o")
         (q, ldq), (k, ldk), (v, ldv) = self._heads(q, "q"), self._heads(k, "k"), self._heads(v, "v")
-        dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+        dq, dk, dv = q.new_empty(q.shape), k.new_empty(k.shape), v.new_empty(v.shape)
         dbias = None if bias is None else torch.empty_like(bias)
         wq, wk = w.heads * w.head_dim, w.kv_heads * w.head_dim
         w2v_attend_backward(self.h, w, q.shape[0], spans.data_ptr(), q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv,
-                            None if bias is None else bias.data_ptr(), o.data_ptr(), wq, lse.data_ptr(), d_o.data_ptr(), ld_do, dq.data_ptr(), wq, dk.data_ptr(), wk, dv.data_ptr(), wk,
-                            None if dbias is None else dbias.data_ptr())
+                            None if bias is None else bias.data_ptr(), o.data_ptr(), wq, lse.data_ptr(), d_o.data_ptr(), ld_do,
+                            dq.data_ptr(), wq, dk.data_ptr(), wk, dv.data_ptr(), wk, None if dbias is None else dbias.data_ptr())
         return dq, dk, dv, dbias
 
     def attend_token(self, q, k, v, cache_k, cache_v, pos, bias=None, left=0, right=0, sinks=0, reach=128, two_sided=False, scale=None):
@@ -651,47 +674,48 @@ class W2V:
         caches [batch, places, kv_heads, dim] (w2v_attend_token)."""
         w = self._window(q, k, v, bias, left, right, sinks, reach, two_sided, scale)
         batch = q.shape[0]
-        if pos.dtype != torch.int32 or pos.shape != (batch,) or not pos.is_contiguous():
+        if pos.dtype is not torch.int32 or pos.shape != (batch,) or not pos.is_contiguous():
             raise ValueError(f"pos must be contiguous int32 of shape ({batch},)")
-        for c in (cache_k, cache_v):
-            if c.dtype != q.dtype or c.dim() != 4 or c.shape[0] != batch or c.shape[2:] != k.shape[1:] or not c.is_contiguous():
-                raise ValueError("caches must be contiguous [batch, places, kv_heads, dim] of the type of q")
-        if cache_k.shape != cache_v.shape:
+        shape = cache_k.shape
+        if cache_v.shape != shape:
             raise ValueError("cache_k and cache_v must have the same shape")
+        if len(shape) != 4 or shape[0] != batch or shape[2:] != k.shape[1:] or cache_k.dtype is not q.dtype or cache_v.dtype is not q.dtype or \
+                not cache_k.is_contiguous() or not cache_v.is_contiguous():
+            raise ValueError("caches must be contiguous [batch, places, kv_heads, dim] of the type of q")
         self._on(pos, cache_k, cache_v)
         q, k, v = q.contiguous(), k.contiguous(), v.contiguous()
-        o = torch.empty_like(q)
+        o = q.new_empty(q.shape)
         w2v_attend_token(self.h, w, batch, pos.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), cache_k.data_ptr(),
-                         cache_v.data_ptr(), cache_k.shape[1], None if bias is None else bias.data_ptr(), o.data_ptr())
+                         cache_v.data_ptr(), shape[1], None if bias is None else bias.data_ptr(), o.data_ptr())
         return o
 
     def fourbit_pack(self, rows, group=32):
         """(packed [n, 16 ceil(d/32)] uint8, scales [n, ceil(d/group)] bfloat16) of fp32 rows [n, d]."""
         self._on(rows)
-        if rows.dtype != torch.float32 or rows.dim() != 2:
+        if rows.dtype is not torch.float32 or rows.dim() != 2:
             raise ValueError("rows must be float32 [n, d]")
         n, d, ld, rows = self._rows(rows)
         if d < 1 or group < 1:
             raise ValueError("d and group must be positive")
-        packed = torch.empty(n, 16 * ((d + 31) // 32), dtype=torch.uint8, device=rows.device)
-        scales = torch.empty(n, (d + group - 1) // group, dtype=torch.bfloat16, device=rows.device)
+        packed = rows.new_empty((n, 16 * ((d + 31) // 32)), dtype=torch.uint8)
+        scales = rows.new_empty((n, (d + group - 1) // group), dtype=torch.bfloat16)
         w2v_fourbit_pack(self.h, rows.data_ptr(), n, d, ld, group, packed.data_ptr(), scales.data_ptr())
         return packed, scales
 
     def fourbit_scores(self, x, packed, scales, group=32):
         """[m, rows] fp32: products of m <= 8 fp32 vectors with every row of a table of fourbit_pack."""
         self._on(x, packed, scales)
-        if x.dtype != torch.float32 or x.dim() != 2:
+        if x.dtype is not torch.float32 or x.dim() != 2:
             raise ValueError("x must be float32 [m, d]")
         m, d, ld, x = self._rows(x)
         if d < 1 or group < 1:
             raise ValueError("d and group must be positive")
         n = packed.shape[0]
-        if packed.dtype != torch.uint8 or packed.shape != (n, 16 * ((d + 31) // 32)) or not packed.is_contiguous():
+        if packed.dtype is not torch.uint8 or packed.shape != (n, 16 * ((d + 31) // 32)) or not packed.is_contiguous():
             raise ValueError(f"packed must be contiguous uint8 [rows, {16 * ((d + 31) // 32)}] for d = {d}")
-        if scales.dtype != torch.bfloat16 or scales.shape != (n, (d + group - 1) // group) or not scales.is_contiguous():
+        if scales.dtype is not torch.bfloat16 or scales.shape != (n, (d + group - 1) // group) or not scales.is_contiguous():
             raise ValueError("scales must be contiguous bfloat16 [rows, ceil(d / group)]")
-        out = torch.empty(m, n, dtype=torch.float32, device=x.device)
+        out = x.new_empty((m, n))
         w2v_fourbit_scores(self.h, x.data_ptr(), m, ld, packed.data_ptr(), scales.data_ptr(), n, d, group, out.data_ptr(), max(n, 1))
         return out
 

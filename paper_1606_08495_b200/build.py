@@ -15,7 +15,7 @@ BUILD = os.path.join(HERE, "_build")
 CU_SOURCES = ["w2v_api.cu", "w2v_sampling.cu", "w2v_sgns.cu", "w2v_rows.cu", "w2v_shard.cu", "w2v_cbow.cu", "w2v_topk.cu", "w2v_topk_tc.cu", "w2v_probe.cu",
               "w2v_norm.cu", "w2v_norm_back.cu", "w2v_spans.cu", "w2v_attend.cu", "w2v_attend_back.cu", "w2v_attend_token.cu", "w2v_fourbit.cu", "w2v_reader_api.cu"]
 CPP_SOURCES = ["w2v_tables.cpp"]
-HEADERS = ["w2v_device.cuh", "w2v_internal.h", "w2v_sample.cuh", "w2v_handle.h", "w2v_reader.h", "w2v_types.cuh", "w2v_norm.cuh", "w2v_attend.cuh", "w2v_tc.cuh", "w2v_tma.h"]
+HEADERS = ["w2v_device.cuh", "w2v_internal.h", "w2v_sample.cuh", "w2v_handle.h", "w2v_reader.h", "w2v_types.cuh", "w2v_norm.cuh", "w2v_attend.cuh", "w2v_tc.cuh", "w2v_tma.h", "w2v_kernel_ready.h"]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

@@ -13,6 +13,7 @@
 #include <type_traits>
 
 #include "w2v_attend.cuh"
+#include "w2v_kernel_ready.h"
 
 namespace w2v {
 
@@ -412,12 +413,7 @@ int launch_attend_shape(const AttendParams &p, int *error, cudaStream_t s)
     using Sh = FwdShape<NB, SMALL>;
     int smem = Sh::kRing + 1024 + (int)(bias_entries(p.b) * sizeof(float));
     if (Sh::kBlocks == 1 && smem < 116 * 1024) smem = 116 * 1024;      // a second block would only wait for tensor memory
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return -1;
-    if (SMALL) {
-        // a block launched with fewer registers could never hand out the softmax's share
-        cudaFuncAttributes at;
-        if (cudaFuncGetAttributes(&at, kernel) != cudaSuccess || at.numRegs < kLaunchRegs) return -1;
-    }
+    if (!kernel_ready<attend_tc_kernel<T, NB, SMALL>>(SMALL ? kLaunchRegs : 0)) return -1;
     const uint64_t tiles = ((uint64_t)p.n + kAttendTile - 1) / kAttendTile;
     CUtensorMap q, k, v;
     const bool bf16 = std::is_same<T, __nv_bfloat16>::value;

@@ -15,6 +15,7 @@
 #include <type_traits>
 
 #include "w2v_attend.cuh"
+#include "w2v_kernel_ready.h"
 
 namespace w2v {
 
@@ -831,12 +832,7 @@ int launch_role(const AttendParams &p, uint32_t tiles, int *error, cudaStream_t 
     int smem = Sh::kRing + 2 * Sh::kOwn + (ROLE == 0 ? (sink_bytes > o_bytes ? sink_bytes : o_bytes) : 0) + 1024 +
                (int)(4 * (((entries + 3u) & ~3u) + (ROLE == 1 ? Sh::kSoft / 32 * entries : 256u)));
     if (!SMALL && smem < 116 * 1024) smem = 116 * 1024;              // a second block would only wait for tensor memory
-    if (SMALL) {
-        // a block launched with fewer registers could never hand out the softmax's share
-        cudaFuncAttributes at;
-        if (cudaFuncGetAttributes(&at, kernel) != cudaSuccess || at.numRegs < kBackLaunchRegs) return -1;
-    }
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return -1;
+    if (!kernel_ready<attend_back_kernel<T, NB, ROLE, SMALL>>(SMALL ? kBackLaunchRegs : 0)) return -1;
     CUtensorMap x, y, a0, a1, o;
     const bool bf16 = std::is_same<T, __nv_bfloat16>::value;
     const uint64_t n = (uint64_t)p.n;

@@ -21,6 +21,7 @@
 #include <cooperative_groups.h>
 
 #include "w2v_attend.cuh"
+#include "w2v_kernel_ready.h"
 
 namespace cg = cooperative_groups;
 
@@ -264,7 +265,7 @@ int launch_token_shape(const TokenParams &p, int sms, cudaStream_t s)
     const uint32_t reach = p.b.n ? (uint32_t)p.b.start[p.b.n - 1] + 1 : 0;
     const size_t smem = sizeof(float) * (2 * rows + (size_t)rows * p.dim + kTokWarps * rows * (2 + (size_t)p.dim) + (size_t)reach * kTokRows);
     auto kernel = attend_token_kernel<T, NB, HI>;
-    if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return -1;
+    if (smem > 48 * 1024 && !kernel_ready<attend_token_kernel<T, NB, HI>>()) return -1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((uint32_t)(items * splits));
     cfg.blockDim = dim3(kTokThreads);

@@ -5,6 +5,7 @@
 // range: trained vectors are of the order 1e-3 to 1, a sum of squares less); scales are [rows][ceil(d/group)].
 #include "w2v_device.cuh"
 #include "w2v_reader.h"
+#include "w2v_kernel_ready.h"
 #include "w2v_tc.cuh"
 #include "w2v_types.cuh"
 
@@ -278,7 +279,7 @@ int launch_scores(const float *x, uint32_t m, uint64_t ldx, const unsigned char 
     const uint32_t unit = ((words + parts - 1) / parts + PER - 1) / PER * PER;
     const uint32_t most = kQFragBytes / (512 * NT) / unit * unit, piece = words <= most ? words : most;
     const int smem = (int)(piece * 512 * NT + kQWarps * 2 * kQRows * (unit | 1u) * 16 + kQWarps * kQRows * kQWords * 4);
-    if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return -1;
+    if (smem > 48 * 1024 && !kernel_ready<fourbit_scores_kernel<NT, PER>>()) return -1;
     const uint64_t want = (rows + kQRows * kQWarps - 1) / (kQRows * kQWarps), full = (uint64_t)sms * (smem <= 112 * 1024 ? 2 : 1);
     kernel<<<(uint32_t)(want < full ? want : full), kQWarps * 32, smem, s>>>(x, m, ldx, packed, scales, rows, d, out, ld_out, piece, unit);
     return cudaPeekAtLastError() == cudaSuccess ? 1 : -1;
