@@ -872,6 +872,7 @@ int32_t w2v_sync(w2v_handle *h)
             if (flag & 2)
                 return fail(h, W2V_ERR_CUDA, "a peer barrier gave up waiting for another shard; the step that followed it "
                                              "used incomplete dot products");
+            if (flag & 16) return fail(h, W2V_ERR_CUDA, "a layer-norm block gave up waiting; its results are incomplete");
             if (flag & 8) return fail(h, W2V_ERR_CUDA, "an attention block gave up waiting; its results are incomplete");
             return fail(h, W2V_ERR_CUDA, "a tensor-core retrieval block gave up waiting; its results are incomplete");
         }

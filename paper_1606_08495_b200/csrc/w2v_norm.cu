@@ -70,12 +70,143 @@ norm_kernel(NormParams p, uint32_t gw, uint32_t groups)
     }
 }
 
+// The same for rows that arrive through a ring (see w2v_norm.cuh): `stages` units per group.
+template <typename TX, typename TY, int E, int NV>
+__global__ void __launch_bounds__(512)
+norm_ring_kernel(NormParams p, uint32_t gw, uint32_t groups, uint32_t stages, uint32_t mode, int *error)
+{
+    extern __shared__ __align__(16) unsigned char ring[];
+    __shared__ float slot[64 * kNormUnit];
+    __shared__ uint64_t full[8][4];
+    __shared__ int abort_flag;
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t group = warp / gw, wig = warp - group * gw, gl = wig * 32 + lane;
+    const uint32_t row_bytes = p.d * sizeof(TX), pitch = norm_pitch(mode, p.d, sizeof(TX)), unit_bytes = (kNormUnit * pitch + 15u) & ~15u;
+    const TX *x = static_cast<const TX *>(p.x);
+    TY *y = static_cast<TY *>(p.y);
+    unsigned char *mine = ring + group * stages * unit_bytes;
+    const float inv_d = 1.0f / (float)p.d;
+    const uint64_t units = (p.rows + kNormUnit - 1) / kNormUnit, step = (uint64_t)gridDim.x * groups;
+    uint64_t u = (uint64_t)blockIdx.x * groups + group;
+    if (threadIdx.x == 0) {
+        for (uint32_t g = 0; g < groups; ++g)
+            for (uint32_t s = 0; s < stages; ++s) mbar_init(&full[g][s], 1);
+        abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_async_proxy();
+    }
+    __syncthreads();
+    auto issue = [&](uint64_t unit, uint32_t stage) {                 // by the group's first lane
+        const uint64_t r = unit * kNormUnit;
+        const uint32_t n = (uint32_t)min((uint64_t)kNormUnit, p.rows - r), dst = smem_addr(mine + stage * unit_bytes);
+        mbar_expect(&full[group][stage], norm_copy(mode, dst, reinterpret_cast<const char *>(x), p.ldx * sizeof(TX), row_bytes, pitch, r, n, &full[group][stage], false));
+        norm_copy(mode, dst, reinterpret_cast<const char *>(x), p.ldx * sizeof(TX), row_bytes, pitch, r, n, &full[group][stage], true);
+    };
+    if (gl == 0)
+        for (uint32_t s = 0; s < stages; ++s) if (u + s * step < units) issue(u + s * step, s);
+    float gamma[NV * E], beta[NV * E];
+    norm_weights_load<E, NV>(gamma, p.gamma, gl, gw, p.d);
+    norm_weights_load<E, NV>(beta, p.beta, gl, gw, p.d);
+    uint32_t flip = 0, stage = 0, phase = 0;
+    for (; u < units; u += step) {
+        const uint64_t r = u * kNormUnit;
+        const uint32_t n = (uint32_t)min((uint64_t)kNormUnit, p.rows - r);
+        unsigned char *rows = mine + stage * unit_bytes;
+        mbar_wait(&full[group][stage], phase, &abort_flag);           // once it has given up the rest runs through on whatever is there
+        if (mode == kCopyUnits && n < kNormUnit) {
+            norm_copy_tail<TX>(mode, rows, x + r * p.ldx, p.d, n, gl, gw * 32);
+            group_barrier(gw, group);
+        }
+        float v[kNormUnit][NV * E], s[kNormUnit], q[kNormUnit];
+#pragma unroll
+        for (int i = 0; i < kNormUnit; ++i) {
+            s[i] = q[i] = 0.f;
+            Pack<TX, E> t[NV];
+            norm_row_load<TX, E, NV>(t, reinterpret_cast<const TX *>(rows + i * pitch), gl, gw, p.d);
+#pragma unroll
+            for (int c = 0; c < NV; ++c)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    v[i][c * E + e] = to_f32(t[c].e[e]);
+                    s[i] += v[i][c * E + e];
+                }
+        }
+        group_sum<kNormUnit>(s, gw, wig, group, lane, slot, flip);
+        flip ^= 1u;
+        if (gw == 1) __syncwarp();                                    // everybody has read the unit
+        if (gl == 0 && u + stages * step < units) issue(u + stages * step, stage);
+        if (++stage == stages) { stage = 0; phase ^= 1u; }
+#pragma unroll
+        for (int i = 0; i < kNormUnit; ++i) {
+            s[i] *= inv_d;
+#pragma unroll
+            for (int c = 0; c < NV; ++c)
+                if ((gl + c * 32u * gw) * E < p.d) {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        v[i][c * E + e] -= s[i];
+                        q[i] = fmaf(v[i][c * E + e], v[i][c * E + e], q[i]);
+                    }
+                }
+        }
+        group_sum<kNormUnit>(q, gw, wig, group, lane, slot, flip);
+        flip ^= 1u;
+#pragma unroll
+        for (int i = 0; i < kNormUnit; ++i) {
+            if ((uint32_t)i >= n) break;
+            const float rstd = rsqrtf(q[i] * inv_d + p.eps);          // 2 units in the last place
+            if (gl == 0) {
+                if (p.mean) p.mean[r + i] = s[i];
+                if (p.rstd) p.rstd[r + i] = rstd;
+            }
+#pragma unroll
+            for (int c = 0; c < NV; ++c) {
+                const uint32_t at = (gl + c * 32u * gw) * E;
+                if (at < p.d) {
+                    Pack<TY, E> t;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) t.e[e] = from_f32<TY>(fmaf(v[i][c * E + e] * rstd, gamma[c * E + e], beta[c * E + e]));
+                    store_pack<TY, E>(y + (r + i) * p.ldy + at, t);
+                }
+            }
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x == 0 && abort_flag) atomicOr(error, kErrRing);
+}
+
+template <typename TX, typename TY, int E, int NV>
+int launch_norm_ring(const NormParams &p, const NormShape &sh, uint32_t stages, uint32_t mode, size_t smem, int *error, int sms, cudaStream_t s)
+{
+    if (!kernel_ready<norm_ring_kernel<TX, TY, E, NV>>()) return -1;
+    const uint32_t threads = sh.gw * sh.groups * 32;
+    const uint64_t units = (p.rows + kNormUnit - 1) / kNormUnit, want = (units + sh.groups - 1) / sh.groups, most = (uint64_t)sms * (512u / threads ? 512u / threads : 1u);
+    norm_ring_kernel<TX, TY, E, NV><<<(uint32_t)(want < most ? want : most), threads, smem, s>>>(p, sh.gw, sh.groups, stages, mode, error);
+    return cudaPeekAtLastError() == cudaSuccess ? 1 : -1;
+}
+
 template <typename TX, typename TY>
-int launch_norm_typed(const NormParams &p, int sms, cudaStream_t s)
+int launch_norm_typed(const NormParams &p, int *error, int sms, cudaStream_t s)
 {
     uint32_t e = widest_access(p.d, sizeof(TX), p.ldx, p.x, 16u / sizeof(TX));
     e = widest_access(p.d, sizeof(TY), p.ldy, p.y, e);
     const NormShape sh = norm_shape(p.d, e);
+    constexpr uint32_t kE = 16 / sizeof(TX);
+    // Rows enough to keep a ring going (fewer are there sooner by direct loads), and copyable ones
+    const uint32_t mode = norm_copy_mode(p.x, p.ldx, p.d, sizeof(TX));
+    if (e == kE && mode != kCopyNot && p.rows >= (uint64_t)sms * 16) {
+        const size_t unit = (kNormUnit * norm_pitch(mode, p.d, sizeof(TX)) + 15u) & ~15u, most = 104 * 1024 / (512u / (sh.gw * sh.groups * 32) ? 512u / (sh.gw * sh.groups * 32) : 1u);
+        uint32_t stages = 4;
+        while (stages > 1 && unit * sh.groups * stages > most) --stages;
+        const size_t smem = unit * sh.groups * stages;
+        if (smem <= most && stages > 1) {
+            if constexpr (kE == 8) return sh.nv <= 1 ? launch_norm_ring<TX, TY, 8, 1>(p, sh, stages, mode, smem, error, sms, s) : launch_norm_ring<TX, TY, 8, 2>(p, sh, stages, mode, smem, error, sms, s);
+            else return sh.nv <= 1 ? launch_norm_ring<TX, TY, 4, 1>(p, sh, stages, mode, smem, error, sms, s)
+                        : sh.nv == 2 ? launch_norm_ring<TX, TY, 4, 2>(p, sh, stages, mode, smem, error, sms, s)
+                        : sh.nv == 3 ? launch_norm_ring<TX, TY, 4, 3>(p, sh, stages, mode, smem, error, sms, s)
+                                     : launch_norm_ring<TX, TY, 4, 4>(p, sh, stages, mode, smem, error, sms, s);
+        }
+    }
     const uint32_t threads = sh.gw * sh.groups * 32;
     const uint64_t want = (p.rows + sh.groups - 1) / sh.groups, most = (uint64_t)sms * (1024u / threads);
     const uint32_t grid = (uint32_t)(want < most ? want : most);
@@ -95,14 +226,14 @@ int launch_norm_typed(const NormParams &p, int sms, cudaStream_t s)
     return cudaPeekAtLastError() == cudaSuccess ? 1 : -1;
 }
 
-int launch_norm(const NormParams &p, uint32_t xt, uint32_t yt, int sms, cudaStream_t s)
+int launch_norm(const NormParams &p, uint32_t xt, uint32_t yt, int *error, int sms, cudaStream_t s)
 {
     if (p.rows == 0) return 0;
-    if (xt == kBF16) return launch_norm_typed<__nv_bfloat16, __nv_bfloat16>(p, sms, s);
-    if (xt == kF16) return launch_norm_typed<__half, __half>(p, sms, s);
-    if (yt == kBF16) return launch_norm_typed<float, __nv_bfloat16>(p, sms, s);
-    if (yt == kF16) return launch_norm_typed<float, __half>(p, sms, s);
-    return launch_norm_typed<float, float>(p, sms, s);
+    if (xt == kBF16) return launch_norm_typed<__nv_bfloat16, __nv_bfloat16>(p, error, sms, s);
+    if (xt == kF16) return launch_norm_typed<__half, __half>(p, error, sms, s);
+    if (yt == kBF16) return launch_norm_typed<float, __nv_bfloat16>(p, error, sms, s);
+    if (yt == kF16) return launch_norm_typed<float, __half>(p, error, sms, s);
+    return launch_norm_typed<float, float>(p, error, sms, s);
 }
 
 }  // namespace w2v

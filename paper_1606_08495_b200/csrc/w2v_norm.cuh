@@ -5,7 +5,9 @@
 // a row belongs to lane c mod 32 gw.  E is the widest access that row length, strides and base addresses allow.
 #pragma once
 #include "w2v_device.cuh"
+#include "w2v_kernel_ready.h"
 #include "w2v_reader.h"
+#include "w2v_tc.cuh"
 #include "w2v_types.cuh"
 
 namespace w2v {
@@ -70,6 +72,56 @@ __device__ __forceinline__ void norm_weights_load(float (&w)[NV * E], const floa
             for (int e = 0; e < E; ++e) w[c * E + e] = at < d ? __ldg(from + at + e) : 0.f;
         }
     }
+}
+
+// ---- rows through a ring in shared memory ------------------------------------------------------------
+// A row in registers is a row's bytes in flight only for as long as it takes to arrive, and the registers of a lane
+// hold few of them.  Where rows can be copied in bulk (16-byte starts and lengths), every group of warps has a ring of
+// units of kNormUnit consecutive rows that are copied in the background, and works on a unit at a time: the
+// barrier and the lane sums of its rows are shared.
+constexpr int kNormUnit = 2;
+
+// How an array of rows is copied: a row at a time (row starts and lengths are multiples of 16 bytes), or a unit at a time
+// (rows without gaps, whose units are), or not.
+enum : uint32_t { kCopyRows = 0, kCopyUnits = 1, kCopyNot = 2 };
+inline uint32_t norm_copy_mode(const void *p, uint64_t ld, uint32_t d, uint32_t size)
+{
+    if (reinterpret_cast<uintptr_t>(p) & 15u) return kCopyNot;
+    if ((ld * size) % 16 == 0 && (d * size) % 16 == 0) return kCopyRows;
+    return ld == d && (kNormUnit * d * size) % 16 == 0 ? kCopyUnits : kCopyNot;
+}
+// Bytes between the rows of a unit in shared memory.
+inline __host__ __device__ uint32_t norm_pitch(uint32_t mode, uint32_t d, uint32_t size) { return mode == kCopyRows ? (d * size + 15u) & ~15u : d * size; }
+
+__device__ __forceinline__ void norm_bulk(uint32_t dst, const void *src, uint32_t bytes, uint64_t *bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(smem_addr(bar)) : "memory");
+}
+// Rows [r, r + n) of an array to shared memory (one lane; returns the bytes to expect).  A unit that is copied whole but is
+// cut off by the end of the array is left to norm_copy_tail.
+__device__ __forceinline__ uint32_t norm_copy(uint32_t mode, uint32_t dst, const char *base, uint64_t ld_bytes, uint32_t row_bytes, uint32_t pitch,
+                                              uint64_t r, uint32_t n, uint64_t *bar, bool issue)
+{
+    if (mode == kCopyUnits) {
+        if (n < kNormUnit) return 0;
+        if (issue) norm_bulk(dst, base + r * ld_bytes, kNormUnit * row_bytes, bar);
+        return kNormUnit * row_bytes;
+    }
+    if (issue) for (uint32_t i = 0; i < n; ++i) norm_bulk(dst + i * pitch, base + (r + i) * ld_bytes, row_bytes, bar);
+    return n * row_bytes;
+}
+// The cut-off unit of an array that is copied in units, by the lanes of a group.
+template <typename T>
+__device__ __forceinline__ void norm_copy_tail(uint32_t mode, unsigned char *dst, const T *row, uint32_t d, uint32_t n, uint32_t gl, uint32_t lanes)
+{
+    if (mode != kCopyUnits || n >= kNormUnit) return;
+    for (uint32_t i = gl; i < n * d; i += lanes) reinterpret_cast<T *>(dst)[i] = row[i];
+}
+__device__ __forceinline__ void group_barrier(uint32_t gw, uint32_t group)
+{
+    if (gw == 1) __syncwarp();
+    else asm volatile("bar.sync %0, %1;" ::"r"(group + 1u), "r"(gw * 32u) : "memory");
 }
 
 struct NormShape {

@@ -8,6 +8,44 @@
 
 namespace w2v {
 
+// The block's groups add up in shared memory ([groups - 1][2][d]), group 0 writes the block's row.
+template <int E, int NV>
+__device__ __forceinline__ void norm_block_sums(const NormParams &p, const float (&dg)[NV * E], const float (&db)[NV * E], float *sums,
+                                                uint32_t gw, uint32_t group, uint32_t groups, uint32_t gl)
+{
+    float *out = p.part + (uint64_t)blockIdx.x * 2 * p.d;
+    if (group > 0) {
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+            const uint32_t at = (gl + c * 32u * gw) * E;
+            if (at < p.d)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    sums[(group - 1) * 2 * p.d + at + e] = dg[c * E + e];
+                    sums[(group - 1) * 2 * p.d + p.d + at + e] = db[c * E + e];
+                }
+        }
+    }
+    __syncthreads();
+    if (group == 0) {
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+            const uint32_t at = (gl + c * 32u * gw) * E;
+            if (at < p.d)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    float a = dg[c * E + e], b = db[c * E + e];
+                    for (uint32_t k = 0; k + 1 < groups; ++k) {
+                        a += sums[k * 2 * p.d + at + e];
+                        b += sums[k * 2 * p.d + p.d + at + e];
+                    }
+                    out[at + e] = a;
+                    out[p.d + at + e] = b;
+                }
+        }
+    }
+}
+
 template <typename TX, typename TY, int E, int NV>
 __global__ void __launch_bounds__(512)
 norm_backward_kernel(NormParams p, uint32_t gw, uint32_t groups)
@@ -74,38 +112,122 @@ norm_backward_kernel(NormParams p, uint32_t gw, uint32_t groups)
             }
         }
     }
-    // the block's groups add up in shared memory, group 0 writes the block's row
-    float *out = p.part + (uint64_t)blockIdx.x * 2 * p.d;
-    if (group > 0) {
-#pragma unroll
-        for (int c = 0; c < NV; ++c) {
-            const uint32_t at = (gl + c * 32u * gw) * E;
-            if (at < p.d)
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    sums[(group - 1) * 2 * p.d + at + e] = dg[c * E + e];
-                    sums[(group - 1) * 2 * p.d + p.d + at + e] = db[c * E + e];
-                }
-        }
+    norm_block_sums<E, NV>(p, dg, db, sums, gw, group, groups, gl);
+}
+
+// The same for rows that arrive through a ring (see w2v_norm.cuh): `stages` units of x and dy per group.  A unit is read
+// twice from shared memory, for the sums and for dx.
+template <typename TX, typename TY, int E, int NV>
+__global__ void __launch_bounds__(512)
+norm_backward_ring_kernel(NormParams p, uint32_t gw, uint32_t groups, uint32_t stages, uint32_t mode_x, uint32_t mode_y, int *error)
+{
+    extern __shared__ __align__(16) unsigned char ring[];
+    __shared__ float slot[128 * kNormUnit];
+    __shared__ uint64_t full[8][4];
+    __shared__ int abort_flag;
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t group = warp / gw, wig = warp - group * gw, gl = wig * 32 + lane;
+    const uint32_t pitch_x = norm_pitch(mode_x, p.d, sizeof(TX)), pitch_y = norm_pitch(mode_y, p.d, sizeof(TY));
+    const uint32_t x_bytes = (kNormUnit * pitch_x + 15u) & ~15u, unit_bytes = x_bytes + ((kNormUnit * pitch_y + 15u) & ~15u);
+    const TX *x = static_cast<const TX *>(p.x);
+    const TY *dy = static_cast<const TY *>(p.dy);
+    TX *dx = static_cast<TX *>(p.dx);
+    unsigned char *mine = ring + group * stages * unit_bytes;
+    const float inv_d = 1.0f / (float)p.d;
+    const uint64_t units = (p.rows + kNormUnit - 1) / kNormUnit, step = (uint64_t)gridDim.x * groups;
+    uint64_t u = (uint64_t)blockIdx.x * groups + group;
+    if (threadIdx.x == 0) {
+        for (uint32_t g = 0; g < groups; ++g)
+            for (uint32_t s = 0; s < stages; ++s) mbar_init(&full[g][s], 1);
+        abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_async_proxy();
     }
     __syncthreads();
-    if (group == 0) {
+    auto issue = [&](uint64_t unit, uint32_t stage) {                 // by the group's first lane
+        const uint64_t r = unit * kNormUnit;
+        const uint32_t n = (uint32_t)min((uint64_t)kNormUnit, p.rows - r), dst = smem_addr(mine + stage * unit_bytes);
+        uint64_t *bar = &full[group][stage];
+        const char *xb = reinterpret_cast<const char *>(x), *yb = reinterpret_cast<const char *>(dy);
+        auto both = [&](bool now) {
+            return norm_copy(mode_x, dst, xb, p.ldx * sizeof(TX), p.d * sizeof(TX), pitch_x, r, n, bar, now) +
+                   norm_copy(mode_y, dst + x_bytes, yb, p.ldy * sizeof(TY), p.d * sizeof(TY), pitch_y, r, n, bar, now);
+        };
+        mbar_expect(bar, both(false));
+        both(true);
+    };
+    if (gl == 0)
+        for (uint32_t s = 0; s < stages; ++s) if (u + s * step < units) issue(u + s * step, s);
+    float gamma[NV * E], dg[NV * E], db[NV * E];
+    norm_weights_load<E, NV>(gamma, p.gamma, gl, gw, p.d);
 #pragma unroll
-        for (int c = 0; c < NV; ++c) {
-            const uint32_t at = (gl + c * 32u * gw) * E;
-            if (at < p.d)
+    for (int i = 0; i < NV * E; ++i) dg[i] = db[i] = 0.f;
+    uint32_t flip = 0, stage = 0, phase = 0;
+    for (; u < units; u += step) {
+        const uint64_t r = u * kNormUnit;
+        const uint32_t n = (uint32_t)min((uint64_t)kNormUnit, p.rows - r);
+        unsigned char *rows_x = mine + stage * unit_bytes, *rows_y = rows_x + x_bytes;
+        float mean[kNormUnit], rstd[kNormUnit], t[2 * kNormUnit];
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    float a = dg[c * E + e], b = db[c * E + e];
-                    for (uint32_t k = 0; k + 1 < groups; ++k) {
-                        a += sums[k * 2 * p.d + at + e];
-                        b += sums[k * 2 * p.d + p.d + at + e];
-                    }
-                    out[at + e] = a;
-                    out[p.d + at + e] = b;
+        for (int i = 0; i < kNormUnit; ++i) {
+            const uint64_t at = min(r + i, p.rows - 1);
+            mean[i] = __ldg(p.mean + at);
+            rstd[i] = (uint32_t)i < n ? __ldg(p.rstd + at) : 0.f;
+            t[2 * i] = t[2 * i + 1] = 0.f;
+        }
+        mbar_wait(&full[group][stage], phase, &abort_flag);           // once it has given up the rest runs through on whatever is there
+        if (n < kNormUnit && (mode_x == kCopyUnits || mode_y == kCopyUnits)) {
+            norm_copy_tail<TX>(mode_x, rows_x, x + r * p.ldx, p.d, n, gl, gw * 32);
+            norm_copy_tail<TY>(mode_y, rows_y, dy + r * p.ldy, p.d, n, gl, gw * 32);
+            group_barrier(gw, group);
+        }
+#pragma unroll
+        for (int i = 0; i < kNormUnit; ++i) {
+            if ((uint32_t)i >= n) break;                              // what a cut-off unit lacks is not in shared memory
+            Pack<TX, E> xc[NV];
+            Pack<TY, E> yc[NV];
+            norm_row_load<TX, E, NV>(xc, reinterpret_cast<const TX *>(rows_x + i * pitch_x), gl, gw, p.d);
+            norm_row_load<TY, E, NV>(yc, reinterpret_cast<const TY *>(rows_y + i * pitch_y), gl, gw, p.d);
+#pragma unroll
+            for (int c = 0; c < NV; ++c)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {                         // past the row's end dy and gamma are zero
+                    const float h = (to_f32(xc[c].e[e]) - mean[i]) * rstd[i], w = to_f32(yc[c].e[e]), g = w * gamma[c * E + e];
+                    dg[c * E + e] = fmaf(w, h, dg[c * E + e]);
+                    db[c * E + e] += w;
+                    t[2 * i] += g;
+                    t[2 * i + 1] = fmaf(g, h, t[2 * i + 1]);
                 }
         }
+        group_sum<2 * kNormUnit>(t, gw, wig, group, lane, slot, flip);
+        flip ^= 1u;
+#pragma unroll
+        for (int i = 0; i < kNormUnit; ++i) {
+            if ((uint32_t)i >= n) break;
+            const float ma = t[2 * i] * inv_d, mb = t[2 * i + 1] * inv_d;
+#pragma unroll
+            for (int c = 0; c < NV; ++c) {
+                const uint32_t at = (gl + c * 32u * gw) * E;
+                if (at < p.d) {
+                    const Pack<TX, E> xc = load_pack<TX, E>(reinterpret_cast<const TX *>(rows_x + i * pitch_x) + at);
+                    const Pack<TY, E> yc = load_pack<TY, E>(reinterpret_cast<const TY *>(rows_y + i * pitch_y) + at);
+                    Pack<TX, E> o;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        const float h = (to_f32(xc.e[e]) - mean[i]) * rstd[i], g = to_f32(yc.e[e]) * gamma[c * E + e];
+                        o.e[e] = from_f32<TX>(rstd[i] * (g - ma - h * mb));
+                    }
+                    store_pack<TX, E>(dx + (r + i) * p.ld_dx + at, o);
+                }
+            }
+        }
+        group_barrier(gw, group);                                     // everybody has read the unit
+        if (gl == 0 && u + stages * step < units) issue(u + stages * step, stage);
+        if (++stage == stages) { stage = 0; phase ^= 1u; }
     }
+    __syncthreads();
+    if (threadIdx.x == 0 && abort_flag) atomicOr(error, kErrRing);
+    norm_block_sums<E, NV>(p, dg, db, reinterpret_cast<float *>(ring), gw, group, groups, gl);
 }
 
 // Column sums of the partial rows: 32 columns per block, 32 threads down each column.
@@ -133,13 +255,41 @@ uint32_t norm_backward_blocks(uint64_t rows, uint32_t d, int sms)
     return (uint32_t)(want < most ? want : most);
 }
 
+template <typename TX, typename TY, int E, int NV>
+int launch_back_ring(const NormParams &p, const NormShape &sh, uint32_t stages, uint32_t mode_x, uint32_t mode_y, size_t smem, uint32_t blocks,
+                     int *error, cudaStream_t s)
+{
+    if (!kernel_ready<norm_backward_ring_kernel<TX, TY, E, NV>>()) return -1;
+    norm_backward_ring_kernel<TX, TY, E, NV><<<blocks, sh.gw * sh.groups * 32, smem, s>>>(p, sh.gw, sh.groups, stages, mode_x, mode_y, error);
+    return cudaPeekAtLastError() == cudaSuccess ? 1 : -1;
+}
+
 template <typename TX, typename TY>
-int launch_typed(const NormParams &p, uint32_t blocks, cudaStream_t s)
+int launch_typed(const NormParams &p, uint32_t blocks, int *error, int sms, cudaStream_t s)
 {
     uint32_t e = widest_access(p.d, sizeof(TX), p.ldx, p.x, 16u / sizeof(TX));
     e = widest_access(p.d, sizeof(TX), p.ld_dx, p.dx, e);
     e = widest_access(p.d, sizeof(TY), p.ldy, p.dy, e);
     const NormShape sh = norm_shape(p.d, e);
+    constexpr uint32_t kE = 16 / sizeof(TX);
+    // rows enough to keep a ring going (fewer are there sooner by direct loads), and copyable ones
+    const uint32_t mode_x = norm_copy_mode(p.x, p.ldx, p.d, sizeof(TX)), mode_y = norm_copy_mode(p.dy, p.ldy, p.d, sizeof(TY));
+    if (e == kE && mode_x != kCopyNot && mode_y != kCopyNot && p.rows >= (uint64_t)sms * 16) {
+        const uint32_t per_sm = 512u / (sh.gw * sh.groups * 32) ? 512u / (sh.gw * sh.groups * 32) : 1u;
+        const size_t unit = ((kNormUnit * norm_pitch(mode_x, p.d, sizeof(TX)) + 15u) & ~15u) + ((kNormUnit * norm_pitch(mode_y, p.d, sizeof(TY)) + 15u) & ~15u);
+        const size_t most = 216 * 1024 / per_sm, add = (size_t)(sh.groups - 1) * 2 * p.d * sizeof(float);
+        uint32_t stages = 4;
+        while (stages > 1 && unit * sh.groups * stages > most) --stages;
+        const size_t smem = unit * sh.groups * stages > add ? unit * sh.groups * stages : add;       // the ring, then the block's sums
+        if (smem <= most && stages > 1) {
+            if constexpr (kE == 8) return sh.nv <= 1 ? launch_back_ring<TX, TY, 8, 1>(p, sh, stages, mode_x, mode_y, smem, blocks, error, s)
+                                                      : launch_back_ring<TX, TY, 8, 2>(p, sh, stages, mode_x, mode_y, smem, blocks, error, s);
+            else return sh.nv <= 1 ? launch_back_ring<TX, TY, 4, 1>(p, sh, stages, mode_x, mode_y, smem, blocks, error, s)
+                        : sh.nv == 2 ? launch_back_ring<TX, TY, 4, 2>(p, sh, stages, mode_x, mode_y, smem, blocks, error, s)
+                        : sh.nv == 3 ? launch_back_ring<TX, TY, 4, 3>(p, sh, stages, mode_x, mode_y, smem, blocks, error, s)
+                                     : launch_back_ring<TX, TY, 4, 4>(p, sh, stages, mode_x, mode_y, smem, blocks, error, s);
+        }
+    }
     const uint32_t threads = sh.gw * sh.groups * 32, smem = (sh.groups - 1) * 2 * p.d * sizeof(float);
 #define W2V_NORM(E, NV) norm_backward_kernel<TX, TY, E, NV><<<blocks, threads, smem, s>>>(p, sh.gw, sh.groups)
     if constexpr (sizeof(TX) == 2) {
@@ -158,15 +308,15 @@ int launch_typed(const NormParams &p, uint32_t blocks, cudaStream_t s)
 }
 
 int launch_norm_backward(const NormParams &p, uint32_t xt, uint32_t yt, float *dgamma, float *dbeta, uint32_t blocks,
-                         cudaStream_t s)
+                         int *error, int sms, cudaStream_t s)
 {
     int k = 0;
     if (blocks) {
-        k = xt == kBF16 ? launch_typed<__nv_bfloat16, __nv_bfloat16>(p, blocks, s)
-            : xt == kF16 ? launch_typed<__half, __half>(p, blocks, s)
-            : yt == kBF16 ? launch_typed<float, __nv_bfloat16>(p, blocks, s)
-            : yt == kF16 ? launch_typed<float, __half>(p, blocks, s)
-                         : launch_typed<float, float>(p, blocks, s);
+        k = xt == kBF16 ? launch_typed<__nv_bfloat16, __nv_bfloat16>(p, blocks, error, sms, s)
+            : xt == kF16 ? launch_typed<__half, __half>(p, blocks, error, sms, s)
+            : yt == kBF16 ? launch_typed<float, __nv_bfloat16>(p, blocks, error, sms, s)
+            : yt == kF16 ? launch_typed<float, __half>(p, blocks, error, sms, s)
+                         : launch_typed<float, float>(p, blocks, error, sms, s);
         if (k < 0) return -1;
     }
     norm_weights_kernel<<<(2 * p.d + 31) / 32, 1024, 0, s>>>(p.part, blocks, p.d, dgamma, dbeta);

@@ -25,9 +25,10 @@ struct NormParams {
 constexpr uint32_t kNormMaxD = 8192;
 // Blocks of the backward kernel (and so rows of `part`).
 uint32_t norm_backward_blocks(uint64_t rows, uint32_t d, int sms);
-int launch_norm(const NormParams &p, uint32_t x_type, uint32_t y_type, int sms, cudaStream_t s);
+constexpr int kErrRing = 16;            // bit of the handle's error word: a ring of rows gave up waiting
+int launch_norm(const NormParams &p, uint32_t x_type, uint32_t y_type, int *error, int sms, cudaStream_t s);
 int launch_norm_backward(const NormParams &p, uint32_t x_type, uint32_t y_type, float *dgamma, float *dbeta,
-                         uint32_t blocks, cudaStream_t s);
+                         uint32_t blocks, int *error, int sms, cudaStream_t s);
 
 // ---- attention over a window of the sentence (w2v_attend*.cu) ----
 constexpr uint32_t kMaxBuckets = 64, kMaxReach = 1024, kMaxSinks = 64, kMaxHeadDim = 128;

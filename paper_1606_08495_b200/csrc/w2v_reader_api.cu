@@ -121,7 +121,8 @@ int32_t w2v_layer_norm(w2v_handle *h, uint64_t rows, uint32_t d, const void *x, 
     std::memset(&p, 0, sizeof(p));
     p.x = x; p.y = y; p.gamma = gamma; p.beta = beta; p.mean = mean; p.rstd = rstd;
     p.rows = rows; p.ldx = x_stride; p.ldy = y_stride; p.d = d; p.eps = eps;
-    return launched(h, launch_norm(p, x_type, y_type, h->sms, h->stream), "layer norm launch");
+    if ((rc = ensure_error_word(h)) != W2V_OK) return rc;
+    return launched(h, launch_norm(p, x_type, y_type, h->tc_error, h->sms, h->stream), "layer norm launch");
 }
 
 int32_t w2v_layer_norm_backward(w2v_handle *h, uint64_t rows, uint32_t d, const void *dy, uint64_t dy_stride, uint32_t y_type,
@@ -144,9 +145,10 @@ int32_t w2v_layer_norm_backward(w2v_handle *h, uint64_t rows, uint32_t d, const 
     p.mean = const_cast<float *>(mean); p.rstd = const_cast<float *>(rstd);
     p.rows = rows; p.ldx = x_stride; p.ldy = dy_stride; p.ld_dx = dx_stride; p.d = d;
     const uint32_t blocks = norm_backward_blocks(rows, d, h->sms);
+    if ((rc = ensure_error_word(h)) != W2V_OK) return rc;
     if ((rc = grow(h, &h->reader_ws, &h->reader_ws_cap, (uint64_t)blocks * 2 * d * sizeof(float) + 16, true)) != W2V_OK) return rc;
     p.part = reinterpret_cast<float *>(h->reader_ws);
-    return launched(h, launch_norm_backward(p, x_type, y_type, dgamma, dbeta, blocks, h->stream), "layer norm backward launch");
+    return launched(h, launch_norm_backward(p, x_type, y_type, dgamma, dbeta, blocks, h->tc_error, h->sms, h->stream), "layer norm backward launch");
 }
 
 int32_t w2v_sentence_spans(w2v_handle *h, const int32_t *tokens, uint64_t n, int32_t *spans)

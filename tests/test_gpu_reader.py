@@ -49,6 +49,28 @@ NORM_TYPES = [(torch.float32, torch.float32), (torch.float32, torch.bfloat16), (
               (torch.bfloat16, torch.bfloat16), (torch.float16, torch.float16)]
 
 
+def check_layer_norm(model, x, xt, yt):
+    rows, d = x.shape
+    g, b = 1 + randn(d, seed=1, by=0.3), randn(d, seed=2, by=0.3)
+    dy = randn(rows, d, seed=5, dtype=yt)
+    y, saved = model.layer_norm(x, g, b, 1e-5, yt)
+    dx, dg, db = model.layer_norm_backward(dy, saved)
+    X, G, B, D = x.double(), g.double(), b.double(), dy.double()
+    mean = X.mean(1, keepdim=True)
+    inv = 1 / torch.sqrt((X - mean).square().mean(1, keepdim=True) + 1e-5)
+    hat = (X - mean) * inv
+    # the subtraction of the mean loses 2^-24 (|x| + |mean|) times the row's 1/deviation
+    lost = 8 * 2.0 ** -24 * (X.abs() + mean.abs()) * inv + F32 * hat.abs()
+    inside(y, hat * G + B, U[yt] * (hat * G + B).abs() + lost * G.abs() + 2.0 ** -24 * (hat * G).abs() + 1e-7, "y")
+    H = D * G
+    dX = inv * (H - H.mean(1, keepdim=True) - hat * (H * hat).mean(1, keepdim=True))
+    soft = inv * (H.abs() + H.abs().mean(1, keepdim=True) + hat.abs() * (H * hat).abs().mean(1, keepdim=True))
+    shift = (lost * H.abs()).mean(1, keepdim=True)
+    inside(dx, dX, U[xt] * dX.abs() + (F32 * soft + inv * (lost * (H * hat).abs().mean(1, keepdim=True) + hat.abs() * shift)) + 1e-7, "dx")
+    inside(dg, (D * hat).sum(0), F32 * (D * hat).abs().sum(0) + (D.abs() * lost).sum(0) + 1e-7, "dgamma")
+    inside(db, D.sum(0), F32 * D.abs().sum(0) + 1e-7, "dbeta")
+
+
 @pytest.mark.parametrize("rows,d", NORM_SHAPES)
 @pytest.mark.parametrize("xt,yt", NORM_TYPES)
 def test_layer_norm(model, rows, d, xt, yt):
@@ -59,24 +81,24 @@ def test_layer_norm(model, rows, d, xt, yt):
             wide[:, lead: lead + d] = x
             x = wide[:, lead: lead + d]
             assert rows == 1 or d == 1 or not x.is_contiguous()
-        g, b = 1 + randn(d, seed=1, by=0.3), randn(d, seed=2, by=0.3)
-        dy = randn(rows, d, seed=5, dtype=yt)
-        y, saved = model.layer_norm(x, g, b, 1e-5, yt)
-        dx, dg, db = model.layer_norm_backward(dy, saved)
-        X, G, B, D = x.double(), g.double(), b.double(), dy.double()
-        mean = X.mean(1, keepdim=True)
-        inv = 1 / torch.sqrt((X - mean).square().mean(1, keepdim=True) + 1e-5)
-        hat = (X - mean) * inv
-        # the subtraction of the mean loses 2^-24 (|x| + |mean|) times the row's 1/deviation
-        lost = 8 * 2.0 ** -24 * (X.abs() + mean.abs()) * inv + F32 * hat.abs()
-        inside(y, hat * G + B, U[yt] * (hat * G + B).abs() + lost * G.abs() + 2.0 ** -24 * (hat * G).abs() + 1e-7, "y")
-        H = D * G
-        dX = inv * (H - H.mean(1, keepdim=True) - hat * (H * hat).mean(1, keepdim=True))
-        soft = inv * (H.abs() + H.abs().mean(1, keepdim=True) + hat.abs() * (H * hat).abs().mean(1, keepdim=True))
-        shift = (lost * H.abs()).mean(1, keepdim=True)
-        inside(dx, dX, U[xt] * dX.abs() + (F32 * soft + inv * (lost * (H * hat).abs().mean(1, keepdim=True) + hat.abs() * shift)) + 1e-7, "dx")
-        inside(dg, (D * hat).sum(0), F32 * (D * hat).abs().sum(0) + (D.abs() * lost).sum(0) + 1e-7, "dgamma")
-        inside(db, D.sum(0), F32 * D.abs().sum(0) + 1e-7, "dbeta")
+        check_layer_norm(model, x, xt, yt)
+
+
+@pytest.mark.parametrize("rows,d,pad,xt,yt", [
+    (5001, 300, 20, torch.float32, torch.bfloat16),      # a padded table, an odd number of rows of 600 bytes
+    (4999, 300, 0, torch.bfloat16, torch.bfloat16),      # rows of 600 bytes without gaps: accesses of 8 bytes
+    (2999, 1000, 0, torch.float16, torch.float16),
+    (3001, 4096, 0, torch.bfloat16, torch.bfloat16),
+    (2500, 2048, 8, torch.float32, torch.float32),
+    (4001, 100, 0, torch.float32, torch.float16),        # dy in rows of 200 bytes
+    (9001, 36, 4, torch.float32, torch.float32),
+    (2401, 8192, 0, torch.bfloat16, torch.bfloat16),
+    (2400, 1536, 0, torch.float32, torch.bfloat16),
+])
+def test_layer_norm_of_many_rows(model, rows, d, pad, xt, yt):
+    """Enough rows for those that go through shared memory; the same bounds."""
+    wide = randn(rows, d + pad, seed=d + pad, dtype=xt, by=0.7) + torch.tensor(0.25, dtype=xt, device="cuda")
+    check_layer_norm(model, wide[:, :d], xt, yt)
 
 
 def test_layer_norm_rows_of_one_value_and_no_rows(model):
