@@ -104,6 +104,7 @@ norm_ring_kernel(NormParams p, uint32_t gw, uint32_t groups, uint32_t stages, ui
     };
     if (gl == 0)
         for (uint32_t s = 0; s < stages; ++s) if (u + s * step < units) issue(u + s * step, s);
+    constexpr int kPairs = NV * E / 2;                                // two columns per instruction
     float gamma[NV * E], beta[NV * E];
     norm_weights_load<E, NV>(gamma, p.gamma, gl, gw, p.d);
     norm_weights_load<E, NV>(beta, p.beta, gl, gw, p.d);
@@ -117,19 +118,21 @@ norm_ring_kernel(NormParams p, uint32_t gw, uint32_t groups, uint32_t stages, ui
             norm_copy_tail<TX>(mode, rows, x + r * p.ldx, p.d, n, gl, gw * 32);
             group_barrier(gw, group);
         }
-        float v[kNormUnit][NV * E], s[kNormUnit], q[kNormUnit];
+        float2 v[kNormUnit][kPairs];
+        float s[kNormUnit], q[kNormUnit];
 #pragma unroll
         for (int i = 0; i < kNormUnit; ++i) {
-            s[i] = q[i] = 0.f;
             Pack<TX, E> t[NV];
             norm_row_load<TX, E, NV>(t, reinterpret_cast<const TX *>(rows + i * pitch), gl, gw, p.d);
+            float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
             for (int c = 0; c < NV; ++c)
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    v[i][c * E + e] = to_f32(t[c].e[e]);
-                    s[i] += v[i][c * E + e];
+                for (int e = 0; e < E / 2; ++e) {
+                    v[i][c * (E / 2) + e] = pair_f32(t[c], e);
+                    sum = add2(sum, v[i][c * (E / 2) + e]);
                 }
+            s[i] = sum.x + sum.y;
         }
         group_sum<kNormUnit>(s, gw, wig, group, lane, slot, flip);
         flip ^= 1u;
@@ -139,15 +142,18 @@ norm_ring_kernel(NormParams p, uint32_t gw, uint32_t groups, uint32_t stages, ui
 #pragma unroll
         for (int i = 0; i < kNormUnit; ++i) {
             s[i] *= inv_d;
+            const float2 less = make_float2(-s[i], -s[i]);
+            float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
             for (int c = 0; c < NV; ++c)
                 if ((gl + c * 32u * gw) * E < p.d) {
 #pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        v[i][c * E + e] -= s[i];
-                        q[i] = fmaf(v[i][c * E + e], v[i][c * E + e], q[i]);
+                    for (int e = c * (E / 2); e < (c + 1) * (E / 2); ++e) {
+                        v[i][e] = add2(v[i][e], less);
+                        sum = fma2(v[i][e], v[i][e], sum);
                     }
                 }
+            q[i] = sum.x + sum.y;
         }
         group_sum<kNormUnit>(q, gw, wig, group, lane, slot, flip);
         flip ^= 1u;
@@ -165,7 +171,10 @@ norm_ring_kernel(NormParams p, uint32_t gw, uint32_t groups, uint32_t stages, ui
                 if (at < p.d) {
                     Pack<TY, E> t;
 #pragma unroll
-                    for (int e = 0; e < E; ++e) t.e[e] = from_f32<TY>(fmaf(v[i][c * E + e] * rstd, gamma[c * E + e], beta[c * E + e]));
+                    for (int e = 0; e < E / 2; ++e) {
+                        const int k = c * E + 2 * e;
+                        set_pair(t, e, fma2(mul2(v[i][k / 2], make_float2(rstd, rstd)), make_float2(gamma[k], gamma[k + 1]), make_float2(beta[k], beta[k + 1])));
+                    }
                     store_pack<TY, E>(y + (r + i) * p.ldy + at, t);
                 }
             }

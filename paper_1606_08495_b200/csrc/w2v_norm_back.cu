@@ -158,10 +158,12 @@ norm_backward_ring_kernel(NormParams p, uint32_t gw, uint32_t groups, uint32_t s
     };
     if (gl == 0)
         for (uint32_t s = 0; s < stages; ++s) if (u + s * step < units) issue(u + s * step, s);
-    float gamma[NV * E], dg[NV * E], db[NV * E];
+    constexpr int kPairs = NV * E / 2;                                // two columns per instruction
+    float gamma[NV * E];
+    float2 dg2[kPairs], db2[kPairs];
     norm_weights_load<E, NV>(gamma, p.gamma, gl, gw, p.d);
 #pragma unroll
-    for (int i = 0; i < NV * E; ++i) dg[i] = db[i] = 0.f;
+    for (int i = 0; i < kPairs; ++i) dg2[i] = db2[i] = make_float2(0.f, 0.f);
     uint32_t flip = 0, stage = 0, phase = 0;
     for (; u < units; u += step) {
         const uint64_t r = u * kNormUnit;
@@ -188,23 +190,30 @@ norm_backward_ring_kernel(NormParams p, uint32_t gw, uint32_t groups, uint32_t s
             Pack<TY, E> yc[NV];
             norm_row_load<TX, E, NV>(xc, reinterpret_cast<const TX *>(rows_x + i * pitch_x), gl, gw, p.d);
             norm_row_load<TY, E, NV>(yc, reinterpret_cast<const TY *>(rows_y + i * pitch_y), gl, gw, p.d);
+            const float2 by = make_float2(rstd[i], rstd[i]), less = make_float2(-mean[i], -mean[i]);
+            float2 sg = make_float2(0.f, 0.f), sh = sg;
 #pragma unroll
             for (int c = 0; c < NV; ++c)
 #pragma unroll
-                for (int e = 0; e < E; ++e) {                         // past the row's end dy and gamma are zero
-                    const float h = (to_f32(xc[c].e[e]) - mean[i]) * rstd[i], w = to_f32(yc[c].e[e]), g = w * gamma[c * E + e];
-                    dg[c * E + e] = fmaf(w, h, dg[c * E + e]);
-                    db[c * E + e] += w;
-                    t[2 * i] += g;
-                    t[2 * i + 1] = fmaf(g, h, t[2 * i + 1]);
+                for (int e = 0; e < E / 2; ++e) {                     // past the row's end dy and gamma are zero
+                    const int k = c * (E / 2) + e;
+                    const float2 h = mul2(add2(pair_f32(xc[c], e), less), by), w = pair_f32(yc[c], e), g = mul2(w, make_float2(gamma[2 * k], gamma[2 * k + 1]));
+                    dg2[k] = fma2(w, h, dg2[k]);
+                    db2[k] = add2(db2[k], w);
+                    sg = add2(sg, g);
+                    sh = fma2(g, h, sh);
                 }
+            t[2 * i] = sg.x + sg.y;
+            t[2 * i + 1] = sh.x + sh.y;
         }
         group_sum<2 * kNormUnit>(t, gw, wig, group, lane, slot, flip);
         flip ^= 1u;
 #pragma unroll
         for (int i = 0; i < kNormUnit; ++i) {
             if ((uint32_t)i >= n) break;
-            const float ma = t[2 * i] * inv_d, mb = t[2 * i + 1] * inv_d;
+            // dx = rstd g - rstd mean(g) - h rstd mean(g h)
+            const float ma = -rstd[i] * t[2 * i] * inv_d, mb = -rstd[i] * t[2 * i + 1] * inv_d;
+            const float2 by = make_float2(rstd[i], rstd[i]), less = make_float2(-mean[i], -mean[i]), ma2 = make_float2(ma, ma), mb2 = make_float2(mb, mb);
 #pragma unroll
             for (int c = 0; c < NV; ++c) {
                 const uint32_t at = (gl + c * 32u * gw) * E;
@@ -213,9 +222,10 @@ norm_backward_ring_kernel(NormParams p, uint32_t gw, uint32_t groups, uint32_t s
                     const Pack<TY, E> yc = load_pack<TY, E>(reinterpret_cast<const TY *>(rows_y + i * pitch_y) + at);
                     Pack<TX, E> o;
 #pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        const float h = (to_f32(xc.e[e]) - mean[i]) * rstd[i], g = to_f32(yc.e[e]) * gamma[c * E + e];
-                        o.e[e] = from_f32<TX>(rstd[i] * (g - ma - h * mb));
+                    for (int e = 0; e < E / 2; ++e) {
+                        const int k = c * (E / 2) + e;
+                        const float2 h = mul2(add2(pair_f32(xc, e), less), by), g = mul2(pair_f32(yc, e), make_float2(gamma[2 * k], gamma[2 * k + 1]));
+                        set_pair(o, e, fma2(g, by, fma2(h, mb2, ma2)));
                     }
                     store_pack<TX, E>(dx + (r + i) * p.ld_dx + at, o);
                 }
@@ -227,6 +237,9 @@ norm_backward_ring_kernel(NormParams p, uint32_t gw, uint32_t groups, uint32_t s
     }
     __syncthreads();
     if (threadIdx.x == 0 && abort_flag) atomicOr(error, kErrRing);
+    float dg[NV * E], db[NV * E];
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) { dg[2 * i] = dg2[i].x; dg[2 * i + 1] = dg2[i].y; db[2 * i] = db2[i].x; db[2 * i + 1] = db2[i].y; }
     norm_block_sums<E, NV>(p, dg, db, reinterpret_cast<float *>(ring), gw, group, groups, gl);
 }
 

@@ -46,4 +46,17 @@ template <> __device__ __forceinline__ uint32_t pack2<__half>(float a, float b)
     return *reinterpret_cast<const uint32_t *>(&x);
 }
 
+// Elements 2 i and 2 i + 1 of a pack in fp32, and back.
+template <int N> __device__ __forceinline__ float2 pair_f32(const Pack<float, N> &p, int i) { return make_float2(p.e[2 * i], p.e[2 * i + 1]); }
+template <int N> __device__ __forceinline__ float2 pair_f32(const Pack<__half, N> &p, int i) { return __half22float2(*reinterpret_cast<const __half2 *>(&p.e[2 * i])); }
+template <int N>
+__device__ __forceinline__ float2 pair_f32(const Pack<__nv_bfloat16, N> &p, int i)
+{
+    const uint32_t u = *reinterpret_cast<const uint32_t *>(&p.e[2 * i]);
+    return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xFFFF0000u));
+}
+template <int N> __device__ __forceinline__ void set_pair(Pack<float, N> &p, int i, float2 v) { p.e[2 * i] = v.x; p.e[2 * i + 1] = v.y; }
+template <typename T, int N>
+__device__ __forceinline__ void set_pair(Pack<T, N> &p, int i, float2 v) { *reinterpret_cast<uint32_t *>(&p.e[2 * i]) = pack2<T>(v.x, v.y); }
+
 }  // namespace w2v
