@@ -16,8 +16,9 @@
 //   output:  lane (g, t) holds chunk g of keys 2t, 2t + 1, 2t + 8, 2t + 9; a byte permutation pairs the keys, and
 //            column g of product e is dimension 8 g + e.
 // The softmax weights enter the second product as the sum of two numbers of the cache's type, so that what is lost is
-// 2^-18 and not 2^-9 of them.  Values of one step are on their way while its scores are formed, the next step's
-// keys while its softmax is.
+// 2^-18 and not 2^-9 of them.  Each warp copies its next step's keys and values to shared memory in the background, so
+// that what is under way does not have to fit in registers.  There chunk c of row r lies at c ^ turn(r), which keeps
+// both ways of reading free of bank conflicts.
 #include <cooperative_groups.h>
 
 #include "w2v_attend.cuh"
@@ -28,6 +29,11 @@ namespace cg = cooperative_groups;
 namespace w2v {
 
 constexpr int kTokWarps = 4, kTokThreads = kTokWarps * 32, kTokRows = 16;
+constexpr int kTokStages = 2;                    // steps of 16 keys and values per warp
+
+// Eight lanes read 16 bytes at once: keys in rows 2 i and 2 i + 1, chunks t = 0..3; values in rows 2 t (or 2 t + 1),
+// chunks 2 i and 2 i + 1.
+__device__ __forceinline__ uint32_t turn(uint32_t row) { return (row & 6u) ^ ((row & 1u) << 2); }
 
 template <typename T>
 __device__ __forceinline__ void mma_token(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1);
@@ -55,10 +61,11 @@ __device__ __forceinline__ void split_pair(float a, float b, uint32_t &head, uin
 
 // NB = 64-column blocks of a head; HI: more than 8 query heads share the key/value head.
 template <typename T, int NB, bool HI>
-__global__ void __launch_bounds__(kTokThreads, NB == 1 ? 4 : 2)
+__global__ void __launch_bounds__(kTokThreads, NB == 1 ? 5 : 3)
 attend_token_kernel(TokenParams p, uint32_t splits, uint32_t passes)
 {
-    extern __shared__ float sm[];
+    extern __shared__ __align__(128) unsigned char token_smem[];        // the warps' stages, then what is joined
+    float *sm = reinterpret_cast<float *>(token_smem + kTokWarps * kTokStages * 2 * 16 * NB * 128);
     constexpr int kR = HI ? 2 : 1;                                      // rows g and g + 8 of a lane
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     const uint32_t group = p.heads / p.kv_heads, chunks = p.dim >> 3;
@@ -71,6 +78,7 @@ attend_token_kernel(TokenParams p, uint32_t splits, uint32_t passes)
     float *wstat = acc_s + kKeep * p.dim;                               // [warps][rows][2]
     float *wacc = wstat + kTokWarps * kKeep * 2;                        // [warps][rows][dim]
     float *bias_s = wacc + kTokWarps * kKeep * p.dim;                   // [rows][reach + 1] bias by distance
+    constexpr uint32_t kRow = NB * 128, kHalf = 16 * kRow, kStage = 2 * kHalf;           // bytes: a row, 16 keys, a step
     const int32_t pos = p.pos[b];
     const int32_t reach = p.b.n ? p.b.start[p.b.n - 1] : 0;             // from here on one bucket
     if (p.b.n)
@@ -110,37 +118,49 @@ attend_token_kernel(TokenParams p, uint32_t splits, uint32_t passes)
             const uint32_t c = value ? tid - chunks : tid;
             reinterpret_cast<uint4 *>((value ? cv : ck) + (size_t)at * row)[c] = __ldg(reinterpret_cast<const uint4 *>(value ? nv : nk) + c);
         }
-        // row of visible position number x in the cache `c`, or the new one
-        auto source = [&](int32_t x, const T *c, const T *fresh) -> const uint4 * {
-            if (x >= total - 1) return reinterpret_cast<const uint4 *>(fresh);
-            int64_t at = x;
-            if (x >= ns) {
-                at = place0 + (x - ns);
-                if (at >= (int64_t)p.places) at -= ring;
-            }
-            return reinterpret_cast<const uint4 *>(c + (size_t)at * row);
-        };
-        auto load_keys = [&](uint4 (&k)[2][NB * 2], int32_t x0) {
+        // 16 keys and values from visible position number x0 on to a stage; zeros past the part's end
+        const uint32_t stages = smem_addr(token_smem) + warp * (kTokStages * kStage);
+        auto copy_step = [&](int32_t x0, uint32_t stage) {
+            constexpr uint32_t kLanes = NB * 8, kAtOnce = 32 / kLanes;   // lanes per row
+            const uint32_t c = lane % kLanes;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int32_t x = x0 + i * 8 + (int32_t)g;
-                const uint4 *s = source(x, ck, nk);
-#pragma unroll
-                for (int j = 0; j < NB * 2; ++j) k[i][j] = x < t1 && 4 * j + t < chunks ? __ldg(s + 4 * j + t) : make_uint4(0, 0, 0, 0);
+            for (uint32_t i = 0; i < 16 / kAtOnce; ++i) {
+                const uint32_t r = i * kAtOnce + lane / kLanes;
+                const int32_t x = x0 + (int32_t)r;
+                const bool real = x < t1 && c < chunks;
+                int64_t at = x;
+                if (x >= ns) {
+                    at = place0 + (x - ns);
+                    if (at >= (int64_t)p.places) at -= ring;
+                }
+                const bool fresh = x >= total - 1;
+                const T *k = fresh ? nk : ck + (size_t)at * row, *v = fresh ? nv : cv + (size_t)at * row;
+                const uint32_t to = stages + stage * kStage + r * kRow + ((c ^ turn(r)) << 4);
+                copy16(to, real ? k + c * 8 : nk, real);
+                copy16(to + kHalf, real ? v + c * 8 : nv, real);
             }
+            copy_commit();
         };
         const int32_t first = t0 + (int32_t)warp * 16;
-        uint4 key[2][NB * 2];
-        if (first < t1) load_keys(key, first);
-        for (int32_t x0 = first; x0 < t1; x0 += kTokWarps * 16) {
-            uint4 val[NB][4];                                           // chunk g + 8 s of keys 2t, 2t + 1, 2t + 8, 2t + 9
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int32_t x = x0 + (i >> 1) * 8 + 2 * (int32_t)t + (i & 1);
-                const uint4 *s = source(x, cv, nv);
-#pragma unroll
-                for (int n = 0; n < NB; ++n) val[n][i] = x < t1 && g + 8 * n < chunks ? __ldg(s + g + 8 * n) : make_uint4(0, 0, 0, 0);
+        if (first < t1) copy_step(first, 0);
+        uint32_t stage = 0;
+        for (int32_t x0 = first; x0 < t1; x0 += kTokWarps * 16, stage ^= 1u) {
+            if (x0 + kTokWarps * 16 < t1) {
+                copy_step(x0 + kTokWarps * 16, stage ^ 1u);
+                copy_wait<1>();
+            } else {
+                copy_wait<0>();
             }
+            __syncwarp();
+            const unsigned char *keys = token_smem + warp * (kTokStages * kStage) + stage * kStage, *vals = keys + kHalf;
+            uint4 key[2][NB * 2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < NB * 2; ++j) {
+                    const uint32_t r = i * 8 + g;
+                    key[i][j] = *reinterpret_cast<const uint4 *>(keys + r * kRow + (((4 * j + t) ^ turn(r)) << 4));
+                }
             float sc[2][4];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
@@ -151,7 +171,6 @@ attend_token_kernel(TokenParams p, uint32_t splits, uint32_t passes)
                     mma_token<T>(sc[i], q[0][j].z, HI ? q[kR - 1][j].z : 0u, q[0][j].w, HI ? q[kR - 1][j].w : 0u, key[i][j].z, key[i][j].w);
                 }
             }
-            if (x0 + kTokWarps * 16 < t1) load_keys(key, x0 + kTokWarps * 16);
             uint32_t head[2][kR], tail[2][kR];
 #pragma unroll
             for (int r = 0; r < kR; ++r) {
@@ -184,8 +203,14 @@ attend_token_kernel(TokenParams p, uint32_t splits, uint32_t passes)
             }
 #pragma unroll
             for (int n = 0; n < NB; ++n) {
-                const uint32_t *v0 = reinterpret_cast<const uint32_t *>(&val[n][0]), *v1 = reinterpret_cast<const uint32_t *>(&val[n][1]);
-                const uint32_t *v2 = reinterpret_cast<const uint32_t *>(&val[n][2]), *v3 = reinterpret_cast<const uint32_t *>(&val[n][3]);
+                uint4 val[4];                                           // chunk g + 8 n of keys 2t, 2t + 1, 2t + 8, 2t + 9
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t r = (i >> 1) * 8 + 2 * t + (i & 1);
+                    val[i] = *reinterpret_cast<const uint4 *>(vals + r * kRow + (((g + 8 * n) ^ turn(r)) << 4));
+                }
+                const uint32_t *v0 = reinterpret_cast<const uint32_t *>(&val[0]), *v1 = reinterpret_cast<const uint32_t *>(&val[1]);
+                const uint32_t *v2 = reinterpret_cast<const uint32_t *>(&val[2]), *v3 = reinterpret_cast<const uint32_t *>(&val[3]);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const uint32_t pick = e & 1 ? 0x7632u : 0x5410u;    // dimension e of two keys in one register
@@ -194,6 +219,7 @@ attend_token_kernel(TokenParams p, uint32_t splits, uint32_t passes)
                     mma_token<T>(acc[n * 8 + e], head[0][0], HI ? head[0][kR - 1] : 0u, head[1][0], HI ? head[1][kR - 1] : 0u, b0, b1);
                 }
             }
+            __syncwarp();                                               // the stage may be filled again
         }
     }
     // join the warps; a lane has columns 2t, 2t + 1 of every product: dimensions 64 n + 8 (2t) + e and 64 n + 8 (2t + 1) + e
@@ -263,7 +289,7 @@ int launch_token_shape(const TokenParams &p, int sms, cudaStream_t s)
     uint32_t splits = 1;
     while (splits < 8 && keys / (2 * splits) >= (items * splits < 2ull * (uint64_t)sms ? 64u : 512u) && items * splits < 8ull * (uint64_t)sms) splits *= 2;
     const uint32_t reach = p.b.n ? (uint32_t)p.b.start[p.b.n - 1] + 1 : 0;
-    const size_t smem = sizeof(float) * (2 * rows + (size_t)rows * p.dim + kTokWarps * rows * (2 + (size_t)p.dim) + (size_t)reach * kTokRows);
+    const size_t smem = (size_t)kTokWarps * kTokStages * 2 * 16 * NB * 128 + sizeof(float) * (2 * rows + (size_t)rows * p.dim + kTokWarps * rows * (2 + (size_t)p.dim) + (size_t)reach * kTokRows);
     auto kernel = attend_token_kernel<T, NB, HI>;
     if (smem > 48 * 1024 && !kernel_ready<attend_token_kernel<T, NB, HI>>()) return -1;
     cudaLaunchConfig_t cfg = {};
