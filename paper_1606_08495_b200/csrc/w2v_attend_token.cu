@@ -61,7 +61,7 @@ __device__ __forceinline__ void split_pair(float a, float b, uint32_t &head, uin
 
 // NB = 64-column blocks of a head; HI: more than 8 query heads share the key/value head.
 template <typename T, int NB, bool HI>
-__global__ void __launch_bounds__(kTokThreads, NB == 1 ? 5 : 3)
+__global__ void __launch_bounds__(kTokThreads, NB == 1 ? 4 : 3)
 attend_token_kernel(TokenParams p, uint32_t splits, uint32_t passes)
 {
     extern __shared__ __align__(128) unsigned char token_smem[];        // the warps' stages, then what is joined
@@ -73,11 +73,12 @@ attend_token_kernel(TokenParams p, uint32_t splits, uint32_t passes)
     const uint32_t pass = item % passes, kvh = (item / passes) % p.kv_heads, b = item / (passes * p.kv_heads);
     const uint32_t h0 = kvh * group + pass * kTokRows, nh = min((uint32_t)kTokRows, group - pass * kTokRows);
     constexpr uint32_t kKeep = 8 * kR;                                  // rows of a block's results
-    float *stat = sm;                                                   // [rows][2] maximum and sum of this block
+    float *bias_s = sm;                                                 // [rows][reach + 1] bias by distance
+    // what is joined lies where the stages were
+    float *stat = reinterpret_cast<float *>(token_smem);                // [rows][2] maximum and sum of this block
     float *acc_s = stat + 2 * kKeep;                                    // [rows][dim] output of this block
     float *wstat = acc_s + kKeep * p.dim;                               // [warps][rows][2]
     float *wacc = wstat + kTokWarps * kKeep * 2;                        // [warps][rows][dim]
-    float *bias_s = wacc + kTokWarps * kKeep * p.dim;                   // [rows][reach + 1] bias by distance
     constexpr uint32_t kRow = NB * 128, kHalf = 16 * kRow, kStage = 2 * kHalf;           // bytes: a row, 16 keys, a step
     const int32_t pos = p.pos[b];
     const int32_t reach = p.b.n ? p.b.start[p.b.n - 1] : 0;             // from here on one bucket
@@ -120,24 +121,33 @@ attend_token_kernel(TokenParams p, uint32_t splits, uint32_t passes)
         }
         // 16 keys and values from visible position number x0 on to a stage; zeros past the part's end
         const uint32_t stages = smem_addr(token_smem) + warp * (kTokStages * kStage);
+        constexpr uint32_t kLanes = NB * 8, kAtOnce = 32 / kLanes;       // lanes per row, rows per request
+        const uint32_t lane_row = lane / kLanes, lane_chunk = lane % kLanes;
+        const bool inside = lane_chunk < chunks;
+        const uint32_t row_bytes = (uint32_t)row * 2u;
+        const char *kb = reinterpret_cast<const char *>(ck) + lane_chunk * 16u, *vb = reinterpret_cast<const char *>(cv) + lane_chunk * 16u;
+        const uint32_t shift = (uint32_t)place0 - (uint32_t)ns, places = (uint32_t)p.places;
         auto copy_step = [&](int32_t x0, uint32_t stage) {
-            constexpr uint32_t kLanes = NB * 8, kAtOnce = 32 / kLanes;   // lanes per row
-            const uint32_t c = lane % kLanes;
+            const uint32_t to = stages + stage * kStage + lane_row * kRow;
+            // all but the steps with a sink, the new token or the part's end in them: places in a row, but for the wrap
+            const bool even = x0 >= ns && x0 + 16 < total && x0 + 16 <= t1;
 #pragma unroll
             for (uint32_t i = 0; i < 16 / kAtOnce; ++i) {
-                const uint32_t r = i * kAtOnce + lane / kLanes;
+                const uint32_t r = i * kAtOnce + lane_row, dst = to + i * kAtOnce * kRow + ((lane_chunk ^ turn(r)) << 4);
                 const int32_t x = x0 + (int32_t)r;
-                const bool real = x < t1 && c < chunks;
-                int64_t at = x;
-                if (x >= ns) {
-                    at = place0 + (x - ns);
-                    if (at >= (int64_t)p.places) at -= ring;
+                uint32_t at = (uint32_t)x + shift;
+                if (at >= places) at -= ring;
+                if (even) {
+                    const uint64_t off = (uint64_t)at * row_bytes;
+                    copy16(dst, kb + off, inside);
+                    copy16(dst + kHalf, vb + off, inside);
+                } else {
+                    if (x < ns) at = (uint32_t)x;
+                    const bool real = inside && x < t1, fresh = x >= total - 1;
+                    const uint64_t off = real && !fresh ? (uint64_t)at * row_bytes : 0u;
+                    copy16(dst, fresh ? reinterpret_cast<const char *>(nk) + lane_chunk * 16u : kb + off, real);
+                    copy16(dst + kHalf, fresh ? reinterpret_cast<const char *>(nv) + lane_chunk * 16u : vb + off, real);
                 }
-                const bool fresh = x >= total - 1;
-                const T *k = fresh ? nk : ck + (size_t)at * row, *v = fresh ? nv : cv + (size_t)at * row;
-                const uint32_t to = stages + stage * kStage + r * kRow + ((c ^ turn(r)) << 4);
-                copy16(to, real ? k + c * 8 : nk, real);
-                copy16(to + kHalf, real ? v + c * 8 : nv, real);
             }
             copy_commit();
         };
@@ -175,14 +185,12 @@ attend_token_kernel(TokenParams p, uint32_t splits, uint32_t passes)
 #pragma unroll
             for (int r = 0; r < kR; ++r) {
                 float s[4], top = mx[r];
+                const float *near = bias_s + min(g + 8 * r, nh - 1) * (uint32_t)(reach + 1);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int32_t x = x0 + (i >> 1) * 8 + 2 * (int32_t)t + (i & 1);
                     s[i] = sc[i >> 1][2 * r + (i & 1)] * (p.scale * kLog2e);
-                    if (p.b.n) {
-                        const int32_t dist = x < ns ? pos - x : total - 1 - x;
-                        s[i] += x < t1 && g + 8 * r < nh ? bias_s[(g + 8 * r) * (uint32_t)(reach + 1) + (uint32_t)min(dist, reach)] : 0.f;
-                    }
+                    if (p.b.n) s[i] += near[x < ns ? min(pos - x, reach) : min(max(total - 1 - x, 0), reach)];
                     if (x >= t1) s[i] = -INFINITY;
                     top = fmaxf(top, s[i]);
                 }
@@ -222,6 +230,7 @@ attend_token_kernel(TokenParams p, uint32_t splits, uint32_t passes)
             __syncwarp();                                               // the stage may be filled again
         }
     }
+    __syncthreads();                                                    // every warp is done with its stages
     // join the warps; a lane has columns 2t, 2t + 1 of every product: dimensions 64 n + 8 (2t) + e and 64 n + 8 (2t + 1) + e
 #pragma unroll
     for (int r = 0; r < kR; ++r) {
@@ -281,7 +290,7 @@ attend_token_kernel(TokenParams p, uint32_t splits, uint32_t passes)
 template <typename T, int NB, bool HI>
 int launch_token_shape(const TokenParams &p, int sms, cudaStream_t s)
 {
-    const uint32_t group = p.heads / p.kv_heads, passes = (group + kTokRows - 1) / kTokRows, rows = HI ? 16 : 8;
+    const uint32_t group = p.heads / p.kv_heads, passes = (group + kTokRows - 1) / kTokRows;
     const uint64_t items = (uint64_t)p.batch * p.kv_heads * passes;
     // parts of a head: enough blocks for several on every SM, as long as a part keeps some 64 keys (one step of its
     // warps) when blocks are few, 512 when there are plenty
@@ -289,7 +298,8 @@ int launch_token_shape(const TokenParams &p, int sms, cudaStream_t s)
     uint32_t splits = 1;
     while (splits < 8 && keys / (2 * splits) >= (items * splits < 2ull * (uint64_t)sms ? 64u : 512u) && items * splits < 8ull * (uint64_t)sms) splits *= 2;
     const uint32_t reach = p.b.n ? (uint32_t)p.b.start[p.b.n - 1] + 1 : 0;
-    const size_t smem = (size_t)kTokWarps * kTokStages * 2 * 16 * NB * 128 + sizeof(float) * (2 * rows + (size_t)rows * p.dim + kTokWarps * rows * (2 + (size_t)p.dim) + (size_t)reach * kTokRows);
+    const size_t smem = (size_t)kTokWarps * kTokStages * 2 * 16 * NB * 128 + sizeof(float) * (size_t)reach * (group < kTokRows ? group : kTokRows);
+    static_assert((size_t)kTokWarps * kTokStages * 2 * 16 * NB * 128 >= sizeof(float) * (HI ? 16 : 8) * (2 + NB * 64) * (kTokWarps + 1), "joined where the stages were");
     auto kernel = attend_token_kernel<T, NB, HI>;
     if (smem > 48 * 1024 && !kernel_ready<attend_token_kernel<T, NB, HI>>()) return -1;
     cudaLaunchConfig_t cfg = {};
