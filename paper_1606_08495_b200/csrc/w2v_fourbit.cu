@@ -95,7 +95,11 @@ __device__ __forceinline__ void unpack8(uint32_t w, uint32_t (&h)[4])
 {
     const uint32_t u = w >> 8;
     const __half2 off = __floats2half2_rn(-1032.f, -1032.f), by = __floats2half2_rn(0.0625f, 0.0625f), off16 = __floats2half2_rn(-72.f, -72.f);
-    const uint32_t t[4] = {(w & 0x000F000Fu) | 0x64006400u, (w & 0x00F000F0u) | 0x64006400u, (u & 0x000F000Fu) | 0x64006400u, (u & 0x00F000F0u) | 0x64006400u};
+    uint32_t t[4];
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(t[0]) : "r"(w), "r"(0x000F000Fu), "r"(0x64006400u));      // (a & b) | c
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(t[1]) : "r"(w), "r"(0x00F000F0u), "r"(0x64006400u));
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(t[2]) : "r"(u), "r"(0x000F000Fu), "r"(0x64006400u));
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(t[3]) : "r"(u), "r"(0x00F000F0u), "r"(0x64006400u));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const __half2 x = *reinterpret_cast<const __half2 *>(&t[i]);
