@@ -111,6 +111,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     tc_fence_after();
     const uint32_t tmem = warp_value(sh.tmem);
     volatile int *abort_flag = &sh.abort_flag;
+    auto ready = [&](uint64_t *bar, uint32_t parity) { return SMALL ? mbar_wait(bar, parity, abort_flag) : mbar_nap(bar, parity, abort_flag); };
     // the run of keys [lo, hi) and the sinks [s, s_end) before it, which are the first tile
     int32_t lo = INT32_MAX, hi = 0, s = INT32_MAX;
 #pragma unroll
@@ -159,8 +160,8 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         for (int32_t t = (int32_t)wg; t < tiles; t += 2) {
             const int32_t k0 = tile_at(t), cols = tile_keys(t);
             const uint32_t stage = t % Sh::kStages;
-            ok = __all_sync(kFullMask, mbar_wait(&sh.full[stage], (t / Sh::kStages) & 1, abort_flag) &&        // the bits of the keys
-                                           mbar_wait(&sh.s_full[wg], (t >> 1) & 1, abort_flag));
+            ok = __all_sync(kFullMask, ready(&sh.full[stage], (t / Sh::kStages) & 1) &&        // the bits of the keys
+                                           ready(&sh.s_full[wg], (t >> 1) & 1));
             if (!ok) break;
             tc_fence_after();
             // far from the warp's rows every key of the tile has the bias of the side's last bucket
@@ -262,7 +263,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         sh.sum[wg][r] = word ? mine : 0.f;
         asm volatile("bar.sync 1, 256;" ::: "memory");
         const float r0 = sh.ref[0][r], r1 = sh.ref[1][r], to = fmaxf(r0, r1);
-        ok = __all_sync(kFullMask, ok && (tiles == 0 || mbar_wait(&sh.done, 0, abort_flag)));
+        ok = __all_sync(kFullMask, ok && (tiles == 0 || ready(&sh.done, 0)));
         tc_fence_after();
         float f0 = to == -INFINITY ? 0.f : fast_exp2(r0 - to), f1 = to == -INFINITY ? 0.f : fast_exp2(r1 - to);
         const float total = sh.sum[0][r] * f0 + sh.sum[1][r] * f1, inv = total > 0.f ? 1.f / total : 0.f;
@@ -326,7 +327,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                 umma_commit(&sh.s_full[b]);
             };
             auto wait = [&](uint64_t *bar, uint32_t parity) {
-                const bool got = __all_sync(kFullMask, mbar_wait(bar, parity, abort_flag));
+                const bool got = __all_sync(kFullMask, ready(bar, parity));
                 tc_fence_after();
                 return got;
             };
@@ -370,7 +371,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             int32_t t = 0;
             for (; t < tiles; ++t) {
                 const uint32_t stage = t % Sh::kStages, round = t / Sh::kStages, base = ring + stage * Sh::kStage;
-                if (round > 0 && !mbar_wait(&sh.empty[stage], (round - 1) & 1, abort_flag)) break;
+                if (round > 0 && !mbar_nap(&sh.empty[stage], (round - 1) & 1, abort_flag)) break;
                 mbar_expect(&sh.landed[stage], Sh::kStage);
 #pragma unroll
                 for (int c = 0; c < NB; ++c) {
@@ -391,7 +392,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         if (t < tiles) word_bits(p, tile_at(t), (uint32_t)tile_keys(t), lane, vis);
         for (; t < tiles; t += 2) {
             const uint32_t stage = t % Sh::kStages;
-            if (!__all_sync(kFullMask, mbar_wait(&sh.landed[stage], (t / Sh::kStages) & 1, abort_flag))) break;
+            if (!__all_sync(kFullMask, mbar_nap(&sh.landed[stage], (t / Sh::kStages) & 1, abort_flag))) break;
             if (lane < 2) sh.vis[stage][lane] = lane ? vis[1] : vis[0];
             // values only: the scores of such a key are masked
             zero_rows<NB>(ring + stage * Sh::kStage + Sh::kOperand, Sh::kRows * 128, (uint32_t)(tile_keys(t) + 15) & ~15u, vis, lane);

@@ -291,7 +291,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
         const bool word = ROLE == 0 ? row.hi > row.lo : q_hi > q_lo;
         float lse = INFINITY, delta = 0.f;
         if (ROLE == 0 && word) lse = __ldg(p.lse + (int64_t)h_own * p.n + own);
-        bool ok = __all_sync(kFullMask, mbar_wait(&sh.own_landed, 0, abort_flag));
+        bool ok = __all_sync(kFullMask, mbar_nap(&sh.own_landed, 0, abort_flag));
         {
             auto chunk = [&](int operand, int c) {                   // 8 columns of this thread's row, from the 128-byte swizzle
                 return *reinterpret_cast<const uint4 *>(own_rows + operand * Sh::kOwn + (c >> 3) * (128 * 128) + r * 128u + (((c & 7) ^ (r & 7u)) << 4));
@@ -355,8 +355,8 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                 const uint32_t b = t % Sh::kBuf, stage = t % Sh::kStages;
                 if (!SMALL && b != wg) continue;
                 const int32_t at0 = tile_at(k), cols = (tile_rows(k) + 15) & ~15;
-                ok = __all_sync(kFullMask, mbar_wait(&sh.full[stage], (t / Sh::kStages) & 1, abort_flag) &&
-                                               mbar_wait(&sh.s_full[b], (t / Sh::kBuf) & 1, abort_flag));
+                ok = __all_sync(kFullMask, mbar_nap(&sh.full[stage], (t / Sh::kStages) & 1, abort_flag) &&
+                                               mbar_nap(&sh.s_full[b], (t / Sh::kBuf) & 1, abort_flag));
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t cs = tmem + lanes + Sh::kScores + b * 2 * Sh::kRows, cd = cs + Sh::kRows;
@@ -508,7 +508,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
             }
             if (wg == 0 && own < p.n) p.delta[(int64_t)h_own * p.n + own] = word ? delta + eps : 0.f;
         }
-        ok = __all_sync(kFullMask, ok && (total == 0 || mbar_wait(&sh.done, 0, abort_flag)));
+        ok = __all_sync(kFullMask, ok && (total == 0 || mbar_nap(&sh.done, 0, abort_flag)));
         tc_fence_after();
         if (ROLE == 0 && p.sink_rec) {
             if (h_own == 0 && tid == 0) p.sink_rec[tile] = !hi ? -1 : s_lo >= t0 ? -2 : sinks ? s_lo : -1;
@@ -613,7 +613,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                 umma_commit(&sh.s_full[b]);
             };
             auto wait = [&](uint64_t *bar, uint32_t parity) {
-                const bool got = __all_sync(kFullMask, mbar_wait(bar, parity, abort_flag));
+                const bool got = __all_sync(kFullMask, mbar_nap(bar, parity, abort_flag));
                 tc_fence_after();
                 return got;
             };
@@ -662,7 +662,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
             int32_t t = 0;
             for (; t < total; ++t) {
                 const uint32_t stage = t % Sh::kStages, round = t / Sh::kStages, base = ring + stage * Sh::kStage;
-                if (round > 0 && !mbar_wait(&sh.empty[stage], (round - 1) & 1, abort_flag)) break;
+                if (round > 0 && !mbar_nap(&sh.empty[stage], (round - 1) & 1, abort_flag)) break;
                 const int32_t head = ROLE == 0 ? (int32_t)kvh : (int32_t)h0 + t / per_head, at = tile_at(t % per_head);
                 mbar_expect(&sh.landed[stage], Sh::kStage);
 #pragma unroll
@@ -673,7 +673,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
             }
             // after a wait that ran out: what is under way lands before the block leaves
             if (*abort_flag)
-                for (int32_t u = max(0, t - Sh::kStages); u < t; ++u) mbar_wait(&sh.landed[u % Sh::kStages], (u / Sh::kStages) & 1, &sh.quiet);
+                for (int32_t u = max(0, t - Sh::kStages); u < t; ++u) mbar_nap(&sh.landed[u % Sh::kStages], (u / Sh::kStages) & 1, &sh.quiet);
         }
         __syncwarp();
     } else {
@@ -681,7 +681,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
         if (SMALL) {
             asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kBackOtherRegs));
             // the block's own rows: one operand each
-            if (__all_sync(kFullMask, mbar_wait(&sh.own_landed, 0, abort_flag))) {
+            if (__all_sync(kFullMask, mbar_nap(&sh.own_landed, 0, abort_flag))) {
                 const uint32_t a = ring + Sh::kRing + (warp - kMmaWarp - 2) * Sh::kOwn, top[2] = {own_words[0], own_words[1]}, low[2] = {own_words[2], own_words[3]};
                 zero_rows<NB>(a, 128 * 128, 64, top, lane);
                 zero_rows<NB>(a + 64 * 128, 128 * 128, 64, low, lane);
@@ -712,7 +712,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                     run_lo = (a[0] | a[1] | b[0] | b[1]) ? row_limits(p, q0 + first).lo : INT32_MAX;
                 }
             }
-            if (!__all_sync(kFullMask, mbar_wait(&sh.landed[stage], (t / Sh::kStages) & 1, abort_flag))) break;
+            if (!__all_sync(kFullMask, mbar_nap(&sh.landed[stage], (t / Sh::kStages) & 1, abort_flag))) break;
             if (ROLE == 0) {
                 if (lane < 2) sh.vis[stage][lane] = lane ? vis[1] : vis[0];
             } else {
