@@ -50,6 +50,32 @@ struct FwdShared {
     float ref[2][128], sum[2][128];              // per warpgroup and row
 };
 
+// The output of row i by a warp, from the pairs that it sees.
+template <typename T>
+__device__ __forceinline__ void output_again(const AttendParams &p, uint32_t h, uint32_t kvh, int64_t i, float lse, uint32_t lane)
+{
+    const RowLimits row = row_limits(p, i);
+    const T *q = static_cast<const T *>(p.q) + i * (int64_t)p.ldq + h * p.dim;
+    const T *k = static_cast<const T *>(p.k) + kvh * p.dim, *v = static_cast<const T *>(p.v) + kvh * p.dim;
+    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int part = 0; part < 2; ++part) {
+        const int32_t a = part ? row.lo : row.s, b = part ? row.hi : row.se;
+#pragma unroll 1
+        for (int64_t j0 = a; j0 < b && !all_nan(acc, p.dim, lane); j0 += 32) {
+            const int64_t j = j0 + lane;
+            const bool seen = j < b && is_word(p, j);
+            float w = 0.f;
+            if (seen) w = fast_exp2(fmaf(row_dot(q, k + j * (int64_t)p.ldk, p.dim), p.scale * kLog2e, pair_bias(p, h, (int32_t)(j - i))) - lse);
+            add_rows(acc, w, __ballot_sync(kFullMask, seen), v + j0 * (int64_t)p.ldv, p.ldv, p.dim, lane);
+        }
+    }
+    T *out = static_cast<T *>(p.out) + i * (int64_t)p.ldo + h * p.dim;
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+        if (lane + 32u * x < p.dim) out[lane + 32u * x] = from_f32<T>(acc[x]);
+}
+
 template <typename T, int NB, bool SMALL>
 __global__ void __launch_bounds__(kFwdThreads, FwdShape<NB, SMALL>::kBlocks)
 attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
@@ -266,14 +292,16 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         ok = __all_sync(kFullMask, ok && (tiles == 0 || ready(&sh.done, 0)));
         tc_fence_after();
         float f0 = to == -INFINITY ? 0.f : fast_exp2(r0 - to), f1 = to == -INFINITY ? 0.f : fast_exp2(r1 - to);
-        const float total = sh.sum[0][r] * f0 + sh.sum[1][r] * f1, inv = total > 0.f ? 1.f / total : 0.f;
-        if (p.lse && wg == 0 && own < p.n) p.lse[(int64_t)h * p.n + own] = total > 0.f ? to + log2f(total) : INFINITY;
+        const float total = sh.sum[0][r] * f0 + sh.sum[1][r] * f1, inv = total == 0.f ? 0.f : 1.f / total;
+        const float lse = total == 0.f ? INFINITY : to + log2f(total);      // a sum that is NaN stays one
+        if (p.lse && wg == 0 && own < p.n) p.lse[(int64_t)h * p.n + own] = lse;
         f0 *= inv;
         f1 *= inv;
         // out through shared memory (every tile is read by now), a row of 16-byte chunks at a time
         const uint32_t row_bytes = p.dim * 2u, part = (warp & 3u) * 32u;
         unsigned char *stripe = smem + part * row_bytes, *line = stripe + lane * row_bytes;
         const uint32_t turn = lane % dch;                            // chunks are turned by the row: fewer bank conflicts
+        float2 zero = make_float2(0.f, 0.f);                         // NaN once an output is not finite
 #pragma unroll
         for (int i = 0; i < NB * 2; ++i) {
             const uint32_t c = i * 32 + wg * 16;
@@ -286,9 +314,11 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             float o[16];
 #pragma unroll
             for (int e = 0; e < 16; ++e) {                           // an accumulator that no tile was added to holds anything
-                const float x = f0 > 0.f ? __uint_as_float(a[e]) * f0 : 0.f;
-                o[e] = f1 > 0.f ? fmaf(__uint_as_float(b[e]), f1, x) : x;
+                const float x = f0 == 0.f ? 0.f : __uint_as_float(a[e]) * f0;
+                o[e] = f1 == 0.f ? x : fmaf(__uint_as_float(b[e]), f1, x);
             }
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) zero = fma2(make_float2(o[e], o[e + 1]), make_float2(0.f, 0.f), zero);
 #pragma unroll
             for (int g = 0; g < 2; ++g)
                 if (c + g * 8 < p.dim) {
@@ -299,9 +329,18 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     *reinterpret_cast<uint4 *>(line + (ch >= dch ? ch - dch : ch) * 16u) = w;
                 }
         }
-        asm volatile("bar.sync %0, 64;" ::"r"(2u + (warp & 3u)) : "memory");        // the two warps of these rows
+        uint32_t bad = __ballot_sync(kFullMask, zero.x + zero.y != 0.f && own < p.n && lse == lse);
+        const bool again = any_of_64(2u + (warp & 3u), bad != 0u);  // the two warps of these rows
         store_rows(static_cast<char *>(p.out) + ((uint64_t)(t0 + part) * p.ldo + (uint64_t)h * p.dim) * 2u, p.ldo * 2u, stripe, dch,
                    (int32_t)min((int64_t)32, p.n - (int64_t)(t0 + part)), wg * 32u + lane, 64u);
+        if (again && ok) {
+            asm volatile("bar.sync %0, 64;" ::"r"(2u + (warp & 3u)) : "memory");     // over what has been stored
+#pragma unroll 1
+            for (; bad; bad &= bad - 1u) {                           // a row that both warps found is written twice, the same
+                const int32_t x = __ffs(bad) - 1;
+                output_again<T>(p, h, kvh, (int64_t)t0 + part + x, __shfl_sync(kFullMask, lse, x), lane);
+            }
+        }
         tc_fence_before();
     } else if (warp == 8) {
         // ============ MMA issue: one lane ============

@@ -137,6 +137,69 @@ __device__ __forceinline__ void zero_rows(uint32_t tile, uint32_t block, uint32_
     }
 }
 
+// ---- rows that came out not finite, once more ----
+// The tensor cores multiply a masked weight, zero, with whatever lies there, and zero times an infinity or NaN is NaN: a
+// value that is not finite spoils the rows of its tile, also of other sentences.  A row of finite inputs that fit is
+// finite, so that a look at what leaves the kernel finds these; a warp forms each again from the pairs it sees alone.
+
+// A pair's bias in base-2 units.
+__device__ __forceinline__ float pair_bias(const AttendParams &p, uint32_t h, int32_t rel)
+{
+    return p.b.n ? log2_bias(__ldg(p.bias + (size_t)bucket_of(p.b, rel) * p.heads + h)) : 0.f;
+}
+
+__device__ __forceinline__ bool is_word(const AttendParams &p, int64_t i)
+{
+    const int2 sp = __ldg(p.spans + i);
+    return sp.y > sp.x;
+}
+
+template <typename T>
+__device__ __forceinline__ float row_dot(const T *a, const T *b, uint32_t dim)
+{
+    float x = 0.f;
+#pragma unroll 1
+    for (uint32_t c = 0; c < dim; c += 8) {
+        const Pack<T, 8> u = load_pack<T, 8>(a + c), w = load_pack<T, 8>(b + c);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x = fmaf(to_f32(u.e[e]), to_f32(w.e[e]), x);
+    }
+    return x;
+}
+
+// acc += the lanes' weights times the lanes' rows, for the lanes in `live`; a lane holds columns lane, lane + 32, ...
+template <typename T>
+__device__ __forceinline__ void add_rows(float (&acc)[4], float w, uint32_t live, const T *rows, uint64_t ld, uint32_t dim, uint32_t lane)
+{
+#pragma unroll 1
+    while (live) {
+        const uint32_t e = (uint32_t)__ffs(live) - 1u;
+        live &= live - 1u;
+        const float by = __shfl_sync(kFullMask, w, e);
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+            if (lane + 32u * x < dim) acc[x] = fmaf(by, to_f32(rows[e * ld + lane + 32u * x]), acc[x]);
+    }
+}
+
+// Nothing finite is left to be found: more pairs change no column.
+__device__ __forceinline__ bool all_nan(const float (&acc)[4], uint32_t dim, uint32_t lane)
+{
+    bool nan = true;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) nan = nan && (lane + 32u * x >= dim || acc[x] != acc[x]);
+    return __all_sync(kFullMask, nan);
+}
+
+// A barrier of 64 threads that says whether any of them found something.
+__device__ __forceinline__ bool any_of_64(uint32_t barrier, bool found)
+{
+    uint32_t any;
+    asm volatile("{ .reg .pred p, q; setp.ne.u32 p, %2, 0; barrier.cta.red.or.pred q, %1, 64, p; selp.u32 %0, 1, 0, q; }"
+                 : "=r"(any) : "r"(barrier), "r"((uint32_t)found) : "memory");
+    return any;
+}
+
 // Rows of `chunks` 16-byte chunks from a stripe of shared memory (chunk c of row r at chunk (c + r) mod chunks) to
 // global memory, by `threads` threads of which this is number `at`.
 __device__ __forceinline__ void store_rows(char *out, uint64_t ld_bytes, const unsigned char *stripe, uint32_t chunks, int32_t rows,

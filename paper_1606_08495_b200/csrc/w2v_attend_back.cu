@@ -88,12 +88,21 @@ __device__ __forceinline__ void write_bucket_sums(const AttendParams &p, const f
 // by the softmax threads.  sink_d holds dS for the first delta, which eps puts right.  A thread takes two columns
 // and a part of the rows, four sinks at a time; `red` is 16 KB for joining the parts.
 template <typename T, int NB, int kSoft>
-__device__ __forceinline__ void sink_sums(const AttendParams &p, const unsigned char *own_rows, const float *sink_p, float *sink_d,
-                                       float eps, float *red, int32_t sinks, int32_t s, int32_t t0, uint32_t wg, uint32_t r,
+__device__ __forceinline__ void sink_sums(const AttendParams &p, unsigned char *own_rows, const float *sink_p, float *sink_d,
+                                       RowLimits row, float eps, float *red, int32_t sinks, int32_t s, int32_t t0, uint32_t wg, uint32_t r,
                                        uint32_t tid, float *out, float *bias_out)
 {
     constexpr int kPairs = 32 * NB, kParts = kSoft / kPairs, kPartRows = 128 / kParts, kOwn = NB * 128 * 128;
-    for (int32_t k = (int32_t)wg; k < sinks; k += kSoft / 128) sink_d[k * 128 + (int32_t)r] -= eps * sink_p[k * 128 + (int32_t)r];
+    // a row of another sentence, or one that has all these sinks in its window, takes no part, whatever it holds
+    const bool part_of = row.s == s && row.s < row.se;
+    for (int32_t k = (int32_t)wg; k < sinks; k += kSoft / 128) {
+        const int32_t at = k * 128 + (int32_t)r;
+        sink_d[at] = part_of ? fmaf(-eps, sink_p[at], sink_d[at]) : 0.f;
+    }
+    if (!part_of)
+#pragma unroll
+        for (int c = 0; c < NB * 8; ++c)
+            *reinterpret_cast<uint4 *>(own_rows + wg * kOwn + (c >> 3) * (128 * 128) + r * 128u + ((c & 7) << 4)) = make_uint4(0, 0, 0, 0);
     soft_barrier(kSoft);
     const uint32_t pair = tid % kPairs, part = tid / kPairs, width = 2 * p.dim;
     for (int32_t k0 = 0; k0 < sinks; k0 += 4) {
@@ -160,6 +169,79 @@ __device__ __forceinline__ void sink_sums(const AttendParams &p, const unsigned 
     }
 }
 
+// Where the run of keys of the query tile that begins at q0 begins; by a warp.
+__device__ __forceinline__ int32_t run_begin(const AttendParams &p, int32_t q0, uint32_t lane)
+{
+    uint32_t a[2], b[2];
+    word_bits(p, q0, 64, lane, a);
+    word_bits(p, (int64_t)q0 + 64, 64, lane, b);
+    const int32_t first = a[0] ? __ffs(a[0]) - 1 : a[1] ? 31 + __ffs(a[1]) : b[0] ? 63 + __ffs(b[0]) : 95 + __ffs(b[1]);
+    return (a[0] | a[1] | b[0] | b[1]) ? row_limits(p, q0 + first).lo : INT32_MAX;
+}
+
+// dQ of row i by a warp, from the pairs that it sees.
+template <typename T>
+__device__ __forceinline__ void dq_again(const AttendParams &p, uint32_t h, uint32_t kvh, int64_t i, float lse, float delta, uint32_t lane)
+{
+    const RowLimits row = row_limits(p, i);
+    const T *q = static_cast<const T *>(p.q) + i * (int64_t)p.ldq + h * p.dim, *d_o = static_cast<const T *>(p.d_o) + i * (int64_t)p.ld_do + h * p.dim;
+    const T *k = static_cast<const T *>(p.k) + kvh * p.dim, *v = static_cast<const T *>(p.v) + kvh * p.dim;
+    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int part = 0; part < 2; ++part) {
+        const int32_t a = part ? row.lo : row.s, b = part ? row.hi : row.se;
+#pragma unroll 1
+        for (int64_t j0 = a; j0 < b && !all_nan(acc, p.dim, lane); j0 += 32) {
+            const int64_t j = j0 + lane;
+            const bool seen = j < b && is_word(p, j);
+            float w = 0.f;
+            if (seen) {
+                w = fast_exp2(fmaf(row_dot(q, k + j * (int64_t)p.ldk, p.dim), p.scale * kLog2e, pair_bias(p, h, (int32_t)(j - i))) - lse);
+                w *= row_dot(d_o, v + j * (int64_t)p.ldv, p.dim) - delta;
+            }
+            add_rows(acc, w, __ballot_sync(kFullMask, seen), k + j0 * (int64_t)p.ldk, p.ldk, p.dim, lane);
+        }
+    }
+    T *out = static_cast<T *>(p.dq) + i * (int64_t)p.ld_dq + h * p.dim;
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+        if (lane + 32u * x < p.dim) out[lane + 32u * x] = from_f32<T>(acc[x] * p.scale);
+}
+
+// dK (which = 0) or dV of key j by a warp, from the queries that see it; `sink`: what queries far behind add.
+template <typename T>
+__device__ __forceinline__ void dkv_again(const AttendParams &p, uint32_t which, uint32_t kvh, int64_t j, const float *sink, uint32_t lane)
+{
+    const int2 sp = __ldg(p.spans + j);
+    const uint32_t group = p.heads / p.kv_heads;
+    const T *k = static_cast<const T *>(p.k) + j * (int64_t)p.ldk + kvh * p.dim, *v = static_cast<const T *>(p.v) + j * (int64_t)p.ldv + kvh * p.dim;
+    const int64_t lo = max((int64_t)sp.x, j - p.right), hi = min((int64_t)sp.y, j + p.left + 1), tile = (j + p.left) / kAttendTile;
+    int64_t end = hi;                                                // and as a sink up to here, as in the tiles
+    if (j - sp.x < p.sinks && hi < sp.y && run_begin(p, (int32_t)(tile * kAttendTile), lane) <= j) end = max(hi, min((int64_t)sp.y, (tile + 1) * kAttendTile));
+    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (uint32_t h = kvh * group; h < (kvh + 1) * group; ++h) {
+        const T *q = static_cast<const T *>(p.q) + h * p.dim, *d_o = static_cast<const T *>(p.d_o) + h * p.dim;
+#pragma unroll 1
+        for (int64_t i0 = lo; i0 < end && !all_nan(acc, p.dim, lane); i0 += 32) {
+            const int64_t i = i0 + lane;
+            const bool seen = i < end && is_word(p, i);
+            float w = 0.f;
+            if (seen) {
+                w = fast_exp2(fmaf(row_dot(q + i * (int64_t)p.ldq, k, p.dim), p.scale * kLog2e, pair_bias(p, h, (int32_t)(j - i))) - __ldg(p.lse + (int64_t)h * p.n + i));
+                if (which == 0) w *= row_dot(d_o + i * (int64_t)p.ld_do, v, p.dim) - p.delta[(int64_t)h * p.n + i];
+            }
+            const uint32_t live = __ballot_sync(kFullMask, seen);
+            if (which == 0) add_rows(acc, w, live, q + i0 * (int64_t)p.ldq, p.ldq, p.dim, lane);
+            else add_rows(acc, w, live, d_o + i0 * (int64_t)p.ld_do, p.ld_do, p.dim, lane);
+        }
+    }
+    T *out = which == 0 ? static_cast<T *>(p.dk) + j * (int64_t)p.ld_dk + kvh * p.dim : static_cast<T *>(p.dv) + j * (int64_t)p.ld_dv + kvh * p.dim;
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+        if (lane + 32u * x < p.dim) out[lane + 32u * x] = from_f32<T>((acc[x] + (sink ? sink[lane + 32u * x] : 0.f)) * (which == 0 ? p.scale : 1.f));
+}
+
 template <typename T, int NB, int ROLE, bool SMALL>
 __global__ void __launch_bounds__(BackShape<NB, SMALL>::kThreads, BackShape<NB, SMALL>::kBlocks)
 attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_y,
@@ -173,7 +255,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
     __shared__ BackShared<Sh> sh;
     unsigned char *smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
     const uint32_t ring = smem_addr(smem);
-    const unsigned char *own_rows = smem + Sh::kRing;                // the two A sides, and o in role 0 (not SMALL), as they land
+    unsigned char *own_rows = smem + Sh::kRing;                      // the two A sides, and o in role 0 (not SMALL), as they land
     float *lut = reinterpret_cast<float *>(smem + Sh::kRing + 2 * Sh::kOwn + (ROLE == 0 ? max(SMALL ? 0 : Sh::kOwn, p.sinks * 1024) : 0));
     const uint32_t entries = bias_entries(p.b);
     float *rel_sums = lut + ((entries + 3u) & ~3u);                  // role 1: [softmax warps][entries]; role 0, SMALL: halves of the first delta
@@ -329,13 +411,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                     }
                     tmem_st16(tmem + lanes + (wg == 0 ? Sh::kA0 : Sh::kA1) + g * 16, x);
                 }
-                if (!word) {
-                    delta = 0.f;
-                    if (ROLE == 0 && p.sinks)                        // the sums for the sinks read the rows again
-#pragma unroll
-                        for (int c = 0; c < NB * 8; ++c)
-                            *reinterpret_cast<uint4 *>(smem + Sh::kRing + wg * Sh::kOwn + (c >> 3) * (128 * 128) + r * 128u + ((c & 7) << 4)) = make_uint4(0, 0, 0, 0);
-                }
+                if (!word) delta = 0.f;
                 tmem_wait_st();
                 tc_fence_before();
                 mbar_arrive(&sh.own_full);
@@ -385,7 +461,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                         }
                         tmem_wait_ld(sv);
                         tmem_held(dv);
-                        // -infinity where the key is hidden; a row or column that sees nothing has lse +infinity
+                        // a row or column that sees nothing has lse +infinity
                         float x[kC];
                         if (far) {
                             const float2 scale2 = make_float2(scale, scale), flat2 = make_float2(flat, flat);
@@ -401,11 +477,19 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
 #pragma unroll
                             for (int e = 0; e < kC; ++e) x[e] = fmaf(__uint_as_float(sv[e]), scale, ROLE == 0 ? near[e] : near[-e]);
                         }
-                        if (!__all_sync(kFullMask, (m | ~kAll) == 0xFFFFFFFFu)) {
-#pragma unroll
-                            for (int e = 0; e < kC; ++e) x[e] = m & (1u << e) ? x[e] : -INFINITY;
-                        }
+                        const bool masked = !__all_sync(kFullMask, (m | ~kAll) == 0xFFFFFFFFu);
                         uint32_t ws[kC / 2], wp[kC / 2];
+                        // masked pairs are taken out of the weights and of dS, not of the scores: a delta, lse or product
+                        // of such a pair may not be finite
+                        auto take_out = [&](float *w, float *d) {
+                            if (masked)
+#pragma unroll
+                                for (int e = 0; e < kC; ++e) {
+                                    w[e] = m & (1u << e) ? w[e] : 0.f;
+                                    d[e] = m & (1u << e) ? d[e] : 0.f;
+                                }
+                        };
+                        float ds[kC];
                         if (ROLE == 0) {
                             const float2 lse2 = make_float2(-lse, -lse), delta2 = make_float2(-delta, -delta);
 #pragma unroll
@@ -414,9 +498,15 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                                 w.x = fast_exp2(w.x);
                                 w.y = fast_exp2(w.y);
                                 const float2 d = mul2(w, add2(pair_of(dv[e], dv[e + 1]), delta2));
-                                eps2 = add2(eps2, d);
-                                wp[e / 2] = pack2<T>(w.x, w.y);
-                                ws[e / 2] = pack2<T>(d.x, d.y);
+                                x[e] = w.x; x[e + 1] = w.y;
+                                ds[e] = d.x; ds[e + 1] = d.y;
+                            }
+                            take_out(x, ds);
+#pragma unroll
+                            for (int e = 0; e < kC; e += 2) {
+                                eps2 = add2(eps2, make_float2(ds[e], ds[e + 1]));
+                                wp[e / 2] = pack2<T>(x[e], x[e + 1]);
+                                ws[e / 2] = pack2<T>(ds[e], ds[e + 1]);
                             }
                             tmem_st(cs + (SMALL ? c0 : c0 / 2), wp);
                             tmem_st(cd + (SMALL ? c0 : c0 / 2), ws);
@@ -425,14 +515,12 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                                 for (int e = 0; e < kC; ++e) {
                                     const int32_t i = (k - run) * Sh::kRows + c0 + e;
                                     if (i < sinks) {
-                                        const float w = fast_exp2(x[e] - lse);
-                                        sink_p[i * 128 + (int32_t)r] = w;
-                                        sink_d[i * 128 + (int32_t)r] = w * (__uint_as_float(dv[e]) - delta);
+                                        sink_p[i * 128 + (int32_t)r] = x[e];
+                                        sink_d[i * 128 + (int32_t)r] = ds[e];
                                     }
                                 }
                             }
                         } else {
-                            float ds[kC];
 #pragma unroll
                             for (int e = 0; e < kC; e += 4) {
                                 const float4 l4 = *reinterpret_cast<const float4 *>(&sh.lse[stage][c0 + e]);        // negated, as delta
@@ -440,13 +528,16 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                                 float2 p0 = add2(make_float2(x[e], x[e + 1]), make_float2(l4.x, l4.y));
                                 float2 p1 = add2(make_float2(x[e + 2], x[e + 3]), make_float2(l4.z, l4.w));
                                 p0.x = fast_exp2(p0.x); p0.y = fast_exp2(p0.y); p1.x = fast_exp2(p1.x); p1.y = fast_exp2(p1.y);
-                                wp[e / 2] = pack2<T>(p0.x, p0.y);
-                                wp[e / 2 + 1] = pack2<T>(p1.x, p1.y);
+                                x[e] = p0.x; x[e + 1] = p0.y; x[e + 2] = p1.x; x[e + 3] = p1.y;
                                 p0 = mul2(p0, add2(pair_of(dv[e], dv[e + 1]), make_float2(d4.x, d4.y)));
                                 p1 = mul2(p1, add2(pair_of(dv[e + 2], dv[e + 3]), make_float2(d4.z, d4.w)));
-                                ws[e / 2] = pack2<T>(p0.x, p0.y);
-                                ws[e / 2 + 1] = pack2<T>(p1.x, p1.y);
                                 ds[e] = p0.x; ds[e + 1] = p0.y; ds[e + 2] = p1.x; ds[e + 3] = p1.y;
+                            }
+                            take_out(x, ds);
+#pragma unroll
+                            for (int e = 0; e < kC; e += 2) {
+                                wp[e / 2] = pack2<T>(x[e], x[e + 1]);
+                                ws[e / 2] = pack2<T>(ds[e], ds[e + 1]);
                             }
                             tmem_st(cs + (SMALL ? c0 : c0 / 2), wp);
                             tmem_st(cd + (SMALL ? c0 : c0 / 2), ws);
@@ -514,7 +605,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
             if (h_own == 0 && tid == 0) p.sink_rec[tile] = !hi ? -1 : s_lo >= t0 ? -2 : sinks ? s_lo : -1;
             const uint32_t buckets = p.b.n * (p.b.two_sided ? 2u : 1u);
             float *bias_out = p.dbias ? p.dbias_part + ((size_t)((uint32_t)((p.n + kAttendTile - 1) / kAttendTile) + tile) * p.heads + h_own) * buckets : nullptr;
-            if (sinks) sink_sums<T, NB, Sh::kSoft>(p, own_rows, sink_p, sink_d, eps, reinterpret_cast<float *>(smem), sinks, s_lo, t0, wg, r, tid,
+            if (sinks) sink_sums<T, NB, Sh::kSoft>(p, own_rows, sink_p, sink_d, row, eps, reinterpret_cast<float *>(smem), sinks, s_lo, t0, wg, r, tid,
                                                    p.sink_part + ((size_t)tile * p.heads + h_own) * p.sinks * 2 * p.dim, bias_out);
             else if (bias_out) for (uint32_t b = tid; b < buckets; b += Sh::kSoft) bias_out[b] = 0.f;
             soft_barrier(Sh::kSoft);
@@ -532,6 +623,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
             const uint32_t row_bytes = p.dim * 2u, chunks = p.dim >> 3, turn = lane % chunks, part = ((warp & 3u) + which * 4u) * 32u;
             unsigned char *mine = smem + part * row_bytes, *line = mine + lane * row_bytes;
             constexpr int kCols = kHalf ? NB * 2 : NB * 4;           // steps of 16 columns
+            float2 zero = make_float2(0.f, 0.f);                     // NaN once a value is not finite
 #pragma unroll
             for (int i = 0; i < kCols; ++i) {
                 const uint32_t c = kHalf ? i * 32 + wg * 16 : i * 16;
@@ -550,12 +642,14 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                     } else {
                         tmem_wait_ld(o);
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) f[e] = __uint_as_float(o[e]);
+                        for (int e = 0; e < 16; ++e) f[e] = word ? __uint_as_float(o[e]) : 0.f;
                     }
                 } else {
 #pragma unroll
                     for (int e = 0; e < 16; ++e) f[e] = 0.f;
                 }
+#pragma unroll
+                for (int e = 0; e < 16; e += 2) zero = fma2(make_float2(f[e], f[e + 1]), make_float2(0.f, 0.f), zero);
 #pragma unroll
                 for (int q = 0; q < 2; ++q)
                     if (c + q * 8 < p.dim) {
@@ -573,12 +667,25 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
             const int32_t rows = (int32_t)min((int64_t)32, p.n - (int64_t)w0);
             const uint64_t ld = ROLE == 0 ? p.ld_dq : which == 0 ? p.ld_dk : p.ld_dv;
             char *out = static_cast<char *>(ROLE == 0 ? p.dq : which == 0 ? p.dk : p.dv) + ((uint64_t)w0 * ld + (uint64_t)h_own * p.dim) * 2u;
+            const bool nan = ROLE == 0 && (lse != lse || delta + eps != delta + eps);        // of its own: nothing to be found
+            uint32_t bad = __ballot_sync(kFullMask, zero.x + zero.y != 0.f && word && !nan);
+            bool again = bad != 0u;
             if (kHalf) {
-                asm volatile("bar.sync %0, 64;" ::"r"(2u + (warp & 3u)) : "memory");    // the two warps of these rows
+                again = any_of_64(2u + (warp & 3u), again);          // the two warps of these rows
                 store_rows(out, ld * 2u, mine, chunks, rows, wg * 32u + lane, 64u);
             } else {
                 __syncwarp();
                 store_rows(out, ld * 2u, mine, chunks, rows, lane, 32u);
+            }
+            if (again && ok) {                                       // over what has been stored
+                if (kHalf) asm volatile("bar.sync %0, 64;" ::"r"(2u + (warp & 3u)) : "memory");
+                else __syncwarp();
+#pragma unroll 1
+                for (; bad; bad &= bad - 1u) {
+                    const int32_t x = __ffs(bad) - 1;
+                    if (ROLE == 0) dq_again<T>(p, h_own, kvh, (int64_t)w0 + x, __shfl_sync(kFullMask, lse, x), __shfl_sync(kFullMask, delta + eps, x), lane);
+                    else dkv_again<T>(p, which, kvh, (int64_t)w0 + x, reinterpret_cast<const float *>(__shfl_sync(kFullMask, reinterpret_cast<unsigned long long>(sink), x)), lane);
+                }
             }
         }
         tc_fence_before();
@@ -703,14 +810,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                     lse[w] = i < p.n ? __ldg(p.lse + (int64_t)h * p.n + i) : INFINITY;
                     delta[w] = i < p.n ? p.delta[(int64_t)h * p.n + i] : 0.f;
                 }
-                if (p.sinks) {                                       // where the run of keys of this query tile begins
-                    uint32_t a[2], b[2];
-                    const int32_t q0 = at / kAttendTile * kAttendTile;
-                    word_bits(p, q0, 64, lane, a);
-                    word_bits(p, (int64_t)q0 + 64, 64, lane, b);
-                    const int32_t first = a[0] ? __ffs(a[0]) - 1 : a[1] ? 31 + __ffs(a[1]) : b[0] ? 63 + __ffs(b[0]) : 95 + __ffs(b[1]);
-                    run_lo = (a[0] | a[1] | b[0] | b[1]) ? row_limits(p, q0 + first).lo : INT32_MAX;
-                }
+                if (p.sinks) run_lo = run_begin(p, at / kAttendTile * kAttendTile, lane);
             }
             if (!__all_sync(kFullMask, mbar_nap(&sh.landed[stage], (t / Sh::kStages) & 1, abort_flag))) break;
             if (ROLE == 0) {

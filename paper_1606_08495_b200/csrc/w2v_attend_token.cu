@@ -256,13 +256,13 @@ attend_token_kernel(TokenParams p, uint32_t splits, uint32_t passes)
         float top = -INFINITY, s = 0.f, a = 0.f;
 #pragma unroll
         for (int w = 0; w < kTokWarps; ++w) top = fmaxf(top, wstat[(w * kKeep + r) * 2]);
-        if (top != -INFINITY)
+        const float from = top == -INFINITY ? 0.f : top;                // no finite score: the sums are zeros, or NaN, which stays
 #pragma unroll
-            for (int w = 0; w < kTokWarps; ++w) {
-                const float f = fast_exp2(wstat[(w * kKeep + r) * 2] - top);
-                s = fmaf(f, wstat[(w * kKeep + r) * 2 + 1], s);
-                a = fmaf(f, wacc[(w * kKeep + r) * p.dim + c], a);
-            }
+        for (int w = 0; w < kTokWarps; ++w) {
+            const float f = fast_exp2(wstat[(w * kKeep + r) * 2] - from);
+            s = fmaf(f, wstat[(w * kKeep + r) * 2 + 1], s);
+            a = fmaf(f, wacc[(w * kKeep + r) * p.dim + c], a);
+        }
         acc_s[i] = a;
         if (c == 0) { stat[2 * r] = top; stat[2 * r + 1] = s; }
     }
@@ -274,15 +274,15 @@ attend_token_kernel(TokenParams p, uint32_t splits, uint32_t passes)
         const uint32_t r = i / p.dim;
         float top = -INFINITY, s = 0.f, a = 0.f;
         for (uint32_t x = 0; x < splits; ++x) top = fmaxf(top, splits > 1 ? cluster.map_shared_rank(stat, x)[2 * r] : stat[2 * r]);
-        if (top != -INFINITY)
-            for (uint32_t x = 0; x < splits; ++x) {
-                const float *st = splits > 1 ? cluster.map_shared_rank(stat, x) : stat;
-                const float *ac = splits > 1 ? cluster.map_shared_rank(acc_s, x) : acc_s;
-                const float f = fast_exp2(st[2 * r] - top);
-                s = fmaf(f, st[2 * r + 1], s);
-                a = fmaf(f, ac[i], a);
-            }
-        out[i] = from_f32<T>(s > 0.f ? a / s : 0.f);
+        const float from = top == -INFINITY ? 0.f : top;
+        for (uint32_t x = 0; x < splits; ++x) {
+            const float *st = splits > 1 ? cluster.map_shared_rank(stat, x) : stat;
+            const float *ac = splits > 1 ? cluster.map_shared_rank(acc_s, x) : acc_s;
+            const float f = fast_exp2(st[2 * r] - from);
+            s = fmaf(f, st[2 * r + 1], s);
+            a = fmaf(f, ac[i], a);
+        }
+        out[i] = from_f32<T>(s == 0.f ? 0.f : a / s);                   // a sum that is NaN is not an empty row
     }
     if (splits > 1) cluster.sync();                                     // nobody leaves while its memory is read
 }

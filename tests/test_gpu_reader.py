@@ -285,6 +285,79 @@ def test_attend_large_scores_and_nonfinite_values_where_nothing_looks(model):
     assert torch.equal(o, o2) and all(torch.equal(a, b) for a, b in zip(g, g2))
 
 
+SPOILED = [(300, (5, 40), 4, 2, 80, 10, 10, 0, 32, 128, True), (900, (400, 800), 4, 2, 64, 60, 0, 4, 32, 128, False),
+           (700, (3, 90), 4, 2, 128, 511, 0, 4, 16, 64, False), (700, (100, 700), 4, 1, 96, 30, 30, 3, 64, 1024, True),
+           (513, (513, 513), 2, 2, 128, 40, 0, 20, 8, 16, False)]
+
+
+@pytest.mark.parametrize("case", range(len(SPOILED)))
+@pytest.mark.parametrize("which", ["q", "k", "v", "d_o"])
+def test_attend_nonfinite_words_reach_who_sees_them_only(model, case, which):
+    """A word that holds NaN spoils every row that its value enters by the formulas, and nothing else: not the other
+    sentences of its tile, nor what lies outside of the window."""
+    n, lens, h, kv, dim, left, right, sinks, buckets, reach, two = SPOILED[case]
+    toks = stream(n, lens, case)
+    clean = {"q": randn(n, h, dim, seed=1, dtype=torch.bfloat16), "k": randn(n, kv, dim, seed=2, dtype=torch.bfloat16),
+             "v": randn(n, kv, dim, seed=3, dtype=torch.bfloat16), "d_o": randn(n, h, dim, seed=4, dtype=torch.bfloat16)}
+    bias = randn(buckets, h, seed=9, by=0.5)
+    want, bound = attend_by_hand(clean["q"], clean["k"], clean["v"], toks, bias, left, right, sinks, reach, two, clean["d_o"], True)
+    sp = torch.from_numpy(spans_by_hand(toks)).cuda().long()
+    seen = sp[:, 1] > sp[:, 0]
+    i, j = torch.arange(n, device="cuda")[:, None], torch.arange(n, device="cuda")[None]
+    ok = (j >= sp[:, :1]) & (j < sp[:, 1:]) & seen[None] & (((j >= i - left) & (j <= i + right)) | ((j < sp[:, :1] + sinks) & (j < i)))
+    buckets_of = bucket(j - i, buckets // 2 if two else buckets, reach, two)
+    spans = model.sentence_spans(torch.from_numpy(toks).cuda())
+    words = torch.nonzero(seen).flatten()
+    # one in the middle, and the first word of the last sentence that has 3 of them (a sink where there are some)
+    starts = [int(w) for w in words if sp[w, 0] == w and sp[w, 1] - w >= 3]
+    for x in (int(words[len(words) // 2]), starts[-1]):
+        for value in (math.nan, math.inf):
+            t = {name: u.clone() for name, u in clean.items()}
+            t[which][x] = value
+            o, saved = model.attend(t["q"], t["k"], t["v"], spans, bias, train=True, left=left, right=right, sinks=sinks, reach=reach, two_sided=two)
+            dq, dk, dv, dbias = model.attend_backward(t["d_o"], saved)
+            model.sync()
+            rows = ok[:, x] if which in "kv" else torch.arange(n, device="cuda") == x       # queries whose weights or dS it enters
+            keys = (rows[:, None] & ok).any(0)
+            none = torch.zeros_like(rows)
+            hit = {"o": none if which == "d_o" else rows, "dq": rows, "dk": keys, "dv": none if which == "v" else keys}
+            for name, got in (("o", o), ("dq", dq), ("dk", dk), ("dv", dv)):
+                inside(got[~hit[name]], want[name][~hit[name]], bound[name][~hit[name]], name)
+                if value != value:
+                    assert torch.isnan(got[hit[name]]).all(), name
+            spoilt = torch.zeros(buckets, dtype=torch.bool, device="cuda")
+            spoilt[buckets_of[rows[:, None] & ok]] = True
+            inside(dbias[~spoilt], want["dbias"][~spoilt], bound["dbias"][~spoilt], "dbias")
+            if value != value:
+                assert torch.isnan(dbias[spoilt]).all()
+
+
+def test_attend_alone_with_nan(model):
+    q = torch.full((1, 1, 64), math.nan, dtype=torch.float16, device="cuda")
+    one = torch.ones_like(q)
+    spans = model.sentence_spans(torch.ones(1, dtype=torch.int32, device="cuda"))
+    for a, b, c in ((q, one, one), (one, q, one), (one, one, q)):
+        assert torch.isnan(model.attend(a, b, c, spans, left=3)).all()
+        cache = torch.zeros(2, 1, 4, 1, 64, dtype=torch.float16, device="cuda")
+        assert torch.isnan(model.attend_token(a, b, c, cache[0], cache[1], torch.zeros(1, dtype=torch.int32, device="cuda"), left=3)).all()
+
+
+def test_attend_token_nonfinite_places(model):
+    """NaN at a place that a sequence sees spoils that sequence, all of its heads of that key/value head, and nothing else."""
+    batch, h, kv, dim, left = 3, 4, 2, 64, 600
+    q, k, v = (randn(batch, x, dim, seed=x + s, dtype=torch.bfloat16) for s, x in ((0, h), (1, kv), (2, kv)))
+    cache = [randn(batch, left + 1, kv, dim, seed=s, dtype=torch.bfloat16) for s in (5, 6)]
+    pos = torch.tensor([500, 590, 31], dtype=torch.int32, device="cuda")
+    want = model.attend_token(q, k, v, cache[0].clone(), cache[1].clone(), pos, left=left)
+    for which in (0, 1):
+        c = [x.clone() for x in cache]
+        c[which][1, 200, 1] = math.nan
+        c[which][2, 32:] = math.nan                                  # beyond what sequence 2 sees
+        got = model.attend_token(q, k, v, *c, pos, left=left)
+        assert torch.isnan(got[1, 2:]).all() and torch.equal(got[1, :2], want[1, :2])
+        assert torch.equal(got[0], want[0]) and torch.equal(got[2], want[2])
+
+
 def test_attend_gradient_against_differences(model):
     """Along a random direction, in float16: the loss moves by its gradient's product with the direction."""
     n, h, kv, dim, dtype = 150, 4, 2, 64, torch.float16
