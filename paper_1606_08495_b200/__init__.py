@@ -4,4 +4,4 @@
 Importing the package is cheap and needs no GPU; the CUDA library is loaded the
 first time `binding` is used and its absence is an error, never a fallback.
 """
-__all__ = ["corpus", "binding", "build"]
+__all__ = ["corpus", "binding", "build", "reader"]
