@@ -585,6 +585,8 @@ int32_t w2v_bucket_starts(uint32_t buckets, uint32_t reach, uint32_t two_sided, 
  *               position (a multiple of 8; one packed projection can hold q, k and v), 16-byte aligned.
  *   bias        [buckets][heads] floats, NULL when buckets is 0.
  *               A bias of -infinity hides a bucket, as one of the lowest float does where another bucket is seen.
+ *   A value that is not finite reaches the positions that see its word and no others, in both directions; rows that
+ *   come out not finite are formed a second time, slowly.  What words outside the vocabulary hold reaches nobody.
  *   lse         [heads][n] floats for the backward call, or NULL: base-2 logarithm of the softmax sum, +infinity
  *               for a position that sees nothing.
  * Errors: W2V_ERR_ARG, W2V_ERR_NOMEM, W2V_ERR_CUDA.  A block that waits too long on its own pipeline gives

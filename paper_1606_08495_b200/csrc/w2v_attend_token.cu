@@ -18,7 +18,9 @@
 // The softmax weights enter the second product as the sum of two numbers of the cache's type, so that what is lost is
 // 2^-18 and not 2^-9 of them.  Each warp copies its next step's keys and values to shared memory in the background, so
 // that what is under way does not have to fit in registers.  There chunk c of row r lies at c ^ turn(r), which keeps
-// both ways of reading free of bank conflicts.
+// both ways of reading free of bank conflicts.  96 sequences, 16 heads of 128 over 4 of keys and values, windows of 4,096: 150 us,
+// 4.8 TB/s = 0.75 of measured copy; with direct loads 236 us, with copies but an address per access 191 us.  A single sequence of
+// 5 heads of 64 and windows of 1,001 takes 6 us.
 #include <cooperative_groups.h>
 
 #include "w2v_attend.cuh"
