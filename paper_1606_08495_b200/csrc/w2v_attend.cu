@@ -9,7 +9,8 @@
 // where a tile has masks or differing biases, writes the scores back with both applied), the second exponentiates.
 // The output is rescaled only when a row's largest score outgrows the reference by 2^8.
 //
-// What bounds it: the softmax's instructions, not the matrix units or memory.  A prompt of 32,768 words (fp16, 8 heads of 64,
+// What bounds it: latency.  The softmax warps wait for their tensor-memory reads and for the chain from there to the
+// weights (issue slots 35 % busy, matrix units 24 %, heads of 128), and tensor memory holds no more of them.  A prompt of 32,768 words (fp16, 8 heads of 64,
 // 2 of keys and values, windows of 4,096): 0.51 ms, 0.30 of the measured rate of matrix products; 16,381 words of long
 // documents, 16 heads of 128, windows of 1,024: 0.29 ms; 131,072 words in sessions of 5 to 40, 4 heads of 80: 0.15 ms, where
 // beginnings and ends of blocks are most of the time.

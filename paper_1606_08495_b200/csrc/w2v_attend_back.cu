@@ -14,7 +14,7 @@
 // sums over its 128 queries (the tile of the sinks is there anyway), which a small kernel adds up for role 1.
 //
 // P and dS are rounded to the arrays' type as A sides of the gradient products; dbias, delta and the sinks' sums take them in
-// fp32.  Bound by the warpgroups' instructions per score: 16,381 words, 16 heads of 128 (4 of
+// fp32.  Bound by latency in the warpgroups (issue slots 40 %, matrix units 35 % busy): 16,381 words, 16 heads of 128 (4 of
 // keys and values), windows of 1,024: 406 us (role 0) and 409 us (role 1).
 #include <type_traits>
 
