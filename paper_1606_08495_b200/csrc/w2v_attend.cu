@@ -334,11 +334,11 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     *reinterpret_cast<uint4 *>(line + (ch >= dch ? ch - dch : ch) * 16u) = w;
                 }
         }
-        uint32_t bad = __ballot_sync(kFullMask, zero.x + zero.y != 0.f && own < p.n && lse == lse);
+        uint32_t bad = __ballot_sync(kFullMask, ok && zero.x + zero.y != 0.f && own < p.n && lse == lse);
         const bool again = any_of_64(2u + (warp & 3u), bad != 0u);  // the two warps of these rows
         store_rows(static_cast<char *>(p.out) + ((uint64_t)(t0 + part) * p.ldo + (uint64_t)h * p.dim) * 2u, p.ldo * 2u, stripe, dch,
                    (int32_t)min((int64_t)32, p.n - (int64_t)(t0 + part)), wg * 32u + lane, 64u);
-        if (again && ok) {
+        if (again) {                                                 // both warps or neither
             asm volatile("bar.sync %0, 64;" ::"r"(2u + (warp & 3u)) : "memory");     // over what has been stored
 #pragma unroll 1
             for (; bad; bad &= bad - 1u) {                           // a row that both warps found is written twice, the same

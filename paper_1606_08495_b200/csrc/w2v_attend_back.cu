@@ -32,7 +32,6 @@ namespace w2v {
 //   else:  all of the tensor memory; the A sides in tensor memory; the warpgroups take the tiles in turn.
 template <int NB, bool SMALL>
 struct BackShape {
-    static constexpr int kWg = 2;                                    // softmax warpgroups
     static constexpr int kTile = SMALL ? 256 : 128;                  // softmax threads that share a tile
     static constexpr int kChunk = SMALL ? 16 : 32;                   // columns a thread takes at once
     static constexpr int kBuf = SMALL && NB == 2 ? 1 : 2;            // score buffers
@@ -44,7 +43,7 @@ struct BackShape {
     static_assert(kScores + kBuf * 2 * kRows <= kAlloc, "tensor memory");
     static constexpr int kOperand = NB * kRows * 128, kStage = 2 * kOperand, kRing = kStages * kStage;
     static constexpr int kOwn = NB * 128 * 128;                      // bytes of one operand of the block's own rows
-    static constexpr int kSoft = 128 * kWg, kThreads = kSoft + 128, kBlocks = 512 / (int)kAlloc;
+    static constexpr int kSoft = 256, kThreads = kSoft + 128, kBlocks = 512 / (int)kAlloc;
     static_assert(kRing + 2 * kOwn >= 2 * NB * 128 * 128, "the outputs are staged where the ring and the own rows were");
 };
 // SMALL: of the 80 registers a thread has at launch, the helpers' warpgroup gives what it has beyond 48 to the two of
@@ -60,7 +59,7 @@ struct BackShared {
     uint32_t vis[Sh::kStages][2];                    // role 0: which keys of the stage are words
     int32_t run_lo[Sh::kStages];                     // role 1: where the run of the stage's query tile begins
     __align__(16) float lse[Sh::kStages][Sh::kRows], delta[Sh::kStages][Sh::kRows];      // role 1: of the stage's queries, negated
-    float eps[Sh::kWg][128];
+    float eps[2][128];
     float far_sum[8][2];
 };
 
@@ -598,11 +597,9 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
         float eps = 0.f;
         if (ROLE == 0) {
             eps = eps2.x + eps2.y;
-            if (Sh::kWg == 2) {
-                sh.eps[wg][r] = eps;
-                soft_barrier(Sh::kSoft);
-                eps = sh.eps[0][r] + sh.eps[Sh::kWg - 1][r];
-            }
+            sh.eps[wg][r] = eps;
+            soft_barrier(Sh::kSoft);
+            eps = sh.eps[0][r] + sh.eps[1][r];
             if (wg == 0 && own < p.n) p.delta[(int64_t)h_own * p.n + own] = word ? delta + eps : 0.f;
         }
         ok = __all_sync(kFullMask, ok && (total == 0 || mbar_nap(&sh.done, 0, abort_flag)));
@@ -616,82 +613,78 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
             else if (bias_out) for (uint32_t b = tid; b < buckets; b += Sh::kSoft) bias_out[b] = 0.f;
             soft_barrier(Sh::kSoft);
         }
-        // outputs leave through shared memory: dQ (with two warpgroups, half of its columns by each), or dK and dV (by one each)
-        constexpr int kTurns = ROLE == 1 && Sh::kWg == 1 ? 2 : 1;
+        // outputs leave through shared memory: dQ (half of its columns by each warpgroup), or dK and dV (one each)
+        constexpr bool kHalf = ROLE == 0;
+        const uint32_t which = ROLE == 0 ? 0u : wg;              // 0: dQ or dK, 1: dV
+        const float by = which == 0 ? p.scale : 1.f;
+        const float *sink = nullptr;
+        if (ROLE == 1 && p.sink_used && word && own - sent < p.sinks && p.sink_used[sent / kAttendTile] == sent)
+            sink = p.sink_sum + ((((size_t)(sent / kAttendTile) * p.kv_heads + kvh) * p.sinks + (size_t)(own - sent)) * 2 + which) * p.dim;
+        const uint32_t row_bytes = p.dim * 2u, chunks = p.dim >> 3, turn = lane % chunks, part = ((warp & 3u) + which * 4u) * 32u;
+        unsigned char *mine = smem + part * row_bytes, *line = mine + lane * row_bytes;
+        constexpr int kCols = kHalf ? NB * 2 : NB * 4;           // steps of 16 columns
+        float2 zero = make_float2(0.f, 0.f);                     // NaN once a value is not finite
 #pragma unroll
-        for (int turn_of = 0; turn_of < kTurns; ++turn_of) {
-            constexpr bool kHalf = ROLE == 0 && Sh::kWg == 2;
-            const uint32_t which = ROLE == 0 ? 0u : Sh::kWg == 2 ? wg : (uint32_t)turn_of;       // 0: dQ or dK, 1: dV
-            const float by = which == 0 ? p.scale : 1.f;
-            const float *sink = nullptr;
-            if (ROLE == 1 && p.sink_used && word && own - sent < p.sinks && p.sink_used[sent / kAttendTile] == sent)
-                sink = p.sink_sum + ((((size_t)(sent / kAttendTile) * p.kv_heads + kvh) * p.sinks + (size_t)(own - sent)) * 2 + which) * p.dim;
-            const uint32_t row_bytes = p.dim * 2u, chunks = p.dim >> 3, turn = lane % chunks, part = ((warp & 3u) + which * 4u) * 32u;
-            unsigned char *mine = smem + part * row_bytes, *line = mine + lane * row_bytes;
-            constexpr int kCols = kHalf ? NB * 2 : NB * 4;           // steps of 16 columns
-            float2 zero = make_float2(0.f, 0.f);                     // NaN once a value is not finite
+        for (int i = 0; i < kCols; ++i) {
+            const uint32_t c = kHalf ? i * 32 + wg * 16 : i * 16;
+            if (c >= dim16) break;
+            float f[16];
+            if (total) {
+                uint32_t o[16];
+                tmem_ld16(tmem + lanes + (which == 0 ? Sh::kG0 : Sh::kG1) + c, o);
+                if (ROLE == 0) {                                 // the correction of the first delta
+                    uint32_t pk[16];
+                    tmem_ld16(tmem + lanes + Sh::kG1 + c, pk);
+                    tmem_wait_ld(o);
+                    tmem_wait_ld(pk);
 #pragma unroll
-            for (int i = 0; i < kCols; ++i) {
-                const uint32_t c = kHalf ? i * 32 + wg * 16 : i * 16;
-                if (c >= dim16) break;
-                float f[16];
-                if (total) {
-                    uint32_t o[16];
-                    tmem_ld16(tmem + lanes + (which == 0 ? Sh::kG0 : Sh::kG1) + c, o);
-                    if (ROLE == 0) {                                 // the correction of the first delta
-                        uint32_t pk[16];
-                        tmem_ld16(tmem + lanes + Sh::kG1 + c, pk);
-                        tmem_wait_ld(o);
-                        tmem_wait_ld(pk);
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) f[e] = word ? fmaf(-eps, __uint_as_float(pk[e]), __uint_as_float(o[e])) : 0.f;
-                    } else {
-                        tmem_wait_ld(o);
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) f[e] = word ? __uint_as_float(o[e]) : 0.f;
-                    }
+                    for (int e = 0; e < 16; ++e) f[e] = word ? fmaf(-eps, __uint_as_float(pk[e]), __uint_as_float(o[e])) : 0.f;
                 } else {
+                    tmem_wait_ld(o);
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) f[e] = 0.f;
+                    for (int e = 0; e < 16; ++e) f[e] = word ? __uint_as_float(o[e]) : 0.f;
                 }
-#pragma unroll
-                for (int e = 0; e < 16; e += 2) zero = fma2(make_float2(f[e], f[e + 1]), make_float2(0.f, 0.f), zero);
-#pragma unroll
-                for (int q = 0; q < 2; ++q)
-                    if (c + q * 8 < p.dim) {
-                        if (sink) {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) f[q * 8 + e] += sink[c + q * 8 + e];
-                        }
-                        uint4 w;
-                        w.x = pack2<T>(f[q * 8] * by, f[q * 8 + 1] * by); w.y = pack2<T>(f[q * 8 + 2] * by, f[q * 8 + 3] * by);
-                        w.z = pack2<T>(f[q * 8 + 4] * by, f[q * 8 + 5] * by); w.w = pack2<T>(f[q * 8 + 6] * by, f[q * 8 + 7] * by);
-                        const uint32_t ch = (c >> 3) + q + turn;
-                        *reinterpret_cast<uint4 *>(line + (ch >= chunks ? ch - chunks : ch) * 16u) = w;
-                    }
-            }
-            const int32_t rows = (int32_t)min((int64_t)32, p.n - (int64_t)w0);
-            const uint64_t ld = ROLE == 0 ? p.ld_dq : which == 0 ? p.ld_dk : p.ld_dv;
-            char *out = static_cast<char *>(ROLE == 0 ? p.dq : which == 0 ? p.dk : p.dv) + ((uint64_t)w0 * ld + (uint64_t)h_own * p.dim) * 2u;
-            const bool nan = ROLE == 0 && (lse != lse || delta + eps != delta + eps);        // of its own: nothing to be found
-            uint32_t bad = __ballot_sync(kFullMask, zero.x + zero.y != 0.f && word && !nan);
-            bool again = bad != 0u;
-            if (kHalf) {
-                again = any_of_64(2u + (warp & 3u), again);          // the two warps of these rows
-                store_rows(out, ld * 2u, mine, chunks, rows, wg * 32u + lane, 64u);
             } else {
-                __syncwarp();
-                store_rows(out, ld * 2u, mine, chunks, rows, lane, 32u);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) f[e] = 0.f;
             }
-            if (again && ok) {                                       // over what has been stored
-                if (kHalf) asm volatile("bar.sync %0, 64;" ::"r"(2u + (warp & 3u)) : "memory");
-                else __syncwarp();
-#pragma unroll 1
-                for (; bad; bad &= bad - 1u) {
-                    const int32_t x = __ffs(bad) - 1;
-                    if (ROLE == 0) dq_again<T>(p, h_own, kvh, (int64_t)w0 + x, __shfl_sync(kFullMask, lse, x), __shfl_sync(kFullMask, delta + eps, x), lane);
-                    else dkv_again<T>(p, which, kvh, (int64_t)w0 + x, reinterpret_cast<const float *>(__shfl_sync(kFullMask, reinterpret_cast<unsigned long long>(sink), x)), lane);
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) zero = fma2(make_float2(f[e], f[e + 1]), make_float2(0.f, 0.f), zero);
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+                if (c + q * 8 < p.dim) {
+                    if (sink) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) f[q * 8 + e] += sink[c + q * 8 + e];
+                    }
+                    uint4 w;
+                    w.x = pack2<T>(f[q * 8] * by, f[q * 8 + 1] * by); w.y = pack2<T>(f[q * 8 + 2] * by, f[q * 8 + 3] * by);
+                    w.z = pack2<T>(f[q * 8 + 4] * by, f[q * 8 + 5] * by); w.w = pack2<T>(f[q * 8 + 6] * by, f[q * 8 + 7] * by);
+                    const uint32_t ch = (c >> 3) + q + turn;
+                    *reinterpret_cast<uint4 *>(line + (ch >= chunks ? ch - chunks : ch) * 16u) = w;
                 }
+        }
+        const int32_t rows = (int32_t)min((int64_t)32, p.n - (int64_t)w0);
+        const uint64_t ld = ROLE == 0 ? p.ld_dq : which == 0 ? p.ld_dk : p.ld_dv;
+        char *out = static_cast<char *>(ROLE == 0 ? p.dq : which == 0 ? p.dk : p.dv) + ((uint64_t)w0 * ld + (uint64_t)h_own * p.dim) * 2u;
+        const bool nan = ROLE == 0 && (lse != lse || delta + eps != delta + eps);        // of its own: nothing to be found
+        uint32_t bad = __ballot_sync(kFullMask, ok && zero.x + zero.y != 0.f && word && !nan);
+        bool again = bad != 0u;
+        if (kHalf) {
+            again = any_of_64(2u + (warp & 3u), again);          // the two warps of these rows
+            store_rows(out, ld * 2u, mine, chunks, rows, wg * 32u + lane, 64u);
+        } else {
+            __syncwarp();
+            store_rows(out, ld * 2u, mine, chunks, rows, lane, 32u);
+        }
+        if (again) {                                             // both warps or neither; over what has been stored
+            if (kHalf) asm volatile("bar.sync %0, 64;" ::"r"(2u + (warp & 3u)) : "memory");
+            else __syncwarp();
+#pragma unroll 1
+            for (; bad; bad &= bad - 1u) {
+                const int32_t x = __ffs(bad) - 1;
+                if (ROLE == 0) dq_again<T>(p, h_own, kvh, (int64_t)w0 + x, __shfl_sync(kFullMask, lse, x), __shfl_sync(kFullMask, delta + eps, x), lane);
+                else dkv_again<T>(p, which, kvh, (int64_t)w0 + x, reinterpret_cast<const float *>(__shfl_sync(kFullMask, reinterpret_cast<unsigned long long>(sink), x)), lane);
             }
         }
         tc_fence_before();
