@@ -143,7 +143,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     const uint32_t tmem = warp_value(sh.tmem);
     volatile int *abort_flag = &sh.abort_flag;
     auto ready = [&](uint64_t *bar, uint32_t parity) { return SMALL ? mbar_wait(bar, parity, abort_flag) : mbar_nap(bar, parity, abort_flag); };
-    // the run of keys [lo, hi) and the sinks [s, s_end) before it, which are the first tile
+    // the run of keys [lo, hi) and the sinks [s, s_end) before it, which are the first tiles
     int32_t lo = INT32_MAX, hi = 0, s = INT32_MAX;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
@@ -155,10 +155,10 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     hi = warp_value(hi);
     s = warp_value(s);
     const int32_t s_end = hi ? min(s + p.sinks, lo) : 0;
-    const int32_t extra = s < s_end ? 1 : 0;
+    const int32_t extra = s < s_end ? (s_end - s + Sh::kRows - 1) / Sh::kRows : 0;
     const int32_t tiles = hi ? extra + (hi - lo + Sh::kRows - 1) / Sh::kRows : 0;
-    auto tile_at = [&](int32_t t) { return extra && t == 0 ? s : lo + (t - extra) * Sh::kRows; };
-    auto tile_keys = [&](int32_t t) { return extra && t == 0 ? s_end - s : min(Sh::kRows, hi - tile_at(t)); };
+    auto tile_at = [&](int32_t t) { return t < extra ? s + t * Sh::kRows : lo + (t - extra) * Sh::kRows; };
+    auto tile_keys = [&](int32_t t) { return min(Sh::kRows, (t < extra ? s_end : hi) - tile_at(t)); };
 
     if (warp < 8) {
         // ============ softmax: one row per thread, tiles in turn ============

@@ -1,0 +1,47 @@
+"""The reader operators where layouts end: many sinks, tiles without words, rows that hold anything.
+
+Definitions and bounds are those of test_gpu_reader.py.
+"""
+import pytest
+import torch
+
+from paper_1606_08495_b200 import binding
+from test_gpu_reader import VOCAB, attend_by_hand, inside, randn, stream
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def model():
+    m = binding.W2V(VOCAB, 64, seed=3)
+    yield m
+    m.close()
+
+
+def both_ways(model, toks, h, kv, dim, dtype, bias, seed, left, right=0, sinks=0, reach=128, two_sided=False, change=None):
+    """Attention and its gradient against the definition; `change` alters what rows hold that nobody may see."""
+    n = len(toks)
+    q, k, v, d_o = (randn(n, x, dim, seed=seed + s, dtype=dtype) for s, x in ((0, h), (1, kv), (2, kv), (3, h)))
+    want, bound = attend_by_hand(q, k, v, toks, bias, left, right, sinks, reach, two_sided, d_o, bias is not None)
+    if change:
+        change(q, k, v, d_o)
+    over = dict(left=left, right=right, sinks=sinks, reach=reach, two_sided=two_sided)
+    spans = model.sentence_spans(torch.from_numpy(toks).cuda())
+    o, saved = model.attend(q, k, v, spans, bias, train=True, **over)
+    dq, dk, dv, dbias = model.attend_backward(d_o, saved)
+    model.sync()
+    for name, x in (("o", o), ("dq", dq), ("dk", dk), ("dv", dv), ("dbias", dbias)):
+        if x is not None:
+            inside(x, want[name], bound[name], name)
+    return (o, dq, dk, dv), saved
+
+
+# ---- sinks that take more than one tile ------------------------------------------------------------
+@pytest.mark.parametrize("dim", [64, 72, 80, 96, 128])
+@pytest.mark.parametrize("sinks", [31, 32, 33, 40, 64])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_attend_many_sinks(model, dim, sinks, dtype):
+    """A sentence much longer than the window, with words among the sinks that the vocabulary does not have."""
+    toks = stream(900, (900, 900), sinks + dim)
+    toks[[1, sinks // 2, sinks - 1, 33]] = VOCAB + 1
+    both_ways(model, toks, 4, 2, dim, dtype, randn(16, 4, seed=9, by=0.5), sinks, left=30, sinks=sinks, reach=64)
