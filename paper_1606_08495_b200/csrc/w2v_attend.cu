@@ -294,7 +294,8 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         sh.sum[wg][r] = word ? mine : 0.f;
         asm volatile("bar.sync 1, 256;" ::: "memory");
         const float r0 = sh.ref[0][r], r1 = sh.ref[1][r], to = fmaxf(r0, r1);
-        ok = __all_sync(kFullMask, ok && (tiles == 0 || ready(&sh.done, 0)));
+        // a block without a word has no products, but its queries land where the output is staged
+        ok = __all_sync(kFullMask, ok && (tiles ? ready(&sh.done, 0) : Sh::kQTmem || ready(&sh.q_full, 0)));
         tc_fence_after();
         float f0 = to == -INFINITY ? 0.f : fast_exp2(r0 - to), f1 = to == -INFINITY ? 0.f : fast_exp2(r1 - to);
         const float total = sh.sum[0][r] * f0 + sh.sum[1][r] * f1, inv = total == 0.f ? 0.f : 1.f / total;
@@ -423,7 +424,9 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     copy_box(base + Sh::kOperand + c * Sh::kRows * 128, &map_v, c * 64, (int32_t)kvh, tile_at(t), &sh.landed[stage]);
                 }
             }
-            // after a wait that ran out: what is under way lands before the block leaves
+            // what nobody has waited for lands before the block leaves: the queries of a block without a word, and after
+            // a wait that ran out all that is under way
+            if (!Sh::kQTmem && (tiles == 0 || *abort_flag)) mbar_wait(&sh.q_full, 0, &sh.quiet);
             if (*abort_flag)
                 for (int32_t u = max(0, t - Sh::kStages); u < t; ++u) mbar_wait(&sh.landed[u % Sh::kStages], (u / Sh::kStages) & 1, &sh.quiet);
         }

@@ -45,3 +45,27 @@ def test_attend_many_sinks(model, dim, sinks, dtype):
     toks = stream(900, (900, 900), sinks + dim)
     toks[[1, sinks // 2, sinks - 1, 33]] = VOCAB + 1
     both_ways(model, toks, 4, 2, dim, dtype, randn(16, 4, seed=9, by=0.5), sinks, left=30, sinks=sinks, reach=64)
+
+
+# ---- 128 positions without a word -------------------------------------------------------------------
+@pytest.mark.parametrize("dim", [8, 64, 80, 128])
+@pytest.mark.parametrize("n,first,last", [(1, 0, 1), (129, 128, 129), (128, 0, 128), (700, 100, 430), (512, 128, 512), (40_000, 0, 40_000)])
+def test_attend_tiles_without_words(model, dim, n, first, last):
+    """Separators and words that the vocabulary does not have in [first, last), which holds whole tiles: zeros, whatever q holds."""
+    toks = stream(n, (20, 90), n + dim)
+    toks[first: last: 2] = VOCAB
+    toks[first + 1: last: 2] = -1
+    toks[last - 1] = -1
+    if n <= 1000:
+        got, saved = both_ways(model, toks, 4, 2, dim, torch.bfloat16, randn(16, 4, seed=9, by=0.5), n, left=30, right=30, sinks=3, two_sided=True)
+        assert all((t[first: last] == 0).all() for t in got)
+        assert (saved[-1][:, first: last] == float("inf")).all()
+        return
+    # many blocks, one after the other on the same SMs
+    q, k, d_o = randn(n, 4, dim, seed=1, dtype=torch.bfloat16), randn(n, 2, dim, seed=2, dtype=torch.bfloat16), randn(n, 4, dim, seed=3, dtype=torch.bfloat16)
+    spans = model.sentence_spans(torch.from_numpy(toks).cuda())
+    for _ in range(5):
+        o, saved = model.attend(q, k, k, spans, left=30, right=30, train=True)
+        grads = model.attend_backward(d_o, saved)[:3]
+        assert all((t == 0).all() for t in (o, *grads))
+    model.sync()
