@@ -47,7 +47,7 @@ struct FwdShape {
 };
 
 struct FwdShared {
-    uint64_t q_full, landed[4], full[4], empty[4], s_full[2], p_full[2], done;
+    uint64_t q_full, landed[4], full[4], empty[4], s_full[2], p_full[2], done, still;
     uint32_t tmem;
     int abort_flag, quiet;
     int32_t limits[4][3];                        // per warp: least lo, largest hi, least sentence start
@@ -103,6 +103,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     const T *q_head = static_cast<const T *>(p.q) + (uint64_t)h * p.dim;
     RowLimits row = {0, 0, 0, 0};
     uint4 q_row[Sh::kQTmem ? NB * 8 : 1];
+    int32_t issued = 0;                                              // tiles whose copies were started (the copying lane's)
 
     if (warp < 8) {
         row = row_limits(p, own);
@@ -127,6 +128,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         for (int i = 0; i < Sh::kStages; ++i) { mbar_init(&sh.landed[i], 1); mbar_init(&sh.full[i], 32); mbar_init(&sh.empty[i], 1 + 128); }
         for (int i = 0; i < 2; ++i) { mbar_init(&sh.s_full[i], 1); mbar_init(&sh.p_full[i], 128); }
         mbar_init(&sh.done, 1);
+        mbar_init(&sh.still, 1);
         sh.abort_flag = sh.quiet = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_proxy();
@@ -424,11 +426,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                     copy_box(base + Sh::kOperand + c * Sh::kRows * 128, &map_v, c * 64, (int32_t)kvh, tile_at(t), &sh.landed[stage]);
                 }
             }
-            // what nobody has waited for lands before the block leaves: the queries of a block without a word, and after
-            // a wait that ran out all that is under way
-            if (!Sh::kQTmem && (tiles == 0 || *abort_flag)) mbar_wait(&sh.q_full, 0, &sh.quiet);
-            if (*abort_flag)
-                for (int32_t u = max(0, t - Sh::kStages); u < t; ++u) mbar_wait(&sh.landed[u % Sh::kStages], (u / Sh::kStages) & 1, &sh.quiet);
+            issued = t;
         }
         __syncwarp();
     } else {
@@ -450,6 +448,18 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     }
     __syncthreads();
     tc_fence_after();
+    if (sh.abort_flag) {
+        // a wait ran out: the copies and products under way end (or have as long again) before the block leaves what they use
+        if (warp == 9 && lane == 0) {
+            if (!Sh::kQTmem) mbar_wait(&sh.q_full, 0, &sh.quiet);
+            for (int32_t u = max(0, issued - Sh::kStages); u < issued; ++u) mbar_wait(&sh.landed[u % Sh::kStages], (u / Sh::kStages) & 1, &sh.quiet);
+        } else if (warp == 8) {
+            if (elect_one()) umma_commit(&sh.still);
+            __syncwarp();
+            mbar_wait(&sh.still, 0, &sh.quiet);
+        }
+        __syncthreads();
+    }
     if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(Sh::kAlloc));
     if (tid == 0 && sh.abort_flag) atomicOr(error, kErrAttend);
 }

@@ -52,7 +52,7 @@ constexpr int kBackLaunchRegs = 80, kBackSoftRegs = 96, kBackOtherRegs = 48;
 
 template <typename Sh>
 struct BackShared {
-    uint64_t own_landed, own_full, landed[Sh::kStages], full[Sh::kStages], empty[Sh::kStages], s_full[2], p_full[2], done;
+    uint64_t own_landed, own_full, landed[Sh::kStages], full[Sh::kStages], empty[Sh::kStages], s_full[2], p_full[2], done, still;
     uint32_t tmem;
     int abort_flag, quiet;
     int32_t limits[4][3];
@@ -272,6 +272,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
     const uint32_t heads_here = ROLE == 0 ? 1u : group, h0 = ROLE == 0 ? h_own : kvh * group;
     const uint32_t dim16 = (p.dim + 15u) & ~15u;
     constexpr uint32_t kSoftWarps = Sh::kSoft / 32, kMmaWarp = kSoftWarps;
+    int32_t issued = 0;                                              // tiles whose copies were started (the copying lane's)
 
     if (warp == kMmaWarp + 1 && lane == 0) {
         mbar_init(&sh.own_landed, 1);
@@ -279,6 +280,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
         for (int i = 0; i < Sh::kStages; ++i) { mbar_init(&sh.landed[i], 1); mbar_init(&sh.full[i], 32); mbar_init(&sh.empty[i], 1 + Sh::kTile); }
         for (int i = 0; i < 2; ++i) { mbar_init(&sh.s_full[i], 1); mbar_init(&sh.p_full[i], Sh::kTile); }
         mbar_init(&sh.done, 1);
+        mbar_init(&sh.still, 1);
         sh.abort_flag = sh.quiet = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_proxy();
@@ -777,9 +779,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                     copy_box(base + Sh::kOperand + c * Sh::kRows * 128, &map_y, c * 64, head, at, &sh.landed[stage]);
                 }
             }
-            // after a wait that ran out: what is under way lands before the block leaves
-            if (*abort_flag)
-                for (int32_t u = max(0, t - Sh::kStages); u < t; ++u) mbar_nap(&sh.landed[u % Sh::kStages], (u / Sh::kStages) & 1, &sh.quiet);
+            issued = t;
         }
         __syncwarp();
     } else {
@@ -828,6 +828,18 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
     }
     __syncthreads();
     tc_fence_after();
+    if (sh.abort_flag) {
+        // a wait ran out: the copies and products under way end (or have as long again) before the block leaves what they use
+        if (warp == kMmaWarp + 1 && lane == 0) {
+            mbar_nap(&sh.own_landed, 0, &sh.quiet);
+            for (int32_t u = max(0, issued - Sh::kStages); u < issued; ++u) mbar_nap(&sh.landed[u % Sh::kStages], (u / Sh::kStages) & 1, &sh.quiet);
+        } else if (warp == kMmaWarp) {
+            if (elect_one()) umma_commit(&sh.still);
+            __syncwarp();
+            mbar_nap(&sh.still, 0, &sh.quiet);
+        }
+        __syncthreads();
+    }
     if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(Sh::kAlloc));
     if (tid == 0 && sh.abort_flag) atomicOr(error, kErrAttend);
 }

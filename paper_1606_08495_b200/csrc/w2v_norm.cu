@@ -82,7 +82,7 @@ norm_ring_kernel(NormParams p, uint32_t gw, uint32_t groups, uint32_t stages, ui
     extern __shared__ __align__(16) unsigned char ring[];
     __shared__ float slot[64 * kNormUnit];
     __shared__ uint64_t full[8][4];
-    __shared__ int abort_flag;
+    __shared__ int abort_flag, quiet;
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const uint32_t group = warp / gw, wig = warp - group * gw, gl = wig * 32 + lane;
     const uint32_t row_bytes = p.d * sizeof(TX), pitch = norm_pitch(mode, p.d, sizeof(TX)), unit_bytes = (kNormUnit * pitch + 15u) & ~15u;
@@ -95,7 +95,7 @@ norm_ring_kernel(NormParams p, uint32_t gw, uint32_t groups, uint32_t stages, ui
     if (threadIdx.x == 0) {
         for (uint32_t g = 0; g < groups; ++g)
             for (uint32_t s = 0; s < stages; ++s) mbar_init(&full[g][s], 1);
-        abort_flag = 0;
+        abort_flag = quiet = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_proxy();
     }
@@ -106,8 +106,10 @@ norm_ring_kernel(NormParams p, uint32_t gw, uint32_t groups, uint32_t stages, ui
         mbar_expect(&full[group][stage], norm_copy(mode, dst, reinterpret_cast<const char *>(x), p.ldx * sizeof(TX), row_bytes, pitch, r, n, &full[group][stage], false));
         norm_copy(mode, dst, reinterpret_cast<const char *>(x), p.ldx * sizeof(TX), row_bytes, pitch, r, n, &full[group][stage], true);
     };
+    uint32_t issued = 0;                                              // the first lane's: units on their way or here
+    bool live = true;                                                 // no wait of this thread has run out
     if (gl == 0)
-        for (uint32_t s = 0; s < stages; ++s) if (u + s * step < units) issue(u + s * step, s);
+        for (; issued < stages && u + issued * step < units; ++issued) issue(u + issued * step, issued);
     constexpr int kPairs = NV * E / 2;                                // two columns per instruction
     float gamma[NV * E], beta[NV * E];
     norm_weights_load<E, NV>(gamma, p.gamma, gl, gw, p.d);
@@ -117,7 +119,7 @@ norm_ring_kernel(NormParams p, uint32_t gw, uint32_t groups, uint32_t stages, ui
         const uint64_t r = u * kNormUnit;
         const uint32_t n = (uint32_t)min((uint64_t)kNormUnit, p.rows - r);
         unsigned char *rows = mine + stage * unit_bytes;
-        mbar_wait(&full[group][stage], phase, &abort_flag);           // once it has given up the rest runs through on whatever is there
+        live = mbar_wait(&full[group][stage], phase, &abort_flag) && live;     // once it has given up the rest runs through on whatever is there
         if (mode == kCopyUnits && n < kNormUnit) {
             norm_copy_tail<TX>(mode, rows, x + r * p.ldx, p.d, n, gl, gw * 32);
             group_barrier(gw, group);
@@ -141,7 +143,7 @@ norm_ring_kernel(NormParams p, uint32_t gw, uint32_t groups, uint32_t stages, ui
         group_sum<kNormUnit>(s, gw, wig, group, lane, slot, flip);
         flip ^= 1u;
         if (gw == 1) __syncwarp();                                    // everybody has read the unit
-        if (gl == 0 && u + stages * step < units) issue(u + stages * step, stage);
+        if (gl == 0 && live && u + stages * step < units) { issue(u + stages * step, stage); ++issued; }
         if (++stage == stages) { stage = 0; phase ^= 1u; }
 #pragma unroll
         for (int i = 0; i < kNormUnit; ++i) {
@@ -184,6 +186,7 @@ norm_ring_kernel(NormParams p, uint32_t gw, uint32_t groups, uint32_t stages, ui
             }
         }
     }
+    norm_ring_drain(full[group], issued, stages, gl == 0 && !live, &quiet);
     __syncthreads();
     if (threadIdx.x == 0 && abort_flag) atomicOr(error, kErrRing);
 }

@@ -111,6 +111,13 @@ __device__ __forceinline__ uint32_t norm_copy(uint32_t mode, uint32_t dst, const
     if (issue) for (uint32_t i = 0; i < n; ++i) norm_bulk(dst + i * pitch, base + (r + i) * ld_bytes, row_bytes, bar);
     return n * row_bytes;
 }
+// After a wait that ran out: what a group's first lane has issued lands (or has as long again) before the block leaves the
+// ring or puts anything else there.  Unit number k of the group is in stage k mod stages.
+__device__ __forceinline__ void norm_ring_drain(uint64_t *full, uint32_t issued, uint32_t stages, bool needed, int *quiet)
+{
+    if (!needed) return;
+    for (uint32_t k = issued > stages ? issued - stages : 0; k < issued; ++k) mbar_wait(full + k % stages, (k / stages) & 1u, quiet);
+}
 // The cut-off unit of an array that is copied in units, by the lanes of a group.
 template <typename T>
 __device__ __forceinline__ void norm_copy_tail(uint32_t mode, unsigned char *dst, const T *row, uint32_t d, uint32_t n, uint32_t gl, uint32_t lanes)

@@ -128,7 +128,7 @@ norm_backward_ring_kernel(NormParams p, uint32_t gw, uint32_t groups, uint32_t s
     extern __shared__ __align__(16) unsigned char ring[];
     __shared__ float slot[128 * kNormUnit];
     __shared__ uint64_t full[8][4];
-    __shared__ int abort_flag;
+    __shared__ int abort_flag, quiet;
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const uint32_t group = warp / gw, wig = warp - group * gw, gl = wig * 32 + lane;
     const uint32_t pitch_x = norm_pitch(mode_x, p.d, sizeof(TX)), pitch_y = norm_pitch(mode_y, p.d, sizeof(TY));
@@ -143,7 +143,7 @@ norm_backward_ring_kernel(NormParams p, uint32_t gw, uint32_t groups, uint32_t s
     if (threadIdx.x == 0) {
         for (uint32_t g = 0; g < groups; ++g)
             for (uint32_t s = 0; s < stages; ++s) mbar_init(&full[g][s], 1);
-        abort_flag = 0;
+        abort_flag = quiet = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_proxy();
     }
@@ -160,8 +160,10 @@ norm_backward_ring_kernel(NormParams p, uint32_t gw, uint32_t groups, uint32_t s
         mbar_expect(bar, both(false));
         both(true);
     };
+    uint32_t issued = 0;                                              // the first lane's: units on their way or here
+    bool live = true;                                                 // no wait of this thread has run out
     if (gl == 0)
-        for (uint32_t s = 0; s < stages; ++s) if (u + s * step < units) issue(u + s * step, s);
+        for (; issued < stages && u + issued * step < units; ++issued) issue(u + issued * step, issued);
     constexpr int kPairs = NV * E / 2;                                // two columns per instruction
     float gamma[NV * E];
     float2 dg2[kPairs], db2[kPairs];
@@ -181,7 +183,7 @@ norm_backward_ring_kernel(NormParams p, uint32_t gw, uint32_t groups, uint32_t s
             rstd[i] = (uint32_t)i < n ? __ldg(p.rstd + at) : 0.f;
             t[2 * i] = t[2 * i + 1] = 0.f;
         }
-        mbar_wait(&full[group][stage], phase, &abort_flag);           // once it has given up the rest runs through on whatever is there
+        live = mbar_wait(&full[group][stage], phase, &abort_flag) && live;     // once it has given up the rest runs through on whatever is there
         if (n < kNormUnit && (mode_x == kCopyUnits || mode_y == kCopyUnits)) {
             norm_copy_tail<TX>(mode_x, rows_x, x + r * p.ldx, p.d, n, gl, gw * 32);
             norm_copy_tail<TY>(mode_y, rows_y, dy + r * p.ldy, p.d, n, gl, gw * 32);
@@ -236,9 +238,10 @@ norm_backward_ring_kernel(NormParams p, uint32_t gw, uint32_t groups, uint32_t s
             }
         }
         group_barrier(gw, group);                                     // everybody has read the unit
-        if (gl == 0 && u + stages * step < units) issue(u + stages * step, stage);
+        if (gl == 0 && live && u + stages * step < units) { issue(u + stages * step, stage); ++issued; }
         if (++stage == stages) { stage = 0; phase ^= 1u; }
     }
+    norm_ring_drain(full[group], issued, stages, gl == 0 && !live, &quiet);
     __syncthreads();
     if (threadIdx.x == 0 && abort_flag) atomicOr(error, kErrRing);
     float dg[NV * E], db[NV * E];
