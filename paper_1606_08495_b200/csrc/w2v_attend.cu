@@ -292,7 +292,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         }
         // the two warpgroups' rows are joined: each takes half of the columns of every row
         const float mine = (sum2[0].x + sum2[0].y) + (sum2[1].x + sum2[1].y);
-        sh.ref[wg][r] = ref;
+        sh.ref[wg][r] = word ? ref : -INFINITY;                      // what a row that is not a word holds may be anything
         sh.sum[wg][r] = word ? mine : 0.f;
         asm volatile("bar.sync 1, 256;" ::: "memory");
         const float r0 = sh.ref[0][r], r1 = sh.ref[1][r], to = fmaxf(r0, r1);

@@ -69,3 +69,25 @@ def test_attend_tiles_without_words(model, dim, n, first, last):
         grads = model.attend_backward(d_o, saved)[:3]
         assert all((t == 0).all() for t in (o, *grads))
     model.sync()
+
+
+# ---- what words outside the vocabulary hold -----------------------------------------------------------
+@pytest.mark.parametrize("dim", [64, 80, 128])
+@pytest.mark.parametrize("value", [float("inf"), -float("inf"), 3e38, float("nan")])
+@pytest.mark.parametrize("biased", [False, True])
+def test_attend_hidden_rows_hold_anything(model, dim, value, biased):
+    """One element, or a whole row, of q, k, v and d_o of words that the vocabulary does not have: zeros and +infinity come out
+    there, and nobody else changes.  Windows well past the bias' reach, so that tiles without masks are among them."""
+    toks = stream(900, (900, 900), 5, oov=0.004)
+    bias = randn(16, 4, seed=9, by=0.5) if biased else None
+    over = dict(left=400, right=300, sinks=2, reach=64, two_sided=True)
+    plain, _ = both_ways(model, toks, 4, 2, dim, torch.bfloat16, bias, 1, **over)
+    hidden = torch.from_numpy(~((toks >= 0) & (toks < VOCAB))).cuda()
+    assert 2 <= int(hidden.sum()) <= 12
+    for columns in (slice(3, 4), slice(None)):
+        def change(q, k, v, d_o):
+            for t in (q, k, v, d_o):
+                t[..., columns][hidden] = value
+        got, saved = both_ways(model, toks, 4, 2, dim, torch.bfloat16, bias, 1, change=change, **over)
+        assert all(torch.equal(a, b) for a, b in zip(got, plain))
+        assert all((t[hidden] == 0).all() for t in got) and (saved[-1][:, hidden] == float("inf")).all()
