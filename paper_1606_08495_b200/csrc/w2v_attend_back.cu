@@ -56,7 +56,7 @@ struct BackShared {
     uint32_t tmem;
     int abort_flag, quiet;
     int32_t limits[4][3];
-    uint32_t vis[Sh::kStages][2];                    // role 0: which keys of the stage are words
+    uint32_t vis[Sh::kStages][2];                    // which streamed rows of the stage are words
     int32_t run_lo[Sh::kStages];                     // role 1: where the run of the stage's query tile begins
     __align__(16) float lse[Sh::kStages][Sh::kRows], delta[Sh::kStages][Sh::kRows];      // role 1: of the stage's queries, negated
     float eps[2][128];
@@ -461,11 +461,12 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                         tmem_ld(cd + c0, dv);
                         const int32_t at = at0 + c0;
                         uint32_t m;
-                        if (ROLE == 0) m = (range_bits(row.lo, row.hi, at) | range_bits(row.s, row.se, at)) & (SMALL ? sh.vis[stage][0] >> c0 : sh.vis[stage][c]);
+                        if (ROLE == 0) m = range_bits(row.lo, row.hi, at) | range_bits(row.s, row.se, at);
                         else {
                             m = range_bits(q_lo, q_hi, at);
                             if (reach) m |= range_bits(far_lo, far_hi, at);
                         }
+                        m &= SMALL ? sh.vis[stage][0] >> c0 : sh.vis[stage][c];
                         tmem_wait_ld(sv);
                         tmem_held(dv);
                         // a row or column that sees nothing has lse +infinity
@@ -812,9 +813,8 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                 if (p.sinks) run_lo = run_begin(p, at / kAttendTile * kAttendTile, lane);
             }
             if (!__all_sync(kFullMask, mbar_nap(&sh.landed[stage], (t / Sh::kStages) & 1, abort_flag))) break;
-            if (ROLE == 0) {
-                if (lane < 2) sh.vis[stage][lane] = lane ? vis[1] : vis[0];
-            } else {
+            if (lane < 2) sh.vis[stage][lane] = lane ? vis[1] : vis[0];
+            if (ROLE == 1) {
 #pragma unroll
                 for (int w = 0; w < Sh::kRows / 32; ++w) { sh.lse[stage][w * 32 + lane] = -lse[w]; sh.delta[stage][w * 32 + lane] = -delta[w]; }
                 if (lane == 0) sh.run_lo[stage] = run_lo;

@@ -91,3 +91,25 @@ def test_attend_hidden_rows_hold_anything(model, dim, value, biased):
         got, saved = both_ways(model, toks, 4, 2, dim, torch.bfloat16, bias, 1, change=change, **over)
         assert all(torch.equal(a, b) for a, b in zip(got, plain))
         assert all((t[hidden] == 0).all() for t in got) and (saved[-1][:, hidden] == float("inf")).all()
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_attend_key_that_no_query_likes(model, dim):
+    """A key with an infinity that every query's score turns into -infinity has weight zero everywhere; a query in its
+    reach that is not a word must not make it NaN."""
+    toks = stream(300, (300, 300), 6, oov=0.0)
+    toks[[90, 171, 202]] = VOCAB
+    bias = randn(16, 2, seed=9, by=0.5)
+
+    def run(change):
+        q, k, v, d_o = (randn(300, 2, dim, seed=s, dtype=torch.bfloat16) for s in (1, 2, 3, 4))
+        q[..., 0] = q[..., 0].abs() + 0.25
+        k[150, :, 0] = -change
+        spans = model.sentence_spans(torch.from_numpy(toks).cuda())
+        o, saved = model.attend(q, k, v, spans, bias, left=120, right=120, reach=32, two_sided=True, train=True)
+        return (o, *model.attend_backward(d_o, saved))
+    hidden, clean = run(float("inf")), run(1e30)                    # both weights are zero; 0 * dS keeps dq finite in the second
+    for a, b, name in zip(hidden, clean, ("o", "dq", "dk", "dv", "dbias")):
+        if name == "dq":                                             # zero weights times an infinite key: NaN by the formula
+            continue
+        assert torch.equal(a, b), name
