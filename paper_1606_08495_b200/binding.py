@@ -315,6 +315,7 @@ def w2v_set_retrieval_kernel(h, kind):
 
 
 # The reader operators take device addresses (`data_ptr()`), since rows may be strided views.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)           # the current stream of a device, without an object for it
 TYPE_F32, TYPE_BF16, TYPE_F16 = 0, 1, 2
 _TYPES = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16}
 
@@ -433,6 +434,7 @@ class W2V:
             self.stream = torch.cuda.current_stream(self.device)
             self.h = w2v_create_shard(self.vocab, self.d_full, self.col_lo, self.col_hi, self.row_stride,
                                       self.seed, self.U, self.V, self.stream.cuda_stream)
+            self._raw = self.stream.cuda_stream
 
     def close(self):
         if getattr(self, "h", None):
@@ -530,8 +532,20 @@ class W2V:
         w2v_sync(self.h)
         return ids.view(-1, K).cpu().numpy(), cs.view(-1, K).cpu().numpy()
 
-    # ---- reader operators: tensors on this model's device, results on its stream ----
-    # (written for short calls: a small operator's time is what happens here)
+    # ---- reader operators: tensors on this model's device ----
+    # They run on this model's stream, in the order of the caller's current stream: after what that was given before, and
+    # before what it is given next, also for memory: copies made within a call and its results belong to the current stream.
+    # (Written for short calls: a small operator's time is what happens here.)
+    def join_streams(self):
+        """What this model's stream and the caller's current stream are given from here on waits for all that both have
+        been given; False if they are the same.  For programs that read or write U and V by other means than this class."""
+        if _raw_stream(self._index) != self._raw:
+            here = torch.cuda.current_stream(self._index)
+            self.stream.wait_stream(here)
+            here.wait_stream(self.stream)
+            return True
+        return False
+
     def _on(self, *tensors):
         for t in tensors:
             if t is not None and t.get_device() != self._index:
@@ -570,8 +584,11 @@ class W2V:
         y = x.new_empty(x.shape, dtype=out_dtype or x.dtype)
         stats = gamma.new_empty((2, rows))
         at = stats.data_ptr()
+        apart = self.join_streams()
         w2v_layer_norm(self.h, rows, d, xv.data_ptr(), ld, self._type(x), gamma.data_ptr(), beta.data_ptr(), eps, y.data_ptr(), d,
                        self._type(y), at, at + 4 * rows)
+        if apart:
+            self.join_streams()
         return y, (xv, gamma, stats, y.dtype, x.shape)
 
     def layer_norm_backward(self, dy, saved):
@@ -585,8 +602,11 @@ class W2V:
         dx = x.new_empty(shape)
         dw = gamma.new_empty((2, d))
         at, to = stats.data_ptr(), dw.data_ptr()
+        apart = self.join_streams()
         w2v_layer_norm_backward(self.h, rows, d, dy.data_ptr(), ld, _TYPES[y_dtype], x.data_ptr(), ldx, self._type(x),
                                 gamma.data_ptr(), at, at + 4 * rows, dx.data_ptr(), d, to, to + 4 * d)
+        if apart:
+            self.join_streams()
         return dx, dw[0], dw[1]
 
     def sentence_spans(self, tokens):
@@ -595,7 +615,10 @@ class W2V:
         t = tokens if tokens.dtype is torch.int32 and tokens.is_contiguous() else tokens.to(torch.int32).contiguous()
         n = t.numel()
         spans = t.new_empty((n, 2))
+        apart = self.join_streams()
         w2v_sentence_spans(self.h, t.data_ptr(), n, spans.data_ptr())
+        if apart:
+            self.join_streams()
         return spans
 
     @staticmethod
@@ -649,8 +672,11 @@ class W2V:
         (q, ldq), (k, ldk), (v, ldv) = self._heads(q, "q"), self._heads(k, "k"), self._heads(v, "v")
         o = q.new_empty(q.shape)
         lse = q.new_empty((w.heads, n), dtype=torch.float32) if train else None
+        apart = self.join_streams()
         w2v_attend(self.h, w, n, spans.data_ptr(), q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv,
                    None if bias is None else bias.data_ptr(), o.data_ptr(), w.heads * w.head_dim, None if lse is None else lse.data_ptr())
+        if apart:
+            self.join_streams()
         return (o, (w, spans, q, k, v, bias, o, lse)) if train else o
 
     def attend_backward(self, d_o, saved):
@@ -664,9 +690,12 @@ class W2V:
         dq, dk, dv = q.new_empty(q.shape), k.new_empty(k.shape), v.new_empty(v.shape)
         dbias = None if bias is None else torch.empty_like(bias)
         wq, wk = w.heads * w.head_dim, w.kv_heads * w.head_dim
+        apart = self.join_streams()
         w2v_attend_backward(self.h, w, q.shape[0], spans.data_ptr(), q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv,
                             None if bias is None else bias.data_ptr(), o.data_ptr(), wq, lse.data_ptr(), d_o.data_ptr(), ld_do,
                             dq.data_ptr(), wq, dk.data_ptr(), wk, dv.data_ptr(), wk, None if dbias is None else dbias.data_ptr())
+        if apart:
+            self.join_streams()
         return dq, dk, dv, dbias
 
     def attend_token(self, q, k, v, cache_k, cache_v, pos, bias=None, left=0, right=0, sinks=0, reach=128, two_sided=False, scale=None):
@@ -685,8 +714,11 @@ class W2V:
         self._on(pos, cache_k, cache_v)
         q, k, v = q.contiguous(), k.contiguous(), v.contiguous()
         o = q.new_empty(q.shape)
+        apart = self.join_streams()
         w2v_attend_token(self.h, w, batch, pos.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), cache_k.data_ptr(),
                          cache_v.data_ptr(), shape[1], None if bias is None else bias.data_ptr(), o.data_ptr())
+        if apart:
+            self.join_streams()
         return o
 
     def fourbit_pack(self, rows, group=32):
@@ -699,7 +731,10 @@ class W2V:
             raise ValueError("d and group must be positive")
         packed = rows.new_empty((n, 16 * ((d + 31) // 32)), dtype=torch.uint8)
         scales = rows.new_empty((n, (d + group - 1) // group), dtype=torch.bfloat16)
+        apart = self.join_streams()
         w2v_fourbit_pack(self.h, rows.data_ptr(), n, d, ld, group, packed.data_ptr(), scales.data_ptr())
+        if apart:
+            self.join_streams()
         return packed, scales
 
     def fourbit_scores(self, x, packed, scales, group=32):
@@ -716,7 +751,10 @@ class W2V:
         if scales.dtype is not torch.bfloat16 or scales.shape != (n, (d + group - 1) // group) or not scales.is_contiguous():
             raise ValueError("scales must be contiguous bfloat16 [rows, ceil(d / group)]")
         out = x.new_empty((m, n))
+        apart = self.join_streams()
         w2v_fourbit_scores(self.h, x.data_ptr(), m, ld, packed.data_ptr(), scales.data_ptr(), n, d, group, out.data_ptr(), max(n, 1))
+        if apart:
+            self.join_streams()
         return out
 
     def set_step(self, s):

@@ -8,7 +8,8 @@ of V in 4 bits:
     x = U[w]    z = x + attend(norm(x) Wqkv) Wo    h = norm(z)    score(w') = h . V[w']
 
 The products with Wqkv and Wo are library products.  `python -m paper_1606_08495_b200.reader` trains both parts on
-a stream of made-up sentences and then continues one.
+a stream of made-up sentences and then continues one.  On another stream than the model's, calls are ordered with
+the model's (`W2V.join_streams`).
 """
 from __future__ import annotations
 
@@ -38,6 +39,7 @@ class Reader:
         """h [n, d] of every position of a token stream (int32, -1 between sentences, words that the vocabulary does not
         have are seen by nobody); with train=True (h, what `gradients` needs)."""
         m, p = self.m, self.p
+        m.join_streams()                                             # the tables' rows are read here
         word = (tokens >= 0) & (tokens < m.vocab)
         x = self.table[torch.where(word, tokens, 0).long()] * word[:, None]
         y, norm = m.layer_norm(x, p["gamma"], p["beta"], out_dtype=torch.bfloat16)
@@ -71,7 +73,9 @@ class Reader:
         in_v = lambda t: (t >= 0) & (t < self.m.vocab)  # noqa: E731
         use = (in_v(here) & in_v(after)).float()[:, None]
         ids = torch.cat([torch.where(use[:, 0] > 0, after, 0)[:, None], drawn[:-1]], 1).long()
+        self.m.join_streams()
         rows = self.answers[ids]
+        self.m.join_streams()                                        # the model may go on writing its rows
         score = torch.einsum("nd,nkd->nk", h[:-1], rows)
         sign = torch.ones_like(score)
         sign[:, 1:] = -1.0
@@ -102,6 +106,7 @@ class Reader:
     def next(self, state, words):
         """(h [batch, d], scores [batch, vocab]) after one more word per sentence; -1: a sentence that waits."""
         m, p = self.m, self.p
+        m.join_streams()
         goes = words >= 0
         x = self.table[torch.where(goes, words, 0).long()]
         y, _ = m.layer_norm(x, p["gamma"], p["beta"], out_dtype=torch.bfloat16)

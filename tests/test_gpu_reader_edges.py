@@ -113,3 +113,78 @@ def test_attend_key_that_no_query_likes(model, dim):
         if name == "dq":                                             # zero weights times an infinite key: NaN by the formula
             continue
         assert torch.equal(a, b), name
+
+
+# ---- calls from another stream than the model's ---------------------------------------------------------
+def every_operator(m, x, spans_of, rows, pos):
+    """All operators once, from tensors that make the calls copy some of them first."""
+    n = x.shape[0]
+    g, b = x.new_ones(64), x.new_zeros(64)
+    wide = x.repeat(1, 2)[:, ::2]                                    # columns two apart: brought together in the call
+    y, saved = m.layer_norm(wide, g, b)
+    out = [y, *m.layer_norm_backward(wide * 0.5, saved)]
+    q = x.bfloat16().view(n, 2, 32).transpose(0, 1).contiguous().transpose(0, 1)
+    spans = m.sentence_spans(spans_of.long())
+    o, kept = m.attend(q, q, q, spans, left=20, right=3, train=True)
+    out += [spans, o, *m.attend_backward(q, kept)[:3]]
+    cache = torch.zeros(2, 4, 9, 2, 32, dtype=torch.bfloat16, device="cuda")
+    out += [m.attend_token(q[:4], q[:4], q[:4], cache[0], cache[1], pos, left=8), cache]
+    packed, scales = m.fourbit_pack(rows.t())
+    return out + [packed, scales, m.fourbit_scores(wide[:3], packed, scales)]
+
+
+def test_operators_on_another_stream(model):
+    """Inputs that are written late on a side stream, results that are read there, and memory that is handed out again."""
+    data = [randn(500, 64, seed=1), torch.from_numpy(stream(500, (20, 60), 1)).cuda(), randn(64, 300, seed=2),
+            torch.tensor([0, 1, 2, -1], dtype=torch.int32, device="cuda")]
+    want = [t.clone() for t in every_operator(model, *data)]
+    model.sync()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        for _ in range(20):
+            late = [torch.zeros_like(t) for t in data]
+            torch.cuda._sleep(3_000_000)                             # some milliseconds
+            for a, b in zip(late, data):
+                a.copy_(b)
+            got = every_operator(model, *late)
+            same = torch.stack([(a == b).all() for a, b in zip(got, want)])
+            del late, got
+            torch.full((4_000_000,), float("nan"), device="cuda")    # over memory that calls have given back
+            assert same.all()
+
+
+def test_reader_on_another_stream(model):
+    """A reader's step while the model's stream is busy writing the tables it reads."""
+    from paper_1606_08495_b200.reader import Reader
+    m = binding.W2V(VOCAB, 64, seed=4)
+    tables = [randn(VOCAB * m.row_stride, seed=s, by=0.5) for s in (1, 2)]
+    toks = torch.from_numpy(stream(300, (20, 60), 2)).cuda()
+    drawn = torch.randint(0, VOCAB, (300, 3), device="cuda")
+    words = torch.arange(3, dtype=torch.int32, device="cuda")
+
+    def step():
+        r = Reader(m, left=20)
+        h, saved = r.read(toks, train=True)
+        loss, dh = r.loss(h, toks, drawn)
+        grads = r.gradients(dh, saved)
+        state = r.start(3)
+        return [h, loss, grads["qkv"], grads["x"], *r.next(state, words)]
+    for t, table in zip((m.U, m.V), tables):
+        t.copy_(table)
+    want = step()
+    m.sync()
+    for t in (m.U, m.V):
+        t.zero_()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        with torch.cuda.stream(m.stream):
+            torch.cuda._sleep(10_000_000)
+            for t, table in zip((m.U, m.V), tables):
+                t.copy_(table)
+        got = step()
+        with torch.cuda.stream(m.stream):
+            m.U.zero_()
+            m.V.zero_()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    m.close()
