@@ -104,11 +104,13 @@ class Reader:
         return {"k": make(), "v": make(), "pos": torch.zeros(batch, dtype=torch.int32, device=self.table.device)}
 
     def next(self, state, words):
-        """(h [batch, d], scores [batch, vocab]) after one more word per sentence; -1: a sentence that waits."""
+        """(h [batch, d], scores [batch, vocab]) after one more word per sentence.  A sentence waits at -1 and at every other
+        word that the vocabulary does not have: its cache and position stay, as if the word were not there (`read` counts
+        such a word's position), and h is that of a word that holds and sees nothing."""
         m, p = self.m, self.p
         m.join_streams()
-        goes = words >= 0
-        x = self.table[torch.where(goes, words, 0).long()]
+        goes = (words >= 0) & (words < m.vocab)
+        x = self.table[torch.where(goes, words, 0).long()] * goes[:, None]
         y, _ = m.layer_norm(x, p["gamma"], p["beta"], out_dtype=torch.bfloat16)
         qkv = (y @ p["qkv"].bfloat16()).view(len(words), -1, self.dim)
         q, k, v = qkv.split([self.heads, self.kv, self.kv], 1)

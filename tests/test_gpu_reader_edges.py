@@ -188,3 +188,39 @@ def test_reader_on_another_stream(model):
             m.V.zero_()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
     m.close()
+
+
+# ---- the reader's ends ------------------------------------------------------------------------------------
+@pytest.fixture(scope="module")
+def reader():
+    from paper_1606_08495_b200.reader import Reader
+    m = binding.W2V(VOCAB, 96, seed=4)
+    for s, t in enumerate((m.U, m.V)):
+        t.copy_(randn(t.numel(), seed=s, by=0.5))
+    r = Reader(m, left=20)
+    r.p["out"].copy_(randn(*r.p["out"].shape, seed=3, by=0.1))
+    r.p["beta_h"].copy_(randn(96, seed=4))
+    yield r
+    m.close()
+
+
+def test_reader_next_takes_words_that_the_vocabulary_lacks(reader):
+    """They move nothing and fault nothing; the other sentences go on as they would."""
+    words = torch.randint(0, VOCAB, (6, 5), generator=torch.Generator().manual_seed(1), dtype=torch.int32).cuda()
+    some, all_known = reader.start(5), reader.start(2)
+    for t in range(6):
+        w = words[t].clone()
+        for at, unknown in ((1, VOCAB), (2, VOCAB + 12_345), (3, 2 ** 31 - 1), (4, -7)):
+            if t != 2:
+                w[at] = unknown
+        h, scores = reader.next(some, w)
+        if t == 2:
+            h2, s2 = reader.next(all_known, w[:2].contiguous())
+            assert torch.equal(h[1:2], h2[1:2])                      # the first word that sentence 1 has moved
+        else:
+            h2, s2 = reader.next(all_known, torch.stack([w[0], w.new_tensor(-1)]))
+            nothing, _ = reader.m.layer_norm(torch.zeros(1, 96, device="cuda"), reader.p["gamma_h"], reader.p["beta_h"])
+            assert torch.equal(h[1:], nothing.expand(4, -1))
+        assert torch.equal(h[0], h2[0]) and torch.isfinite(scores).all()
+    assert some["pos"].tolist() == [6, 1, 1, 1, 1]
+    torch.cuda.synchronize()
