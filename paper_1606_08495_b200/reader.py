@@ -96,11 +96,11 @@ class Reader:
 
     # ---- word by word ---------------------------------------------------------------------------------
     def start(self, batch):
-        """Caches for `batch` sentences that grow one word at a time."""
+        """Caches for `batch` sentences that grow one word at a time.  Packs the table of answers as it is now: `next` scores with
+        the copy of the last `start`, whatever training has done to V since."""
         places = self.over["sinks"] + self.over["left"] + 1
         make = lambda: torch.zeros(batch, places, self.kv, self.dim, dtype=torch.bfloat16, device=self.table.device)  # noqa: E731
-        if self.packed is None:
-            self.packed = self.m.fourbit_pack(self.answers)
+        self.packed = self.m.fourbit_pack(self.answers)
         return {"k": make(), "v": make(), "pos": torch.zeros(batch, dtype=torch.int32, device=self.table.device)}
 
     def next(self, state, words):

@@ -224,3 +224,17 @@ def test_reader_next_takes_words_that_the_vocabulary_lacks(reader):
         assert torch.equal(h[0], h2[0]) and torch.isfinite(scores).all()
     assert some["pos"].tolist() == [6, 1, 1, 1, 1]
     torch.cuda.synchronize()
+
+
+def test_reader_answers_from_the_table_as_it_is_at_start(reader):
+    words = torch.tensor([3, 4], dtype=torch.int32, device="cuda")
+    reader.next(reader.start(2), words)
+    keep = reader.m.V.clone()
+    reader.m.V.mul_(-3.0)
+    h, scores = reader.next(reader.start(2), words)
+    want = h @ reader.answers.t()
+    reader.m.V.copy_(keep)
+    # 4 bits a column: half a step of a group's largest / 7 each, a tenth of the vectors' own size at the most
+    assert (scores - want).abs().max() <= 0.1 * h.norm(dim=1).max() * 3 * keep.view(VOCAB, -1).norm(dim=1).max()
+    again = reader.next(reader.start(2), words)[1]
+    assert (torch.nn.functional.cosine_similarity(again, scores) < -0.99).all()
