@@ -43,7 +43,7 @@ class Reader:
         word = (tokens >= 0) & (tokens < m.vocab)
         x = self.table[torch.where(word, tokens, 0).long()] * word[:, None]
         y, norm = m.layer_norm(x, p["gamma"], p["beta"], out_dtype=torch.bfloat16)
-        qkv = (y @ p["qkv"].bfloat16()).view(len(tokens), -1, self.dim)
+        qkv = (y @ p["qkv"].bfloat16()).view(len(tokens), self.heads + 2 * self.kv, self.dim)
         q, k, v = qkv.split([self.heads, self.kv, self.kv], 1)
         spans = m.sentence_spans(tokens)
         o = m.attend(q, k, v, spans, p["bias"], train=train, **self.over)
@@ -112,13 +112,13 @@ class Reader:
         goes = (words >= 0) & (words < m.vocab)
         x = self.table[torch.where(goes, words, 0).long()] * goes[:, None]
         y, _ = m.layer_norm(x, p["gamma"], p["beta"], out_dtype=torch.bfloat16)
-        qkv = (y @ p["qkv"].bfloat16()).view(len(words), -1, self.dim)
+        qkv = (y @ p["qkv"].bfloat16()).view(len(words), self.heads + 2 * self.kv, self.dim)
         q, k, v = qkv.split([self.heads, self.kv, self.kv], 1)
         pos = torch.where(goes, state["pos"], -1)
         o = m.attend_token(q, k, v, state["k"], state["v"], pos, p["bias"], **self.over)
         state["pos"] += goes
         h, _ = m.layer_norm(x + (o.flatten(1) @ p["out"].bfloat16()).float(), p["gamma_h"], p["beta_h"])
-        return h, torch.cat([m.fourbit_scores(h[i: i + 8], *self.packed) for i in range(0, len(words), 8)])
+        return h, torch.cat([m.fourbit_scores(h[i: i + 8], *self.packed) for i in range(0, max(len(words), 1), 8)])
 
 
 def main():

@@ -238,3 +238,17 @@ def test_reader_answers_from_the_table_as_it_is_at_start(reader):
     assert (scores - want).abs().max() <= 0.1 * h.norm(dim=1).max() * 3 * keep.view(VOCAB, -1).norm(dim=1).max()
     again = reader.next(reader.start(2), words)[1]
     assert (torch.nn.functional.cosine_similarity(again, scores) < -0.99).all()
+
+
+@pytest.mark.parametrize("n", [0, 1])
+def test_reader_of_no_words_and_one(reader, n):
+    keep = {name: t.clone() for name, t in reader.p.items()}
+    toks = torch.full((n,), 7, dtype=torch.int32, device="cuda")
+    h, saved = reader.read(toks, train=True)
+    assert h.shape == (n, 96) and torch.equal(reader.read(toks), h)
+    grads = reader.gradients(torch.ones_like(h), saved)
+    assert all(grads[name].shape == t.shape and torch.isfinite(grads[name]).all() for name, t in reader.p.items())
+    loss = reader.train_step(toks, torch.zeros(n, 3, dtype=torch.int64, device="cuda"), 0.1)       # nothing follows: no loss, no step
+    assert float(loss) == 0 and all(torch.equal(t, keep[name]) for name, t in reader.p.items())
+    h, scores = reader.next(reader.start(n), toks)
+    assert h.shape == (n, 96) and scores.shape == (n, VOCAB)
