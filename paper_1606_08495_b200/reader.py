@@ -68,11 +68,12 @@ class Reader:
         return g
 
     def loss(self, h, tokens, drawn):
-        """(mean loss, its gradient in h): logistic, the next word of the sentence against the words drawn [n, k]."""
-        here, after = tokens[:-1], tokens[1:]
+        """(mean loss, its gradient in h): logistic, the next word of the sentence against the words drawn [n, k]; a drawn
+        word that the vocabulary does not have takes no part."""
+        here, after, drawn = tokens[:-1], tokens[1:], drawn[:-1]
         in_v = lambda t: (t >= 0) & (t < self.m.vocab)  # noqa: E731
         use = (in_v(here) & in_v(after)).float()[:, None]
-        ids = torch.cat([torch.where(use[:, 0] > 0, after, 0)[:, None], drawn[:-1]], 1).long()
+        ids = torch.cat([torch.where(use[:, 0] > 0, after, 0)[:, None], torch.where(in_v(drawn), drawn, 0)], 1).long()
         self.m.join_streams()
         rows = self.answers[ids]
         self.m.join_streams()                                        # the model may go on writing its rows
@@ -80,6 +81,7 @@ class Reader:
         sign = torch.ones_like(score)
         sign[:, 1:] = -1.0
         count = use.sum().clamp(min=1)
+        use = torch.cat([use, use * in_v(drawn)], 1)
         loss = (torch.nn.functional.softplus(-sign * score) * use).sum() / count
         dh = torch.zeros_like(h)
         dh[:-1] = torch.einsum("nk,nkd->nd", -sign * torch.sigmoid(-sign * score) * use / count, rows)

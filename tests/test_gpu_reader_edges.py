@@ -252,3 +252,15 @@ def test_reader_of_no_words_and_one(reader, n):
     assert float(loss) == 0 and all(torch.equal(t, keep[name]) for name, t in reader.p.items())
     h, scores = reader.next(reader.start(n), toks)
     assert h.shape == (n, 96) and scores.shape == (n, VOCAB)
+
+
+def test_reader_loss_leaves_out_drawn_words_that_the_vocabulary_lacks(reader):
+    toks = torch.from_numpy(stream(200, (20, 60), 3)).cuda()
+    h = randn(200, 96, seed=1)
+    drawn = torch.randint(0, VOCAB, (200, 4), generator=torch.Generator().manual_seed(2)).cuda()
+    want = reader.loss(h, toks, drawn)
+    wider = torch.cat([drawn, drawn.new_tensor([-1, VOCAB, 2 ** 40]).expand(200, -1)], 1)
+    got = reader.loss(h, toks, wider)
+    # sums of the same terms, and zeros, in another order
+    assert abs(float(got[0] - want[0])) <= 1e-5 * float(want[0]) and (got[1] - want[1]).abs().max() <= 1e-5 * want[1].abs().max()
+    torch.cuda.synchronize()
