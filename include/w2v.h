@@ -528,7 +528,8 @@ enum { W2V_TYPE_F32 = 0, W2V_TYPE_BF16 = 1, W2V_TYPE_F16 = 2 };
  * square distance from the mean.
  *   x, y        row r starts at element r * stride (any stride >= d, any alignment of whole elements;
  *               16-byte aligned rows whose length is a multiple of 4 or 8 elements are the fast ones).
- *               y has the type of x, or any of the three types when x is W2V_TYPE_F32.  y may be x.
+ *               y has the type of x, or any of the three types when x is W2V_TYPE_F32.  y may be x when their types and
+ *               strides are the same; apart from that nothing of y may lie over x.
  *   gamma, beta d floats.
  *   mean, rstd  rows floats each, for the backward call; may be NULL.
  * Limits: 1 <= d <= 8192, rows < 2^40.  Errors: W2V_ERR_ARG, W2V_ERR_CUDA.
@@ -539,7 +540,8 @@ int32_t w2v_layer_norm(w2v_handle *h, uint64_t rows, uint32_t d, const void *x, 
 
 /*
  * Its gradient: dx (type of x), and dgamma, dbeta (d floats, written, not added to; zeros for no rows).
- *   dy  has the type y had.  dx may be dy when their types are the same.
+ *   dy  has the type y had.  dx may be dy, or x, when their types and strides are the same; apart from that nothing of
+ *       dx may lie over dy or x.
  */
 int32_t w2v_layer_norm_backward(w2v_handle *h, uint64_t rows, uint32_t d, const void *dy, uint64_t dy_stride, uint32_t y_type,
                                 const void *x, uint64_t x_stride, uint32_t x_type, const float *gamma, const float *mean,

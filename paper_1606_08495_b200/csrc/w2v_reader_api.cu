@@ -27,6 +27,12 @@ int32_t check_norm(w2v_handle *h, uint64_t rows, uint32_t d, uint32_t x_type, ui
     return W2V_OK;
 }
 
+// Do two arrays at one address have their rows at the same places?  (Otherwise rows lie over others that are not read yet.)
+bool same_rows(uint64_t rows, uint32_t a_type, uint64_t a_stride, uint32_t b_type, uint64_t b_stride)
+{
+    return a_type == b_type && (rows < 2 || a_stride == b_stride);
+}
+
 // First distances of a side's n buckets: n/2 buckets of one distance each, then bucket n/2 + k starts at
 // ceil(e (reach/e)^(k/(n-e))), e = n/2.  The last bit of the power is forgiven (1e-12), so that a power
 // that is a whole number counts as that number.
@@ -115,6 +121,8 @@ int32_t w2v_layer_norm(w2v_handle *h, uint64_t rows, uint32_t d, const void *x, 
     if (x_stride < d || y_stride < d) return fail(h, W2V_ERR_ARG, "strides must be at least d");
     if (!aligned(x, type_size(x_type)) || !aligned(y, type_size(y_type)) || !aligned(gamma, 4) || !aligned(beta, 4))
         return fail(h, W2V_ERR_ARG, "x, y, gamma and beta must be aligned to their elements");
+    if (rows && x == y && !same_rows(rows, x_type, x_stride, y_type, y_stride))
+        return fail(h, W2V_ERR_ARG, "y may be x only with the same type and stride");
     if (!(eps >= 0.f) || std::isinf(eps)) return fail(h, W2V_ERR_ARG, "eps must be finite and not negative");
     DeviceGuard g(h->device);
     NormParams p;
@@ -138,6 +146,8 @@ int32_t w2v_layer_norm_backward(w2v_handle *h, uint64_t rows, uint32_t d, const 
     if (!aligned(x, type_size(x_type)) || !aligned(dx, type_size(x_type)) || !aligned(dy, type_size(y_type)) || !aligned(gamma, 4) ||
         !aligned(dgamma, 4) || !aligned(dbeta, 4) || !aligned(mean, 4) || !aligned(rstd, 4))
         return fail(h, W2V_ERR_ARG, "arrays must be aligned to their elements");
+    if (rows && ((dx == dy && !same_rows(rows, x_type, dx_stride, y_type, dy_stride)) || (dx == x && !same_rows(rows, x_type, dx_stride, x_type, x_stride))))
+        return fail(h, W2V_ERR_ARG, "dx may be dy or x only with the same type and stride");
     DeviceGuard g(h->device);
     NormParams p;
     std::memset(&p, 0, sizeof(p));

@@ -264,3 +264,57 @@ def test_reader_loss_leaves_out_drawn_words_that_the_vocabulary_lacks(reader):
     # sums of the same terms, and zeros, in another order
     assert abs(float(got[0] - want[0])) <= 1e-5 * float(want[0]) and (got[1] - want[1]).abs().max() <= 1e-5 * want[1].abs().max()
     torch.cuda.synchronize()
+
+
+# ---- layer norm in place -----------------------------------------------------------------------------------
+def norm_raw(m, x, y, g, b, stats, x_stride, y_stride, rows=None):
+    from paper_1606_08495_b200.binding import _TYPES
+    rows, d = x.shape[0] if rows is None else rows, g.numel()
+    binding.w2v_layer_norm(m.h, rows, d, x.data_ptr(), x_stride, _TYPES[x.dtype], g.data_ptr(), b.data_ptr(), 1e-5, y.data_ptr(), y_stride,
+                           _TYPES[y.dtype], stats.data_ptr(), stats.data_ptr() + 4 * rows)
+
+
+def norm_back_raw(m, dy, x, dx, g, stats, dw, dy_stride, x_stride, dx_stride):
+    from paper_1606_08495_b200.binding import _TYPES
+    rows, d = x.shape[0], g.numel()
+    binding.w2v_layer_norm_backward(m.h, rows, d, dy.data_ptr(), dy_stride, _TYPES[dy.dtype], x.data_ptr(), x_stride, _TYPES[x.dtype], g.data_ptr(),
+                                    stats.data_ptr(), stats.data_ptr() + 4 * rows, dx.data_ptr(), dx_stride, dw.data_ptr(), dw.data_ptr() + 4 * d)
+
+
+@pytest.mark.parametrize("rows,d,pad", [(1, 300, 0), (77, 300, 4), (5001, 300, 20), (3001, 4096, 0), (4999, 101, 3)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_layer_norm_in_place(model, rows, d, pad, dtype):
+    """y over x, dx over dy and dx over x, with few rows and with enough for the ring: the same bits as side by side."""
+    x, dy = randn(rows, d + pad, seed=1, dtype=dtype), randn(rows, d + pad, seed=2, dtype=dtype)
+    g, b, ld = 1 + randn(d, seed=3, by=0.2), randn(d, seed=4), d + pad
+    stats, dw = torch.empty(2, rows, device="cuda"), torch.empty(2, d, device="cuda")
+    y, dx = torch.zeros_like(x), torch.zeros_like(x)
+    norm_raw(model, x, y, g, b, stats, ld, ld)
+    norm_back_raw(model, dy, x, dx, g, stats, dw, ld, ld, ld)
+    for over in (0, 1):
+        t, dw2 = (dy, x)[over].clone(), torch.empty_like(dw)
+        norm_back_raw(model, (t, dy)[over], (x, t)[over], t, g, stats, dw2, ld, ld, ld)
+        assert torch.equal(t[:, :d], dx[:, :d]) and torch.equal(t[:, d:], (dy, x)[over][:, d:]) and torch.equal(dw, dw2)
+    t, stats2 = x.clone(), torch.empty_like(stats)
+    norm_raw(model, t, t, g, b, stats2, ld, ld)
+    assert torch.equal(t[:, :d], y[:, :d]) and torch.equal(t[:, d:], x[:, d:]) and torch.equal(stats, stats2)
+
+
+def test_layer_norm_in_place_refusals(model):
+    x, g, b = randn(4, 64, seed=1), torch.ones(32, device="cuda"), torch.zeros(32, device="cuda")
+    half, stats, dw, other = x.view(torch.bfloat16), torch.zeros(2, 4, device="cuda"), torch.zeros(2, 32, device="cuda"), randn(4, 64, seed=2)
+    keep = x.clone()
+
+    def refused(*call):
+        with pytest.raises(binding.W2VError, match="same type and stride") as e:
+            call[0](*call[1:])
+        assert e.value.code == binding.W2V_ERR_ARG
+    refused(norm_raw, model, x, x, g, b, stats, 64, 32)
+    refused(norm_raw, model, x, half, g, b, stats, 64, 64)
+    refused(norm_raw, model, x, half, g, b, stats, 64, 64, 1)
+    refused(norm_back_raw, model, x, other, x, g, stats, dw, 64, 64, 32)
+    refused(norm_back_raw, model, other, x, x, g, stats, dw, 64, 64, 32)
+    refused(norm_back_raw, model, half, other, x, g, stats, dw, 64, 64, 64)
+    model.sync()
+    assert torch.equal(x, keep)
+    norm_raw(model, x, x, g, b, stats, 64, 32, 1)                    # a single row has no stride
