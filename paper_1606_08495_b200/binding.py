@@ -570,9 +570,11 @@ class W2V:
         if t.dim() == 2:
             rows, d = t.shape
             ld, one = t.stride()
-            if (one == 1 or d == 1) and (ld >= d or rows <= 1):
+            if (one == 1 or d == 1) and (ld >= d or rows <= 1) and d < 1 << 32:
                 return rows, d, ld if ld >= d else d, t
         d = t.shape[-1]
+        if d >= 1 << 32:
+            raise ValueError("rows must be shorter than 2^32")
         t = t.contiguous()
         return t.numel() // max(d, 1), d, d, t
 
@@ -654,6 +656,9 @@ class W2V:
         key = (dtype, qs[1], ks[1], qs[2], left, right, sinks, buckets, reach, two_sided, scale)
         w = self._windows.get(key)
         if w is None:
+            for what, x in (("heads", qs[1]), ("kv_heads", ks[1]), ("head_dim", qs[2]), ("left", left), ("right", right), ("sinks", sinks), ("reach", reach)):
+                if not 0 <= x < 1 << 32:                             # the struct's fields would take it modulo 2^32
+                    raise ValueError(f"{what} = {x} is out of range")
             w = Window(_TYPES[dtype], qs[1], ks[1], qs[2], left, right, sinks, buckets, reach, int(two_sided),
                        qs[2] ** -0.5 if scale is None else scale)
             if len(self._windows) > 256:
@@ -727,8 +732,8 @@ class W2V:
         if rows.dtype is not torch.float32 or rows.dim() != 2:
             raise ValueError("rows must be float32 [n, d]")
         n, d, ld, rows = self._rows(rows)
-        if d < 1 or group < 1:
-            raise ValueError("d and group must be positive")
+        if d < 1 or group not in (32, 64, 128):
+            raise ValueError("d must be positive and group 32, 64 or 128")
         packed = rows.new_empty((n, 16 * ((d + 31) // 32)), dtype=torch.uint8)
         scales = rows.new_empty((n, (d + group - 1) // group), dtype=torch.bfloat16)
         apart = self.join_streams()
@@ -743,8 +748,10 @@ class W2V:
         if x.dtype is not torch.float32 or x.dim() != 2:
             raise ValueError("x must be float32 [m, d]")
         m, d, ld, x = self._rows(x)
-        if d < 1 or group < 1:
-            raise ValueError("d and group must be positive")
+        if m > 8:
+            raise ValueError("m must be at most 8")
+        if d < 1 or group not in (32, 64, 128):
+            raise ValueError("d must be positive and group 32, 64 or 128")
         n = packed.shape[0]
         if packed.dtype is not torch.uint8 or packed.shape != (n, 16 * ((d + 31) // 32)) or not packed.is_contiguous():
             raise ValueError(f"packed must be contiguous uint8 [rows, {16 * ((d + 31) // 32)}] for d = {d}")

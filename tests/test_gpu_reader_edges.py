@@ -318,3 +318,29 @@ def test_layer_norm_in_place_refusals(model):
     model.sync()
     assert torch.equal(x, keep)
     norm_raw(model, x, x, g, b, stats, 64, 32, 1)                    # a single row has no stride
+
+
+# ---- numbers that do not fit ----------------------------------------------------------------------------------
+def test_numbers_beyond_32_bits_are_refused(model):
+    """Not taken modulo 2^32: a group of 2^32 + 32 would have written 32-column scales into one scale a row."""
+    big = 1 << 32
+    q = randn(4, 4, 64, seed=1, dtype=torch.bfloat16)
+    spans = model.sentence_spans(torch.ones(4, dtype=torch.int32, device="cuda"))
+    bias = randn(8, 4, seed=2)
+    for name, value in (("left", big), ("left", big + 3), ("left", -1), ("right", big), ("sinks", big + 1), ("sinks", -big), ("reach", big + 16)):
+        with pytest.raises(ValueError, match=name):
+            model.attend(q, q, q, spans, bias, **{"reach": 16, name: value})
+    cache = torch.zeros(4, 8, 4, 64, dtype=torch.bfloat16, device="cuda")
+    pos = torch.zeros(4, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError, match="left"):
+        model.attend_token(q, q, q, cache, cache.clone(), pos, left=big)
+    rows = randn(40, 300, seed=3)
+    packed, scales = model.fourbit_pack(rows)
+    for group in (big + 32, big, -32, 0, 33):
+        with pytest.raises(ValueError, match="group"):
+            model.fourbit_pack(rows, group)
+        with pytest.raises(ValueError, match="group"):
+            model.fourbit_scores(rows[:1], packed, scales, group)
+    with pytest.raises(ValueError, match="m must"):
+        model.fourbit_scores(rows[:9], packed, scales)
+    model.sync()
