@@ -67,6 +67,7 @@ int32_t check_window(w2v_handle *h, const w2v_window *w, const float *bias, Buck
     if (w->left >= (1u << 30) || w->right >= (1u << 30)) return fail(h, W2V_ERR_ARG, "left and right must be below 2^30");
     if (w->sinks > kMaxSinks) return fail(h, W2V_ERR_ARG, "sinks must be at most 64");
     if (!(w->scale > 0.f) || std::isinf(w->scale)) return fail(h, W2V_ERR_ARG, "scale must be positive and finite");
+    if (!aligned(bias, 4)) return fail(h, W2V_ERR_ARG, "bias must be aligned to its elements");
     std::memset(b, 0, sizeof(*b));
     if (w->buckets) {
         const int32_t rc = check_buckets(h, w->buckets, w->reach, w->two_sided);
@@ -119,8 +120,8 @@ int32_t w2v_layer_norm(w2v_handle *h, uint64_t rows, uint32_t d, const void *x, 
     if (rc != W2V_OK) return rc;
     if (!gamma || !beta || (rows && (!x || !y))) return fail(h, W2V_ERR_ARG, "x, y, gamma or beta is NULL");
     if (x_stride < d || y_stride < d) return fail(h, W2V_ERR_ARG, "strides must be at least d");
-    if (!aligned(x, type_size(x_type)) || !aligned(y, type_size(y_type)) || !aligned(gamma, 4) || !aligned(beta, 4))
-        return fail(h, W2V_ERR_ARG, "x, y, gamma and beta must be aligned to their elements");
+    if (!aligned(x, type_size(x_type)) || !aligned(y, type_size(y_type)) || !aligned(gamma, 4) || !aligned(beta, 4) || !aligned(mean, 4) || !aligned(rstd, 4))
+        return fail(h, W2V_ERR_ARG, "x, y, gamma, beta, mean and rstd must be aligned to their elements");
     if (rows && x == y && !same_rows(rows, x_type, x_stride, y_type, y_stride))
         return fail(h, W2V_ERR_ARG, "y may be x only with the same type and stride");
     if (!(eps >= 0.f) || std::isinf(eps)) return fail(h, W2V_ERR_ARG, "eps must be finite and not negative");
@@ -195,6 +196,7 @@ int32_t w2v_attend(w2v_handle *h, const w2v_window *w, uint64_t n, const int32_t
     if ((rc = check_rows(h, q, q_stride, wq, bad)) != W2V_OK || (rc = check_rows(h, k, k_stride, wk, bad)) != W2V_OK ||
         (rc = check_rows(h, v, v_stride, wk, bad)) != W2V_OK || (rc = check_rows(h, o, o_stride, wq, bad)) != W2V_OK)
         return rc;
+    if (!aligned(lse, 4)) return fail(h, W2V_ERR_ARG, "lse must be aligned to its elements");
     DeviceGuard g(h->device);
     if ((rc = ensure_error_word(h)) != W2V_OK) return rc;
     p.q = q; p.k = k; p.v = v; p.out = o; p.lse = lse;
@@ -211,6 +213,7 @@ int32_t w2v_attend_backward(w2v_handle *h, const w2v_window *w, uint64_t n, cons
     AttendParams p;
     int32_t rc = fill_attend(h, w, n, spans, bias, &p);
     if (rc != W2V_OK) return rc;
+    if (!aligned(lse, 4) || !aligned(dbias, 4)) return fail(h, W2V_ERR_ARG, "lse and dbias must be aligned to their elements");
     if (dbias && !w->buckets) return fail(h, W2V_ERR_ARG, "dbias given but buckets is 0");
     const uint64_t wq = (uint64_t)w->heads * w->head_dim, wk = (uint64_t)w->kv_heads * w->head_dim;
     const char *bad = "q, k, v, o, d_o, dq, dk and dv must be 16-byte aligned, with strides that are multiples of 8 and hold every head";
@@ -248,6 +251,7 @@ int32_t w2v_attend_token(w2v_handle *h, const w2v_window *w, uint32_t batch, con
     if (!pos || !q || !k || !v || !cache_k || !cache_v || !o) return fail(h, W2V_ERR_ARG, "an array is NULL");
     if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(cache_k, 16) || !aligned(cache_v, 16) || !aligned(o, 16))
         return fail(h, W2V_ERR_ARG, "q, k, v, the cache and o must be 16-byte aligned");
+    if (!aligned(pos, 4)) return fail(h, W2V_ERR_ARG, "pos must be aligned to its elements");
     DeviceGuard g(h->device);
     p.q = q; p.k = k; p.v = v; p.ck = cache_k; p.cv = cache_v; p.out = o; p.pos = pos; p.bias = bias; p.places = places;
     p.batch = batch; p.heads = w->heads; p.kv_heads = w->kv_heads; p.dim = w->head_dim;

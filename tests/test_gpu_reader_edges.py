@@ -344,3 +344,22 @@ def test_numbers_beyond_32_bits_are_refused(model):
     with pytest.raises(ValueError, match="m must"):
         model.fourbit_scores(rows[:9], packed, scales)
     model.sync()
+
+
+def test_misaligned_small_arrays_are_refused(model):
+    """Addresses of lse, bias, dbias, pos, mean and rstd that are not multiples of their elements' size end in an error, not in a fault."""
+    q, bias, f = randn(4, 4, 64, seed=1, dtype=torch.bfloat16), randn(8, 4, seed=2), torch.zeros(64, device="cuda")
+    spans, pos = model.sentence_spans(torch.ones(4, dtype=torch.int32, device="cuda")), torch.zeros(4, dtype=torch.int32, device="cuda")
+    cache = torch.zeros(4, 8, 4, 64, dtype=torch.bfloat16, device="cuda")
+    w = binding.Window(binding.TYPE_BF16, 4, 4, 64, 3, 0, 0, 8, 16, 0, 0.125)
+    a, s, b, e, h = q.data_ptr(), spans.data_ptr(), bias.data_ptr(), f.data_ptr(), model.h
+    attend = lambda bias, lse: binding.w2v_attend(h, w, 4, s, a, 256, a, 256, a, 256, bias, a, 256, lse)  # noqa: E731
+    back = lambda bias, lse, dbias: binding.w2v_attend_backward(h, w, 4, s, a, 256, a, 256, a, 256, bias, a, 256, lse, a, 256, a, 256, a, 256, a, 256, dbias)  # noqa: E731
+    token = lambda pos, bias: binding.w2v_attend_token(h, w, 4, pos, a, a, a, cache.data_ptr(), cache.data_ptr(), 8, bias, a)  # noqa: E731
+    norm = lambda mean, rstd: binding.w2v_layer_norm(h, 4, 16, e, 16, 0, b, b, 1e-5, e, 16, 0, mean, rstd)  # noqa: E731
+    for call in (lambda: attend(b + 1, None), lambda: attend(b, e + 2), lambda: back(b + 2, e, e), lambda: back(b, e + 1, e), lambda: back(b, e, e + 3),
+                 lambda: token(pos.data_ptr() + 2, b), lambda: token(pos.data_ptr(), b + 2), lambda: norm(e + 2, None), lambda: norm(None, e + 1)):
+        with pytest.raises(binding.W2VError, match="aligned") as err:
+            call()
+        assert err.value.code == binding.W2V_ERR_ARG
+    model.sync()
