@@ -582,7 +582,8 @@ int32_t w2v_bucket_starts(uint32_t buckets, uint32_t reach, uint32_t two_sided, 
  * i - left <= j <= i + right, or j among the sentence's first `sinks` words and before i,
  *   o(i) = sum_j softmax_j(scale q(i).k(j) + bias[bucket(j - i)][head]) v(j);
  * a position that sees nothing (a sentence end, a word outside the vocabulary) gets zeros.
- *   spans       of w2v_sentence_spans.
+ *   spans       of w2v_sentence_spans for the same n positions, or for more (sentences then end with the n); a pair that is
+ *               not around its position counts as empty.
  *   q, k, v, o  [n][heads or kv_heads][head_dim], heads side by side, `stride` elements from position to
  *               position (a multiple of 8; one packed projection can hold q, k and v), 16-byte aligned.
  *   bias        [buckets][heads] floats, NULL when buckets is 0.

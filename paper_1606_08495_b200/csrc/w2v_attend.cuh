@@ -17,6 +17,14 @@ namespace w2v {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kErrAttend = 8;                    // bit of the handle's error word
 
+// The sentence of position i (0 <= i < n), empty for one that is not a word.  It ends with the stream; a pair that is not
+// around i, which w2v_sentence_spans does not write for this position, counts as empty: nothing is read by such an index.
+__device__ __forceinline__ int2 word_span(const AttendParams &p, int64_t i)
+{
+    const int2 sp = __ldg(p.spans + i);
+    return sp.x >= 0 && sp.x <= i && sp.y > i ? make_int2(sp.x, min(sp.y, (int32_t)p.n)) : make_int2(0, 0);
+}
+
 // What one row sees; an empty row has all limits 0.
 struct RowLimits {
     int32_t lo, hi;                              // window
@@ -27,7 +35,7 @@ __device__ __forceinline__ RowLimits row_limits(const AttendParams &p, int64_t i
 {
     RowLimits r = {0, 0, 0, 0};
     if (i < 0 || i >= p.n) return r;
-    const int2 sp = __ldg(p.spans + i);
+    const int2 sp = word_span(p, i);
     if (sp.y <= sp.x) return r;
     r.lo = (int32_t)max((int64_t)sp.x, i - p.left);
     r.hi = (int32_t)min((int64_t)sp.y, i + p.right + 1);
@@ -114,7 +122,7 @@ __device__ __forceinline__ void word_bits(const AttendParams &p, int64_t at, uin
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
         const int64_t j = at + w * 32 + lane;
-        sp[w] = w * 32u + lane < rows && j < p.n ? __ldg(p.spans + j) : make_int2(0, 0);
+        sp[w] = w * 32u + lane < rows && j < p.n ? word_span(p, j) : make_int2(0, 0);
     }
 #pragma unroll
     for (int w = 0; w < 2; ++w) vis[w] = __ballot_sync(kFullMask, sp[w].y > sp[w].x);
@@ -150,7 +158,7 @@ __device__ __forceinline__ float pair_bias(const AttendParams &p, uint32_t h, in
 
 __device__ __forceinline__ bool is_word(const AttendParams &p, int64_t i)
 {
-    const int2 sp = __ldg(p.spans + i);
+    const int2 sp = word_span(p, i);
     return sp.y > sp.x;
 }
 

@@ -217,7 +217,7 @@ __device__ __forceinline__ void dq_again(const AttendParams &p, uint32_t h, uint
 template <typename T>
 __device__ __forceinline__ void dkv_again(const AttendParams &p, uint32_t which, uint32_t kvh, int64_t j, const float *sink, uint32_t lane)
 {
-    const int2 sp = __ldg(p.spans + j);
+    const int2 sp = word_span(p, j);
     const uint32_t group = p.heads / p.kv_heads;
     const T *k = static_cast<const T *>(p.k) + j * (int64_t)p.ldk + kvh * p.dim, *v = static_cast<const T *>(p.v) + j * (int64_t)p.ldv + kvh * p.dim;
     const int64_t lo = max((int64_t)sp.x, j - p.right), hi = min((int64_t)sp.y, j + p.left + 1), tile = (j + p.left) / kAttendTile;
@@ -303,7 +303,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
             row = row_limits(p, own);
             if (row.hi > row.lo) { least = row.lo; most = row.hi; s = row.s; }
         } else if (own < p.n) {
-            const int2 sp = __ldg(p.spans + own);
+            const int2 sp = word_span(p, own);
             if (sp.y > sp.x) {
                 sent = sp.x;
                 q_lo = (int32_t)max((int64_t)sp.x, own - p.right);
@@ -335,7 +335,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
             const int64_t i = (int64_t)t0 + w * 32 + lane;
-            const int2 sp = i < p.n ? __ldg(p.spans + i) : make_int2(0, 0);
+            const int2 sp = i < p.n ? word_span(p, i) : make_int2(0, 0);
             own_words[w] = __ballot_sync(kFullMask, sp.y > sp.x);
         }
     }
@@ -848,7 +848,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
 __device__ __forceinline__ int64_t first_word(const AttendParams &p, int32_t tile)
 {
     int64_t i = (int64_t)tile * kAttendTile;
-    while (i + 1 < p.n && p.spans[i].y <= p.spans[i].x) ++i;
+    while (i + 1 < p.n && !is_word(p, i)) ++i;
     return i;
 }
 
@@ -869,7 +869,7 @@ attend_sink_sum_kernel(AttendParams p, int32_t tiles)
         if (blockIdx.x == 0 && threadIdx.x == 0) p.sink_used[a] = here ? s : -1;
         if (!here) continue;
         // the sentence's last tile is that of its last word; tiles without words in between have nothing
-        const int32_t end = min(tiles, (p.spans[first_word(p, first)].y - 1) / kAttendTile + 1);
+        const int32_t end = min(tiles, (word_span(p, first_word(p, first)).y - 1) / kAttendTile + 1);
         const int32_t items = (end - first) * (int32_t)group;
         float x[4] = {0.f, 0.f, 0.f, 0.f};
         if (e < width)

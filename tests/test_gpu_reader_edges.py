@@ -363,3 +363,25 @@ def test_misaligned_small_arrays_are_refused(model):
             call()
         assert err.value.code == binding.W2V_ERR_ARG
     model.sync()
+
+
+# ---- spans that are not this stream's -----------------------------------------------------------------------------
+@pytest.mark.parametrize("dim", [64, 80, 128])
+def test_attend_with_spans_of_another_stream(model, dim):
+    """Pairs that do not lie around their position count as empty: zeros there, and no index is formed from them."""
+    n, h, kv = 700, 4, 2
+    q, k, v, d_o = (randn(n, x, dim, seed=s, dtype=torch.bfloat16) for s, x in ((1, h), (2, kv), (3, kv), (4, h)))
+    bias = randn(16, h, seed=5)
+    longer = model.sentence_spans(torch.from_numpy(stream(5000, (300, 2000), 1)).cuda())
+    at = torch.arange(n, device="cuda")
+    wild = torch.randint(-2 ** 31, 2 ** 31 - 1, (n, 2), generator=torch.Generator().manual_seed(1), dtype=torch.int64).to(torch.int32).cuda()
+    near = torch.randint(-40, 40, (n, 2), generator=torch.Generator().manual_seed(2)).to(torch.int32).cuda() + at[:, None].int()
+    o = model.attend(q, k, v, longer[:n].contiguous(), bias, left=90, right=20, sinks=40, reach=64)
+    cut = model.sentence_spans(torch.from_numpy(stream(5000, (300, 2000), 1)[:n].copy()).cuda())
+    assert not torch.equal(cut, longer[:n]) and torch.equal(o, model.attend(q, k, v, cut, bias, left=90, right=20, sinks=40, reach=64))
+    for spans in (longer[3000: 3000 + n].contiguous(), longer[:n].contiguous(), wild, near, torch.full_like(wild, 2 ** 31 - 1)):
+        o, saved = model.attend(q, k, v, spans, bias, left=90, right=20, sinks=40, reach=64, train=True)
+        got = (o, *model.attend_backward(d_o, saved))
+        model.sync()
+        empty = ~((spans[:, 0] >= 0) & (spans[:, 0] <= at) & (spans[:, 1] > at))
+        assert all(torch.isfinite(t).all() for t in got) and all((t[empty] == 0).all() for t in got[:4])
