@@ -55,9 +55,9 @@ struct FwdShared {
     float ref[2][128], sum[2][128];              // per warpgroup and row
 };
 
-// The output of row i by a warp, from the pairs that it sees.
+// The output of row i by a warp, from the pairs that it sees; `ref` and `inv` are the row's reference and inverse sum.
 template <typename T>
-__device__ __forceinline__ void output_again(const AttendParams &p, uint32_t h, uint32_t kvh, int64_t i, float lse, uint32_t lane)
+__device__ __forceinline__ void output_again(const AttendParams &p, uint32_t h, uint32_t kvh, int64_t i, float ref, float inv, uint32_t lane)
 {
     const RowLimits row = row_limits(p, i);
     const T *q = static_cast<const T *>(p.q) + i * (int64_t)p.ldq + h * p.dim;
@@ -71,7 +71,7 @@ __device__ __forceinline__ void output_again(const AttendParams &p, uint32_t h, 
             const int64_t j = j0 + lane;
             const bool seen = j < b && is_word(p, j);
             float w = 0.f;
-            if (seen) w = fast_exp2(fmaf(row_dot(q, k + j * (int64_t)p.ldk, p.dim), p.scale * kLog2e, pair_bias(p, h, (int32_t)(j - i))) - lse);
+            if (seen) w = fast_exp2(fmaf(row_dot(q, k + j * (int64_t)p.ldk, p.dim), p.scale * kLog2e, pair_bias(p, h, (int32_t)(j - i))) - ref) * inv;
             add_rows(acc, w, __ballot_sync(kFullMask, seen), v + j0 * (int64_t)p.ldv, p.ldv, p.dim, lane);
         }
     }
@@ -201,7 +201,10 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             const bool far_left = k0 + Sh::kRows - 1 - w0 <= -last, far = p.b.n == 0 || far_left || k0 - (w0 + 31) >= last;
             const float flat = p.b.n ? lut[far_left ? 0 : bias_entries(p.b) - 1] : 0.f;
             const uint32_t vis0 = sh.vis[stage][0], vis1 = Sh::kRows == 64 ? sh.vis[stage][1] : 0xFFFFFFFFu;
-            const bool plain = far && k0 >= all_lo && k0 + Sh::kRows <= all_hi && (vis0 & vis1) == 0xFFFFFFFFu;
+            // in a plain tile the bias joins the reference first; scores beside a bias far from zero lose their digits as in every
+            // other tile, or not at all, so that only a bias that leaves nothing of them is taken there
+            const bool hidden = flat <= kLowestBias;
+            const bool plain = far && (fabsf(flat) <= kFarLse || hidden) && k0 >= all_lo && k0 + Sh::kRows <= all_hi && (vis0 & vis1) == 0xFFFFFFFFu;
             float top = -INFINITY, by = 1.f, add = 0.f;
             if (plain) {
                 float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -218,8 +221,8 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                         float &x = m[(e >> 1) & 3];
                         x = fmaxf(x, fmaxf(__uint_as_float(v[c][e]), __uint_as_float(v[c][e + 1])));
                     }
-                top = fmaf(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])), scale, flat);
-                by = scale;
+                by = hidden ? 0.f : scale;
+                top = fmaf(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])), by, flat);
                 add = flat;
             } else {
 #pragma unroll 1
@@ -346,7 +349,7 @@ attend_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
 #pragma unroll 1
             for (; bad; bad &= bad - 1u) {                           // a row that both warps found is written twice, the same
                 const int32_t x = __ffs(bad) - 1;
-                output_again<T>(p, h, kvh, (int64_t)t0 + part + x, __shfl_sync(kFullMask, lse, x), lane);
+                output_again<T>(p, h, kvh, (int64_t)t0 + part + x, __shfl_sync(kFullMask, to, x), __shfl_sync(kFullMask, inv, x), lane);
             }
         }
         tc_fence_before();

@@ -71,6 +71,7 @@ __device__ __forceinline__ uint32_t bucket_of(const BucketStarts &b, int32_t rel
 }
 
 // A bias in base-2 units; one of the lowest float stays finite, so that a row of nothing else is still a row.
+constexpr float kLowestBias = -1e30f * kLog2e;
 __device__ __forceinline__ float log2_bias(float b) { return b == -INFINITY ? b : fmaxf(b, -1e30f) * kLog2e; }
 
 // Relative positions [r0, r1) (key - query, within -off .. off) whose bias is bucket b's.
@@ -149,6 +150,11 @@ __device__ __forceinline__ void zero_rows(uint32_t tile, uint32_t block, uint32_
 // The tensor cores multiply a masked weight, zero, with whatever lies there, and zero times an infinity or NaN is NaN: a
 // value that is not finite spoils the rows of its tile, also of other sentences.  A row of finite inputs that fit is
 // finite, so that a look at what leaves the kernel finds these; a warp forms each again from the pairs it sees alone.
+
+// A row's softmax sum is known from lse.  Scores so far from zero that lse does not hold the sum's digits (beyond 1,024 in
+// base-2 units it is off by 2^-14, at 2^30 by 64) make a far row: the backward pass adds up its weights and takes the rest off.
+constexpr float kFarLse = 1024.f;
+__device__ __forceinline__ bool far_row(float lse) { return fabsf(lse) > kFarLse && fabsf(lse) < INFINITY; }
 
 // A pair's bias in base-2 units.
 __device__ __forceinline__ float pair_bias(const AttendParams &p, uint32_t h, int32_t rel)

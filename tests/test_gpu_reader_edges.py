@@ -385,3 +385,17 @@ def test_attend_with_spans_of_another_stream(model, dim):
         model.sync()
         empty = ~((spans[:, 0] >= 0) & (spans[:, 0] <= at) & (spans[:, 1] > at))
         assert all(torch.isfinite(t).all() for t in got) and all((t[empty] == 0).all() for t in got[:4])
+
+
+# ---- rows whose every bias is far from zero -----------------------------------------------------------------------------
+@pytest.mark.parametrize("dim", [64, 80, 128])
+@pytest.mark.parametrize("low", [-1e5, -1e9, torch.finfo(torch.float32).min, 1e5])
+def test_attend_bias_that_swallows_scores(model, dim, low):
+    """Keys are alike, so that softmax is a mean whatever the bias: tiles with and without masks must lose the same digits."""
+    toks = stream(900, (900, 900), 8, oov=0.002)
+    bias = torch.full((16, 4), low, device="cuda")
+    q, v = randn(900, 4, dim, seed=1, dtype=torch.bfloat16), randn(900, 2, dim, seed=3, dtype=torch.bfloat16)
+    k = randn(1, 2, dim, seed=12, dtype=torch.bfloat16).expand(900, -1, -1)
+    want, bound = attend_by_hand(q, k, v, toks, bias, 500, 0, 40, 64, False, q, True)
+    o = model.attend(q, k, v, model.sentence_spans(torch.from_numpy(toks).cuda()), bias, left=500, sinks=40, reach=64)
+    inside(o, want["o"], bound["o"], "o")
