@@ -2,6 +2,8 @@
 //
 // With P = exp2(S - lse) and dP = dO V^T:  dS = P (dP - delta), delta = rowsum(P dP) = rowsum(dO o),
 //   dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO,  dbias[b] = sum of dS over the pairs of bucket b.
+// (A far row, whose lse cannot hold its sum's digits, has weights that are all off by one factor; role 0 adds them up and puts
+// its own results right, role 1 takes the factor from there.)
 // Two passes over the scores, so that nothing is added up with atomics and the same inputs give the same bits:
 //   role 0, a block per 128 queries: dQ and delta.  The rounded o gives a first delta; the row's sum of dS, which is
 //           zero for an exact one, says how far it is off, and dQ is put right with the product P K that is formed
@@ -58,8 +60,8 @@ struct BackShared {
     int32_t limits[4][3];
     uint32_t vis[Sh::kStages][2];                    // which streamed rows of the stage are words
     int32_t run_lo[Sh::kStages];                     // role 1: where the run of the stage's query tile begins
-    __align__(16) float lse[Sh::kStages][Sh::kRows], delta[Sh::kStages][Sh::kRows];      // role 1: of the stage's queries, negated
-    float eps[2][128];
+    __align__(16) float lse[Sh::kStages][Sh::kRows], delta[Sh::kStages][Sh::kRows], extra[Sh::kStages][Sh::kRows];       // role 1: of the stage's queries, negated
+    int far[Sh::kStages];                            // role 1: there are far rows among them
     float far_sum[8][2];
 };
 
@@ -90,11 +92,12 @@ __device__ __forceinline__ void write_bucket_sums(const AttendParams &p, const f
 }
 
 // What this block's queries add to the sinks before its run: dK (before the scale) and dV of each, and the bias' sums,
-// by the softmax threads.  sink_d holds dS for the first delta, which eps puts right.  A thread takes two columns
+// by the softmax threads.  sink_d holds dS for the first delta, which eps puts right, sink_p the weights; `by` puts a far row
+// right.  A thread takes two columns
 // and a part of the rows, four sinks at a time; `red` is 16 KB for joining the parts.
 template <typename T, int NB, int kSoft>
-__device__ __forceinline__ void sink_sums(const AttendParams &p, unsigned char *own_rows, const float *sink_p, float *sink_d,
-                                       RowLimits row, float eps, float *red, int32_t sinks, int32_t s, int32_t t0, uint32_t wg, uint32_t r,
+__device__ __forceinline__ void sink_sums(const AttendParams &p, unsigned char *own_rows, float *sink_p, float *sink_d,
+                                       RowLimits row, float eps, float by, float *red, int32_t sinks, int32_t s, int32_t t0, uint32_t wg, uint32_t r,
                                        uint32_t tid, float *out, float *bias_out)
 {
     constexpr int kPairs = 32 * NB, kParts = kSoft / kPairs, kPartRows = 128 / kParts, kOwn = NB * 128 * 128;
@@ -102,7 +105,8 @@ __device__ __forceinline__ void sink_sums(const AttendParams &p, unsigned char *
     const bool part_of = row.s == s && row.s < row.se;
     for (int32_t k = (int32_t)wg; k < sinks; k += kSoft / 128) {
         const int32_t at = k * 128 + (int32_t)r;
-        sink_d[at] = part_of ? fmaf(-eps, sink_p[at], sink_d[at]) : 0.f;
+        sink_d[at] = part_of ? fmaf(-eps, sink_p[at], sink_d[at]) * by : 0.f;
+        if (by != 1.f) sink_p[at] *= by;
     }
     if (!part_of)
 #pragma unroll
@@ -186,7 +190,7 @@ __device__ __forceinline__ int32_t run_begin(const AttendParams &p, int32_t q0, 
 
 // dQ of row i by a warp, from the pairs that it sees.
 template <typename T>
-__device__ __forceinline__ void dq_again(const AttendParams &p, uint32_t h, uint32_t kvh, int64_t i, float lse, float delta, uint32_t lane)
+__device__ __forceinline__ void dq_again(const AttendParams &p, uint32_t h, uint32_t kvh, int64_t i, float lse, float by, float delta, uint32_t lane)
 {
     const RowLimits row = row_limits(p, i);
     const T *q = static_cast<const T *>(p.q) + i * (int64_t)p.ldq + h * p.dim, *d_o = static_cast<const T *>(p.d_o) + i * (int64_t)p.ld_do + h * p.dim;
@@ -201,7 +205,7 @@ __device__ __forceinline__ void dq_again(const AttendParams &p, uint32_t h, uint
             const bool seen = j < b && is_word(p, j);
             float w = 0.f;
             if (seen) {
-                w = fast_exp2(fmaf(row_dot(q, k + j * (int64_t)p.ldk, p.dim), p.scale * kLog2e, pair_bias(p, h, (int32_t)(j - i))) - lse);
+                w = fast_exp2(fmaf(row_dot(q, k + j * (int64_t)p.ldk, p.dim), p.scale * kLog2e, pair_bias(p, h, (int32_t)(j - i))) - lse) * by;
                 w *= row_dot(d_o, v + j * (int64_t)p.ldv, p.dim) - delta;
             }
             add_rows(acc, w, __ballot_sync(kFullMask, seen), k + j0 * (int64_t)p.ldk, p.ldk, p.dim, lane);
@@ -233,7 +237,7 @@ __device__ __forceinline__ void dkv_again(const AttendParams &p, uint32_t which,
             const bool seen = i < end && is_word(p, i);
             float w = 0.f;
             if (seen) {
-                w = fast_exp2(fmaf(row_dot(q + i * (int64_t)p.ldq, k, p.dim), p.scale * kLog2e, pair_bias(p, h, (int32_t)(j - i))) - __ldg(p.lse + (int64_t)h * p.n + i));
+                w = fast_exp2(fmaf(row_dot(q + i * (int64_t)p.ldq, k, p.dim), p.scale * kLog2e, pair_bias(p, h, (int32_t)(j - i))) - __ldg(p.lse + (int64_t)h * p.n + i) - p.extra[(int64_t)h * p.n + i]);
                 if (which == 0) w *= row_dot(d_o + i * (int64_t)p.ld_do, v, p.dim) - p.delta[(int64_t)h * p.n + i];
             }
             const uint32_t live = __ballot_sync(kFullMask, seen);
@@ -263,7 +267,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
     unsigned char *own_rows = smem + Sh::kRing;                      // the two A sides, and o in role 0 (not SMALL), as they land
     float *lut = reinterpret_cast<float *>(smem + Sh::kRing + 2 * Sh::kOwn + (ROLE == 0 ? max(SMALL ? 0 : Sh::kOwn, p.sinks * 1024) : 0));
     const uint32_t entries = bias_entries(p.b);
-    float *rel_sums = lut + ((entries + 3u) & ~3u);                  // role 1: [softmax warps][entries]; role 0, SMALL: halves of the first delta
+    float *rel_sums = lut + ((entries + 3u) & ~3u);                  // role 1: [softmax warps][entries]; role 0: [2][warpgroups][rows], parts of what is added up
 
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t group = p.heads / p.kv_heads, across = ROLE == 0 ? p.heads : p.kv_heads;
@@ -425,6 +429,8 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
             }
         }
         float2 eps2 = make_float2(0.f, 0.f);
+        float weights = 0.f;                                         // role 0: their sum, for far rows
+        const bool far_rows = ROLE == 0 && __any_sync(kFullMask, far_row(lse));
         for (uint32_t g = 0; g < heads_here; ++g) {
             if (ROLE == 1 && p.b.n && g > 0) {
                 soft_barrier(Sh::kSoft);                             // the sums of the head before are written
@@ -518,6 +524,10 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                             }
                             tmem_st(cs + (SMALL ? c0 : c0 / 2), wp);
                             tmem_st(cd + (SMALL ? c0 : c0 / 2), ws);
+                            if (far_rows) {
+#pragma unroll
+                                for (int e = 0; e < kC; ++e) weights += x[e];
+                            }
                             if (k >= run) {                          // sinks: kept in fp32 for their own sums
 #pragma unroll
                                 for (int e = 0; e < kC; ++e) {
@@ -529,9 +539,15 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                                 }
                             }
                         } else {
+                            const float *less = sh.lse[stage];       // negated, as delta and extra
+                            if (sh.far[stage]) {
+#pragma unroll
+                                for (int e = 0; e < kC; ++e) x[e] += less[c0 + e];
+                                less = sh.extra[stage];
+                            }
 #pragma unroll
                             for (int e = 0; e < kC; e += 4) {
-                                const float4 l4 = *reinterpret_cast<const float4 *>(&sh.lse[stage][c0 + e]);        // negated, as delta
+                                const float4 l4 = *reinterpret_cast<const float4 *>(less + c0 + e);
                                 const float4 d4 = *reinterpret_cast<const float4 *>(&sh.delta[stage][c0 + e]);
                                 float2 p0 = add2(make_float2(x[e], x[e + 1]), make_float2(l4.x, l4.y));
                                 float2 p1 = add2(make_float2(x[e + 2], x[e + 3]), make_float2(l4.z, l4.w));
@@ -597,13 +613,21 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                 write_bucket_sums(p, rel_sums, off, sh.far_sum, warp, kSoftWarps, lane, p.dbias_part + ((size_t)tile * p.heads + h0 + g) * buckets);
             }
         }
-        float eps = 0.f;
+        float eps = 0.f, far_by = 1.f;                               // far_by: what a far row's weights are to be multiplied by
         if (ROLE == 0) {
             eps = eps2.x + eps2.y;
-            sh.eps[wg][r] = eps;
+            if (SMALL) soft_barrier(Sh::kSoft);                      // everybody has read the first delta's parts
+            rel_sums[wg * 128 + r] = eps;
+            rel_sums[256 + wg * 128 + r] = weights;
             soft_barrier(Sh::kSoft);
-            eps = sh.eps[0][r] + sh.eps[1][r];
-            if (wg == 0 && own < p.n) p.delta[(int64_t)h_own * p.n + own] = word ? delta + eps : 0.f;
+            eps = rel_sums[r] + rel_sums[128 + r];
+            weights = far_row(lse) ? rel_sums[256 + r] + rel_sums[384 + r] : 1.f;
+            far_by = 1.f / weights;
+            eps *= far_by;
+            if (wg == 0 && own < p.n) {
+                p.delta[(int64_t)h_own * p.n + own] = word ? delta + eps : 0.f;
+                p.extra[(int64_t)h_own * p.n + own] = weights == 1.f ? 0.f : log2f(weights);
+            }
         }
         ok = __all_sync(kFullMask, ok && (total == 0 || mbar_nap(&sh.done, 0, abort_flag)));
         tc_fence_after();
@@ -611,7 +635,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
             if (h_own == 0 && tid == 0) p.sink_rec[tile] = !hi ? -1 : s_lo >= t0 ? -2 : sinks ? s_lo : -1;
             const uint32_t buckets = p.b.n * (p.b.two_sided ? 2u : 1u);
             float *bias_out = p.dbias ? p.dbias_part + ((size_t)((uint32_t)((p.n + kAttendTile - 1) / kAttendTile) + tile) * p.heads + h_own) * buckets : nullptr;
-            if (sinks) sink_sums<T, NB, Sh::kSoft>(p, own_rows, sink_p, sink_d, row, eps, reinterpret_cast<float *>(smem), sinks, s_lo, t0, wg, r, tid,
+            if (sinks) sink_sums<T, NB, Sh::kSoft>(p, own_rows, sink_p, sink_d, row, eps, far_by, reinterpret_cast<float *>(smem), sinks, s_lo, t0, wg, r, tid,
                                                    p.sink_part + ((size_t)tile * p.heads + h_own) * p.sinks * 2 * p.dim, bias_out);
             else if (bias_out) for (uint32_t b = tid; b < buckets; b += Sh::kSoft) bias_out[b] = 0.f;
             soft_barrier(Sh::kSoft);
@@ -619,7 +643,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
         // outputs leave through shared memory: dQ (half of its columns by each warpgroup), or dK and dV (one each)
         constexpr bool kHalf = ROLE == 0;
         const uint32_t which = ROLE == 0 ? 0u : wg;              // 0: dQ or dK, 1: dV
-        const float by = which == 0 ? p.scale : 1.f;
+        const float by = (which == 0 ? p.scale : 1.f) * far_by;
         const float *sink = nullptr;
         if (ROLE == 1 && p.sink_used && word && own - sent < p.sinks && p.sink_used[sent / kAttendTile] == sent)
             sink = p.sink_sum + ((((size_t)(sent / kAttendTile) * p.kv_heads + kvh) * p.sinks + (size_t)(own - sent)) * 2 + which) * p.dim;
@@ -686,7 +710,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
 #pragma unroll 1
             for (; bad; bad &= bad - 1u) {
                 const int32_t x = __ffs(bad) - 1;
-                if (ROLE == 0) dq_again<T>(p, h_own, kvh, (int64_t)w0 + x, __shfl_sync(kFullMask, lse, x), __shfl_sync(kFullMask, delta + eps, x), lane);
+                if (ROLE == 0) dq_again<T>(p, h_own, kvh, (int64_t)w0 + x, __shfl_sync(kFullMask, lse, x), __shfl_sync(kFullMask, far_by, x), __shfl_sync(kFullMask, delta + eps, x), lane);
                 else dkv_again<T>(p, which, kvh, (int64_t)w0 + x, reinterpret_cast<const float *>(__shfl_sync(kFullMask, reinterpret_cast<unsigned long long>(sink), x)), lane);
             }
         }
@@ -801,7 +825,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
             const int32_t k = t % per_head, at = tile_at(k), rows = tile_rows(k);
             uint32_t vis[2];
             word_bits(p, at, (uint32_t)rows, lane, vis);
-            float lse[2], delta[2];
+            float lse[2], delta[2], extra[2];
             int32_t run_lo = 0;
             if (ROLE == 1) {
 #pragma unroll
@@ -809,6 +833,7 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                     const int64_t i = (int64_t)at + w * 32 + lane;
                     lse[w] = i < p.n ? __ldg(p.lse + (int64_t)h * p.n + i) : INFINITY;
                     delta[w] = i < p.n ? p.delta[(int64_t)h * p.n + i] : 0.f;
+                    extra[w] = i < p.n ? p.extra[(int64_t)h * p.n + i] : 0.f;
                 }
                 if (p.sinks) run_lo = run_begin(p, at / kAttendTile * kAttendTile, lane);
             }
@@ -816,8 +841,16 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
             if (lane < 2) sh.vis[stage][lane] = lane ? vis[1] : vis[0];
             if (ROLE == 1) {
 #pragma unroll
-                for (int w = 0; w < Sh::kRows / 32; ++w) { sh.lse[stage][w * 32 + lane] = -lse[w]; sh.delta[stage][w * 32 + lane] = -delta[w]; }
-                if (lane == 0) sh.run_lo[stage] = run_lo;
+                for (int w = 0; w < Sh::kRows / 32; ++w) {
+                    sh.lse[stage][w * 32 + lane] = -lse[w];
+                    sh.delta[stage][w * 32 + lane] = -delta[w];
+                    sh.extra[stage][w * 32 + lane] = -extra[w];
+                }
+                bool far = false;
+#pragma unroll
+                for (int w = 0; w < Sh::kRows / 32; ++w) far = far || extra[w] != 0.f;
+                far = __any_sync(kFullMask, far);
+                if (lane == 0) { sh.run_lo[stage] = run_lo; sh.far[stage] = far; }
             }
             const uint32_t x = ring + stage * Sh::kStage, cols = (uint32_t)(rows + 15) & ~15u;
             zero_rows<NB>(x, Sh::kRows * 128, cols, vis, lane);
@@ -911,7 +944,7 @@ attend_dbias_kernel(const float *part, uint64_t rows, uint32_t columns, uint32_t
 namespace {
 
 struct BackWs {
-    uint64_t delta, part, sink_part, sink_sum, rec, used, bytes;
+    uint64_t delta, extra, part, sink_part, sink_sum, rec, used, bytes;
 };
 
 bool far_sinks(const AttendParams &p) { return p.sinks > 0 && p.n > (int64_t)p.left + 1; }
@@ -924,6 +957,7 @@ BackWs back_ws(const AttendParams &p, bool want_dbias)
     uint64_t at = 0;
     auto take = [&](uint64_t floats) { const uint64_t x = at; at += (floats * 4 + 15) & ~15ull; return x; };
     w.delta = take((uint64_t)p.n * p.heads);
+    w.extra = take((uint64_t)p.n * p.heads);
     w.part = take(want_dbias ? (sinks ? 2 : 1) * tiles * p.heads * buckets : 0);
     w.sink_part = take(sinks ? tiles * p.heads * p.sinks * 2 * p.dim : 0);
     w.sink_sum = take(sinks ? tiles * p.kv_heads * p.sinks * 2 * p.dim : 0);
@@ -941,7 +975,7 @@ int launch_role(const AttendParams &p, uint32_t tiles, int *error, cudaStream_t 
     const uint32_t entries = bias_entries(p.b);
     const int o_bytes = SMALL ? 0 : Sh::kOwn, sink_bytes = p.sinks * 1024;
     int smem = Sh::kRing + 2 * Sh::kOwn + (ROLE == 0 ? (sink_bytes > o_bytes ? sink_bytes : o_bytes) : 0) + 1024 +
-               (int)(4 * (((entries + 3u) & ~3u) + (ROLE == 1 ? Sh::kSoft / 32 * entries : 256u)));
+               (int)(4 * (((entries + 3u) & ~3u) + (ROLE == 1 ? Sh::kSoft / 32 * entries : 512u)));
     if (!SMALL && smem < 116 * 1024) smem = 116 * 1024;              // a second block would only wait for tensor memory
     if (!kernel_ready<attend_back_kernel<T, NB, ROLE, SMALL>>(SMALL ? kBackLaunchRegs : 0)) return -1;
     CUtensorMap x, y, a0, a1, o;
@@ -993,6 +1027,7 @@ int launch_attend_backward(AttendParams &p, uint32_t type, unsigned char *ws, in
     int k = 0;
     if (p.n) {
         p.delta = reinterpret_cast<float *>(ws + w.delta);
+        p.extra = reinterpret_cast<float *>(ws + w.extra);
         p.dbias_part = reinterpret_cast<float *>(ws + w.part);
         if (far_sinks(p)) {
             p.sink_part = reinterpret_cast<float *>(ws + w.sink_part);

@@ -47,6 +47,7 @@ struct AttendParams {
     const float *bias;              // [buckets][heads]
     float *lse;                     // [heads][n] base-2 logarithm of the softmax sum (scores scaled by log2 e), +inf for an empty row
     float *delta;                   // [heads][n] backward: rowsum(dO o)
+    float *extra;                   // [heads][n] backward: base-2 logarithm of what a row's weights sum to with lse as it is, for far rows; else 0
     float *dbias, *dbias_part;      // [buckets][heads]; [key tiles, then query tiles with sinks][heads][buckets]
     float *sink_part;               // [query tiles][heads][sinks][dk, dv][dim] sums over one query tile
     int32_t *sink_rec;              // [query tiles] start of the sentence that reaches into the tile, -1: no word, -2: none

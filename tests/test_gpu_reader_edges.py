@@ -399,3 +399,47 @@ def test_attend_bias_that_swallows_scores(model, dim, low):
     want, bound = attend_by_hand(q, k, v, toks, bias, 500, 0, 40, 64, False, q, True)
     o = model.attend(q, k, v, model.sentence_spans(torch.from_numpy(toks).cuda()), bias, left=500, sinks=40, reach=64)
     inside(o, want["o"], bound["o"], "o")
+
+
+@pytest.mark.parametrize("dim", [64, 80, 128])
+@pytest.mark.parametrize("low", [-1e3, -1e5, -1e9, torch.finfo(torch.float32).min, 1e5])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_attend_rows_of_nothing_but_low_biases(model, dim, low, dtype):
+    """A head without any other bias, and words that see hidden buckets only (the first ones of their sentence): softmax does not
+    know a constant, forwards and backwards.  Keys are alike, so that the scores' digits, which a bias of 1e9 swallows in 32
+    bits, do not matter; the bounds are the usual ones."""
+    n, h, kv = 700, 4, 2
+    toks = stream(n, (1, 300), 8)
+    bias = randn(16, h, seed=9, by=0.5)
+    bias[:, 1] = low                                                 # a whole head
+    bias[:4, 2] = low                                                # distances 0 to 3
+    one = randn(1, kv, dim, seed=12, dtype=dtype)
+    q, k, v, d_o = randn(n, h, dim, seed=1, dtype=dtype), one.expand(n, -1, -1), randn(n, kv, dim, seed=3, dtype=dtype), randn(n, h, dim, seed=4, dtype=dtype)
+    for left, right, sinks, two in ((60, 0, 4, False), (500, 90, 0, True), (100, 5, 40, False)):
+        want, bound = attend_by_hand(q, k, v, toks, bias, left, right, sinks, 64, two, d_o, True)
+        spans = model.sentence_spans(torch.from_numpy(toks).cuda())
+        o, saved = model.attend(q, k, v, spans, bias, left=left, right=right, sinks=sinks, reach=64, two_sided=two, train=True)
+        for name, x in zip(("o", "dq", "dk", "dv", "dbias"), (o, *model.attend_backward(d_o, saved))):
+            inside(x, want[name], bound[name], name)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("low", [-float("inf"), torch.finfo(torch.float32).min, -1e5, 2e3])
+def test_attend_far_buckets_hidden(model, dim, low):
+    """The last bucket, which whole tiles without masks lie in, and sinks beyond it; with -infinity in every bucket of a head its rows
+    are empty."""
+    toks = stream(1200, (1200, 1200), 8, oov=0.002)
+    bias = randn(16, 4, seed=9, by=0.5)
+    bias[15, :2] = low
+    if low == -float("inf"):
+        bias[:, 3] = low
+    q, k, v, d_o = (randn(1200, x, dim, seed=s, dtype=torch.bfloat16) for s, x in ((1, 4), (2, 2), (3, 2), (4, 4)))
+    if low > 0:
+        k[:] = k[:1].clone()                                         # scores alike: what a bias of thousands swallows of them does not matter
+    want, bound = attend_by_hand(q, k, v, toks, bias, 700, 0, 8, 64, False, d_o, True)
+    spans = model.sentence_spans(torch.from_numpy(toks).cuda())
+    o, saved = model.attend(q, k, v, spans, bias, left=700, sinks=8, reach=64, train=True)
+    for name, x in zip(("o", "dq", "dk", "dv", "dbias"), (o, *model.attend_backward(d_o, saved))):
+        inside(x, want[name], bound[name], name)
+    if low == -float("inf"):
+        assert (o[:, 3] == 0).all() and (saved[-1][3] == float("inf")).all()
