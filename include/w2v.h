@@ -587,7 +587,8 @@ int32_t w2v_bucket_starts(uint32_t buckets, uint32_t reach, uint32_t two_sided, 
  *   q, k, v, o  [n][heads or kv_heads][head_dim], heads side by side, `stride` elements from position to
  *               position (a multiple of 8; one packed projection can hold q, k and v), 16-byte aligned.
  *   bias        [buckets][heads] floats, NULL when buckets is 0.
- *               A bias of -infinity hides a bucket, as one of the lowest float does where another bucket is seen.
+ *               A bias of -infinity hides a bucket, as one of the lowest float does where another bucket is seen (where
+ *               none is, o is the mean of the values).
  *   A value that is not finite reaches the positions that see its word and no others, in both directions; rows that
  *   come out not finite are formed a second time, slowly.  What words outside the vocabulary hold reaches nobody.
  *   lse         [heads][n] floats for the backward call, or NULL: base-2 logarithm of the softmax sum, +infinity

@@ -70,9 +70,10 @@ __device__ __forceinline__ uint32_t bucket_of(const BucketStarts &b, int32_t rel
     return lo + (b.two_sided && rel > 0 ? b.n : 0u);
 }
 
-// A bias in base-2 units; one of the lowest float stays finite, so that a row of nothing else is still a row.
-constexpr float kLowestBias = -1e30f * kLog2e;
-__device__ __forceinline__ float log2_bias(float b) { return b == -INFINITY ? b : fmaxf(b, -1e30f) * kLog2e; }
+// A bias in base-2 units; one of the lowest float stays finite (the lowest that does is 2.35e38 below zero), so that a row of
+// nothing else is still a row.
+constexpr float kLowest = -2.35e38f, kLowestBias = kLowest * kLog2e;
+__device__ __forceinline__ float log2_bias(float b) { return b == -INFINITY ? b : fmaxf(b, kLowest) * kLog2e; }
 
 // Relative positions [r0, r1) (key - query, within -off .. off) whose bias is bucket b's.
 __device__ __forceinline__ void bucket_range(const BucketStarts &s, uint32_t b, int32_t off, int32_t &r0, int32_t &r1)

@@ -443,3 +443,22 @@ def test_attend_far_buckets_hidden(model, dim, low):
         inside(x, want[name], bound[name], name)
     if low == -float("inf"):
         assert (o[:, 3] == 0).all() and (saved[-1][3] == float("inf")).all()
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_attend_very_low_biases_keep_their_order(model, dim):
+    """A bias of -1e32 outweighs one of the lowest float, in every kernel."""
+    toks, bias = stream(600, (600, 600), 3, oov=0.0), torch.full((16, 4), torch.finfo(torch.float32).min, device="cuda")
+    bias[2], bias[15, 1] = -1e32, -1e31
+    q, v, d_o = (randn(600, x, dim, seed=s, dtype=torch.bfloat16) for s, x in ((1, 4), (3, 2), (4, 4)))
+    k = randn(1, 2, dim, seed=12, dtype=torch.bfloat16).expand(600, -1, -1)
+    want, bound = attend_by_hand(q, k, v, toks, bias, 300, 0, 4, 64, False, d_o, True)
+    spans = model.sentence_spans(torch.from_numpy(toks).cuda())
+    o, saved = model.attend(q, k, v, spans, bias, left=300, sinks=4, reach=64, train=True)
+    for name, x in zip(("o", "dq", "dk", "dv", "dbias"), (o, *model.attend_backward(d_o, saved))):
+        inside(x, want[name], bound[name], name)
+    cache = torch.zeros(2, 1, 305, 2, dim, dtype=torch.bfloat16, device="cuda")
+    for t in range(5):
+        one = model.attend_token(q[t: t + 1], k[t: t + 1].contiguous(), v[t: t + 1], cache[0], cache[1], torch.tensor([t], dtype=torch.int32, device="cuda"), bias,
+                                 left=300, sinks=4, reach=64)
+        inside(one[0], want["o"][t], bound["o"][t], f"word {t}")
