@@ -632,7 +632,10 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
         ok = __all_sync(kFullMask, ok && (total == 0 || mbar_nap(&sh.done, 0, abort_flag)));
         tc_fence_after();
         if (ROLE == 0 && p.sink_rec) {
-            if (h_own == 0 && tid == 0) p.sink_rec[tile] = !hi ? -1 : s_lo >= t0 ? -2 : sinks ? s_lo : -1;
+            if (h_own == 0 && tid == 0) {
+                p.sink_rec[tile] = !hi ? -1 : s_lo >= t0 ? -2 : sinks ? s_lo : -1;
+                p.sink_used[tile] = -1;
+            }
             const uint32_t buckets = p.b.n * (p.b.two_sided ? 2u : 1u);
             float *bias_out = p.dbias ? p.dbias_part + ((size_t)((uint32_t)((p.n + kAttendTile - 1) / kAttendTile) + tile) * p.heads + h_own) * buckets : nullptr;
             if (sinks) sink_sums<T, NB, Sh::kSoft>(p, own_rows, sink_p, sink_d, row, eps, far_by, reinterpret_cast<float *>(smem), sinks, s_lo, t0, wg, r, tid,
@@ -893,14 +896,17 @@ attend_sink_sum_kernel(AttendParams p, int32_t tiles)
     __shared__ float part[8][32];
     const uint32_t kvh = blockIdx.x % p.kv_heads, group = p.heads / p.kv_heads, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const size_t width = (size_t)p.sinks * 2 * p.dim, e = (size_t)(blockIdx.x / p.kv_heads) * 32 + lane;
-    // most slots are empty, which takes one look to see: a block goes over many
-    for (int32_t a = (int32_t)blockIdx.y; a < tiles; a += (int32_t)gridDim.y) {
-        int32_t first = a + 1;
-        while (first < tiles && p.sink_rec[first] == -1) ++first;
-        const int32_t s = first < tiles ? p.sink_rec[first] : -2;
-        const bool here = s >= 0 && s / kAttendTile == a;
-        if (blockIdx.x == 0 && threadIdx.x == 0) p.sink_used[a] = here ? s : -1;
-        if (!here) continue;
+    // a sentence is added up from the first tile that has sums for it; most tiles have none or are not the first, which takes
+    // one look to see: a block goes over many.  (Looking ahead from where a sentence begins took 182 ms for 2,000 words in a
+    // buffer of 2,000,000 positions, 15,600 tiles of nothing.)
+    for (int32_t first = (int32_t)blockIdx.y; first < tiles; first += (int32_t)gridDim.y) {
+        const int32_t s = p.sink_rec[first];
+        if (s < 0) continue;
+        const int32_t a = s / kAttendTile, least = (int32_t)max((int64_t)a + 1, ((int64_t)s + p.left) / kAttendTile);     // none before that
+        int32_t before = first - 1;                                  // over tiles of the sentence without a word
+        while (before >= least && p.sink_rec[before] == -1) --before;
+        if (before >= least) continue;
+        if (blockIdx.x == 0 && threadIdx.x == 0) p.sink_used[a] = s;
         // the sentence's last tile is that of its last word; tiles without words in between have nothing
         const int32_t end = min(tiles, (word_span(p, first_word(p, first)).y - 1) / kAttendTile + 1);
         const int32_t items = (end - first) * (int32_t)group;

@@ -462,3 +462,41 @@ def test_attend_very_low_biases_keep_their_order(model, dim):
         one = model.attend_token(q[t: t + 1], k[t: t + 1].contiguous(), v[t: t + 1], cache[0], cache[1], torch.tensor([t], dtype=torch.int32, device="cuda"), bias,
                                  left=300, sinks=4, reach=64)
         inside(one[0], want["o"][t], bound["o"][t], f"word {t}")
+
+
+# ---- sinks of sentences with long stretches that nobody sees -----------------------------------------------------------------
+@pytest.mark.parametrize("left", [30, 300, 700])
+@pytest.mark.parametrize("kv", [1, 4])
+def test_attend_sinks_across_empty_tiles(model, left, kv):
+    """Words that the vocabulary does not have fill whole tiles within a sentence, at its beginning and between sentences; the sinks'
+    gradients come from the tiles behind them."""
+    n = 2000
+    toks = stream(n, (n, n), 4, oov=0.02)
+    toks[[0, 100, 101, 1300]] = -1
+    toks[102: 110] = 5                                               # sinks, and then nothing for three tiles
+    for a, b in ((110, 560), (700, 980), (1301, 1600), (1900, 2000)):
+        toks[a: b] = VOCAB + 9
+    both_ways(model, toks, 4, kv, 64, torch.bfloat16, randn(16, 4, seed=9, by=0.5), left, left=left, right=3, sinks=6, reach=64, two_sided=True)
+
+
+def test_attend_backward_of_a_padded_stream(model):
+    """A short stream in a long buffer of separators or unknown words: the gradient's time goes with the words."""
+    n, words = 2_000_000, 2000
+    toks = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    toks[:words] = torch.from_numpy(stream(words, (400, 900), 4)).cuda()
+    q, k = randn(n, 1, 64, seed=1, dtype=torch.bfloat16), randn(n, 1, 64, seed=2, dtype=torch.bfloat16)
+    times = {}
+    for sinks in (0, 4):
+        for pad in (-1, VOCAB):
+            toks[words:] = pad
+            spans = model.sentence_spans(toks)
+            _, saved = model.attend(q, k, k, spans, left=60, sinks=sinks, train=True)
+            for _ in range(3):
+                begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+                begin.record()
+                grads = model.attend_backward(q, saved)
+                end.record()
+                torch.cuda.synchronize()
+                times[sinks, pad] = min(times.get((sinks, pad), 1e9), begin.elapsed_time(end))
+            assert all((g[words:] == 0).all() for g in grads[:3])
+    assert max(times.values()) < 10 * min(times.values())            # sinks cost a small part; looking for them from every tile on cost 170 times the rest
