@@ -77,7 +77,7 @@ norm_kernel(NormParams p, uint32_t gw, uint32_t groups)
 // The same for rows that arrive through a ring (see w2v_norm.cuh): `stages` units per group.
 template <typename TX, typename TY, int E, int NV>
 __global__ void __launch_bounds__(512)
-norm_ring_kernel(NormParams p, uint32_t gw, uint32_t groups, uint32_t stages, uint32_t mode, int *error)
+norm_ring_kernel(NormParams p, uint32_t gw, uint32_t groups, uint32_t stages, int *error)
 {
     extern __shared__ __align__(16) unsigned char ring[];
     __shared__ float slot[64 * kNormUnit];
@@ -85,7 +85,7 @@ norm_ring_kernel(NormParams p, uint32_t gw, uint32_t groups, uint32_t stages, ui
     __shared__ int abort_flag, quiet;
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const uint32_t group = warp / gw, wig = warp - group * gw, gl = wig * 32 + lane;
-    const uint32_t row_bytes = p.d * sizeof(TX), pitch = norm_pitch(mode, p.d, sizeof(TX)), unit_bytes = (kNormUnit * pitch + 15u) & ~15u;
+    const uint32_t row_bytes = p.d * sizeof(TX), unit_bytes = kNormUnit * row_bytes;
     const TX *x = static_cast<const TX *>(p.x);
     TY *y = static_cast<TY *>(p.y);
     unsigned char *mine = ring + group * stages * unit_bytes;
@@ -103,8 +103,8 @@ norm_ring_kernel(NormParams p, uint32_t gw, uint32_t groups, uint32_t stages, ui
     auto issue = [&](uint64_t unit, uint32_t stage) {                 // by the group's first lane
         const uint64_t r = unit * kNormUnit;
         const uint32_t n = (uint32_t)min((uint64_t)kNormUnit, p.rows - r), dst = smem_addr(mine + stage * unit_bytes);
-        mbar_expect(&full[group][stage], norm_copy(mode, dst, reinterpret_cast<const char *>(x), p.ldx * sizeof(TX), row_bytes, pitch, r, n, &full[group][stage], false));
-        norm_copy(mode, dst, reinterpret_cast<const char *>(x), p.ldx * sizeof(TX), row_bytes, pitch, r, n, &full[group][stage], true);
+        mbar_expect(&full[group][stage], n * row_bytes);
+        norm_copy(kCopyRows, dst, reinterpret_cast<const char *>(x), p.ldx * sizeof(TX), row_bytes, row_bytes, r, n, &full[group][stage], true);
     };
     uint32_t issued = 0;                                              // the first lane's: units on their way or here
     bool live = true;                                                 // no wait of this thread has run out
@@ -120,16 +120,12 @@ norm_ring_kernel(NormParams p, uint32_t gw, uint32_t groups, uint32_t stages, ui
         const uint32_t n = (uint32_t)min((uint64_t)kNormUnit, p.rows - r);
         unsigned char *rows = mine + stage * unit_bytes;
         live = mbar_wait(&full[group][stage], phase, &abort_flag) && live;     // once it has given up the rest runs through on whatever is there
-        if (mode == kCopyUnits && n < kNormUnit) {
-            norm_copy_tail<TX>(mode, rows, x + r * p.ldx, p.d, n, gl, gw * 32);
-            group_barrier(gw, group);
-        }
         float2 v[kNormUnit][kPairs];
         float s[kNormUnit], q[kNormUnit];
 #pragma unroll
         for (int i = 0; i < kNormUnit; ++i) {
             Pack<TX, E> t[NV];
-            norm_row_load<TX, E, NV>(t, reinterpret_cast<const TX *>(rows + i * pitch), gl, gw, p.d);
+            norm_row_load<TX, E, NV>(t, reinterpret_cast<const TX *>(rows + i * row_bytes), gl, gw, p.d);
             float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
             for (int c = 0; c < NV; ++c)
@@ -192,12 +188,12 @@ norm_ring_kernel(NormParams p, uint32_t gw, uint32_t groups, uint32_t stages, ui
 }
 
 template <typename TX, typename TY, int E, int NV>
-int launch_norm_ring(const NormParams &p, const NormShape &sh, uint32_t stages, uint32_t mode, size_t smem, int *error, int sms, cudaStream_t s)
+int launch_norm_ring(const NormParams &p, const NormShape &sh, uint32_t stages, size_t smem, int *error, int sms, cudaStream_t s)
 {
     if (!kernel_ready<norm_ring_kernel<TX, TY, E, NV>>()) return -1;
     const uint32_t threads = sh.gw * sh.groups * 32;
     const uint64_t units = (p.rows + kNormUnit - 1) / kNormUnit, want = (units + sh.groups - 1) / sh.groups, most = (uint64_t)sms * (512u / threads ? 512u / threads : 1u);
-    norm_ring_kernel<TX, TY, E, NV><<<(uint32_t)(want < most ? want : most), threads, smem, s>>>(p, sh.gw, sh.groups, stages, mode, error);
+    norm_ring_kernel<TX, TY, E, NV><<<(uint32_t)(want < most ? want : most), threads, smem, s>>>(p, sh.gw, sh.groups, stages, error);
     return cudaPeekAtLastError() == cudaSuccess ? 1 : -1;
 }
 
@@ -208,21 +204,20 @@ int launch_norm_typed(const NormParams &p, int *error, int sms, cudaStream_t s)
     e = widest_access(p.d, sizeof(TY), p.ldy, p.y, e);
     const NormShape sh = norm_shape(p.d, e);
     constexpr uint32_t kE = 16 / sizeof(TX);
-    // Rows enough to keep a ring going, and copyable ones.  Registers against ring, us: 592 rows of 4,096 bf16 11.3 and 9.2,
+    // Rows enough to keep a ring going, and ones that can be copied.  Registers against ring, us: 592 rows of 4,096 bf16 11.3 and 9.2,
     // 592 of 768 8.2 and 9.2, 2,368 (16 per SM) of 768 11.1 and 9.2, 9,472 of 300 fp32 13.3 and 12.3; 262,144 of 300
     // 135 and 115, 37,888 of 4,096 237 and 121.
-    const uint32_t mode = norm_copy_mode(p.x, p.ldx, p.d, sizeof(TX));
-    if (e == kE && mode != kCopyNot && p.rows >= (uint64_t)sms * 16) {
-        const size_t unit = (kNormUnit * norm_pitch(mode, p.d, sizeof(TX)) + 15u) & ~15u, most = 104 * 1024 / (512u / (sh.gw * sh.groups * 32) ? 512u / (sh.gw * sh.groups * 32) : 1u);
+    if (e == kE && p.rows >= (uint64_t)sms * 16) {
+        const size_t unit = kNormUnit * p.d * sizeof(TX), most = 104 * 1024 / (512u / (sh.gw * sh.groups * 32) ? 512u / (sh.gw * sh.groups * 32) : 1u);
         uint32_t stages = 4;
         while (stages > 1 && unit * sh.groups * stages > most) --stages;
         const size_t smem = unit * sh.groups * stages;
         if (smem <= most && stages > 1) {
-            if constexpr (kE == 8) return sh.nv <= 1 ? launch_norm_ring<TX, TY, 8, 1>(p, sh, stages, mode, smem, error, sms, s) : launch_norm_ring<TX, TY, 8, 2>(p, sh, stages, mode, smem, error, sms, s);
-            else return sh.nv <= 1 ? launch_norm_ring<TX, TY, 4, 1>(p, sh, stages, mode, smem, error, sms, s)
-                        : sh.nv == 2 ? launch_norm_ring<TX, TY, 4, 2>(p, sh, stages, mode, smem, error, sms, s)
-                        : sh.nv == 3 ? launch_norm_ring<TX, TY, 4, 3>(p, sh, stages, mode, smem, error, sms, s)
-                                     : launch_norm_ring<TX, TY, 4, 4>(p, sh, stages, mode, smem, error, sms, s);
+            if constexpr (kE == 8) return sh.nv <= 1 ? launch_norm_ring<TX, TY, 8, 1>(p, sh, stages, smem, error, sms, s) : launch_norm_ring<TX, TY, 8, 2>(p, sh, stages, smem, error, sms, s);
+            else return sh.nv <= 1 ? launch_norm_ring<TX, TY, 4, 1>(p, sh, stages, smem, error, sms, s)
+                        : sh.nv == 2 ? launch_norm_ring<TX, TY, 4, 2>(p, sh, stages, smem, error, sms, s)
+                        : sh.nv == 3 ? launch_norm_ring<TX, TY, 4, 3>(p, sh, stages, smem, error, sms, s)
+                                     : launch_norm_ring<TX, TY, 4, 4>(p, sh, stages, smem, error, sms, s);
         }
     }
     const uint32_t threads = sh.gw * sh.groups * 32;

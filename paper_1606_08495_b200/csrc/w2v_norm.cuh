@@ -81,8 +81,8 @@ __device__ __forceinline__ void norm_weights_load(float (&w)[NV * E], const floa
 // barrier and the lane sums of its rows are shared.
 constexpr int kNormUnit = 2;
 
-// How an array of rows is copied: a row at a time (row starts and lengths are multiples of 16 bytes), or a unit at a time
-// (rows without gaps, whose units are), or not.
+// How an array of rows is copied: a row at a time (row starts and lengths are multiples of 16 bytes: x always, since the
+// kernels with a ring read it in 16-byte accesses), or a unit at a time (rows without gaps, whose units are; dy beside fp32 x), or not.
 enum : uint32_t { kCopyRows = 0, kCopyUnits = 1, kCopyNot = 2 };
 inline uint32_t norm_copy_mode(const void *p, uint64_t ld, uint32_t d, uint32_t size)
 {
@@ -120,9 +120,8 @@ __device__ __forceinline__ void norm_ring_drain(uint64_t *full, uint32_t issued,
 }
 // The cut-off unit of an array that is copied in units, by the lanes of a group.
 template <typename T>
-__device__ __forceinline__ void norm_copy_tail(uint32_t mode, unsigned char *dst, const T *row, uint32_t d, uint32_t n, uint32_t gl, uint32_t lanes)
+__device__ __forceinline__ void norm_copy_tail(unsigned char *dst, const T *row, uint32_t d, uint32_t n, uint32_t gl, uint32_t lanes)
 {
-    if (mode != kCopyUnits || n >= kNormUnit) return;
     for (uint32_t i = gl; i < n * d; i += lanes) reinterpret_cast<T *>(dst)[i] = row[i];
 }
 __device__ __forceinline__ void group_barrier(uint32_t gw, uint32_t group)

@@ -123,7 +123,7 @@ norm_backward_kernel(NormParams p, uint32_t gw, uint32_t groups)
 // twice from shared memory, for the sums and for dx.
 template <typename TX, typename TY, int E, int NV>
 __global__ void __launch_bounds__(512)
-norm_backward_ring_kernel(NormParams p, uint32_t gw, uint32_t groups, uint32_t stages, uint32_t mode_x, uint32_t mode_y, int *error)
+norm_backward_ring_kernel(NormParams p, uint32_t gw, uint32_t groups, uint32_t stages, uint32_t mode_y, int *error)
 {
     extern __shared__ __align__(16) unsigned char ring[];
     __shared__ float slot[128 * kNormUnit];
@@ -131,8 +131,8 @@ norm_backward_ring_kernel(NormParams p, uint32_t gw, uint32_t groups, uint32_t s
     __shared__ int abort_flag, quiet;
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const uint32_t group = warp / gw, wig = warp - group * gw, gl = wig * 32 + lane;
-    const uint32_t pitch_x = norm_pitch(mode_x, p.d, sizeof(TX)), pitch_y = norm_pitch(mode_y, p.d, sizeof(TY));
-    const uint32_t x_bytes = (kNormUnit * pitch_x + 15u) & ~15u, unit_bytes = x_bytes + ((kNormUnit * pitch_y + 15u) & ~15u);
+    const uint32_t pitch_x = p.d * sizeof(TX), pitch_y = norm_pitch(mode_y, p.d, sizeof(TY));
+    const uint32_t x_bytes = kNormUnit * pitch_x, unit_bytes = x_bytes + ((kNormUnit * pitch_y + 15u) & ~15u);
     const TX *x = static_cast<const TX *>(p.x);
     const TY *dy = static_cast<const TY *>(p.dy);
     TX *dx = static_cast<TX *>(p.dx);
@@ -154,7 +154,7 @@ norm_backward_ring_kernel(NormParams p, uint32_t gw, uint32_t groups, uint32_t s
         uint64_t *bar = &full[group][stage];
         const char *xb = reinterpret_cast<const char *>(x), *yb = reinterpret_cast<const char *>(dy);
         auto both = [&](bool now) {
-            return norm_copy(mode_x, dst, xb, p.ldx * sizeof(TX), p.d * sizeof(TX), pitch_x, r, n, bar, now) +
+            return norm_copy(kCopyRows, dst, xb, p.ldx * sizeof(TX), p.d * sizeof(TX), pitch_x, r, n, bar, now) +
                    norm_copy(mode_y, dst + x_bytes, yb, p.ldy * sizeof(TY), p.d * sizeof(TY), pitch_y, r, n, bar, now);
         };
         mbar_expect(bar, both(false));
@@ -184,9 +184,8 @@ norm_backward_ring_kernel(NormParams p, uint32_t gw, uint32_t groups, uint32_t s
             t[2 * i] = t[2 * i + 1] = 0.f;
         }
         live = mbar_wait(&full[group][stage], phase, &abort_flag) && live;     // once it has given up the rest runs through on whatever is there
-        if (n < kNormUnit && (mode_x == kCopyUnits || mode_y == kCopyUnits)) {
-            norm_copy_tail<TX>(mode_x, rows_x, x + r * p.ldx, p.d, n, gl, gw * 32);
-            norm_copy_tail<TY>(mode_y, rows_y, dy + r * p.ldy, p.d, n, gl, gw * 32);
+        if (n < kNormUnit && mode_y == kCopyUnits) {
+            norm_copy_tail<TY>(rows_y, dy + r * p.ldy, p.d, n, gl, gw * 32);
             group_barrier(gw, group);
         }
 #pragma unroll
@@ -276,11 +275,11 @@ uint32_t norm_backward_blocks(uint64_t rows, uint32_t d, int sms)
 }
 
 template <typename TX, typename TY, int E, int NV>
-int launch_back_ring(const NormParams &p, const NormShape &sh, uint32_t stages, uint32_t mode_x, uint32_t mode_y, size_t smem, uint32_t blocks,
+int launch_back_ring(const NormParams &p, const NormShape &sh, uint32_t stages, uint32_t mode_y, size_t smem, uint32_t blocks,
                      int *error, cudaStream_t s)
 {
     if (!kernel_ready<norm_backward_ring_kernel<TX, TY, E, NV>>()) return -1;
-    norm_backward_ring_kernel<TX, TY, E, NV><<<blocks, sh.gw * sh.groups * 32, smem, s>>>(p, sh.gw, sh.groups, stages, mode_x, mode_y, error);
+    norm_backward_ring_kernel<TX, TY, E, NV><<<blocks, sh.gw * sh.groups * 32, smem, s>>>(p, sh.gw, sh.groups, stages, mode_y, error);
     return cudaPeekAtLastError() == cudaSuccess ? 1 : -1;
 }
 
@@ -292,23 +291,23 @@ int launch_typed(const NormParams &p, uint32_t blocks, int *error, int sms, cuda
     e = widest_access(p.d, sizeof(TY), p.ldy, p.dy, e);
     const NormShape sh = norm_shape(p.d, e);
     constexpr uint32_t kE = 16 / sizeof(TX);
-    const uint32_t mode_x = norm_copy_mode(p.x, p.ldx, p.d, sizeof(TX)), mode_y = norm_copy_mode(p.dy, p.ldy, p.d, sizeof(TY));
+    const uint32_t mode_y = norm_copy_mode(p.dy, p.ldy, p.d, sizeof(TY));
     // From 16 copyable rows per SM on the ring: registers against ring, us, with the sums over blocks: 2,368 rows of 4,096 bf16 44.0 and 37.9, 37,888
     // 329 and 197, 262,144 of 512 bf16 220 and 177; rows of 300 fp32 are even (2,368: 15.4 and 17.4; 262,144: 171 and 167).
-    if (e == kE && mode_x != kCopyNot && mode_y != kCopyNot && p.rows >= (uint64_t)sms * 16) {
+    if (e == kE && mode_y != kCopyNot && p.rows >= (uint64_t)sms * 16) {
         const uint32_t per_sm = 512u / (sh.gw * sh.groups * 32) ? 512u / (sh.gw * sh.groups * 32) : 1u;
-        const size_t unit = ((kNormUnit * norm_pitch(mode_x, p.d, sizeof(TX)) + 15u) & ~15u) + ((kNormUnit * norm_pitch(mode_y, p.d, sizeof(TY)) + 15u) & ~15u);
+        const size_t unit = kNormUnit * p.d * sizeof(TX) + ((kNormUnit * norm_pitch(mode_y, p.d, sizeof(TY)) + 15u) & ~15u);
         const size_t most = 216 * 1024 / per_sm, add = (size_t)(sh.groups - 1) * 2 * p.d * sizeof(float);
         uint32_t stages = 4;
         while (stages > 1 && unit * sh.groups * stages > most) --stages;
         const size_t smem = unit * sh.groups * stages > add ? unit * sh.groups * stages : add;       // the ring, then the block's sums
         if (smem <= most && stages > 1) {
-            if constexpr (kE == 8) return sh.nv <= 1 ? launch_back_ring<TX, TY, 8, 1>(p, sh, stages, mode_x, mode_y, smem, blocks, error, s)
-                                                      : launch_back_ring<TX, TY, 8, 2>(p, sh, stages, mode_x, mode_y, smem, blocks, error, s);
-            else return sh.nv <= 1 ? launch_back_ring<TX, TY, 4, 1>(p, sh, stages, mode_x, mode_y, smem, blocks, error, s)
-                        : sh.nv == 2 ? launch_back_ring<TX, TY, 4, 2>(p, sh, stages, mode_x, mode_y, smem, blocks, error, s)
-                        : sh.nv == 3 ? launch_back_ring<TX, TY, 4, 3>(p, sh, stages, mode_x, mode_y, smem, blocks, error, s)
-                                     : launch_back_ring<TX, TY, 4, 4>(p, sh, stages, mode_x, mode_y, smem, blocks, error, s);
+            if constexpr (kE == 8) return sh.nv <= 1 ? launch_back_ring<TX, TY, 8, 1>(p, sh, stages, mode_y, smem, blocks, error, s)
+                                                      : launch_back_ring<TX, TY, 8, 2>(p, sh, stages, mode_y, smem, blocks, error, s);
+            else return sh.nv <= 1 ? launch_back_ring<TX, TY, 4, 1>(p, sh, stages, mode_y, smem, blocks, error, s)
+                        : sh.nv == 2 ? launch_back_ring<TX, TY, 4, 2>(p, sh, stages, mode_y, smem, blocks, error, s)
+                        : sh.nv == 3 ? launch_back_ring<TX, TY, 4, 3>(p, sh, stages, mode_y, smem, blocks, error, s)
+                                     : launch_back_ring<TX, TY, 4, 4>(p, sh, stages, mode_y, smem, blocks, error, s);
         }
     }
     const uint32_t threads = sh.gw * sh.groups * 32, smem = (sh.groups - 1) * 2 * p.d * sizeof(float);
