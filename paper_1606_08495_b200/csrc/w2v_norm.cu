@@ -204,20 +204,22 @@ int launch_norm_typed(const NormParams &p, int *error, int sms, cudaStream_t s)
     e = widest_access(p.d, sizeof(TY), p.ldy, p.y, e);
     const NormShape sh = norm_shape(p.d, e);
     constexpr uint32_t kE = 16 / sizeof(TX);
-    // Rows enough to keep a ring going, and ones that can be copied.  Registers against ring, us: 592 rows of 4,096 bf16 11.3 and 9.2,
-    // 592 of 768 8.2 and 9.2, 2,368 (16 per SM) of 768 11.1 and 9.2, 9,472 of 300 fp32 13.3 and 12.3; 262,144 of 300
-    // 135 and 115, 37,888 of 4,096 237 and 121.
-    if (e == kE && p.rows >= (uint64_t)sms * 16) {
+    // Registers against ring, us, at KB of x per SM, by type and by accesses per lane and row (nv):
+    //   16-bit, 1:     rows of 256: 64 KB 6.7 and 7.6, 256 KB 21.6 and 21.2, 886 KB 73 and 66; of 128: 128 KB 20.7 and 21.3, 443 KB 68 and 66
+    //   16-bit, more:  rows of 320: 10 KB 2.6 and 3.8, 20 KB 5.0 and 4.4; of 4,096: 16 KB 3.4 and 3.6, 32 KB 6.0 and 4.4, 512 KB 60 and 32
+    //   fp32, 1 and 2: rows of 128: 886 KB 56 and 61; of 256: 512 KB 27.3 and 27.4, 1,771 KB 89 and 98
+    //   fp32, 3:       rows of 300: 19 KB 2.9 and 4.1, 75 KB 6.5 and 6.4, 150 KB 9.9 and 9.3, 2,076 KB 113 and 78; of 768: 48 KB 5.5 and 4.7
+    //   fp32, 4:       rows of 400: 200 KB 10.7 and 11.1, 400 KB 20.0 and 18.4, 2,768 KB 126 and 100
+    const uint64_t from_kb = kE == 8 ? (sh.nv <= 1 ? 400 : 20) : sh.nv <= 2 ? kNever : sh.nv == 3 ? 48 : 300;
+    if (e == kE && ring_pays(p.rows, p.d, sizeof(TX), sms, from_kb)) {
         const size_t unit = kNormUnit * p.d * sizeof(TX), most = 104 * 1024 / (512u / (sh.gw * sh.groups * 32) ? 512u / (sh.gw * sh.groups * 32) : 1u);
         uint32_t stages = 4;
         while (stages > 1 && unit * sh.groups * stages > most) --stages;
         const size_t smem = unit * sh.groups * stages;
         if (smem <= most && stages > 1) {
             if constexpr (kE == 8) return sh.nv <= 1 ? launch_norm_ring<TX, TY, 8, 1>(p, sh, stages, smem, error, sms, s) : launch_norm_ring<TX, TY, 8, 2>(p, sh, stages, smem, error, sms, s);
-            else return sh.nv <= 1 ? launch_norm_ring<TX, TY, 4, 1>(p, sh, stages, smem, error, sms, s)
-                        : sh.nv == 2 ? launch_norm_ring<TX, TY, 4, 2>(p, sh, stages, smem, error, sms, s)
-                        : sh.nv == 3 ? launch_norm_ring<TX, TY, 4, 3>(p, sh, stages, smem, error, sms, s)
-                                     : launch_norm_ring<TX, TY, 4, 4>(p, sh, stages, smem, error, sms, s);
+            else return sh.nv == 3 ? launch_norm_ring<TX, TY, 4, 3>(p, sh, stages, smem, error, sms, s)
+                                   : launch_norm_ring<TX, TY, 4, 4>(p, sh, stages, smem, error, sms, s);
         }
     }
     const uint32_t threads = sh.gw * sh.groups * 32;

@@ -130,6 +130,13 @@ __device__ __forceinline__ void group_barrier(uint32_t gw, uint32_t group)
     else asm volatile("bar.sync %0, %1;" ::"r"(group + 1u), "r"(gw * 32u) : "memory");
 }
 
+// A ring pays from this many KB of x per SM on; less, and the registers' next row is enough and the ring's start is not.
+constexpr uint64_t kNever = ~0ull;
+inline bool ring_pays(uint64_t rows, uint32_t d, uint32_t size, int sms, uint64_t from_kb)
+{
+    return from_kb != kNever && rows * d * size >= from_kb * 1024 * (uint64_t)sms;
+}
+
 struct NormShape {
     uint32_t gw;        // warps per row
     uint32_t groups;    // rows per block

@@ -292,9 +292,15 @@ int launch_typed(const NormParams &p, uint32_t blocks, int *error, int sms, cuda
     const NormShape sh = norm_shape(p.d, e);
     constexpr uint32_t kE = 16 / sizeof(TX);
     const uint32_t mode_y = norm_copy_mode(p.dy, p.ldy, p.d, sizeof(TY));
-    // From 16 copyable rows per SM on the ring: registers against ring, us, with the sums over blocks: 2,368 rows of 4,096 bf16 44.0 and 37.9, 37,888
-    // 329 and 197, 262,144 of 512 bf16 220 and 177; rows of 300 fp32 are even (2,368: 15.4 and 17.4; 262,144: 171 and 167).
-    if (e == kE && mode_y != kCopyNot && p.rows >= (uint64_t)sms * 16) {
+    // Registers against ring, us with the sums over blocks, at KB of x per SM, by type and by accesses per lane and row (nv):
+    //   16-bit:        rows of 64: 8 KB 10.5 and 10.5, 16 KB 15.9 and 14.2; of 256: 16 KB 10.0 and 10.3, 64 KB 17.4 and 16.5;
+    //                  of 4,096: 8 KB 12.2 and 12.5, 16 KB 19.2 and 17.5, 512 KB 89 and 62
+    //   fp32, 1:       rows of 64: 443 KB 99 and 107; of 128: 886 KB 100 and 113
+    //   fp32, 2 and 3: rows of 200: 400 KB 44.1 and 43.6, 1,384 KB 132 and 127; of 300: 300 KB 30.9 and 32.6, 600 KB 53.9 and 53.5,
+    //                  2,076 KB 163 and 153; of 320: 640 KB 31.5 and 34.0, 2,214 KB 167 and 163; of 768: 192 KB 18.7 and 20.2, 768 KB 61 and 54
+    //   fp32, 4:       rows of 400: 25 KB 12.3 and 12.5, 50 KB 14.2 and 13.4; of 512: 32 KB 12.5 and 12.7, 256 KB 29.8 and 27.1
+    const uint64_t from_kb = kE == 8 ? 16 : sh.nv <= 1 ? kNever : sh.nv <= 3 ? 700 : 48;
+    if (e == kE && mode_y != kCopyNot && ring_pays(p.rows, p.d, sizeof(TX), sms, from_kb)) {
         const uint32_t per_sm = 512u / (sh.gw * sh.groups * 32) ? 512u / (sh.gw * sh.groups * 32) : 1u;
         const size_t unit = kNormUnit * p.d * sizeof(TX) + ((kNormUnit * norm_pitch(mode_y, p.d, sizeof(TY)) + 15u) & ~15u);
         const size_t most = 216 * 1024 / per_sm, add = (size_t)(sh.groups - 1) * 2 * p.d * sizeof(float);
@@ -304,8 +310,7 @@ int launch_typed(const NormParams &p, uint32_t blocks, int *error, int sms, cuda
         if (smem <= most && stages > 1) {
             if constexpr (kE == 8) return sh.nv <= 1 ? launch_back_ring<TX, TY, 8, 1>(p, sh, stages, mode_y, smem, blocks, error, s)
                                                       : launch_back_ring<TX, TY, 8, 2>(p, sh, stages, mode_y, smem, blocks, error, s);
-            else return sh.nv <= 1 ? launch_back_ring<TX, TY, 4, 1>(p, sh, stages, mode_y, smem, blocks, error, s)
-                        : sh.nv == 2 ? launch_back_ring<TX, TY, 4, 2>(p, sh, stages, mode_y, smem, blocks, error, s)
+            else return sh.nv == 2 ? launch_back_ring<TX, TY, 4, 2>(p, sh, stages, mode_y, smem, blocks, error, s)
                         : sh.nv == 3 ? launch_back_ring<TX, TY, 4, 3>(p, sh, stages, mode_y, smem, blocks, error, s)
                                      : launch_back_ring<TX, TY, 4, 4>(p, sh, stages, mode_y, smem, blocks, error, s);
         }

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_1606_08495_b200 import binding
-from test_gpu_reader import VOCAB, attend_by_hand, inside, randn, stream
+from test_gpu_reader import VOCAB, attend_by_hand, check_layer_norm, inside, randn, stream
 
 pytestmark = pytest.mark.gpu
 
@@ -500,3 +500,20 @@ def test_attend_backward_of_a_padded_stream(model):
                 times[sinks, pad] = min(times.get((sinks, pad), 1e9), begin.elapsed_time(end))
             assert all((g[words:] == 0).all() for g in grads[:3])
     assert max(times.values()) < 10 * min(times.values())            # sinks cost a small part; looking for them from every tile on cost 170 times the rest
+
+
+# ---- layer norm: rows enough for the kernels with a ring ------------------------------------------------------------------------
+@pytest.mark.parametrize("rows,d,pad,xt,yt", [
+    (7001, 300, 20, torch.float32, torch.bfloat16),       # 3 accesses a lane, forwards
+    (30_001, 400, 0, torch.float32, torch.float32),       # 4 accesses a lane, both ways
+    (155_001, 256, 0, torch.bfloat16, torch.bfloat16),    # 1 access a lane, both ways
+    (19_001, 64, 8, torch.float16, torch.float16),        # backwards
+    (11_001, 320, 0, torch.bfloat16, torch.bfloat16),
+    (140_001, 200, 0, torch.float32, torch.bfloat16),     # backwards
+    (90_001, 300, 20, torch.float32, torch.float16),      # dy in rows of 600 bytes without gaps, an odd number of them
+    (5001, 404, 0, torch.float32, torch.bfloat16),        # dy in rows of 808 bytes
+    (299, 8192, 8, torch.bfloat16, torch.bfloat16),
+])
+def test_layer_norm_of_rows_for_the_ring(model, rows, d, pad, xt, yt):
+    wide = randn(rows, d + pad, seed=d + pad, dtype=xt, by=0.7) + torch.tensor(0.25, dtype=xt, device="cuda")
+    check_layer_norm(model, wide[:, :d], xt, yt)
