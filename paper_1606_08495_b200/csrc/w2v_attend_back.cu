@@ -35,9 +35,10 @@ namespace w2v {
 template <int NB, bool SMALL>
 struct BackShape {
     static constexpr int kTile = SMALL ? 256 : 128;                  // softmax threads that share a tile
-    static constexpr int kChunk = SMALL ? 16 : 32;                   // columns a thread takes at once
     static constexpr int kBuf = SMALL && NB == 2 ? 1 : 2;            // score buffers
-    static constexpr int kRows = SMALL || NB == 2 ? 32 : 64;         // streamed rows per tile
+    static constexpr int kRows = 32;                                 // streamed rows per tile
+    static constexpr int kChunk = SMALL ? kRows / 2 : kRows;         // columns of a tile that a thread takes
+    static_assert(SMALL || NB == 2, "heads of up to 64 are SMALL");
     static constexpr int kStages = SMALL && NB == 2 ? 2 : 4;
     static constexpr uint32_t kWide = !SMALL ? NB * 64 : NB == 1 ? 64 : 96;              // columns of a gradient
     static constexpr uint32_t kA0 = 0, kA1 = NB * 32, kG0 = SMALL ? 0 : NB * 64, kG1 = kG0 + kWide;      // tensor-memory columns
@@ -58,7 +59,7 @@ struct BackShared {
     uint32_t tmem;
     int abort_flag, quiet;
     int32_t limits[4][3];
-    uint32_t vis[Sh::kStages][2];                    // which streamed rows of the stage are words
+    uint32_t vis[Sh::kStages];                       // which streamed rows of the stage are words
     int32_t run_lo[Sh::kStages];                     // role 1: where the run of the stage's query tile begins
     __align__(16) float lse[Sh::kStages][Sh::kRows], delta[Sh::kStages][Sh::kRows], extra[Sh::kStages][Sh::kRows];       // role 1: of the stage's queries, negated
     int far[Sh::kStages];                            // role 1: there are far rows among them
@@ -259,7 +260,6 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
 {
     using Sh = BackShape<NB, SMALL>;
     constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
-    constexpr int kChunks = SMALL ? 1 : Sh::kRows / Sh::kChunk;      // of a thread per tile
     extern __shared__ unsigned char smem_raw[];
     __shared__ BackShared<Sh> sh;
     unsigned char *smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
@@ -454,140 +454,135 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
                 const int32_t rel1 = ROLE == 0 ? at0 + Sh::kRows - 1 - w0 : w0 + 31 - at0;
                 const bool far_left = rel1 <= -last, far = p.b.n == 0 || far_left || rel0 >= last;
                 const float flat = p.b.n ? lut[far_left ? 0 : entries - 1] : 0.f;
-                float acc_p = 0.f, acc_n = 0.f;
                 const bool reach = ROLE == 1 && p.sinks && sh.run_lo[stage] <= own;
+                constexpr int kC = Sh::kChunk;
+                constexpr uint32_t kAll = kC == 32 ? 0xFFFFFFFFu : (1u << kC) - 1u;
+                const int32_t c0 = SMALL ? (int32_t)wg * kC : 0;     // first column
+                if (c0 < cols) {
+                    uint32_t sv[kC], dv[kC];
+                    tmem_ld(cs + c0, sv);
+                    tmem_ld(cd + c0, dv);
+                    const int32_t at = at0 + c0;
+                    uint32_t m;
+                    if (ROLE == 0) m = range_bits(row.lo, row.hi, at) | range_bits(row.s, row.se, at);
+                    else {
+                        m = range_bits(q_lo, q_hi, at);
+                        if (reach) m |= range_bits(far_lo, far_hi, at);
+                    }
+                    m &= sh.vis[stage] >> c0;
+                    tmem_wait_ld(sv);
+                    tmem_held(dv);
+                    // a row or column that sees nothing has lse +infinity
+                    float x[kC];
+                    if (far) {
+                        const float2 scale2 = make_float2(scale, scale), flat2 = make_float2(flat, flat);
 #pragma unroll
-                for (int c = 0; c < kChunks; ++c) {
-                    constexpr int kC = Sh::kChunk;
-                    constexpr uint32_t kAll = kC == 32 ? 0xFFFFFFFFu : (1u << kC) - 1u;
-                    const int32_t c0 = SMALL ? (int32_t)wg * kC : c * kC;    // first column
-                    if (c0 < cols) {
-                        uint32_t sv[kC], dv[kC];
-                        tmem_ld(cs + c0, sv);
-                        tmem_ld(cd + c0, dv);
-                        const int32_t at = at0 + c0;
-                        uint32_t m;
-                        if (ROLE == 0) m = range_bits(row.lo, row.hi, at) | range_bits(row.s, row.se, at);
-                        else {
-                            m = range_bits(q_lo, q_hi, at);
-                            if (reach) m |= range_bits(far_lo, far_hi, at);
+                        for (int e = 0; e < kC; e += 2) {
+                            const float2 y = fma2(pair_of(sv[e], sv[e + 1]), scale2, flat2);
+                            x[e] = y.x;
+                            x[e + 1] = y.y;
                         }
-                        m &= SMALL ? sh.vis[stage][0] >> c0 : sh.vis[stage][c];
-                        tmem_wait_ld(sv);
-                        tmem_held(dv);
-                        // a row or column that sees nothing has lse +infinity
-                        float x[kC];
-                        if (far) {
-                            const float2 scale2 = make_float2(scale, scale), flat2 = make_float2(flat, flat);
+                    } else {
+                        // key - query grows with the column in role 0 and falls with it in role 1
+                        const float *near = ROLE == 0 ? lut + (at - (int32_t)own + off) : lut + ((int32_t)own - at + off);
 #pragma unroll
-                            for (int e = 0; e < kC; e += 2) {
-                                const float2 y = fma2(pair_of(sv[e], sv[e + 1]), scale2, flat2);
-                                x[e] = y.x;
-                                x[e + 1] = y.y;
+                        for (int e = 0; e < kC; ++e) x[e] = fmaf(__uint_as_float(sv[e]), scale, ROLE == 0 ? near[e] : near[-e]);
+                    }
+                    const bool masked = !__all_sync(kFullMask, (m | ~kAll) == 0xFFFFFFFFu);
+                    uint32_t ws[kC / 2], wp[kC / 2];
+                    // masked pairs are taken out of the weights and of dS, not of the scores: a delta, lse or product
+                    // of such a pair may not be finite
+                    auto take_out = [&](float *w, float *d) {
+                        if (masked)
+#pragma unroll
+                            for (int e = 0; e < kC; ++e) {
+                                w[e] = m & (1u << e) ? w[e] : 0.f;
+                                d[e] = m & (1u << e) ? d[e] : 0.f;
                             }
-                        } else {
-                            // key - query grows with the column in role 0 and falls with it in role 1
-                            const float *near = ROLE == 0 ? lut + (at - (int32_t)own + off) : lut + ((int32_t)own - at + off);
+                    };
+                    float ds[kC];
+                    if (ROLE == 0) {
+                        const float2 lse2 = make_float2(-lse, -lse), delta2 = make_float2(-delta, -delta);
 #pragma unroll
-                            for (int e = 0; e < kC; ++e) x[e] = fmaf(__uint_as_float(sv[e]), scale, ROLE == 0 ? near[e] : near[-e]);
+                        for (int e = 0; e < kC; e += 2) {
+                            float2 w = add2(make_float2(x[e], x[e + 1]), lse2);
+                            w.x = fast_exp2(w.x);
+                            w.y = fast_exp2(w.y);
+                            const float2 d = mul2(w, add2(pair_of(dv[e], dv[e + 1]), delta2));
+                            x[e] = w.x; x[e + 1] = w.y;
+                            ds[e] = d.x; ds[e + 1] = d.y;
                         }
-                        const bool masked = !__all_sync(kFullMask, (m | ~kAll) == 0xFFFFFFFFu);
-                        uint32_t ws[kC / 2], wp[kC / 2];
-                        // masked pairs are taken out of the weights and of dS, not of the scores: a delta, lse or product
-                        // of such a pair may not be finite
-                        auto take_out = [&](float *w, float *d) {
-                            if (masked)
+                        take_out(x, ds);
+#pragma unroll
+                        for (int e = 0; e < kC; e += 2) {
+                            eps2 = add2(eps2, make_float2(ds[e], ds[e + 1]));
+                            wp[e / 2] = pack2<T>(x[e], x[e + 1]);
+                            ws[e / 2] = pack2<T>(ds[e], ds[e + 1]);
+                        }
+                        tmem_st(cs + (SMALL ? c0 : c0 / 2), wp);
+                        tmem_st(cd + (SMALL ? c0 : c0 / 2), ws);
+                        if (far_rows) {
+#pragma unroll
+                            for (int e = 0; e < kC; ++e) weights += x[e];
+                        }
+                        if (k >= run) {                          // sinks: kept in fp32 for their own sums
+#pragma unroll
+                            for (int e = 0; e < kC; ++e) {
+                                const int32_t i = (k - run) * Sh::kRows + c0 + e;
+                                if (i < sinks) {
+                                    sink_p[i * 128 + (int32_t)r] = x[e];
+                                    sink_d[i * 128 + (int32_t)r] = ds[e];
+                                }
+                            }
+                        }
+                    } else {
+                        const float *less = sh.lse[stage];       // negated, as delta and extra
+                        if (sh.far[stage]) {
+#pragma unroll
+                            for (int e = 0; e < kC; ++e) x[e] += less[c0 + e];
+                            less = sh.extra[stage];
+                        }
+#pragma unroll
+                        for (int e = 0; e < kC; e += 4) {
+                            const float4 l4 = *reinterpret_cast<const float4 *>(less + c0 + e);
+                            const float4 d4 = *reinterpret_cast<const float4 *>(&sh.delta[stage][c0 + e]);
+                            float2 p0 = add2(make_float2(x[e], x[e + 1]), make_float2(l4.x, l4.y));
+                            float2 p1 = add2(make_float2(x[e + 2], x[e + 3]), make_float2(l4.z, l4.w));
+                            p0.x = fast_exp2(p0.x); p0.y = fast_exp2(p0.y); p1.x = fast_exp2(p1.x); p1.y = fast_exp2(p1.y);
+                            x[e] = p0.x; x[e + 1] = p0.y; x[e + 2] = p1.x; x[e + 3] = p1.y;
+                            p0 = mul2(p0, add2(pair_of(dv[e], dv[e + 1]), make_float2(d4.x, d4.y)));
+                            p1 = mul2(p1, add2(pair_of(dv[e + 2], dv[e + 3]), make_float2(d4.z, d4.w)));
+                            ds[e] = p0.x; ds[e + 1] = p0.y; ds[e + 2] = p1.x; ds[e + 3] = p1.y;
+                        }
+                        take_out(x, ds);
+#pragma unroll
+                        for (int e = 0; e < kC; e += 2) {
+                            wp[e / 2] = pack2<T>(x[e], x[e + 1]);
+                            ws[e / 2] = pack2<T>(ds[e], ds[e + 1]);
+                        }
+                        tmem_st(cs + (SMALL ? c0 : c0 / 2), wp);
+                        tmem_st(cd + (SMALL ? c0 : c0 / 2), ws);
+                        if (p.dbias) {
+                            if (far) {
+                                float a[4] = {ds[0], ds[1], ds[2], ds[3]};
+#pragma unroll
+                                for (int e = 4; e < kC; ++e) a[e & 3] += ds[e];
+                                if (far_left) far_l += (a[0] + a[1]) + (a[2] + a[3]); else far_r += (a[0] + a[1]) + (a[2] + a[3]);
+                            } else {
+                                // over 32 columns lane l gathers the diagonal key - query = base + l (acc_p) and the one 32 below (acc_n)
+                                const int32_t base = w0 - at0;
+                                float acc_p = 0.f, acc_n = 0.f;
 #pragma unroll
                                 for (int e = 0; e < kC; ++e) {
-                                    w[e] = m & (1u << e) ? w[e] : 0.f;
-                                    d[e] = m & (1u << e) ? d[e] : 0.f;
+                                    const uint32_t from = lane + (uint32_t)c0 + e;
+                                    const float y = __shfl_sync(kFullMask, ds[e], from & 31u);
+                                    if (from < 32u) acc_p += y; else acc_n += y;
                                 }
-                        };
-                        float ds[kC];
-                        if (ROLE == 0) {
-                            const float2 lse2 = make_float2(-lse, -lse), delta2 = make_float2(-delta, -delta);
-#pragma unroll
-                            for (int e = 0; e < kC; e += 2) {
-                                float2 w = add2(make_float2(x[e], x[e + 1]), lse2);
-                                w.x = fast_exp2(w.x);
-                                w.y = fast_exp2(w.y);
-                                const float2 d = mul2(w, add2(pair_of(dv[e], dv[e + 1]), delta2));
-                                x[e] = w.x; x[e + 1] = w.y;
-                                ds[e] = d.x; ds[e + 1] = d.y;
-                            }
-                            take_out(x, ds);
-#pragma unroll
-                            for (int e = 0; e < kC; e += 2) {
-                                eps2 = add2(eps2, make_float2(ds[e], ds[e + 1]));
-                                wp[e / 2] = pack2<T>(x[e], x[e + 1]);
-                                ws[e / 2] = pack2<T>(ds[e], ds[e + 1]);
-                            }
-                            tmem_st(cs + (SMALL ? c0 : c0 / 2), wp);
-                            tmem_st(cd + (SMALL ? c0 : c0 / 2), ws);
-                            if (far_rows) {
-#pragma unroll
-                                for (int e = 0; e < kC; ++e) weights += x[e];
-                            }
-                            if (k >= run) {                          // sinks: kept in fp32 for their own sums
-#pragma unroll
-                                for (int e = 0; e < kC; ++e) {
-                                    const int32_t i = (k - run) * Sh::kRows + c0 + e;
-                                    if (i < sinks) {
-                                        sink_p[i * 128 + (int32_t)r] = x[e];
-                                        sink_d[i * 128 + (int32_t)r] = ds[e];
-                                    }
-                                }
-                            }
-                        } else {
-                            const float *less = sh.lse[stage];       // negated, as delta and extra
-                            if (sh.far[stage]) {
-#pragma unroll
-                                for (int e = 0; e < kC; ++e) x[e] += less[c0 + e];
-                                less = sh.extra[stage];
-                            }
-#pragma unroll
-                            for (int e = 0; e < kC; e += 4) {
-                                const float4 l4 = *reinterpret_cast<const float4 *>(less + c0 + e);
-                                const float4 d4 = *reinterpret_cast<const float4 *>(&sh.delta[stage][c0 + e]);
-                                float2 p0 = add2(make_float2(x[e], x[e + 1]), make_float2(l4.x, l4.y));
-                                float2 p1 = add2(make_float2(x[e + 2], x[e + 3]), make_float2(l4.z, l4.w));
-                                p0.x = fast_exp2(p0.x); p0.y = fast_exp2(p0.y); p1.x = fast_exp2(p1.x); p1.y = fast_exp2(p1.y);
-                                x[e] = p0.x; x[e + 1] = p0.y; x[e + 2] = p1.x; x[e + 3] = p1.y;
-                                p0 = mul2(p0, add2(pair_of(dv[e], dv[e + 1]), make_float2(d4.x, d4.y)));
-                                p1 = mul2(p1, add2(pair_of(dv[e + 2], dv[e + 3]), make_float2(d4.z, d4.w)));
-                                ds[e] = p0.x; ds[e + 1] = p0.y; ds[e + 2] = p1.x; ds[e + 3] = p1.y;
-                            }
-                            take_out(x, ds);
-#pragma unroll
-                            for (int e = 0; e < kC; e += 2) {
-                                wp[e / 2] = pack2<T>(x[e], x[e + 1]);
-                                ws[e / 2] = pack2<T>(ds[e], ds[e + 1]);
-                            }
-                            tmem_st(cs + (SMALL ? c0 : c0 / 2), wp);
-                            tmem_st(cd + (SMALL ? c0 : c0 / 2), ws);
-                            if (p.dbias) {
-                                if (far) {
-                                    float a[4] = {ds[0], ds[1], ds[2], ds[3]};
-#pragma unroll
-                                    for (int e = 4; e < kC; ++e) a[e & 3] += ds[e];
-                                    if (far_left) far_l += (a[0] + a[1]) + (a[2] + a[3]); else far_r += (a[0] + a[1]) + (a[2] + a[3]);
-                                } else {
-                                    // over 32 columns lane l gathers the diagonal key - query = base + l (acc_p) and the one 32 below (acc_n)
-                                    const int32_t base = w0 - (SMALL ? at0 : at);
-#pragma unroll
-                                    for (int e = 0; e < kC; ++e) {
-                                        const uint32_t from = lane + (SMALL ? (uint32_t)c0 : 0u) + e;
-                                        const float y = __shfl_sync(kFullMask, ds[e], from & 31u);
-                                        if (from < 32u) acc_p += y; else acc_n += y;
-                                    }
-                                    float *mine = rel_sums + warp * entries + base + off + (int32_t)lane;
-                                    mine[0] += acc_p;
-                                    __syncwarp();
-                                    if (c + 1 == kChunks) mine[-32] += acc_n;
-                                    __syncwarp();
-                                    acc_p = acc_n;
-                                    acc_n = 0.f;
-                                }
+                                float *mine = rel_sums + warp * entries + base + off + (int32_t)lane;
+                                mine[0] += acc_p;
+                                __syncwarp();
+                                mine[-32] += acc_n;
+                                __syncwarp();
                             }
                         }
                     }
@@ -828,31 +823,22 @@ attend_back_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
             const int32_t k = t % per_head, at = tile_at(k), rows = tile_rows(k);
             uint32_t vis[2];
             word_bits(p, at, (uint32_t)rows, lane, vis);
-            float lse[2], delta[2], extra[2];
+            float lse = 0.f, delta = 0.f, extra = 0.f;
             int32_t run_lo = 0;
             if (ROLE == 1) {
-#pragma unroll
-                for (int w = 0; w < Sh::kRows / 32; ++w) {
-                    const int64_t i = (int64_t)at + w * 32 + lane;
-                    lse[w] = i < p.n ? __ldg(p.lse + (int64_t)h * p.n + i) : INFINITY;
-                    delta[w] = i < p.n ? p.delta[(int64_t)h * p.n + i] : 0.f;
-                    extra[w] = i < p.n ? p.extra[(int64_t)h * p.n + i] : 0.f;
-                }
+                const int64_t i = (int64_t)at + lane;
+                lse = i < p.n ? __ldg(p.lse + (int64_t)h * p.n + i) : INFINITY;
+                delta = i < p.n ? p.delta[(int64_t)h * p.n + i] : 0.f;
+                extra = i < p.n ? p.extra[(int64_t)h * p.n + i] : 0.f;
                 if (p.sinks) run_lo = run_begin(p, at / kAttendTile * kAttendTile, lane);
             }
             if (!__all_sync(kFullMask, mbar_nap(&sh.landed[stage], (t / Sh::kStages) & 1, abort_flag))) break;
-            if (lane < 2) sh.vis[stage][lane] = lane ? vis[1] : vis[0];
+            if (lane == 0) sh.vis[stage] = vis[0];
             if (ROLE == 1) {
-#pragma unroll
-                for (int w = 0; w < Sh::kRows / 32; ++w) {
-                    sh.lse[stage][w * 32 + lane] = -lse[w];
-                    sh.delta[stage][w * 32 + lane] = -delta[w];
-                    sh.extra[stage][w * 32 + lane] = -extra[w];
-                }
-                bool far = false;
-#pragma unroll
-                for (int w = 0; w < Sh::kRows / 32; ++w) far = far || extra[w] != 0.f;
-                far = __any_sync(kFullMask, far);
+                sh.lse[stage][lane] = -lse;
+                sh.delta[stage][lane] = -delta;
+                sh.extra[stage][lane] = -extra;
+                const bool far = __any_sync(kFullMask, extra != 0.f);
                 if (lane == 0) { sh.run_lo[stage] = run_lo; sh.far[stage] = far; }
             }
             const uint32_t x = ring + stage * Sh::kStage, cols = (uint32_t)(rows + 15) & ~15u;
