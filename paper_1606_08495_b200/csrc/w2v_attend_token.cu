@@ -16,12 +16,14 @@
 //   output:  lane (g, t) holds chunk g of keys 2t, 2t + 1, 2t + 8, 2t + 9; a byte permutation pairs the keys, and
 //            column g of product e is dimension 8 g + e.
 // The softmax weights enter the second product as the sum of two numbers of the cache's type, so that what is lost is
-// 2^-18 and not 2^-9 of them.  Each warp copies its next step's keys and values to shared memory in the background, so
+// 2^-18 and not 2^-9 of them; fp16 weights are 2^15 times as large, so that one below 2^-25 of the largest is not zero beside
+// the sum, in which it counts.  Each warp copies its next step's keys and values to shared memory in the background, so
 // that what is under way does not have to fit in registers.  There chunk c of row r lies at c ^ turn(r), which keeps
 // both ways of reading free of bank conflicts.  96 sequences, 16 heads of 128 over 4 of keys and values, windows of 4,096: 150 us,
 // 4.8 TB/s = 0.75 of measured copy; with direct loads 236 us, with copies but an address per access 191 us.  A single sequence of
 // 5 heads of 64 and windows of 1,001 takes 6 us.
 #include <cooperative_groups.h>
+#include <type_traits>
 
 #include "w2v_attend.cuh"
 #include "w2v_kernel_ready.h"
@@ -74,6 +76,7 @@ attend_token_kernel(TokenParams p, uint32_t splits, uint32_t passes)
     const uint32_t split = blockIdx.x % splits, item = blockIdx.x / splits;
     const uint32_t pass = item % passes, kvh = (item / passes) % p.kv_heads, b = item / (passes * p.kv_heads);
     const uint32_t h0 = kvh * group + pass * kTokRows, nh = min((uint32_t)kTokRows, group - pass * kTokRows);
+    constexpr float kLift = std::is_same<T, __half>::value ? 15.f : 0.f;               // of the weights, base 2
     constexpr uint32_t kKeep = 8 * kR;                                  // rows of a block's results
     float *bias_s = sm;                                                 // [rows][reach + 1] bias by distance
     // what is joined lies where the stages were
@@ -207,7 +210,7 @@ attend_token_kernel(TokenParams p, uint32_t splits, uint32_t passes)
                     mx[r] = top;
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) { s[i] = fast_exp2(s[i] - from); sum[r] += s[i]; }
+                for (int i = 0; i < 4; ++i) { s[i] = fast_exp2(s[i] - (from - kLift)); sum[r] += s[i]; }
                 split_pair<T>(s[0], s[1], head[0][r], tail[0][r]);
                 split_pair<T>(s[2], s[3], head[1][r], tail[1][r]);
             }

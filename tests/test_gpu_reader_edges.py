@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_1606_08495_b200 import binding
-from test_gpu_reader import VOCAB, attend_by_hand, check_layer_norm, inside, randn, stream
+from test_gpu_reader import F32, U, VOCAB, attend_by_hand, check_layer_norm, inside, randn, stream
 
 pytestmark = pytest.mark.gpu
 
@@ -517,3 +517,22 @@ def test_attend_backward_of_a_padded_stream(model):
 def test_layer_norm_of_rows_for_the_ring(model, rows, d, pad, xt, yt):
     wide = randn(rows, d + pad, seed=d + pad, dtype=xt, by=0.7) + torch.tensor(0.25, dtype=xt, device="cuda")
     check_layer_norm(model, wide[:, :d], xt, yt)
+
+
+# ---- single tokens over long windows ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("score", [-12.5, -17.6875, -19.0])
+def test_attend_token_many_small_weights(model, dtype, score):
+    """One key ahead of 200,000 that are alike: together they matter, each of them is less than the smallest float16."""
+    left, dim = 200_000, 64
+    ck = torch.zeros(1, left + 1, 1, dim, dtype=dtype, device="cuda")
+    cv = torch.ones_like(ck)
+    ck[..., 0] = score
+    ck[:, 0], cv[:, 0] = 0, 0                                        # the first key seen, with score 0 and value 0
+    q, k, v = torch.zeros(1, 1, dim, dtype=dtype, device="cuda"), ck[:, 1].clone(), cv[:, 1].clone()
+    q[..., 0] = 8.0                                                  # dim ** -0.5 * 8 = 1
+    pos = torch.full((1,), left, dtype=torch.int32, device="cuda")
+    o = model.attend_token(q, k, v, ck, cv, pos, left=left)
+    w = left * torch.tensor(float(torch.tensor(score, dtype=dtype)), dtype=torch.float64, device="cuda").exp()
+    want = (w / (1 + w)).expand_as(o)
+    inside(o, want, U[dtype] * want + F32 * want + 1e-6, "o")
