@@ -614,7 +614,12 @@ class W2V:
     def sentence_spans(self, tokens):
         """[n, 2] int32: sentence bounds of every position of a token stream (-1 ends a sentence)."""
         self._on(tokens)
-        t = tokens if tokens.dtype is torch.int32 and tokens.is_contiguous() else tokens.to(torch.int32).contiguous()
+        if tokens.dtype is torch.int32:
+            t = tokens.contiguous()
+        elif tokens.dtype.is_floating_point or tokens.dtype.is_complex:
+            raise TypeError(f"tokens must be whole numbers, not {tokens.dtype}")
+        else:                                                        # an id beyond 32 bits stays one that no vocabulary has
+            t = tokens.long().clamp(-2, 2 ** 31 - 1).to(torch.int32).contiguous()
         n = t.numel()
         spans = t.new_empty((n, 2))
         apart = self.join_streams()

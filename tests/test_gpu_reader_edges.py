@@ -536,3 +536,13 @@ def test_attend_token_many_small_weights(model, dtype, score):
     w = left * torch.tensor(float(torch.tensor(score, dtype=dtype)), dtype=torch.float64, device="cuda").exp()
     want = (w / (1 + w)).expand_as(o)
     inside(o, want, U[dtype] * want + F32 * want + 1e-6, "o")
+
+
+def test_sentence_spans_of_wide_ids(model):
+    """Ids beyond 32 bits are words that the vocabulary does not have, not what is left of them modulo 2^32."""
+    toks = torch.tensor([3, 2 ** 32 + 5, 4, 2 ** 32 - 1, -2 ** 32 - 1, 2 ** 40, -1, 7, -2 ** 63, 2 ** 63 - 1], device="cuda")
+    want = torch.tensor([[0, 6], [1, 1], [0, 6], [3, 3], [4, 4], [5, 5], [6, 6], [7, 10], [8, 8], [9, 9]], dtype=torch.int32, device="cuda")
+    assert torch.equal(model.sentence_spans(toks), want)
+    assert torch.equal(model.sentence_spans(toks[::3].to(torch.int16)), model.sentence_spans(torch.tensor([3, -1, -1, -1], dtype=torch.int32, device="cuda")))
+    with pytest.raises(TypeError, match="whole numbers"):
+        model.sentence_spans(toks.float())
