@@ -517,9 +517,13 @@ int32_t w2v_sample_pairs_noalloc(w2v_handle *h, const int32_t *tokens, uint64_t 
  * sentence, both with their gradients, the same attention for one new word per sequence, and the
  * product of a few vectors with a whole table held in 4 bits.  All arrays are device memory; all
  * calls are asynchronous on the handle's stream (arrays that another stream wrote need the caller's
- * event), and wait only when scratch grows on the first call of a larger size.  Sums, statistics and
- * softmaxes are held in 32 bits whatever the arrays' type; every result is the same on every call with
- * the same inputs (nothing is added up in an order that changes).
+ * event), and wait only when scratch grows on the first call of a larger size.  Outputs lie over no input
+ * but where a call says so.  Sums, statistics, softmax sums and references are held in 32 bits whatever the
+ * arrays' type, but matrix products take operands of that type: w2v_attend rounds the softmax weights to it
+ * (2^-9 or 2^-12 of each; fp16 ones below 2^-25 of the row's largest are zero), w2v_attend_backward the weights and
+ * the scores' gradients (fp16 ones below 2^-25 are zero: scale the loss), while dbias takes both in 32 bits;
+ * w2v_attend_token takes its weights as sums of two such numbers.  Every result is the same on every call with the
+ * same inputs (nothing is added up in an order that changes).
  */
 enum { W2V_TYPE_F32 = 0, W2V_TYPE_BF16 = 1, W2V_TYPE_F16 = 2 };
 
@@ -636,7 +640,8 @@ int32_t w2v_fourbit_pack(w2v_handle *h, const float *rows, uint64_t n, uint32_t 
 
 /*
  * out[v][r] = sum over the groups g of scale[r][g] * sum over the group's columns of value[r][c] x[v][c], for m <= 8
- * vectors x (fp32, x_stride >= d apart) and every row; out fp32, out_stride >= rows apart.
+ * vectors x (fp32, x_stride >= d apart) and every row; out fp32, out_stride >= rows apart.  A column of x below 2^-18 of its
+ * vector's largest is taken to 2^-40 of that largest; a vector that holds a value that is not finite gives NaN.
  */
 int32_t w2v_fourbit_scores(w2v_handle *h, const float *x, uint32_t m, uint64_t x_stride, const uint8_t *packed, const void *scales,
                            uint64_t rows, uint32_t d, uint32_t group, float *out, uint64_t out_stride);

@@ -12,7 +12,7 @@
 // What bounds it: latency.  The softmax warps wait for their tensor-memory reads and for the chain from there to the
 // weights (issue slots 35 % busy, matrix units 24 %, heads of 128), and tensor memory holds no more of them.  A prompt of 32,768 words (fp16, 8 heads of 64,
 // 2 of keys and values, windows of 4,096): 0.51 ms, 0.30 of the measured rate of matrix products; 16,381 words of long
-// documents, 16 heads of 128, windows of 1,024: 0.29 ms; 131,072 words in sessions of 5 to 40, 4 heads of 80: 0.15 ms, where
+// documents, 16 heads of 128, windows of 1,024: 0.29 ms; 131,072 words in sessions of 5 to 40, 4 heads of 80: 0.16 ms, where
 // beginnings and ends of blocks are most of the time.
 #include <type_traits>
 
@@ -30,7 +30,8 @@ constexpr float kRescale = 8.f;                  // base-2: how far a row's scor
 // NB = 64-column blocks of a head (1: head_dim <= 64, 2: up to 128).  SMALL (up to 96): half of the tensor memory, so that
 // two blocks share an SM and one's beginning and end lie under the other's middle; tiles of 32 keys where two 96-column
 // outputs leave room for no more.  Against the whole of the tensor memory and one block: those sessions 240 -> 153 us, 65,536
-// words in sentences of 1,000 (5 heads of 64, windows of 257) 201 -> 132 us, the prompt 708 -> 511 us.
+// words in sentences of 1,000 (5 heads of 64, windows of 257) 201 -> 132 us, the prompt 708 -> 511 us (with what came since 158, 132
+// and 514).
 template <int NB, bool SMALL>
 struct FwdShape {
     static constexpr int kBlocks = SMALL ? 2 : 1;                   // resident per SM: tensor memory is the limit

@@ -17,7 +17,7 @@
 //
 // P and dS are rounded to the arrays' type as A sides of the gradient products; dbias, delta and the sinks' sums take them in
 // fp32.  Bound by latency in the warpgroups (issue slots 40 %, matrix units 35 % busy): 16,381 words, 16 heads of 128 (4 of
-// keys and values), windows of 1,024: 406 us (role 0) and 409 us (role 1).
+// keys and values), windows of 1,024: 420 us (role 0) and 427 us (role 1).
 #include <type_traits>
 
 #include "w2v_attend.cuh"
@@ -30,7 +30,7 @@ namespace w2v {
 //          and one's beginning and end lie under the other's middle; the A sides stay in shared memory; the two softmax
 //          warpgroups take half of the columns of every tile.  Against the other, role 1 and role 0: 131,072
 //          words in sessions of 5 to 40, 4 heads of 80, 370 -> 284 us and 270 -> 220 us; 65,536 words in sentences of 1,000, 5
-//          heads of 64, windows of 257, 312 -> 217 us and 262 -> 201 us.
+//          heads of 64, windows of 257, 312 -> 217 us and 262 -> 201 us (with what came since 290, 229, 227 and 208).
 //   else:  all of the tensor memory; the A sides in tensor memory; the warpgroups take the tiles in turn.
 template <int NB, bool SMALL>
 struct BackShape {

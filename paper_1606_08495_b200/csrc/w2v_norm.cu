@@ -5,8 +5,9 @@
 // under way while one is worked on.
 //
 // With many rows a ring in shared memory, filled by bulk copies, has several units of two rows under way instead, and the
-// two rows' sums go through the same shuffles.  262,144 rows of 300 (fp32 in a padded table to bf16): 78 us, 6.1 TB/s = 0.94
-// of measured copy; in registers 110 us.  9,472 rows of 4,096 bf16: 37 us from event to event, 4.2 TB/s.
+// two rows' sums go through the same shuffles.  262,144 rows of 300 (fp32 in a padded table to bf16): 76 us, 6.2 TB/s = 0.96
+// of measured copy; in registers 113 us.  9,472 rows of 4,096 bf16: 32 us, 4.9 TB/s = 0.76 (two barriers of eight warps per two
+// rows); in registers 60 us.
 #include "w2v_norm.cuh"
 
 namespace w2v {

@@ -7,7 +7,7 @@
 //
 // Many rows come through a ring in shared memory, as forwards; both sums over the row are formed from there and the second
 // reading for dx costs no memory traffic.  262,144 rows of 300 (fp32, dy bf16): 149 us, 5.3 TB/s = 0.82 of measured copy; in
-// registers 158 us.
+// registers 158 us.  9,472 rows of 4,096 bf16 62 us with the sums over blocks, 3.8 TB/s = 0.58; in registers 89 us.
 #include "w2v_norm.cuh"
 
 namespace w2v {
