@@ -106,7 +106,8 @@ __device__ __forceinline__ void sink_sums(const AttendParams &p, unsigned char *
     const bool part_of = row.s == s && row.s < row.se;
     for (int32_t k = (int32_t)wg; k < sinks; k += kSoft / 128) {
         const int32_t at = k * 128 + (int32_t)r;
-        sink_d[at] = part_of ? fmaf(-eps, sink_p[at], sink_d[at]) * by : 0.f;
+        // nor does any with a sink that is not a word: its weight is zero, but eps may not be finite
+        sink_d[at] = part_of && is_word(p, s + k) ? fmaf(-eps, sink_p[at], sink_d[at]) * by : 0.f;
         if (by != 1.f) sink_p[at] *= by;
     }
     if (!part_of)

@@ -546,3 +546,29 @@ def test_sentence_spans_of_wide_ids(model):
     assert torch.equal(model.sentence_spans(toks[::3].to(torch.int16)), model.sentence_spans(torch.tensor([3, -1, -1, -1], dtype=torch.int32, device="cuda")))
     with pytest.raises(TypeError, match="whole numbers"):
         model.sentence_spans(toks.float())
+
+
+@pytest.mark.parametrize("dim", [64, 80, 128])
+@pytest.mark.parametrize("which", ["q", "k", "v", "d_o"])
+def test_attend_nonfinite_words_and_sinks_that_are_no_words(model, dim, which):
+    """A word that holds NaN spoils the bias' gradient at the distances of pairs that are seen, not at those to a sink that
+    the vocabulary does not have."""
+    toks = stream(300, (300, 300), 2, oov=0.0)
+    toks[:30] = VOCAB                                                # of forty sinks
+    t = {"q": randn(300, 2, dim, seed=1, dtype=torch.bfloat16), "k": randn(300, 1, dim, seed=2, dtype=torch.bfloat16),
+         "v": randn(300, 1, dim, seed=3, dtype=torch.bfloat16), "d_o": randn(300, 2, dim, seed=4, dtype=torch.bfloat16)}
+    bias, over = randn(64, 2, seed=5, by=0.5), dict(left=1, sinks=40, reach=1024)
+    want, bound = attend_by_hand(t["q"], t["k"], t["v"], toks, bias, 1, 0, 40, 1024, False, t["d_o"], True)
+    spans = model.sentence_spans(torch.from_numpy(toks).cuda())
+    starts = torch.from_numpy(binding.w2v_bucket_starts(64, 1024, False)).cuda().long()
+    for x in (50, 140, 270):
+        spoilt = {name: u.clone() for name, u in t.items()}
+        spoilt[which][x] = float("nan")
+        _, saved = model.attend(spoilt["q"], spoilt["k"], spoilt["v"], spans, bias, train=True, **over)
+        dbias = model.attend_backward(spoilt["d_o"], saved)[3]
+        rows = [x] if which in ("q", "d_o") else [x, x + 1]
+        seen = torch.tensor([i - j for i in rows for j in (*range(30, 40), i - 1, i)], device="cuda")
+        hit = torch.zeros(64, dtype=torch.bool, device="cuda")
+        hit[torch.searchsorted(starts, seen, right=True) - 1] = True
+        assert torch.isnan(dbias[hit]).all()
+        inside(dbias[~hit], want["dbias"][~hit], bound["dbias"][~hit], "dbias")
