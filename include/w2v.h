@@ -520,7 +520,7 @@ int32_t w2v_sample_pairs_noalloc(w2v_handle *h, const int32_t *tokens, uint64_t 
  * event), and wait only when scratch grows on the first call of a larger size.  Outputs lie over no input
  * but where a call says so.  Sums, statistics, softmax sums and references are held in 32 bits whatever the
  * arrays' type, but matrix products take operands of that type: w2v_attend rounds the softmax weights to it
- * (2^-9 or 2^-12 of each; fp16 ones below 2^-25 of the row's largest are zero), w2v_attend_backward the weights and
+ * (at most 2^-8 or 2^-11 of each; fp16 ones below 2^-25 of the row's largest are zero), w2v_attend_backward the weights and
  * the scores' gradients (fp16 ones below 2^-25 are zero: scale the loss), while dbias takes both in 32 bits;
  * w2v_attend_token takes its weights as sums of two such numbers.  Every result is the same on every call with the
  * same inputs (nothing is added up in an order that changes).

@@ -15,8 +15,8 @@
 //   scores:  lane (g, t) holds chunk 4 j + t (8 dimensions) of key g, the same of query head g;
 //   output:  lane (g, t) holds chunk g of keys 2t, 2t + 1, 2t + 8, 2t + 9; a byte permutation pairs the keys, and
 //            column g of product e is dimension 8 g + e.
-// The softmax weights enter the second product as the sum of two numbers of the cache's type, so that what is lost is
-// 2^-18 and not 2^-9 of them; fp16 weights are 2^15 times as large, so that one below 2^-25 of the largest is not zero beside
+// The softmax weights enter the second product as the sum of two numbers of the cache's type, so that what is lost is at most
+// 2^-16 (bf16) and not 2^-8 of them; fp16 weights are 2^15 times as large, so that one below 2^-25 of the largest is not zero beside
 // the sum, in which it counts.  Each warp copies its next step's keys and values to shared memory in the background, so
 // that what is under way does not have to fit in registers.  There chunk c of row r lies at c ^ turn(r), which keeps
 // both ways of reading free of bank conflicts.  96 sequences, 16 heads of 128 over 4 of keys and values, windows of 4,096: 150 us,
